@@ -339,6 +339,98 @@ onnxb_status onnx_maxpool2d_run(const int64_t x_dims[4], const int64_t kernel_sh
 onnxb_status onnx_global_average_pool_run(const int64_t x_dims[4], const float *X, float *Y, void *cuda_stream);
 onnxb_status onnx_global_average_pool_channel_major_run(const int64_t x_dims[4], const float *X, float *Y, void *cuda_stream);
 
+/*
+ * Feed-forward layers of language models: products of 8-bit integers, and the gated block in 16 bits (forward and backward) and in 8.
+ * (The paper has no counterpart; they stand beside Gemm as its dense layers of other types.)
+ *
+ * Tensors here are two-dimensional views: rows `ld` elements apart, the elements of a row one right after the other.  `type` is the
+ * ONNX code of the element type.  Rows may begin anywhere an element may (the 16-byte rule above holds for `workspace` alone): where
+ * an input's rows do not all begin at multiples of 16 bytes, a call asks for workspace and lays it out there first, so constant weights are
+ * best kept with rows at such multiples.  What lies between a view's rows is neither read as a value nor written.
+ * Sizes: rows may be 0 where they are tokens (nothing is launched, but for gradients of weights, which are then zeros);
+ * each size at most 2^30, `ld` at most 2^31-1, and at least `cols` where there are two rows and more (no rows that overlap).  Tensors
+ * of more than 2^31-1 elements are taken.  Outputs must not overlap inputs or each other (those that begin at the same address are refused).
+ * scale: one 32-bit float a row.  Errors common to these calls: ERR_NULL (a required view, its data or a scale); ERR_SHAPE (sizes that do not fit
+ * together or a row pitch below the width); ERR_ATTR (a type or an activation that the call does not take); ERR_UNSUPPORTED (sizes
+ * above those limits, a misaligned element, outputs in one place); ERR_WORKSPACE; ERR_CUDA.
+ */
+typedef enum { ONNXB_FLOAT = 1, ONNXB_INT8 = 3, ONNXB_FLOAT16 = 10, ONNXB_BFLOAT16 = 16 } onnxb_type;
+
+typedef struct {
+    void *data;              /* device (inputs are only read) */
+    int64_t rows, cols;
+    int64_t ld;              /* elements from one row to the next */
+    int32_t type;            /* onnxb_type */
+    int32_t reserved;        /* must be 0 */
+} onnxb_matrix;
+
+typedef enum {
+    ONNXB_SILU = 0,          /* g / (1 + exp(-g)) */
+    ONNXB_GELU = 1,          /* g * Phi(g), Phi the normal distribution */
+    ONNXB_GELU_TANH = 2,     /* g / 2 * (1 + tanh(sqrt(2/pi) * (g + 0.044715 g^3))) */
+    ONNXB_RELU = 3           /* g > 0 ? g : +0 (NaN -> 0, as fuse_relu; slope 1 where g > 0, else 0) */
+} onnxb_activation;
+
+/*
+ * onnx_quantize_rows_run - 8-bit integers and a scale for each row (token, or channel of weights):
+ *
+ *   scale[i] = max_k |X[i,k]| / 127        (rounded to a 32-bit float)
+ *   Q[i,k]   = the nearest integer to X[i,k] / scale[i] (of the exact quotient, ties to even), at most 127 in magnitude
+ *
+ * X [M,K] of 32- or 16-bit floats, Q [M,K] of 8-bit integers, scale [M].  A row whose scale is 0 becomes zeros.  A row with a NaN
+ * or an infinity becomes zeros with a scale of NaN: whatever is computed from it is NaN, not a number that looks right.
+ */
+onnxb_status onnx_quantize_rows_run(const onnxb_matrix *X, const onnxb_matrix *Q, float *scale, void *cuda_stream);
+
+/*
+ * onnx_gemm_int8_run - a Gemm of 8-bit integers with a scale for each token and each channel:
+ *
+ *   Y[i,j] = relu?( a_scale[i] * b_scale[j] * sum_k A[i,k] * B[j,k] + C[j] )
+ *
+ * A [M,K], B [N,K] (a row for each output channel; as onnx_gemm_run with transB), both 8-bit, any values (-128 too).  C [N] 32-bit
+ * floats or NULL.  Y [M,N] of 32- or 16-bit floats.  The sum is exact (32-bit integers; K at most 131071, so that it cannot overflow), the scaling is in
+ * 32 bits, and one rounding takes the result to Y's type.
+ */
+size_t onnx_gemm_int8_workspace_bytes(const onnxb_matrix *A, const onnxb_matrix *B);       /* host only */
+onnxb_status onnx_gemm_int8_run(const onnxb_matrix *A, const float *a_scale, const onnxb_matrix *B, const float *b_scale, const float *C,
+                                int fuse_relu, const onnxb_matrix *Y, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * onnx_gated_run - the gated block: both projections, the activation and the product in one pass over X,
+ *
+ *   G = X Wg^T,  U = X Wu^T,  H = act(G) * U
+ *
+ * X [M,K], Wg and Wu [F,K] (a row for each channel; they may be halves of one tensor), H [M,F], all of one type, 16-bit floats.
+ * G and U [M,F], of the same type: what onnx_gated_backward_run wants; both NULL where they are not kept.  Sums, activation
+ * and product are in 32 bits (H is computed from the unrounded G and U), and each output is rounded once.
+ * onnx_gated_int8_run - the same of 8-bit operands with scales as in onnx_gemm_int8_run: G = a_scale[i] * g_scale[j] * sum.., H [M,F] of
+ * 32- or 16-bit floats.
+ */
+size_t onnx_gated_workspace_bytes(const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu);      /* host only; of either */
+onnxb_status onnx_gated_run(const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu, int activation, const onnxb_matrix *H,
+                            const onnxb_matrix *G, const onnxb_matrix *U, void *workspace, size_t workspace_bytes, void *cuda_stream);
+onnxb_status onnx_gated_int8_run(const onnxb_matrix *A, const float *a_scale, const onnxb_matrix *Wg, const float *g_scale,
+                                 const onnxb_matrix *Wu, const float *u_scale, int activation, const onnxb_matrix *H, void *workspace,
+                                 size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * onnx_gated_backward_run - the gradients of onnx_gated_run, from dH and the G and U that it kept:
+ *
+ *   dG = dH * U * act'(G),  dU = dH * act(G)
+ *   dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X
+ *
+ * All of one type, 16-bit floats; shapes as the forward call's.  dX, dWg, dWu: each may be NULL where it is not wanted (not all of
+ * them); X is not read (and may be NULL) without dWg and dWu, Wg and Wu neither without dX.  dG and dU are rounded to the
+ * type between the two steps (the tensor cores take 16-bit operands), sums are in 32 bits, dX is one sum over both terms, and each
+ * result is rounded once.  Deterministic: no atomics.
+ */
+size_t onnx_gated_backward_workspace_bytes(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
+                                           const onnxb_matrix *dX, const onnxb_matrix *dWg, const onnxb_matrix *dWu);      /* host only */
+onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
+                                     const onnxb_matrix *G, const onnxb_matrix *U, int activation, const onnxb_matrix *dX,
+                                     const onnxb_matrix *dWg, const onnxb_matrix *dWu, void *workspace, size_t workspace_bytes,
+                                     void *cuda_stream);
+
 /* Human-readable name of a status code (static storage, never NULL). */
 const char *onnxb_status_string(onnxb_status status);
 

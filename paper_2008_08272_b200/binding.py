@@ -35,7 +35,11 @@ EXPORTS = [
     "onnx_conv2d_run_packed_sampled", "onnx_conv2d_run_packed_rounded", "onnx_conv2d_desc_layout", "onnxb_channel_pitch",
     "onnx_global_average_pool_channel_major_run", "onnxb_dispatch_state",
     "onnxb_probe_wait_timeout",
+    "onnx_quantize_rows_run", "onnx_gemm_int8_workspace_bytes", "onnx_gemm_int8_run", "onnx_gated_workspace_bytes", "onnx_gated_run",
+    "onnx_gated_int8_run", "onnx_gated_backward_workspace_bytes", "onnx_gated_backward_run",
 ]
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
+TYPE_CODES = {"float32": 1, "int8": 3, "float16": 10, "bfloat16": 16}      # ONNX's
 
 
 class OnnxB200Error(RuntimeError):
@@ -53,6 +57,12 @@ class ConvAttrs(ctypes.Structure):
         ("group", ctypes.c_int64), ("auto_pad", ctypes.c_int32), ("has_bias", ctypes.c_int32),
         ("fuse_relu", ctypes.c_int32), ("reserved", ctypes.c_int32),
     ]
+
+
+class Matrix(ctypes.Structure):
+    """``onnxb_matrix``: a two-dimensional view."""
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -169,6 +179,18 @@ def load(build_if_missing: bool = True):
     lib.onnxb_probe_tf32_mma_rate.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_double), vp]
     lib.onnxb_probe_wait_timeout.restype = ctypes.c_int
     lib.onnxb_probe_wait_timeout.argtypes = [ctypes.c_longlong, vp]
+    mp = ctypes.POINTER(Matrix)
+    for name, args in (("onnx_quantize_rows_run", [mp, mp, vp, vp]),
+                       ("onnx_gemm_int8_run", [mp, vp, mp, vp, vp, ctypes.c_int, mp, vp, sz, vp]),
+                       ("onnx_gated_run", [mp, mp, mp, ctypes.c_int, mp, mp, mp, vp, sz, vp]),
+                       ("onnx_gated_int8_run", [mp, vp, mp, vp, mp, vp, ctypes.c_int, mp, vp, sz, vp]),
+                       ("onnx_gated_backward_run", [mp] * 6 + [ctypes.c_int] + [mp] * 3 + [vp, sz, vp])):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = args
+    for name, args in (("onnx_gemm_int8_workspace_bytes", [mp, mp]), ("onnx_gated_workspace_bytes", [mp] * 3),
+                       ("onnx_gated_backward_workspace_bytes", [mp] * 7)):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = args
     _lib = lib
     return lib
 
@@ -577,3 +599,175 @@ def onnx_global_average_pool(X, *, Y=None, stream=None):
     _check(load().onnx_global_average_pool_run(_i64(tuple(X.shape), 4), _dev_ptr(X, "X"), _dev_ptr(Y, "Y"),
                                                _stream_ptr(stream)), "onnx_global_average_pool_run")
     return Y
+
+
+# --------------------------------------------------------------------- dense layers of 8- and 16-bit operands
+class _Views:
+    """The two-dimensional tensors of one call as the library takes them, all on one device, which is made the current one."""
+
+    def __init__(self, where, stream):
+        self.where, self.stream, self.device = where, stream, None
+
+    def _on_device(self, t, name):
+        import torch
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a torch CUDA tensor (there is no CPU path)")
+        if self.device is None:
+            self.device = t.device
+            of_stream = getattr(self.stream, "device", None)
+            if of_stream is not None and of_stream != t.device:
+                raise ValueError(f"{self.where}: the stream is one of {of_stream}, {name} is on {t.device}")
+        if t.device != self.device:
+            raise ValueError(f"{self.where}: {name} is on {t.device}, others are on {self.device}")
+
+    def matrix(self, t, name, types, like=None):
+        """``like``: a tensor whose type it has to have."""
+        if t is None:
+            raise OnnxB200Error(1, f"{name} is None")
+        self._on_device(t, name)
+        kind = str(t.dtype)[6:]
+        if kind not in types or (like is not None and t.dtype != like.dtype):
+            raise TypeError(f"{name} must be {' or '.join(types)}" + ("" if like is None else ", all of one type"))
+        if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise TypeError(f"{name} must have two dimensions, the elements of a row one right after the other")
+        rows, cols = t.shape
+        return Matrix(t.data_ptr() or None, rows, cols, t.stride(0) if rows > 1 else cols, TYPE_CODES[kind], 0)
+
+    def vector(self, t, name, size, allow_none=False):
+        if t is None and allow_none:
+            return None
+        if t is None:
+            raise OnnxB200Error(1, f"{name} is None")
+        self._on_device(t, name)
+        if str(t.dtype) != "torch.float32" or not t.is_contiguous():
+            raise TypeError(f"{name} must be contiguous float32")
+        if t.numel() != size:
+            raise OnnxB200Error(3, f"{self.where}: {name} has {t.numel()} values, not {size}")
+        return ctypes.c_void_p(t.data_ptr())
+
+    def new(self, rows, cols, dtype, kept=True):
+        return _new((rows, cols), self.device, self.stream, dtype, kept)
+
+    def workspace(self, given, need):
+        """(tensor, pointer, bytes): the caller's, or one of ``need`` bytes."""
+        if given is None and need:
+            given = _new(need, self.device, self.stream, "uint8", kept=False)
+        if given is None:
+            return None, None, 0
+        self._on_device(given, "workspace")
+        if not given.is_contiguous():
+            raise TypeError("workspace must be contiguous")
+        return given, ctypes.c_void_p(given.data_ptr()), given.numel() * given.element_size()
+
+    def call(self, function, *args):
+        import torch
+        with torch.cuda.device(self.device):
+            _check(function(*args, _stream_ptr(self.stream)), self.where)
+
+
+_FLOATS, _HALVES, _INT8 = ("float32", "float16", "bfloat16"), ("float16", "bfloat16"), ("int8",)
+
+
+def _activation(name) -> int:
+    if name not in ACTIVATIONS:
+        raise OnnxB200Error(2, f"activation must be one of {', '.join(ACTIVATIONS)}")
+    return ACTIVATIONS[name]
+
+
+def _ref(m):
+    return None if m is None else ctypes.byref(m)
+
+
+def onnx_quantize_rows(X, *, Q=None, scale=None, stream=None):
+    """``onnx_quantize_rows_run``: (Q, scale), the 8-bit integers nearest to X[i,k] / scale[i], scale[i] = max |X[i,:]| / 127.  The rows of
+    a Q made here begin at multiples of 16 bytes, as the products that read it want them."""
+    lib = load()
+    v = _Views("onnx_quantize_rows", stream)
+    x = v.matrix(X, "X", _FLOATS)
+    if Q is None:
+        Q = v.new(x.rows, (x.cols + 15) // 16 * 16, "int8")
+        Q = Q if Q.shape[1] == x.cols else Q[:, :x.cols]
+    if scale is None:
+        scale = _new(x.rows, v.device, stream)
+    q = v.matrix(Q, "Q", _INT8)
+    v.call(lib.onnx_quantize_rows_run, x, q, v.vector(scale, "scale", x.rows))
+    return Q, scale
+
+
+def _float_name(dtype) -> str:
+    name = str(dtype).removeprefix("torch.")
+    if name not in _FLOATS:
+        raise TypeError(f"dtype must be {' or '.join(_FLOATS)}")
+    return name
+
+
+def onnx_gemm_int8(A, a_scale, B, b_scale, C=None, *, fuse_relu=False, dtype="float32", Y=None, workspace=None, stream=None):
+    """``onnx_gemm_int8_run``: Y[i,j] = relu?(a_scale[i] * b_scale[j] * sum_k A[i,k] B[j,k] + C[j]) of 8-bit A [M,K] and B [N,K].
+    ``dtype``: of a Y made here (float32, float16 or bfloat16, by name or torch's)."""
+    lib = load()
+    v = _Views("onnx_gemm_int8", stream)
+    a, b = v.matrix(A, "A", _INT8), v.matrix(B, "B", _INT8)
+    if Y is None:
+        Y = v.new(a.rows, b.rows, _float_name(dtype))
+    y = v.matrix(Y, "Y", _FLOATS)
+    held, ws, ws_len = v.workspace(workspace, lib.onnx_gemm_int8_workspace_bytes(a, b))
+    v.call(lib.onnx_gemm_int8_run, a, v.vector(a_scale, "a_scale", a.rows), b, v.vector(b_scale, "b_scale", b.rows),
+           v.vector(C, "C", b.rows, allow_none=True), int(bool(fuse_relu)), y, ws, ws_len)
+    return Y
+
+
+def onnx_gated(X, Wg, Wu, *, activation="silu", save=False, H=None, G=None, U=None, workspace=None, stream=None):
+    """``onnx_gated_run``: H = act(X Wg^T) * (X Wu^T), X [M,K], Wg and Wu [F,K], all float16 or all bfloat16.  ``save`` (or a G and a U to
+    write to): (H, G, U) with the two projections, which ``onnx_gated_backward`` takes."""
+    lib = load()
+    v = _Views("onnx_gated", stream)
+    x, wg, wu = v.matrix(X, "X", _HALVES), v.matrix(Wg, "Wg", _HALVES, X), v.matrix(Wu, "Wu", _HALVES, X)
+    save = save or G is not None or U is not None
+    kind = str(X.dtype)[6:]
+    H = v.new(x.rows, wg.rows, kind) if H is None else H
+    if save:
+        G = v.new(x.rows, wg.rows, kind) if G is None else G
+        U = v.new(x.rows, wg.rows, kind) if U is None else U
+    h = v.matrix(H, "H", _HALVES, X)
+    g, u = (v.matrix(G, "G", _HALVES, X), v.matrix(U, "U", _HALVES, X)) if save else (None, None)
+    held, ws, ws_len = v.workspace(workspace, lib.onnx_gated_workspace_bytes(x, wg, wu))
+    v.call(lib.onnx_gated_run, x, wg, wu, _activation(activation), h, _ref(g), _ref(u), ws, ws_len)
+    return (H, G, U) if save else H
+
+
+def onnx_gated_int8(A, a_scale, Wg, g_scale, Wu, u_scale, *, activation="silu", dtype="float32", H=None, workspace=None, stream=None):
+    """``onnx_gated_int8_run``: H = act(G) * U of 8-bit A [M,K], Wg and Wu [F,K], G and U as ``onnx_gemm_int8`` has them."""
+    lib = load()
+    v = _Views("onnx_gated_int8", stream)
+    a, wg, wu = v.matrix(A, "A", _INT8), v.matrix(Wg, "Wg", _INT8), v.matrix(Wu, "Wu", _INT8)
+    if H is None:
+        H = v.new(a.rows, wg.rows, _float_name(dtype))
+    h = v.matrix(H, "H", _FLOATS)
+    held, ws, ws_len = v.workspace(workspace, lib.onnx_gated_workspace_bytes(a, wg, wu))
+    v.call(lib.onnx_gated_int8_run, a, v.vector(a_scale, "a_scale", a.rows), wg, v.vector(g_scale, "g_scale", wg.rows), wu,
+           v.vector(u_scale, "u_scale", wu.rows), _activation(activation), h, ws, ws_len)
+    return H
+
+
+def onnx_gated_backward(dH, X, Wg, Wu, G, U, *, activation="silu", wanted=(True, True, True), dX=None, dWg=None, dWu=None, workspace=None,
+                        stream=None):
+    """``onnx_gated_backward_run``: (dX, dWg, dWu) of ``onnx_gated``, from its G and U.  ``wanted``: which of the three (None in the
+    place of the others; weights that are not needed for them, or X, may be None)."""
+    lib = load()
+    v = _Views("onnx_gated_backward", stream)
+    dh, g, u = v.matrix(dH, "dH", _HALVES), v.matrix(G, "G", _HALVES, dH), v.matrix(U, "U", _HALVES, dH)
+    kind = str(dH.dtype)[6:]
+    want = [w or given is not None for w, given in zip(wanted, (dX, dWg, dWu))]
+    x = v.matrix(X, "X", _HALVES, dH) if want[1] or want[2] else None
+    wg, wu = (v.matrix(Wg, "Wg", _HALVES, dH), v.matrix(Wu, "Wu", _HALVES, dH)) if want[0] else (None, None)
+    if not any(want):
+        raise OnnxB200Error(1, "onnx_gated_backward: no gradient is wanted")
+    width = x.cols if x else wg.cols
+    outs = [None if not w else v.new(rows, width, kind) if given is None else given
+            for w, given, rows in zip(want, (dX, dWg, dWu), (dh.rows, dh.cols, dh.cols))]
+    dx, dwg, dwu = (None if o is None else v.matrix(o, name, _HALVES, dH) for o, name in zip(outs, ("dX", "dWg", "dWu")))
+    held, ws, ws_len = v.workspace(workspace, lib.onnx_gated_backward_workspace_bytes(
+        _ref(dh), _ref(x), _ref(wg), _ref(wu), _ref(dx), _ref(dwg), _ref(dwu)))
+    v.call(lib.onnx_gated_backward_run, dh, _ref(x), _ref(wg), _ref(wu), g, u, _activation(activation), _ref(dx), _ref(dwg), _ref(dwu), ws,
+           ws_len)
+    return tuple(outs)

@@ -1,0 +1,60 @@
+// Elementwise mathematics of the dense layers, in 32 bits: activations, their slopes, and conversions to and from the types that
+// tensors are kept in.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "onnx_b200.h"
+
+namespace onnxb {
+namespace dense {
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// 1 / (1 + exp(-z)): exp(-z) is finite up to z = -88 and infinite below, where the quotient is 0 as it should be (to 1e-38)
+__device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+// sqrt(8/pi) (g + 0.044715 g^3): tanh's argument in the approximation of gelu, twice, since (1 + tanh(y)) / 2 = logistic(2y).
+// (As tanh the factor would lose all its digits where it is small.)
+__device__ __forceinline__ float gelu_argument(float g) { return 1.5957691216057308f * fmaf(0.044715f * g * g, g, g); }
+
+// act(g)
+__device__ __forceinline__ float activate(int kind, float g) {
+    if (kind == ONNXB_SILU) return g * logistic(g);
+    if (kind == ONNXB_GELU) return 0.5f * g * erfcf(-0.70710678118654752f * g);      // (1 + erf would lose its digits for negative g)
+    if (kind == ONNXB_GELU_TANH) return g * logistic(gelu_argument(g));
+    return g > 0.f ? g : 0.f;
+}
+
+// act(g) and act'(g)
+__device__ __forceinline__ void activate_with_slope(int kind, float g, float &value, float &slope) {
+    if (kind == ONNXB_SILU) {
+        const float p = logistic(g);
+        value = g * p;
+        slope = fmaf(value, 1.f - p, p);
+    } else if (kind == ONNXB_GELU) {
+        const float p = 0.5f * erfcf(-0.70710678118654752f * g);
+        value = g * p;
+        slope = fmaf(g * 0.39894228040143268f, __expf(-0.5f * g * g), p);
+    } else if (kind == ONNXB_GELU_TANH) {
+        const float p = logistic(gelu_argument(g));
+        value = g * p;
+        const float c = fminf(fmaxf(g, -30.f), 30.f);            // (p (1 - p) is 0 beyond; g^2 could be infinite)
+        slope = fmaf(c * p * (1.f - p), 1.5957691216057308f * fmaf(0.134145f * c, c, 1.f), p);
+    } else {
+        value = g > 0.f ? g : 0.f;
+        slope = g > 0.f ? 1.f : 0.f;
+    }
+}
+
+}  // namespace dense
+}  // namespace onnxb
