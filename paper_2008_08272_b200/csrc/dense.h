@@ -35,7 +35,8 @@ struct DenseProblem {
 
 inline int type_bytes(int type) { return type == ONNXB_FLOAT ? 4 : type == ONNXB_INT8 ? 1 : 2; }
 
-int launch_dense(const DenseProblem &p, cudaStream_t stream);
+// On the tensor cores (tc_dense.cu).  Operands' rows begin at multiples of 16 bytes.
+int launch_tc_dense(const DenseProblem &p, cudaStream_t stream);
 
 // dG = dH U act'(G), dU = dH act(G), each [M,F]; all of one 16-bit type
 struct GatedSlopeProblem {

@@ -31,6 +31,30 @@ bool has_size(const onnxb_matrix *m, int64_t rows, int64_t cols) { return m->row
 DenseOperand operand(const onnxb_matrix *m) { return DenseOperand{m->data, m->rows > 1 ? (long long)m->ld : (long long)m->cols}; }
 bool same_place(const onnxb_matrix *a, const onnxb_matrix *b) { return a && b && a->rows > 0 && a->data == b->data; }
 
+// Whether TMA can address a view's rows; what its copy in the workspace takes otherwise, rows at multiples of 16 bytes.
+int64_t copy_pitch(const onnxb_matrix *m) { return (m->cols * type_bytes(m->type) + 15) / 16 * 16; }
+bool in_place(const onnxb_matrix *m) {
+    return reinterpret_cast<uintptr_t>(m->data) % 16 == 0 && (m->rows <= 1 || m->ld * type_bytes(m->type) % 16 == 0);
+}
+size_t copy_bytes(const onnxb_matrix *m) {
+    if (!m || m->rows < 1 || m->cols < 1 || m->rows > kMostSize || m->cols > kMostSize || in_place(m)) return 0;
+    return (size_t)(copy_pitch(m) * m->rows);
+}
+onnxb_status check_workspace(const void *workspace, size_t bytes, size_t need) {
+    if (need == 0) return ONNXB_OK;
+    if (!workspace || bytes < need) return ONNXB_ERR_WORKSPACE;
+    return reinterpret_cast<uintptr_t>(workspace) % 16 ? ONNXB_ERR_UNSUPPORTED : ONNXB_OK;
+}
+// The operand as the kernels read it: where it lies, or copied to the front of `workspace`, which moves on.
+DenseOperand placed(const onnxb_matrix *m, char *&workspace, int &err, cudaStream_t stream) {
+    const size_t bytes = copy_bytes(m);
+    if (bytes == 0 || err != 0) return operand(m);
+    const DenseOperand o{workspace, copy_pitch(m) / type_bytes(m->type)};
+    err = launch_repack_rows(m->data, operand(m).ld * type_bytes(m->type), (int)m->rows, m->cols * type_bytes(m->type), workspace, copy_pitch(m), stream);
+    workspace += bytes;
+    return o;
+}
+
 onnxb_status status_of(int cuda_error) { return cuda_error == 0 ? ONNXB_OK : ONNXB_ERR_CUDA; }
 
 #define CHECK(expr)                                      \
@@ -55,8 +79,7 @@ extern "C" onnxb_status onnx_quantize_rows_run(const onnxb_matrix *X, const onnx
 }
 
 extern "C" size_t onnx_gemm_int8_workspace_bytes(const onnxb_matrix *A, const onnxb_matrix *B) {
-    (void)A; (void)B;
-    return 0;
+    return copy_bytes(A) + copy_bytes(B);
 }
 
 extern "C" onnxb_status onnx_gemm_int8_run(const onnxb_matrix *A, const float *a_scale, const onnxb_matrix *B, const float *b_scale, const float *C,
@@ -76,18 +99,19 @@ extern "C" onnxb_status onnx_gemm_int8_run(const onnxb_matrix *A, const float *a
     d.mode = kDensePlain;
     d.type = ONNXB_INT8;
     d.M = (int)M; d.N = (int)N; d.K = (int)K;
-    d.A[0] = operand(A);
-    d.B[0] = operand(B);
     d.a_scale = a_scale; d.b_scale[0] = b_scale; d.bias = C; d.relu = fuse_relu != 0;
     d.y_type = Y->type;
     d.Y[0] = Y->data; d.y_ld[0] = operand(Y).ld;
-    (void)workspace; (void)workspace_bytes;
-    return status_of(launch_dense(d, (cudaStream_t)cuda_stream));
+    CHECK(check_workspace(workspace, workspace_bytes, onnx_gemm_int8_workspace_bytes(A, B)));
+    char *ws = static_cast<char *>(workspace);
+    int err = 0;
+    d.A[0] = placed(A, ws, err, (cudaStream_t)cuda_stream);
+    d.B[0] = placed(B, ws, err, (cudaStream_t)cuda_stream);
+    return status_of(err ? err : launch_tc_dense(d, (cudaStream_t)cuda_stream));
 }
 
 extern "C" size_t onnx_gated_workspace_bytes(const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu) {
-    (void)X; (void)Wg; (void)Wu;
-    return 0;
+    return copy_bytes(X) + copy_bytes(Wg) + copy_bytes(Wu);
 }
 
 // What both types of operands share; *done: there is nothing to compute.
@@ -106,13 +130,21 @@ static onnxb_status gated_problem(const onnxb_matrix *X, const onnxb_matrix *Wg,
     d.mode = kDenseGated;
     d.type = X->type;
     d.M = (int)M; d.N = (int)F; d.K = (int)K;
-    d.A[0] = operand(X);
-    d.B[0] = operand(Wg);
-    d.B[1] = operand(Wu);
     d.activation = activation;
     d.y_type = H->type;
     d.Y[0] = H->data; d.y_ld[0] = operand(H).ld;
     return ONNXB_OK;
+}
+
+static onnxb_status run_gated(DenseProblem &d, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu, void *workspace,
+                              size_t workspace_bytes, cudaStream_t stream) {
+    CHECK(check_workspace(workspace, workspace_bytes, onnx_gated_workspace_bytes(X, Wg, Wu)));
+    char *ws = static_cast<char *>(workspace);
+    int err = 0;
+    d.A[0] = placed(X, ws, err, stream);
+    d.B[0] = placed(Wg, ws, err, stream);
+    d.B[1] = placed(Wu, ws, err, stream);
+    return status_of(err ? err : launch_tc_dense(d, stream));
 }
 
 extern "C" onnxb_status onnx_gated_run(const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu, int activation, const onnxb_matrix *H,
@@ -132,8 +164,7 @@ extern "C" onnxb_status onnx_gated_run(const onnxb_matrix *X, const onnxb_matrix
         d.Y[2] = U->data; d.y_ld[2] = operand(U).ld;
     }
     if (done) return ONNXB_OK;
-    (void)workspace; (void)workspace_bytes;
-    return status_of(launch_dense(d, (cudaStream_t)cuda_stream));
+    return run_gated(d, X, Wg, Wu, workspace, workspace_bytes, (cudaStream_t)cuda_stream);
 }
 
 extern "C" onnxb_status onnx_gated_int8_run(const onnxb_matrix *A, const float *a_scale, const onnxb_matrix *Wg, const float *g_scale,
@@ -148,8 +179,7 @@ extern "C" onnxb_status onnx_gated_int8_run(const onnxb_matrix *A, const float *
     if (!a_scale || !g_scale || !u_scale) return ONNXB_ERR_NULL;
     if ((reinterpret_cast<uintptr_t>(a_scale) | reinterpret_cast<uintptr_t>(g_scale) | reinterpret_cast<uintptr_t>(u_scale)) % 4) return ONNXB_ERR_UNSUPPORTED;
     d.a_scale = a_scale; d.b_scale[0] = g_scale; d.b_scale[1] = u_scale;
-    (void)workspace; (void)workspace_bytes;
-    return status_of(launch_dense(d, (cudaStream_t)cuda_stream));
+    return run_gated(d, A, Wg, Wu, workspace, workspace_bytes, (cudaStream_t)cuda_stream);
 }
 
 // The gradients' workspace: dG and dU, their rows at multiples of 16 bytes.
@@ -158,9 +188,8 @@ static size_t slope_bytes(int64_t M, int64_t F) { return (size_t)(M * slope_pitc
 
 extern "C" size_t onnx_gated_backward_workspace_bytes(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
                                                       const onnxb_matrix *dX, const onnxb_matrix *dWg, const onnxb_matrix *dWu) {
-    (void)X; (void)Wg; (void)Wu; (void)dX; (void)dWg; (void)dWu;
     if (!dH || dH->rows < 1 || dH->cols < 1 || dH->rows > kMostSize || dH->cols > kMostSize) return 0;
-    return 2 * slope_bytes(dH->rows, dH->cols);
+    return 2 * slope_bytes(dH->rows, dH->cols) + (dX ? copy_bytes(Wg) + copy_bytes(Wu) : 0) + (dWg || dWu ? copy_bytes(X) : 0);
 }
 
 extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
@@ -202,15 +231,16 @@ extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const on
                 return ONNXB_ERR_CUDA;
         return ONNXB_OK;
     }
-    if (!workspace || workspace_bytes < onnx_gated_backward_workspace_bytes(dH, X, Wg, Wu, dX, dWg, dWu)) return ONNXB_ERR_WORKSPACE;
-    if (reinterpret_cast<uintptr_t>(workspace) % 16) return ONNXB_ERR_UNSUPPORTED;
+    CHECK(check_workspace(workspace, workspace_bytes, onnx_gated_backward_workspace_bytes(dH, X, Wg, Wu, dX, dWg, dWu)));
     GatedSlopeProblem s{};
     s.type = dH->type; s.activation = activation;
     s.M = (int)M; s.F = (int)F;
     s.dH = operand(dH); s.G = operand(G); s.U = operand(U);
     s.d_ld = slope_pitch(F);
-    s.dG = workspace;
-    s.dU = static_cast<char *>(workspace) + slope_bytes(M, F);
+    char *ws = static_cast<char *>(workspace);
+    s.dG = ws;
+    s.dU = ws + slope_bytes(M, F);
+    ws += 2 * slope_bytes(M, F);
     int err = launch_gated_slope(s, stream);
     DenseProblem d{};
     d.type = d.y_type = dH->type;
@@ -219,20 +249,20 @@ extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const on
     if (err == 0 && dX) {
         d.mode = kDenseGradX;
         d.M = (int)M; d.N = (int)K; d.K = (int)F;
-        d.B[0] = operand(Wg);
-        d.B[1] = operand(Wu);
+        d.B[0] = placed(Wg, ws, err, stream);
+        d.B[1] = placed(Wu, ws, err, stream);
         d.Y[0] = dX->data; d.y_ld[0] = operand(dX).ld;
-        err = launch_dense(d, stream);
+        if (err == 0) err = launch_tc_dense(d, stream);
     }
     if (err == 0 && weights) {
         d.mode = kDenseGradW;
         d.M = (int)F; d.N = (int)K; d.K = (int)M;
-        d.B[0] = operand(X);
+        d.B[0] = placed(X, ws, err, stream);
         for (int z = 0; z < 2; ++z) {
             d.Y[z] = outs[1 + z] ? outs[1 + z]->data : nullptr;
             d.y_ld[z] = outs[1 + z] ? operand(outs[1 + z]).ld : 0;
         }
-        err = launch_dense(d, stream);
+        if (err == 0) err = launch_tc_dense(d, stream);
     }
     return status_of(err);
 }

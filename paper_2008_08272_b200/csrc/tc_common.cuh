@@ -183,6 +183,17 @@ __device__ __forceinline__ void tma_load_4d_pair(void *dst, const CUtensorMap *m
         ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(cluster_bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
         : "memory");
 }
+__device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *m, uint32_t cluster_bar, int c0, int c1) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(cluster_bar), "r"(c0), "r"(c1)
+        : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *m, const void *src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(src)), "r"(c0), "r"(c1)
+                 : "memory");
+}
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap *m, const void *src, int c0, int c1, int c2) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2)
@@ -278,6 +289,20 @@ __device__ __forceinline__ void mma_tf32_lohi_pair(uint32_t d_tmem, uint32_t a_l
         ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// The instruction for 16-bit floats (fp32 sums) or 8-bit integers (32-bit sums), for one CTA or a pair: one thread issues
+#define ONNXB_MMA_KIND(name, group, kind)                                                                                        \
+    __device__ __forceinline__ void name(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,            \
+                                         uint32_t idesc, uint32_t accumulate) {                                                  \
+        asm volatile("{\n.reg .pred p;\n.reg .b64 da, db;\nsetp.ne.b32 p, %6, 0;\nmov.b64 da, {%1, %2};\nmov.b64 db, {%3, %4};\n" \
+                     "tcgen05.mma.cta_group::" group ".kind::" kind " [%0], da, db, %5, p;\n}\n"                                 \
+                     ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)                      \
+                     : "memory");                                                                                                \
+    }
+ONNXB_MMA_KIND(mma_f16_lohi, "1", "f16")
+ONNXB_MMA_KIND(mma_f16_lohi_pair, "2", "f16")
+ONNXB_MMA_KIND(mma_i8_lohi, "1", "i8")
+ONNXB_MMA_KIND(mma_i8_lohi_pair, "2", "i8")
+#undef ONNXB_MMA_KIND
 // completion of the pair's MMAs, signalled on the barrier at this offset in both CTAs of the pair
 __device__ __forceinline__ void mma_commit_pair(uint64_t *bar) {
     asm volatile(
@@ -352,6 +377,15 @@ __device__ __forceinline__ uint64_t make_smem_desc(uint32_t saddr, uint32_t lbo_
 __host__ __device__ inline uint32_t make_idesc_tf32(int m, int n, int a_mn_major, int b_mn_major) {
     return (1u << 4) | (2u << 7) | (2u << 10) | ((uint32_t)(a_mn_major != 0) << 15) |
            ((uint32_t)(b_mn_major != 0) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// The same fields for kind::f16 (D f32; operands f16 = 0, bf16 = 1) and kind::i8 (D s32 = 2; operands s8 = 1).
+__host__ __device__ inline uint32_t make_idesc_f16(int m, int n, int bf16, int a_mn_major, int b_mn_major) {
+    return (1u << 4) | ((uint32_t)(bf16 != 0) << 7) | ((uint32_t)(bf16 != 0) << 10) | ((uint32_t)(a_mn_major != 0) << 15) |
+           ((uint32_t)(b_mn_major != 0) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+__host__ __device__ inline uint32_t make_idesc_s8(int m, int n) {
+    return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
 }  // namespace tc

@@ -607,8 +607,8 @@ static EncodeTiledFn encode_fn() {
     return fn;
 }
 
-bool make_tmap(CUtensorMap *out, const void *base, int rank, const uint64_t *dims, const uint64_t *strides_bytes,
-               const uint32_t *box, int swizzle) {
+bool make_tmap_of(int element_bytes, CUtensorMap *out, const void *base, int rank, const uint64_t *dims, const uint64_t *strides_bytes,
+                  const uint32_t *box, int swizzle) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t gdim[5], gstr[4];
@@ -619,12 +619,20 @@ bool make_tmap(CUtensorMap *out, const void *base, int rank, const uint64_t *dim
         estr[i] = 1;
         if (i > 0) gstr[i - 1] = strides_bytes[i - 1];
     }
-    return fn(out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, (cuuint32_t)rank, const_cast<void *>(base), gdim, gstr, bdim, estr,
+    const CUtensorMapDataType type = element_bytes == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                     : element_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16
+                                                          : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+    return fn(out, type, (cuuint32_t)rank, const_cast<void *>(base), gdim, gstr, bdim, estr,
               CU_TENSOR_MAP_INTERLEAVE_NONE,
               swizzle == kTmapSwizzle128 ? CU_TENSOR_MAP_SWIZZLE_128B
               : swizzle == kTmapSwizzle128Atom32 ? CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B
                                                  : CU_TENSOR_MAP_SWIZZLE_NONE,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool make_tmap(CUtensorMap *out, const void *base, int rank, const uint64_t *dims, const uint64_t *strides_bytes,
+               const uint32_t *box, int swizzle) {
+    return make_tmap_of(4, out, base, rank, dims, strides_bytes, box, swizzle);
 }
 
 int num_sms() {

@@ -112,6 +112,9 @@ inline cudaError_t launch_pdl_cluster(void (*kernel)(KArgs...), unsigned cluster
 constexpr int kTmapSwizzleNone = 0, kTmapSwizzle128 = 1, kTmapSwizzle128Atom32 = 2;
 bool make_tmap(CUtensorMap *out, const void *base, int rank, const uint64_t *dims, const uint64_t *strides_bytes,
                const uint32_t *box, int swizzle);
+// The same for elements of 1 or 2 bytes (as bits: what lies outside reads as zero bytes) or of 4 (fp32)
+bool make_tmap_of(int element_bytes, CUtensorMap *out, const void *base, int rank, const uint64_t *dims, const uint64_t *strides_bytes,
+                  const uint32_t *box, int swizzle);
 int num_sms();
 }  // namespace tc_host
 
