@@ -681,6 +681,9 @@ def _ref(m):
 def onnx_quantize_rows(X, *, Q=None, scale=None, stream=None):
     """``onnx_quantize_rows_run``: (Q, scale), the 8-bit integers nearest to X[i,k] / scale[i], scale[i] = max |X[i,:]| / 127.  The rows of
     a Q made here begin at multiples of 16 bytes, as the products that read it want them."""
+    done = (_fast_mod or _fast()).quantize_rows(X, Q, scale, stream)
+    if done is not None:
+        return done
     lib = load()
     v = _Views("onnx_quantize_rows", stream)
     x = v.matrix(X, "X", _FLOATS)
@@ -704,6 +707,9 @@ def _float_name(dtype) -> str:
 def onnx_gemm_int8(A, a_scale, B, b_scale, C=None, *, fuse_relu=False, dtype="float32", Y=None, workspace=None, stream=None):
     """``onnx_gemm_int8_run``: Y[i,j] = relu?(a_scale[i] * b_scale[j] * sum_k A[i,k] B[j,k] + C[j]) of 8-bit A [M,K] and B [N,K].
     ``dtype``: of a Y made here (float32, float16 or bfloat16, by name or torch's)."""
+    y = (_fast_mod or _fast()).gemm_int8(A, a_scale, B, b_scale, C, fuse_relu, dtype, Y, workspace, stream)
+    if y is not None:
+        return y
     lib = load()
     v = _Views("onnx_gemm_int8", stream)
     a, b = v.matrix(A, "A", _INT8), v.matrix(B, "B", _INT8)
@@ -719,6 +725,9 @@ def onnx_gemm_int8(A, a_scale, B, b_scale, C=None, *, fuse_relu=False, dtype="fl
 def onnx_gated(X, Wg, Wu, *, activation="silu", save=False, H=None, G=None, U=None, workspace=None, stream=None):
     """``onnx_gated_run``: H = act(X Wg^T) * (X Wu^T), X [M,K], Wg and Wu [F,K], all float16 or all bfloat16.  ``save`` (or a G and a U to
     write to): (H, G, U) with the two projections, which ``onnx_gated_backward`` takes."""
+    h = (_fast_mod or _fast()).gated(X, Wg, Wu, activation, save, H, G, U, workspace, stream)
+    if h is not None:
+        return h
     lib = load()
     v = _Views("onnx_gated", stream)
     x, wg, wu = v.matrix(X, "X", _HALVES), v.matrix(Wg, "Wg", _HALVES, X), v.matrix(Wu, "Wu", _HALVES, X)
@@ -737,6 +746,9 @@ def onnx_gated(X, Wg, Wu, *, activation="silu", save=False, H=None, G=None, U=No
 
 def onnx_gated_int8(A, a_scale, Wg, g_scale, Wu, u_scale, *, activation="silu", dtype="float32", H=None, workspace=None, stream=None):
     """``onnx_gated_int8_run``: H = act(G) * U of 8-bit A [M,K], Wg and Wu [F,K], G and U as ``onnx_gemm_int8`` has them."""
+    h = (_fast_mod or _fast()).gated_int8(A, a_scale, Wg, g_scale, Wu, u_scale, activation, dtype, H, workspace, stream)
+    if h is not None:
+        return h
     lib = load()
     v = _Views("onnx_gated_int8", stream)
     a, wg, wu = v.matrix(A, "A", _INT8), v.matrix(Wg, "Wg", _INT8), v.matrix(Wu, "Wu", _INT8)
@@ -753,6 +765,9 @@ def onnx_gated_backward(dH, X, Wg, Wu, G, U, *, activation="silu", wanted=(True,
                         stream=None):
     """``onnx_gated_backward_run``: (dX, dWg, dWu) of ``onnx_gated``, from its G and U.  ``wanted``: which of the three (None in the
     place of the others; weights that are not needed for them, or X, may be None)."""
+    done = (_fast_mod or _fast()).gated_backward(dH, X, Wg, Wu, G, U, activation, *wanted, dX, dWg, dWu, workspace, stream)
+    if done is not None:
+        return done
     lib = load()
     v = _Views("onnx_gated_backward", stream)
     dh, g, u = v.matrix(dH, "dH", _HALVES), v.matrix(G, "G", _HALVES, dH), v.matrix(U, "U", _HALVES, dH)

@@ -1,4 +1,4 @@
-// The elementwise kernels of the dense layers: rows laid out for TMA, and the gated block's gradients before its products.
+// The dense layers' choice of kernel, and their elementwise ones: rows laid out for TMA, and the gated block's gradients before its products.
 #include <algorithm>
 
 #include "dense.h"
@@ -55,6 +55,8 @@ __global__ void gated_slope_kernel(const GatedSlopeProblem p) {
 }
 
 }  // namespace
+
+int launch_dense(const DenseProblem &p, cudaStream_t stream) { return dense_few_fits(p) ? launch_dense_few(p, stream) : launch_tc_dense(p, stream); }
 
 int launch_repack_rows(const void *src, long long src_pitch, int rows, long long row_bytes, void *dst, long long dst_pitch, cudaStream_t stream) {
     const long long chunks = dst_pitch / 16, total = chunks * rows;

@@ -35,6 +35,10 @@ struct DenseProblem {
 
 inline int type_bytes(int type) { return type == ONNXB_FLOAT ? 4 : type == ONNXB_INT8 ? 1 : 2; }
 
+// A product as its size asks for: by the kernel for a few tokens (dense_few.cu) or the one for many (tc_dense.cu).
+int launch_dense(const DenseProblem &p, cudaStream_t stream);
+bool dense_few_fits(const DenseProblem &p);
+int launch_dense_few(const DenseProblem &p, cudaStream_t stream);
 // On the tensor cores (tc_dense.cu).  Operands' rows begin at multiples of 16 bytes.
 int launch_tc_dense(const DenseProblem &p, cudaStream_t stream);
 

@@ -107,7 +107,7 @@ extern "C" onnxb_status onnx_gemm_int8_run(const onnxb_matrix *A, const float *a
     int err = 0;
     d.A[0] = placed(A, ws, err, (cudaStream_t)cuda_stream);
     d.B[0] = placed(B, ws, err, (cudaStream_t)cuda_stream);
-    return status_of(err ? err : launch_tc_dense(d, (cudaStream_t)cuda_stream));
+    return status_of(err ? err : launch_dense(d, (cudaStream_t)cuda_stream));
 }
 
 extern "C" size_t onnx_gated_workspace_bytes(const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu) {
@@ -144,7 +144,7 @@ static onnxb_status run_gated(DenseProblem &d, const onnxb_matrix *X, const onnx
     d.A[0] = placed(X, ws, err, stream);
     d.B[0] = placed(Wg, ws, err, stream);
     d.B[1] = placed(Wu, ws, err, stream);
-    return status_of(err ? err : launch_tc_dense(d, stream));
+    return status_of(err ? err : launch_dense(d, stream));
 }
 
 extern "C" onnxb_status onnx_gated_run(const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu, int activation, const onnxb_matrix *H,
@@ -252,7 +252,7 @@ extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const on
         d.B[0] = placed(Wg, ws, err, stream);
         d.B[1] = placed(Wu, ws, err, stream);
         d.Y[0] = dX->data; d.y_ld[0] = operand(dX).ld;
-        if (err == 0) err = launch_tc_dense(d, stream);
+        if (err == 0) err = launch_dense(d, stream);
     }
     if (err == 0 && weights) {
         d.mode = kDenseGradW;
@@ -262,7 +262,7 @@ extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const on
             d.Y[z] = outs[1 + z] ? outs[1 + z]->data : nullptr;
             d.y_ld[z] = outs[1 + z] ? operand(outs[1 + z]).ld : 0;
         }
-        if (err == 0) err = launch_tc_dense(d, stream);
+        if (err == 0) err = launch_dense(d, stream);
     }
     return status_of(err);
 }

@@ -14,6 +14,7 @@
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <vector>
@@ -34,6 +35,14 @@ struct Abi {
     decltype(&onnx_maxpool2d_run) maxpool2d_run;
     decltype(&onnx_global_average_pool_run) global_average_pool_run;
     decltype(&onnxb_dispatch_state) dispatch_state;
+    decltype(&onnx_quantize_rows_run) quantize_rows_run;
+    decltype(&onnx_gemm_int8_workspace_bytes) gemm_int8_workspace_bytes;
+    decltype(&onnx_gemm_int8_run) gemm_int8_run;
+    decltype(&onnx_gated_workspace_bytes) gated_workspace_bytes;
+    decltype(&onnx_gated_run) gated_run;
+    decltype(&onnx_gated_int8_run) gated_int8_run;
+    decltype(&onnx_gated_backward_workspace_bytes) gated_backward_workspace_bytes;
+    decltype(&onnx_gated_backward_run) gated_backward_run;
 } abi;
 
 struct Plan {                    // what a convolution descriptor resolved to
@@ -128,6 +137,14 @@ PyObject *py_bind(PyObject *, PyObject *arg) {
     get(abi.maxpool2d_run, "onnx_maxpool2d_run");
     get(abi.global_average_pool_run, "onnx_global_average_pool_run");
     get(abi.dispatch_state, "onnxb_dispatch_state");
+    get(abi.quantize_rows_run, "onnx_quantize_rows_run");
+    get(abi.gemm_int8_workspace_bytes, "onnx_gemm_int8_workspace_bytes");
+    get(abi.gemm_int8_run, "onnx_gemm_int8_run");
+    get(abi.gated_workspace_bytes, "onnx_gated_workspace_bytes");
+    get(abi.gated_run, "onnx_gated_run");
+    get(abi.gated_int8_run, "onnx_gated_int8_run");
+    get(abi.gated_backward_workspace_bytes, "onnx_gated_backward_workspace_bytes");
+    get(abi.gated_backward_run, "onnx_gated_backward_run");
     if (!ok) { PyErr_SetString(PyExc_OSError, "a symbol of the C ABI is missing"); return nullptr; }
     Py_RETURN_NONE;
 }
@@ -271,6 +288,224 @@ PyObject *py_gap(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return abi.global_average_pool_run(xt->sizes().data(), x, y, stream) == ONNXB_OK ? result(a[1], ym) : slow_path();
 }
 
+// --------------------------------------------------------------------- dense layers of 8- and 16-bit operands
+// One call's tensors: CUDA tensors of the current device, two-dimensional with the elements of a row one right after the other (`matrix`),
+// or contiguous fp32 of a given length (`vector`).  Anything else clears `fine`.
+struct Views {
+    bool fine = true;
+    c10::DeviceIndex device = -1;
+    PyObject *given_stream;
+    void *stream = nullptr;
+
+    explicit Views(PyObject *given) : given_stream(given) {}
+
+    const at::Tensor *on_device(PyObject *o) {
+        if (!THPVariable_CheckExact(o)) { fine = false; return nullptr; }
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!t.is_cuda()) { fine = false; return nullptr; }
+        if (device < 0) {
+            device = t.device().index();
+            if (device != c10::cuda::current_device()) fine = false;
+            stream = stream_ptr(given_stream, fine);
+            if (fine && given_stream != Py_None) {              // (a stream of another device: the checked path says so)
+                PyObject *a = PyObject_GetAttrString(given_stream, "device_index");
+                if (!a) PyErr_Clear();
+                else {
+                    fine = PyLong_AsLong(a) == device;
+                    Py_DECREF(a);
+                    if (PyErr_Occurred()) { PyErr_Clear(); fine = false; }
+                }
+            }
+        }
+        if (t.device().index() != device) fine = false;
+        return &t;
+    }
+    void take(const at::Tensor &t, onnxb_matrix &m) {
+        const at::ScalarType type = t.scalar_type();
+        m.type = type == at::kFloat ? ONNXB_FLOAT : type == at::kChar ? ONNXB_INT8 : type == at::kHalf ? ONNXB_FLOAT16 : type == at::kBFloat16 ? ONNXB_BFLOAT16 : 0;
+        if (!m.type || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) { fine = false; return; }
+        m.data = t.data_ptr();
+        m.rows = t.size(0);
+        m.cols = t.size(1);
+        m.ld = m.rows > 1 ? t.stride(0) : m.cols;
+        m.reserved = 0;
+    }
+    // the view, or nullptr for None
+    onnxb_matrix *matrix(PyObject *o, onnxb_matrix &m) {
+        if (o == Py_None) return nullptr;
+        const at::Tensor *t = on_device(o);
+        if (t) take(*t, m);
+        return &m;
+    }
+    float *vector(PyObject *o, int64_t size) {
+        if (o == Py_None) return nullptr;
+        const at::Tensor *t = on_device(o);
+        if (!t || t->scalar_type() != at::kFloat || !t->is_contiguous() || t->numel() != size) { fine = false; return nullptr; }
+        return static_cast<float *>(t->data_ptr());
+    }
+    at::Tensor made(at::IntArrayRef size, at::ScalarType type, bool is_result = true) {
+        return new_tensor(size, type, at::Device(at::kCUDA, device), given_stream, stream, is_result);
+    }
+    // a result: the caller's, or one made here
+    onnxb_matrix *result(PyObject *given, int64_t rows, int64_t cols, int32_t type, at::Tensor &t, onnxb_matrix &m) {
+        if (given != Py_None) return matrix(given, m);
+        t = made({rows, cols}, type == ONNXB_FLOAT ? at::kFloat : type == ONNXB_FLOAT16 ? at::kHalf : at::kBFloat16);
+        m = onnxb_matrix{t.data_ptr(), rows, cols, cols, type, 0};
+        return &m;
+    }
+    // the caller's workspace, or one of `need` bytes
+    void *workspace(PyObject *given, size_t need, at::Tensor &t, size_t &bytes) {
+        bytes = 0;
+        if (given != Py_None) {
+            const at::Tensor *g = on_device(given);
+            if (!g || !g->is_contiguous()) { fine = false; return nullptr; }
+            bytes = g->nbytes();
+            return g->data_ptr();
+        }
+        if (!need) return nullptr;
+        t = made({(int64_t)need}, at::kByte, false);
+        bytes = need;
+        return t.data_ptr();
+    }
+};
+
+// The code of an activation's name; -1 for none
+inline int activation_of(PyObject *o) {
+    static const char *const names[] = {"silu", "gelu", "gelu_tanh", "relu"};
+    if (PyUnicode_Check(o))
+        for (int i = 0; i < 4; ++i)
+            if (PyUnicode_CompareWithASCIIString(o, names[i]) == 0) return i;
+    return -1;
+}
+// The code of a type of floats, by torch's object or by name; 0 for anything else
+inline int32_t float_type_of(PyObject *o) {
+    if (THPDtype_Check(o)) {
+        const at::ScalarType t = reinterpret_cast<THPDtype *>(o)->scalar_type;
+        return t == at::kFloat ? ONNXB_FLOAT : t == at::kHalf ? ONNXB_FLOAT16 : t == at::kBFloat16 ? ONNXB_BFLOAT16 : 0;
+    }
+    if (!PyUnicode_Check(o)) return 0;
+    return PyUnicode_CompareWithASCIIString(o, "float32") == 0 ? ONNXB_FLOAT : PyUnicode_CompareWithASCIIString(o, "float16") == 0 ? ONNXB_FLOAT16
+           : PyUnicode_CompareWithASCIIString(o, "bfloat16") == 0 ? ONNXB_BFLOAT16 : 0;
+}
+
+// quantize_rows(X, Q, scale, stream) -> (Q, scale)
+PyObject *py_quantize_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 4) return slow_path();
+    Views v(a[3]);
+    onnxb_matrix x, q;
+    if (!v.matrix(a[0], x) || !v.fine || x.rows < 1) return slow_path();
+    at::Tensor qt, st;
+    if (a[1] != Py_None) v.matrix(a[1], q);
+    else {
+        const int64_t pitch = (x.cols + 15) / 16 * 16;
+        qt = v.made({x.rows, pitch}, at::kChar);
+        if (pitch != x.cols) qt = qt.narrow(1, 0, x.cols);
+        v.take(qt, q);
+    }
+    float *scale = v.vector(a[2], x.rows);
+    if (!v.fine) return slow_path();
+    if (!scale) {
+        st = v.made({x.rows}, at::kFloat);
+        scale = static_cast<float *>(st.data_ptr());
+    }
+    if (abi.quantize_rows_run(&x, &q, scale, v.stream) != ONNXB_OK) return slow_path();
+    return Py_BuildValue("(NN)", result(a[1], qt), result(a[2], st));
+}
+
+// gemm_int8(A, a_scale, B, b_scale, C, relu, dtype, Y, workspace, stream)
+PyObject *py_gemm_int8(PyObject *, PyObject *const *o, Py_ssize_t n) {
+    if (n != 10) return slow_path();
+    Views v(o[9]);
+    onnxb_matrix a, b, y;
+    if (!v.matrix(o[0], a) || !v.matrix(o[2], b) || !v.fine) return slow_path();
+    const float *sa = v.vector(o[1], a.rows), *sb = v.vector(o[3], b.rows), *c = v.vector(o[4], b.rows);
+    const int relu = PyObject_IsTrue(o[5]);
+    const int32_t type = o[7] == Py_None ? float_type_of(o[6]) : ONNXB_FLOAT;
+    if (PyErr_Occurred()) { PyErr_Clear(); return slow_path(); }
+    if (!v.fine || !type) return slow_path();
+    at::Tensor yt, wt;
+    size_t ws_bytes;
+    v.result(o[7], a.rows, b.rows, type, yt, y);
+    void *ws = v.workspace(o[8], abi.gemm_int8_workspace_bytes(&a, &b), wt, ws_bytes);
+    if (!v.fine || abi.gemm_int8_run(&a, sa, &b, sb, c, relu, &y, ws, ws_bytes, v.stream) != ONNXB_OK) return slow_path();
+    return result(o[7], yt);
+}
+
+// gated(X, Wg, Wu, activation, save, H, G, U, workspace, stream) -> H, or (H, G, U)
+PyObject *py_gated(PyObject *, PyObject *const *o, Py_ssize_t n) {
+    if (n != 10) return slow_path();
+    Views v(o[9]);
+    onnxb_matrix x, wg, wu, h, g, u;
+    if (!v.matrix(o[0], x) || !v.matrix(o[1], wg) || !v.matrix(o[2], wu) || !v.fine) return slow_path();
+    const int activation = activation_of(o[3]), asked = PyObject_IsTrue(o[4]);
+    if (PyErr_Occurred()) { PyErr_Clear(); return slow_path(); }
+    if (activation < 0 || (x.type != ONNXB_FLOAT16 && x.type != ONNXB_BFLOAT16)) return slow_path();
+    const bool save = asked || o[6] != Py_None || o[7] != Py_None;
+    at::Tensor ht, gt, ut, wt;
+    size_t ws_bytes;
+    v.result(o[5], x.rows, wg.rows, x.type, ht, h);
+    if (save) {
+        v.result(o[6], x.rows, wg.rows, x.type, gt, g);
+        v.result(o[7], x.rows, wg.rows, x.type, ut, u);
+    }
+    void *ws = v.workspace(o[8], abi.gated_workspace_bytes(&x, &wg, &wu), wt, ws_bytes);
+    if (!v.fine || abi.gated_run(&x, &wg, &wu, activation, &h, save ? &g : nullptr, save ? &u : nullptr, ws, ws_bytes, v.stream) != ONNXB_OK)
+        return slow_path();
+    if (!save) return result(o[5], ht);
+    return Py_BuildValue("(NNN)", result(o[5], ht), result(o[6], gt), result(o[7], ut));
+}
+
+// gated_int8(A, a_scale, Wg, g_scale, Wu, u_scale, activation, dtype, H, workspace, stream)
+PyObject *py_gated_int8(PyObject *, PyObject *const *o, Py_ssize_t n) {
+    if (n != 11) return slow_path();
+    Views v(o[10]);
+    onnxb_matrix a, wg, wu, h;
+    if (!v.matrix(o[0], a) || !v.matrix(o[2], wg) || !v.matrix(o[4], wu) || !v.fine) return slow_path();
+    const float *sa = v.vector(o[1], a.rows), *sg = v.vector(o[3], wg.rows), *su = v.vector(o[5], wu.rows);
+    const int activation = activation_of(o[6]);
+    const int32_t type = o[8] == Py_None ? float_type_of(o[7]) : ONNXB_FLOAT;
+    if (!v.fine || activation < 0 || !type) return slow_path();
+    at::Tensor ht, wt;
+    size_t ws_bytes;
+    v.result(o[8], a.rows, wg.rows, type, ht, h);
+    void *ws = v.workspace(o[9], abi.gated_workspace_bytes(&a, &wg, &wu), wt, ws_bytes);
+    if (!v.fine || abi.gated_int8_run(&a, sa, &wg, sg, &wu, su, activation, &h, ws, ws_bytes, v.stream) != ONNXB_OK) return slow_path();
+    return result(o[8], ht);
+}
+
+// gated_backward(dH, X, Wg, Wu, G, U, activation, dX wanted, dWg wanted, dWu wanted, dX, dWg, dWu, workspace, stream) -> (dX, dWg, dWu)
+PyObject *py_gated_backward(PyObject *, PyObject *const *o, Py_ssize_t n) {
+    if (n != 15) return slow_path();
+    Views v(o[14]);
+    onnxb_matrix in[6], out[3];
+    onnxb_matrix *ins[6], *outs[3] = {nullptr, nullptr, nullptr};
+    const int activation = activation_of(o[6]);
+    bool want[3];
+    for (int i = 0; i < 3; ++i) want[i] = o[10 + i] != Py_None || PyObject_IsTrue(o[7 + i]) == 1;
+    if (PyErr_Occurred()) { PyErr_Clear(); return slow_path(); }
+    for (int i = 0; i < 6; ++i) {
+        const bool used = i == 1 ? want[1] || want[2] : i == 2 || i == 3 ? want[0] : true;
+        ins[i] = used ? v.matrix(o[i], in[i]) : nullptr;
+        if (used && !ins[i]) return slow_path();
+    }
+    if (!v.fine || activation < 0 || !(want[0] || want[1] || want[2]) || (in[0].type != ONNXB_FLOAT16 && in[0].type != ONNXB_BFLOAT16)) return slow_path();
+    const int64_t width = ins[1] ? in[1].cols : in[2].cols;
+    at::Tensor ts[3], wt;
+    for (int i = 0; i < 3; ++i)
+        if (want[i]) outs[i] = v.result(o[10 + i], i == 0 ? in[0].rows : in[0].cols, width, in[0].type, ts[i], out[i]);
+    size_t ws_bytes;
+    void *ws = v.workspace(o[13], abi.gated_backward_workspace_bytes(ins[0], ins[1], ins[2], ins[3], outs[0], outs[1], outs[2]), wt, ws_bytes);
+    if (!v.fine || abi.gated_backward_run(ins[0], ins[1], ins[2], ins[3], ins[4], ins[5], activation, outs[0], outs[1], outs[2], ws, ws_bytes,
+                                          v.stream) != ONNXB_OK)
+        return slow_path();
+    PyObject *got[3];
+    for (int i = 0; i < 3; ++i) {
+        got[i] = want[i] ? result(o[10 + i], ts[i]) : Py_None;
+        if (!want[i]) Py_INCREF(Py_None);
+    }
+    return Py_BuildValue("(NNN)", got[0], got[1], got[2]);
+}
+
 // Address, type, sizes and strides of a tensor, or of those in a tuple or a dict (whose entry "input" is left out); false for anything else
 bool add_state(PyObject *o, std::vector<int64_t> &out) {
     if (THPVariable_CheckExact(o)) {
@@ -322,6 +557,11 @@ PyMethodDef methods[] = {
     {"gemm", reinterpret_cast<PyCFunction>(&guarded<py_gemm>), METH_FASTCALL, nullptr},
     {"maxpool", reinterpret_cast<PyCFunction>(&guarded<py_maxpool>), METH_FASTCALL, nullptr},
     {"gap", reinterpret_cast<PyCFunction>(&guarded<py_gap>), METH_FASTCALL, nullptr},
+    {"quantize_rows", reinterpret_cast<PyCFunction>(&guarded<py_quantize_rows>), METH_FASTCALL, nullptr},
+    {"gemm_int8", reinterpret_cast<PyCFunction>(&guarded<py_gemm_int8>), METH_FASTCALL, nullptr},
+    {"gated", reinterpret_cast<PyCFunction>(&guarded<py_gated>), METH_FASTCALL, nullptr},
+    {"gated_int8", reinterpret_cast<PyCFunction>(&guarded<py_gated_int8>), METH_FASTCALL, nullptr},
+    {"gated_backward", reinterpret_cast<PyCFunction>(&guarded<py_gated_backward>), METH_FASTCALL, nullptr},
     {"state", reinterpret_cast<PyCFunction>(&guarded<py_state>), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_onnxb_fast", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
