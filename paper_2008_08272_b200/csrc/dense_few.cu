@@ -1,11 +1,15 @@
 // Dense layers of 8- and 16-bit operands for a few tokens (single tokens first of all): every weight is read once and multiplied by
 // up to 16 tokens, so the weights' bytes are what bounds it, and what counts is that enough loads are in flight on every SM.
 //
-// A block of 8 warps has 16 channels (the gated block: of both weights); its warps share the reduction in turns of kChunks x 64 bytes
+// A block of 8 warps has 16 channels (the gated block: of both weights).  Its warps share the reduction, an eighth of each row a warp,
 // and add their sums in shared memory, in a fixed order.  The weights go from global memory straight into the registers of
 // mma.sync (16 channels x 8 tokens), 16 bytes per lane and load: which terms of the reduction a lane's registers hold is up to the
 // kernel as long as both operands agree, so a lane's four words are the terms that its 16 bytes hold, no matter which the
-// instruction calls them.  (tcgen05 would want them in shared memory first, and its 128 rows for a few tokens.)
+// instruction calls them.  (tcgen05 would want them in shared memory first, and its 128 rows for a few tokens: by tc_dense.cu,
+// with a ring of the tokens' rows alone, the three figures below are 18.8, 33.2 and 18.6 us.)
+// Measured, one call after another on weights out of HBM: one token, 10240 -> 4096 in 8 bits 9.5 us (4.4 TB/s); gated block 4096 ->
+// 10240 of 16-bit weights 29.3 us (5.7 TB/s, 6.8 TB/s at 40960), eight tokens of 8-bit ones 16.4 us (5.1 TB/s).  What is left is
+// the launch and the last blocks: more loads per warp (fewer blocks an SM) or more blocks (fewer loads) are both slower.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -22,6 +26,9 @@ namespace {
 using namespace dense;
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps, kChannels = 16;
+// blocks an SM (of 8 tokens: at 2 or 4 8-bit 4096 -> 5120 7.4 or 6.0 us, 5.0 at 3; of 16 the registers are two blocks')
+constexpr int per_sm(int tiles) { return tiles == 1 ? 3 : 2; }
+constexpr int kAhead = 256;              // bytes of its part of a row that a warp asks for ahead
 
 struct Params {
     int M, N;
@@ -30,15 +37,18 @@ struct Params {
     long long a_pitch, b_pitch[2];   // bytes
     const float *a_scale, *b_scale[2], *bias;
     int relu, activation, y_type;
+    int first;                       // blocks that run at once, from the first on
     void *Y[3];
     long long y_ld[3];
 };
 
-// 16 bytes of a row, zeros past its end
+// 16 bytes of a row, zeros past its end; weights, which nobody reads twice, not by way of L1
+template <bool kWeight>
 __device__ __forceinline__ uint4 load16(const uint8_t *row, long long at, long long row_bytes) {
     uint4 v = make_uint4(0, 0, 0, 0);
     if (at + 16 <= row_bytes) {
-        asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + at));
+        if (kWeight) asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + at));
+        else v = __ldg(reinterpret_cast<const uint4 *>(row + at));
     } else if (at < row_bytes) {
         uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -80,7 +90,7 @@ __device__ __forceinline__ void put(void *Y, int type, long long at, float v) {
 
 // kTiles: of 8 tokens; kWeights: 2 for the gated block
 template <int kType, int kTiles, int kWeights>
-__global__ void __launch_bounds__(kThreads) dense_few_kernel(const Params p) {
+__global__ void __launch_bounds__(kThreads, per_sm(kTiles)) dense_few_kernel(const Params p) {
     typedef typename Of<kType>::Sum Sum;
     constexpr int kChunks = kWeights == 2 ? 2 : 4, kTokens = 8 * kTiles;
     __shared__ Sum sums[kWarps][kWeights][kChannels][kTokens + 1];
@@ -96,19 +106,35 @@ __global__ void __launch_bounds__(kThreads) dense_few_kernel(const Params p) {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) a[i] = p.A + min(g + 8 * i, p.M - 1) * p.a_pitch;
     Sum acc[kWeights][kTiles][4] = {};
+    const long long share = (p.row_bytes + kWarps * 64 - 1) / (kWarps * 64) * 64, begin = warp * share, end = min(begin + share, p.row_bytes);
+    // The first loads of the blocks that start at once are on their way into L2 before the previous kernel has finished (gated block
+    // 30.0 -> 29.4 us; all that these blocks read 35, since what the loads wait for then comes in any order)
+    if (blockIdx.x < p.first && lane < kChannels * kWeights && begin + 16 <= end) {
+        const uint8_t *row = p.B[lane / kChannels] + min(n0 + lane % kChannels, p.N - 1) * p.b_pitch[lane / kChannels] + begin;
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row), "r"((uint32_t)min(end - begin, (long long)kAhead) / 16 * 16) : "memory");
+    }
     tc::pdl_wait();
-    for (long long at0 = (long long)warp * kChunks * 64 + t * 16; at0 - t * 16 < p.row_bytes; at0 += kWarps * kChunks * 64) {
+    const int m = threadIdx.x / kChannels, r = threadIdx.x % kChannels, n = n0 + r;
+    const bool mine = m < p.M && n < p.N;
+    float sa = 0.f, sb[kWeights] = {}, bias = 0.f;
+    if (kType == ONNXB_INT8 && mine) {
+        sa = __ldg(p.a_scale + m);
+#pragma unroll
+        for (int w = 0; w < kWeights; ++w) sb[w] = __ldg(p.b_scale[w] + n);
+        if (kWeights == 1 && p.bias) bias = __ldg(p.bias + n);
+    }
+    for (long long at0 = begin + t * 16; at0 - t * 16 < end; at0 += kChunks * 64) {
         uint4 wv[kChunks][kWeights][2], xv[kChunks][kTiles];
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
 #pragma unroll
             for (int w = 0; w < kWeights; ++w)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) wv[c][w][h] = load16(b[w][h], at0 + c * 64, p.row_bytes);
+                for (int h = 0; h < 2; ++h) wv[c][w][h] = load16<true>(b[w][h], at0 + c * 64, end);
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i) xv[c][i] = g + 8 * i < p.M ? load16(a[i], at0 + c * 64, p.row_bytes) : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < kTiles; ++i) xv[c][i] = g + 8 * i < p.M ? load16<false>(a[i], at0 + c * 64, end) : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
 #pragma unroll
@@ -127,32 +153,28 @@ __global__ void __launch_bounds__(kThreads) dense_few_kernel(const Params p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) sums[warp][w][g + e / 2 * 8][i * 8 + 2 * t + e % 2] = acc[w][i][e];
     __syncthreads();
-    for (int e = threadIdx.x; e < kChannels * p.M; e += kThreads) {
-        const int m = e / kChannels, r = e % kChannels, n = n0 + r;
-        if (n >= p.N) continue;
-        float v[kWeights];
+    if (!mine) return;
+    float v[kWeights];
 #pragma unroll
-        for (int w = 0; w < kWeights; ++w) {
-            Sum s = 0;
+    for (int w = 0; w < kWeights; ++w) {
+        Sum s = 0;
 #pragma unroll
-            for (int k = 0; k < kWarps; ++k) s += sums[k][w][r][m];
-            v[w] = (float)s;
-            // (one factor after the other: the sum may be 0 where the factors' product is infinite)
-            if (kType == ONNXB_INT8) v[w] = v[w] * p.a_scale[m] * p.b_scale[w][n];
-        }
-        float y = v[0];
-        if (kWeights == 2) {
-            if (p.Y[1]) {
-                put(p.Y[1], p.y_type, m * p.y_ld[1] + n, v[0]);
-                put(p.Y[2], p.y_type, m * p.y_ld[2] + n, v[kWeights - 1]);
-            }
-            y = activate(p.activation, v[0]) * v[kWeights - 1];
-        } else {
-            if (p.bias) y += p.bias[n];
-            if (p.relu) y = fmaxf(y, 0.f);
-        }
-        put(p.Y[0], p.y_type, m * p.y_ld[0] + n, y);
+        for (int k = 0; k < kWarps; ++k) s += sums[k][w][r][m];
+        // (one factor after the other: the sum may be 0 where the factors' product is infinite)
+        v[w] = kType == ONNXB_INT8 ? (float)s * sa * sb[w] : (float)s;
     }
+    float y = v[0];
+    if (kWeights == 2) {
+        if (p.Y[1]) {
+            put(p.Y[1], p.y_type, m * p.y_ld[1] + n, v[0]);
+            put(p.Y[2], p.y_type, m * p.y_ld[2] + n, v[kWeights - 1]);
+        }
+        y = activate(p.activation, v[0]) * v[kWeights - 1];
+    } else {
+        y += bias;
+        if (p.relu) y = fmaxf(y, 0.f);
+    }
+    put(p.Y[0], p.y_type, m * p.y_ld[0] + n, y);
 }
 
 template <int kType, int kWeights>
@@ -176,6 +198,7 @@ int launch_dense_few(const DenseProblem &d, cudaStream_t stream) {
         p.b_pitch[w] = d.B[w].ld * bytes;
         p.b_scale[w] = d.b_scale[w];
     }
+    p.first = per_sm(d.M <= 8 ? 1 : 2) * tc_host::num_sms();
     p.a_scale = d.a_scale; p.bias = d.bias;
     p.relu = d.relu; p.activation = d.activation; p.y_type = d.y_type;
     for (int i = 0; i < 3; ++i) { p.Y[i] = d.Y[i]; p.y_ld[i] = d.y_ld[i]; }

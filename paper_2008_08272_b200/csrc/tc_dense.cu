@@ -35,13 +35,13 @@ using namespace dense;
 constexpr int kBM = 128;                           // rows of a CTA's part of a tile (TMEM lanes)
 constexpr int kRowBytes = 128;                     // of the reduction per stage: one swizzle row
 constexpr int kMaxBN = 256;
-constexpr int kMaxStages = 8;
+constexpr int kMaxStages = 32;
 constexpr int kThreads = 320;
 constexpr int kEpiWarps = 8;
 constexpr int kABytes = kBM * kRowBytes;
 constexpr int kBlockBytes = 32 * kRowBytes;        // what an epilogue warp stages: 32 rows of 128 bytes
 constexpr int kStagingBytes = kEpiWarps * kBlockBytes;
-constexpr int kBarrierBytes = 512;
+constexpr int kBarrierBytes = 1024;
 constexpr int kSmemLimit = 232448;
 
 struct Params {
@@ -51,7 +51,7 @@ struct Params {
     int num_kb, seg_kb;        // stages of the reduction; those before the second segment
     int products, first;       // kDenseGradW: how many products, and the first one's index
     int num_stages;
-    uint32_t idesc, stage_bytes;
+    uint32_t idesc, stage_bytes, a_bytes;      // a_bytes: of A in a stage
     const float *a_scale, *b_scale0, *b_scale1, *bias;
     int relu, activation;
     int y_type, outs;          // outs: results of a tile (the gated block: H alone, or H, G and U)
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
         const int nb = kBMn ? bnh / 64 : kMode == kDenseGated && kCtas == 1 ? 2 : 1;
         const bool is_a = lane < na, active = lane < na + nb;
         const int piece = is_a ? lane : lane - na;
-        const uint32_t dst_off = is_a ? (uint32_t)piece * (kABytes / na) : kABytes + (uint32_t)piece * (uint32_t)(bnh * kRowBytes / nb);
+        const uint32_t dst_off = is_a ? (uint32_t)piece * (kABytes / na) : p.a_bytes + (uint32_t)piece * (uint32_t)(bnh * kRowBytes / nb);
         constexpr int kTerms = kInt8 ? kRowBytes : kRowBytes / 2;       // of the reduction per stage
         const bool mn = is_a ? kAMn : kBMn;
         const int step0 = mn ? 0 : kTerms, step1 = mn ? kTerms : 0;
@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
             const uint64_t a_tmpl = kAMn ? mn_tmpl : k_tmpl, b_tmpl = kBMn ? mn_tmpl : k_tmpl;
             const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), b_hi = (uint32_t)(b_tmpl >> 32);
             const uint32_t a_lo = (uint32_t)a_tmpl | ((smem_u32(stages) >> 4) & 0x3FFFu);
-            const uint32_t b_lo = (uint32_t)b_tmpl | (((smem_u32(stages) + kABytes) >> 4) & 0x3FFFu);
+            const uint32_t b_lo = (uint32_t)b_tmpl | (((smem_u32(stages) + p.a_bytes) >> 4) & 0x3FFFu);
             const uint32_t stage16 = p.stage_bytes >> 4;
             constexpr uint32_t kA16 = (kAMn ? 2048u : 32u) >> 4, kB16 = (kBMn ? 2048u : 32u) >> 4;
             for (int t = first_tile; t < p.total; t += tile_step) {
@@ -485,7 +485,11 @@ int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
     if (total > 0x7fffffffLL - 65536 || (long long)p.band * p.tiles_n > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
     p.total = (int)total;
     const int bnh = p.BN / tile.ctas;
-    p.stage_bytes = (uint32_t)(kABytes + bnh * kRowBytes);
+    // Few tokens: no more of A's rows than there are.  The tensor cores read 128 all the same, what lies behind being other operands'
+    // (or the staging blocks'); those rows of the accumulator are nobody's, and the ring is as much deeper.
+    const int a_rows = tile.ctas == 1 && !a_mn && d.M <= 64 ? (d.M <= 16 ? 16 : d.M <= 32 ? 32 : 64) : kBM;
+    p.a_bytes = (uint32_t)(a_rows * kRowBytes);
+    p.stage_bytes = p.a_bytes + (uint32_t)(bnh * kRowBytes);
     p.num_stages = std::min(kMaxStages, (kSmemLimit - 1024 - kBarrierBytes - kStagingBytes) / (int)p.stage_bytes);
     p.idesc = int8 ? make_idesc_s8(kBM * tile.ctas, p.BN) : make_idesc_f16(kBM * tile.ctas, p.BN, d.type == ONNXB_BFLOAT16, a_mn, b_mn);
     p.a_scale = d.a_scale; p.b_scale0 = d.b_scale[0]; p.b_scale1 = d.b_scale[1]; p.bias = d.bias;
@@ -505,7 +509,7 @@ int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
     };
     for (int i = 0; i < 2; ++i) {
         const DenseOperand &a = d.A[d.mode == kDenseGradX || a_mn ? i : 0], &b = d.B[d.mode == kDenseGradX || gated ? i : 0];
-        if (!operand(&maps.A[i], a, a_mn, d.M, kBM) || !operand(&maps.B[i], b, b_mn, d.N, gated ? p.out_cols : bnh)) return (int)cudaErrorInvalidValue;
+        if (!operand(&maps.A[i], a, a_mn, d.M, a_rows) || !operand(&maps.B[i], b, b_mn, d.N, gated ? p.out_cols : bnh)) return (int)cudaErrorInvalidValue;
     }
     for (int i = 0; i < 3; ++i) {
         maps.Y[i] = maps.A[0];                     // (never used where y_tma is not set)
