@@ -70,6 +70,29 @@ __global__ void __launch_bounds__(256) gated_slope_kernel(const GatedSlopeProble
     }
 }
 
+// Four columns a thread, 8 rows by 128 columns a block
+template <typename T>
+__global__ void __launch_bounds__(256) sum_parts_kernel(const SumPartsProblem p) {
+    const int j = (blockIdx.x * 32 + threadIdx.x % 32) * 4;
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
+    if (j >= p.N) return;
+    for (int i = blockIdx.y * 8 + threadIdx.x / 32; i < p.M; i += gridDim.y * 8) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int s = 0; s < p.parts; ++s) {
+            const float4 w = __ldg(reinterpret_cast<const float4 *>(p.P + ((long long)s * p.part_rows + i) * p.p_ld + j));
+            v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
+        }
+        T *y = static_cast<T *>(p.Y) + i * p.y_ld + j;
+        alignas(8) const T out[4] = {from_float<T>(v.x), from_float<T>(v.y), from_float<T>(v.z), from_float<T>(v.w)};
+        if (j + 4 <= p.N && reinterpret_cast<uintptr_t>(y) % 8 == 0) *reinterpret_cast<uint2 *>(y) = *reinterpret_cast<const uint2 *>(out);
+        else
+            for (int e = 0; e < 4; ++e)
+                if (j + e < p.N) y[e] = out[e];
+    }
+}
+
 template <typename T>
 int launch_slope(const GatedSlopeProblem &p, cudaStream_t stream) {
     auto aligned = [&](const DenseOperand &o) { return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && (p.M == 1 || o.ld % 8 == 0); };
@@ -90,6 +113,14 @@ int launch_repack_rows(const void *src, long long src_pitch, int rows, long long
     repack_rows_kernel<<<grid, 256, 0, stream>>>(static_cast<const uint8_t *>(src), src_pitch, chunks, total, row_bytes, static_cast<uint8_t *>(dst), dst_pitch);
     count_launch();
     return (int)cudaGetLastError();
+}
+
+int launch_sum_parts(const SumPartsProblem &p, cudaStream_t stream) {
+    const dim3 grid((p.N + 127) / 128, std::min(65535, (p.M + 7) / 8));
+    const cudaError_t e = p.type == ONNXB_FLOAT16 ? tc_host::launch_pdl(sum_parts_kernel<__half>, grid, dim3(256), 0, stream, p)
+                                                  : tc_host::launch_pdl(sum_parts_kernel<__nv_bfloat16>, grid, dim3(256), 0, stream, p);
+    count_launch();
+    return (int)e;
 }
 
 int launch_gated_slope(const GatedSlopeProblem &p, cudaStream_t stream) {

@@ -7,13 +7,11 @@
 
 namespace onnxb {
 
-// What is multiplied and what becomes of the sums.  "Rows" of an operand run along the output's rows (A) or columns (B); an operand is
-// MN-major when they are the contiguous ones in memory, K-major when the reduction is.
+// What is multiplied and what becomes of the sums
 enum DenseMode {
     kDensePlain = 0,     // Y[0] = A[0] B[0]^T, scaled
     kDenseGated = 1,     // G = A[0] B[0]^T, U = A[0] B[1]^T; Y[0] = act(G) U, Y[1] = G and Y[2] = U where they are kept
-    kDenseGradX = 2,     // Y[0] = A[0] B[0] + A[1] B[1], B MN-major
-    kDenseGradW = 3      // Y[z] = A[z]^T B[0], z = 0, 1 (of those that are not NULL), both MN-major
+    kDenseGrad = 2       // dX = Y[0] = A[0] B[0] + A[1] B[1], dWg = Y[1] = A[0]^T B[2], dWu = Y[2] = A[1]^T B[2]; those that are not NULL
 };
 
 struct DenseOperand {
@@ -24,13 +22,14 @@ struct DenseOperand {
 struct DenseProblem {
     int mode;
     int type;            // of the operands
-    int M, N, K;         // of one product
-    DenseOperand A[2], B[2];
+    int M, N, K;         // tokens; columns of the results; the other size (of the gradients: channels)
+    DenseOperand A[2], B[3];
     const float *a_scale, *b_scale[2], *bias;      // 8-bit operands
     int relu, activation;
     int y_type;
     void *Y[3];
     long long y_ld[3];
+    void *partial;       // kDenseGrad: tc_grad_workspace bytes
 };
 
 inline int type_bytes(int type) { return type == ONNXB_FLOAT ? 4 : type == ONNXB_INT8 ? 1 : 2; }
@@ -41,6 +40,18 @@ bool dense_few_fits(const DenseProblem &p);
 int launch_dense_few(const DenseProblem &p, cudaStream_t stream);
 // On the tensor cores (tc_dense.cu).  Operands' rows begin at multiples of 16 bytes.
 int launch_tc_dense(const DenseProblem &p, cudaStream_t stream);
+// Scratch that the gradients' products need (dX in parts of its long reduction, where there would be few tiles)
+size_t tc_grad_workspace(int tokens, int channels, int width, bool dX, int weights);
+
+// Y[i,j] = the sum over s < parts of P[s * part_rows + i][j], in that order, rounded to `type`; P's rows p_ld floats apart (a multiple of 4)
+struct SumPartsProblem {
+    int parts, part_rows, M, N, type;
+    const float *P;
+    long long p_ld;
+    void *Y;
+    long long y_ld;
+};
+int launch_sum_parts(const SumPartsProblem &p, cudaStream_t stream);
 
 // dG = dH U act'(G), dU = dH act(G), each [M,F]; all of one 16-bit type
 struct GatedSlopeProblem {

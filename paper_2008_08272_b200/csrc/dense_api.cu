@@ -189,7 +189,10 @@ static size_t slope_bytes(int64_t M, int64_t F) { return (size_t)(M * slope_pitc
 extern "C" size_t onnx_gated_backward_workspace_bytes(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
                                                       const onnxb_matrix *dX, const onnxb_matrix *dWg, const onnxb_matrix *dWu) {
     if (!dH || dH->rows < 1 || dH->cols < 1 || dH->rows > kMostSize || dH->cols > kMostSize) return 0;
-    return 2 * slope_bytes(dH->rows, dH->cols) + (dX ? copy_bytes(Wg) + copy_bytes(Wu) : 0) + (dWg || dWu ? copy_bytes(X) : 0);
+    const onnxb_matrix *one = dX ? dX : dWg ? dWg : dWu;
+    if (!one || one->cols < 1 || one->cols > kMostSize) return 0;
+    return 2 * slope_bytes(dH->rows, dH->cols) + (dX ? copy_bytes(Wg) + copy_bytes(Wu) : 0) + (dWg || dWu ? copy_bytes(X) : 0) +
+           tc_grad_workspace((int)dH->rows, (int)dH->cols, (int)one->cols, dX != nullptr, (dWg != nullptr) + (dWu != nullptr));
 }
 
 extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
@@ -243,26 +246,20 @@ extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const on
     ws += 2 * slope_bytes(M, F);
     int err = launch_gated_slope(s, stream);
     DenseProblem d{};
+    d.mode = kDenseGrad;
     d.type = d.y_type = dH->type;
+    d.M = (int)M; d.N = (int)K; d.K = (int)F;
     d.A[0] = DenseOperand{s.dG, s.d_ld};
     d.A[1] = DenseOperand{s.dU, s.d_ld};
-    if (err == 0 && dX) {
-        d.mode = kDenseGradX;
-        d.M = (int)M; d.N = (int)K; d.K = (int)F;
+    if (dX) {
         d.B[0] = placed(Wg, ws, err, stream);
         d.B[1] = placed(Wu, ws, err, stream);
-        d.Y[0] = dX->data; d.y_ld[0] = operand(dX).ld;
-        if (err == 0) err = launch_dense(d, stream);
     }
-    if (err == 0 && weights) {
-        d.mode = kDenseGradW;
-        d.M = (int)F; d.N = (int)K; d.K = (int)M;
-        d.B[0] = placed(X, ws, err, stream);
-        for (int z = 0; z < 2; ++z) {
-            d.Y[z] = outs[1 + z] ? outs[1 + z]->data : nullptr;
-            d.y_ld[z] = outs[1 + z] ? operand(outs[1 + z]).ld : 0;
-        }
-        if (err == 0) err = launch_dense(d, stream);
+    if (weights) d.B[2] = placed(X, ws, err, stream);
+    for (int i = 0; i < 3; ++i) {
+        d.Y[i] = outs[i] ? outs[i]->data : nullptr;
+        d.y_ld[i] = outs[i] ? operand(outs[i]).ld : 0;
     }
-    return status_of(err);
+    d.partial = ws;
+    return status_of(err ? err : launch_tc_dense(d, stream));
 }

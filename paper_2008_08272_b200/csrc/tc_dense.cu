@@ -10,14 +10,17 @@
 //   - The gated block is one product: half of a tile's B rows are Wg's, half Wu's of the same channels, so that an accumulator holds
 //     a channel's gate in column j and its other factor in column BN/2 + j, in the same TMEM lane.  X is read once for both, and
 //     the pair's form costs nothing: each CTA stages one of the two.
+//   - The gradients are one launch: dX's tiles, which are few and long, then those of dWg and dWu, handed out so that the units that got
+//     one tile of dX less get as many more of the others as that one takes.
 //   - dX = dG Wg + dU Wu is one sum: the reduction runs over dG's channels, then dU's, with the other tensor maps from there on.
-//   - dWg and dWu = dG^T X and dU^T X take their operands as they lie, the reduction (tokens) along the rows: MN-major, 64 x 64 boxes.
-//     The same for Wg and Wu in dX.  No transposed copy is made.
+//   - dWg = dG^T X and dWu = dU^T X take their operands as they lie, the reduction (tokens) along the rows: MN-major, 64 x 64 boxes.
+//     The same for Wg and Wu in dX.  No transposed copy is made, and dG's map serves both uses: its boxes are 64 x 64 either way.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdlib>
 
 #include "dense.h"
@@ -48,8 +51,13 @@ struct Params {
     int M, N;                  // of the output
     int BN, out_cols;          // columns of an accumulator; of the output per tile (half of them for the gated block)
     int tiles_m, tiles_n, band, total;
-    int num_kb, seg_kb;        // stages of the reduction; those before the second segment
-    int products, first;       // kDenseGradW: how many products, and the first one's index
+    int num_kb;                // stages of the reduction
+    // kDenseGrad.  dX: row tiles, all tiles (of all parts of the reduction), stages (half of them of the first of its two terms), parts,
+    // stages of a part, rows of a part's plane.  dWg and dWu: row tiles, all tiles, stages, the first that is wanted, tiles that a
+    // unit with one tile of dX less takes before the others.
+    int x_tiles_m, x_tiles, x_kb, x_parts, x_part_kb, x_part_rows;
+    int channels, w_tiles_m, w_tiles, w_kb, w_first, w_before;
+    uint32_t idesc_x;
     int num_stages;
     uint32_t idesc, stage_bytes, a_bytes;      // a_bytes: of A in a stage
     const float *a_scale, *b_scale0, *b_scale1, *bias;
@@ -62,21 +70,51 @@ struct Params {
 };
 
 struct Maps {
-    CUtensorMap A[2], B[2], Y[3];
+    CUtensorMap A[2], B[3], Y[3];
 };
 
-// Tiles in the order they are run in: product by product, in bands of `band` row tiles, a band's columns one after the other, so that
-// the tiles in flight share their operands in L2 (of 148 SMs' 74 pairs at band 8: 8 row tiles and 9 column tiles).
 struct TileAt {
-    int z, tm, tn;
+    int tm, tn, z;             // z: the product, or the part of dX's reduction
+    int kb0, kb1;              // stages
+    bool x;                    // a tile of dX
 };
-__device__ __forceinline__ TileAt tile_at(const Params &p, int t) {
-    const int per = p.tiles_m * p.tiles_n;
-    const int z = t / per, r = t - z * per;
-    const int b = r / (p.band * p.tiles_n), rr = r - b * p.band * p.tiles_n;
-    const int rows = min(p.band, p.tiles_m - b * p.band);
-    const int tn = rr / rows;
-    return TileAt{z, b * p.band + rr - tn * rows, tn};
+// Tiles of one product lie in bands of `band` row tiles, a band's columns one after the other, so that the tiles in flight share
+// their operands in L2 (of 148 SMs' 74 pairs at band 8: 8 row tiles and 9 column tiles).
+__device__ __forceinline__ void place(const Params &p, int tiles_m, int t, TileAt &at) {
+    const int per = tiles_m * p.tiles_n;
+    at.z = t / per;
+    const int r = t - at.z * per, b = r / (p.band * p.tiles_n), rr = r - b * p.band * p.tiles_n;
+    const int rows = min(p.band, tiles_m - b * p.band);
+    at.tn = rr / rows;
+    at.tm = b * p.band + rr - at.tn * rows;
+}
+// The n-th tile of a unit (a CTA or a pair) of `units`; false: there is none
+template <int kMode>
+__device__ __forceinline__ bool nth_tile(const Params &p, int unit, int units, int n, TileAt &at) {
+    at.x = false;
+    at.kb0 = 0;
+    at.kb1 = kMode == kDenseGrad ? p.w_kb : p.num_kb;
+    if (kMode != kDenseGrad) {
+        const int t = unit + n * units;
+        if (t >= p.total) return false;
+        place(p, p.tiles_m, t, at);
+        return true;
+    }
+    const int longer = p.x_tiles % units, own = p.x_tiles / units + (unit < longer);        // (units with one tile of dX more)
+    if (n < own) {
+        place(p, p.x_tiles_m, unit + n * units, at);
+        at.x = true;
+        at.kb0 = at.z * p.x_part_kb;
+        at.kb1 = min(at.kb0 + p.x_part_kb, p.x_kb);
+        return true;
+    }
+    const int m = n - own, before = longer && unit >= longer ? p.w_before : 0;
+    int t;
+    if (m < before) t = unit - longer + m * (units - longer);
+    else t = (longer ? p.w_before * (units - longer) : 0) + (m - before) * units + (unit >= longer ? unit - longer : unit - longer + units);
+    if (t >= p.w_tiles) return false;
+    place(p, p.w_tiles_m, t, at);
+    return true;
 }
 
 // Two 32-bit results as one word of 16-bit ones
@@ -95,7 +133,7 @@ __device__ __forceinline__ uint32_t pack<__nv_bfloat162>(float a, float b) {
 
 template <int kCtas, bool kInt8, int kMode>
 __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_constant__ Maps maps, const Params p) {
-    constexpr bool kAMn = kMode == kDenseGradW, kBMn = kMode == kDenseGradW || kMode == kDenseGradX;
+    constexpr bool kGrad = kMode == kDenseGrad;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t *stages = smem;
@@ -107,7 +145,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = kCtas == 2 ? (int)cluster_ctarank() : 0;
-    const int first_tile = blockIdx.x / kCtas, tile_step = gridDim.x / kCtas;
+    const int unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
+    TileAt at;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.num_stages; ++s) {
@@ -141,49 +180,45 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
         uint32_t phase = 0;
         const uint32_t full_issuer = kCtas == 2 ? map_to_cta(smem_u32(&full[0]), 0) : 0u;
         const int bnh = p.BN / kCtas;                                   // B rows that this CTA stages
-        const int na = kAMn ? kBM / 64 : 1;
-        const int nb = kBMn ? bnh / 64 : kMode == kDenseGated && kCtas == 1 ? 2 : 1;
+        const int na = kGrad ? kBM / 64 : 1;
+        const int nb = kGrad ? bnh / 64 : kMode == kDenseGated && kCtas == 1 ? 2 : 1;
         const bool is_a = lane < na, active = lane < na + nb;
         const int piece = is_a ? lane : lane - na;
         const uint32_t dst_off = is_a ? (uint32_t)piece * (kABytes / na) : p.a_bytes + (uint32_t)piece * (uint32_t)(bnh * kRowBytes / nb);
         constexpr int kTerms = kInt8 ? kRowBytes : kRowBytes / 2;       // of the reduction per stage
-        const bool mn = is_a ? kAMn : kBMn;
-        const int step0 = mn ? 0 : kTerms, step1 = mn ? kTerms : 0;
-        bool first = true;
-        for (int t = first_tile; t < p.total; t += tile_step) {
-            const TileAt at = tile_at(p, t);
-            const int z = kMode == kDenseGradW ? p.first + at.z : 0;
-            // the first of the rows that this copy brings
-            int row;
-            const CUtensorMap *map = is_a ? &maps.A[z] : &maps.B[0];
-            if (is_a) {
-                row = (at.tm * kCtas + rank) * kBM + piece * 64;        // (of MN-major pieces; else piece is 0)
-            } else if (kMode == kDenseGated) {
+        for (int n = 0; nth_tile<kMode>(p, unit, units, n, at); ++n) {
+            // the first of the rows that this copy brings (along the output's rows or columns), and whether they lie along a row in memory
+            int row = is_a ? (at.tm * kCtas + rank) * kBM : at.tn * p.BN + rank * bnh;
+            if (kGrad) row += piece * 64;
+            const bool mn = kGrad && !(is_a && at.x);
+            const CUtensorMap *map = is_a ? &maps.A[0] : &maps.B[0];
+            int term = at.kb0 * kTerms;
+            if (kMode == kDenseGated && !is_a) {
                 // a pair's CTA has one of the two weights, a lone CTA both
                 row = at.tn * p.out_cols;
                 map = &maps.B[kCtas == 2 ? rank : piece & 1];
-            } else {
-                row = at.tn * p.BN + rank * bnh + piece * 64;
             }
-            int c0 = mn ? row : 0, c1 = mn ? 0 : row;
-            if (first) pdl_wait();
-            first = false;
-            for (int kb = 0; kb < p.num_kb; ++kb) {
+            if (kGrad && !at.x) map = is_a ? &maps.A[p.w_first + at.z] : &maps.B[2];
+            if (kGrad && at.x && at.kb0 * 2 >= p.x_kb) {
+                map += 1;
+                term -= p.x_kb / 2 * kTerms;
+            }
+            if (n == 0) pdl_wait();
+            for (int kb = at.kb0; kb < at.kb1; ++kb) {
                 mbar_wait(&empty[stage], phase ^ 1, p.err, 1);
                 if (lane == 0 && rank == 0) mbar_arrive_expect_tx(&full[stage], p.stage_bytes * kCtas);
                 __syncwarp();
-                if (kMode == kDenseGradX && kb == p.seg_kb) {
-                    map = is_a ? &maps.A[1] : &maps.B[1];
-                    c0 = mn ? row : 0;
-                    c1 = mn ? 0 : row;
+                if (kGrad && at.x && kb > at.kb0 && kb * 2 == p.x_kb) {
+                    map += 1;
+                    term = 0;
                 }
                 uint8_t *dst = stages + (size_t)stage * p.stage_bytes + dst_off;
                 if (active) {
+                    const int c0 = mn ? row : term, c1 = mn ? term : row;
                     if (kCtas == 2) tma_load_2d_pair(dst, map, full_issuer + (uint32_t)stage * 8u, c0, c1);
                     else tma_load_2d(dst, map, &full[stage], c0, c1);
                 }
-                c0 += step0;
-                c1 += step1;
+                term += kTerms;
                 if (++stage == p.num_stages) { stage = 0; phase ^= 1; }
             }
         }
@@ -195,30 +230,33 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
             // K-major: 8-row groups 1024 bytes apart, an instruction 32 bytes further along the swizzled rows.  MN-major: blocks of 64
             // rows or columns 64 x 128 bytes apart, groups of 8 terms 1024 bytes apart, an instruction two of those further.
             const uint64_t k_tmpl = make_smem_desc(0, 16, 1024, kSwizzle128B), mn_tmpl = make_smem_desc(0, 64 * kRowBytes, 1024, kSwizzle128B);
-            const uint64_t a_tmpl = kAMn ? mn_tmpl : k_tmpl, b_tmpl = kBMn ? mn_tmpl : k_tmpl;
-            const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), b_hi = (uint32_t)(b_tmpl >> 32);
-            const uint32_t a_lo = (uint32_t)a_tmpl | ((smem_u32(stages) >> 4) & 0x3FFFu);
-            const uint32_t b_lo = (uint32_t)b_tmpl | (((smem_u32(stages) + p.a_bytes) >> 4) & 0x3FFFu);
+            const uint64_t b_tmpl = kGrad ? mn_tmpl : k_tmpl;
+            const uint32_t b_hi = (uint32_t)(b_tmpl >> 32);
+            const uint32_t a_at = (smem_u32(stages) >> 4) & 0x3FFFu, b_lo = (uint32_t)b_tmpl | (((smem_u32(stages) + p.a_bytes) >> 4) & 0x3FFFu);
             const uint32_t stage16 = p.stage_bytes >> 4;
-            constexpr uint32_t kA16 = (kAMn ? 2048u : 32u) >> 4, kB16 = (kBMn ? 2048u : 32u) >> 4;
-            for (int t = first_tile; t < p.total; t += tile_step) {
+            constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kB16 = kGrad ? kMn16 : kK16;
+            for (int n = 0; nth_tile<kMode>(p, unit, units, n, at); ++n) {
+                const bool a_mn = kGrad && !at.x;
+                const uint64_t a_tmpl = a_mn ? mn_tmpl : k_tmpl;
+                const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), a_lo = (uint32_t)a_tmpl | a_at, a16 = a_mn ? kMn16 : kK16;
+                const uint32_t idesc = kGrad && at.x ? p.idesc_x : p.idesc;
                 if (kCtas == 2) mbar_wait_cluster(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 else mbar_wait(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 tc_fence_after_sync();
                 const uint32_t d_tmem = tmem_base + (uint32_t)acc * kMaxBN;
                 uint32_t accumulate = 0;
-                for (int kb = 0; kb < p.num_kb; ++kb) {
+                for (int kb = at.kb0; kb < at.kb1; ++kb) {
                     mbar_wait(&full[stage], phase, p.err, 3);
                     tc_fence_after_sync();
                     const uint32_t al = a_lo + (uint32_t)stage * stage16, bl = b_lo + (uint32_t)stage * stage16;
 #pragma unroll
                     for (uint32_t k = 0; k < 4; ++k) {
                         if (kInt8) {
-                            if (kCtas == 2) mma_i8_lohi_pair(d_tmem, al + k * kA16, a_hi, bl + k * kB16, b_hi, p.idesc, accumulate);
-                            else mma_i8_lohi(d_tmem, al + k * kA16, a_hi, bl + k * kB16, b_hi, p.idesc, accumulate);
+                            if (kCtas == 2) mma_i8_lohi_pair(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
+                            else mma_i8_lohi(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
                         } else {
-                            if (kCtas == 2) mma_f16_lohi_pair(d_tmem, al + k * kA16, a_hi, bl + k * kB16, b_hi, p.idesc, accumulate);
-                            else mma_f16_lohi(d_tmem, al + k * kA16, a_hi, bl + k * kB16, b_hi, p.idesc, accumulate);
+                            if (kCtas == 2) mma_f16_lohi_pair(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
+                            else mma_f16_lohi(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
                         }
                         accumulate = 1;
                     }
@@ -237,19 +275,20 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
         pdl_wait();
         const int q = warp & 3, half = (warp - 2) >> 2;
         uint8_t *buf = staging + (warp - 2) * kBlockBytes;
-        const bool wide = p.y_type == ONNXB_FLOAT;
-        const int block_cols = wide ? 32 : 64;                 // columns of 128 bytes
         int acc = 0;
         uint32_t acc_phase = 0;
         const uint32_t peer_tmem_empty = kCtas == 2 ? map_to_cta(smem_u32(&tmem_empty[0]), 0) : 0u;
-        for (int t = first_tile; t < p.total; t += tile_step) {
-            const TileAt at = tile_at(p, t);
+        for (int n = 0; nth_tile<kMode>(p, unit, units, n, at); ++n) {
+            // 32-bit results: of 8-bit operands where asked for, and the parts of a dX whose reduction is shared
+            const bool parts = kGrad && at.x && p.x_parts > 1, wide = kGrad ? parts : p.y_type == ONNXB_FLOAT;
+            const int block_cols = wide ? 32 : 64;             // columns of 128 bytes
+            const int M = kGrad && !at.x ? p.channels : p.M;
             const int row0 = (at.tm * kCtas + rank) * kBM + q * 32, row = row0 + lane;
             const int n0 = at.tn * p.out_cols, cols = min(p.out_cols, p.N - n0);
             const int blocks = (cols + block_cols - 1) / block_cols;
             const int lo = half ? (blocks + 1) / 2 : 0, hi = half ? blocks : (blocks + 1) / 2;
             // Scales and addends: the row's, and this lane's column's of the chunk of 32 that comes next, asked for ahead of it
-            const float sa = kInt8 && row < p.M ? __ldg(p.a_scale + row) : 0.f;
+            const float sa = kInt8 && row < M ? __ldg(p.a_scale + row) : 0.f;
             float s0 = 0.f, s1 = 0.f;                          // (s1: Wu's scale, or the plain product's addend)
             auto fetch = [&](int col) {
                 const bool in = col + lane < cols;
@@ -259,10 +298,10 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
             if (kInt8) fetch(lo * block_cols);
             mbar_wait(&tmem_full[acc], acc_phase, p.err, 4);
             tc_fence_after_sync();
-            if (row0 < p.M) {
+            if (row0 < M) {
                 const uint32_t tbase = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * kMaxBN);
                 for (int which = 0; which < p.outs; ++which) {
-                    const int y = kMode == kDenseGradW ? p.first + at.z : which;
+                    const int y = !kGrad ? which : at.x ? 0 : 1 + p.w_first + at.z;
 #pragma unroll 1
                     for (int b = lo; b < hi; ++b) {
                         // (TMA writes whole pieces of 16 bytes: not where the last columns fill none, since what follows is not Y's)
@@ -342,13 +381,13 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                             fence_proxy_async_smem();
                             __syncwarp();
                             if (lane == 0) {
-                                tma_store_2d(&maps.Y[y], buf, col0, row0);
+                                tma_store_2d(&maps.Y[y], buf, col0, parts ? at.z * p.x_part_rows + row0 : row0);
                                 tma_store_commit();
                             }
                         } else {
                             // rows that TMA cannot address: read back row by row, a word per lane
                             __syncwarp();
-                            const int rows = min(32, p.M - row0), left = cols - b * block_cols;
+                            const int rows = min(32, M - row0), left = cols - b * block_cols;
                             for (int r = 0; r < rows; ++r) {
                                 const uint32_t word = *reinterpret_cast<const uint32_t *>(buf + r * kRowBytes + ((((lane >> 2) ^ (r & 7)) << 4) | ((lane & 3) << 2)));
                                 const long long at_row = (long long)(row0 + r) * p.y_ld[y] + col0;
@@ -392,9 +431,7 @@ typedef void (*Kernel)(const Maps, const Params);
 template <int kCtas>
 Kernel kernel_for(int mode, bool int8) {
     if (int8) return mode == kDenseGated ? tc_dense_kernel<kCtas, true, kDenseGated> : tc_dense_kernel<kCtas, true, kDensePlain>;
-    return mode == kDenseGated   ? tc_dense_kernel<kCtas, false, kDenseGated>
-           : mode == kDenseGradX ? tc_dense_kernel<kCtas, false, kDenseGradX>
-                                 : tc_dense_kernel<kCtas, false, kDenseGradW>;
+    return mode == kDenseGated ? tc_dense_kernel<kCtas, false, kDenseGated> : tc_dense_kernel<kCtas, false, kDenseGrad>;
 }
 
 // CTA pairs that run at once, asked of the device's occupancy once (as for tc_gemm_kernel, whose shared memory and threads are the same)
@@ -430,30 +467,33 @@ int max_pairs() {
 struct Tile {
     int ctas, BN;
 };
-bool tile_allowed(const DenseProblem &d, Tile t) {
-    const bool b_mn = d.mode == kDenseGradX || d.mode == kDenseGradW;
+bool tile_allowed(int mode, Tile t) {
     if (t.BN < 32 * t.ctas || t.BN > kMaxBN || t.BN % (32 * t.ctas)) return false;
-    if (d.mode == kDenseGated) return t.BN % 64 == 0 && (t.BN == 64 || t.BN % 128 == 0);
-    return !b_mn || t.BN % (64 * t.ctas) == 0;
+    if (mode == kDenseGated) return t.BN % 64 == 0 && (t.BN == 64 || t.BN % 128 == 0);
+    return mode != kDenseGrad || t.BN % (64 * t.ctas) == 0;
 }
-Tile pick_tile(const DenseProblem &d, int products, int num_kb) {
-    if (const char *e = getenv("ONNXB_DENSE_TILE")) {          // "<CTAs>x<BN>" pins the shape for A/B measurements and tests
-        const Tile t{e[0] - '0', e[0] && e[1] == 'x' ? atoi(e + 2) : 0};
-        if ((t.ctas == 1 || t.ctas == 2) && tile_allowed(d, t)) return t;
-    }
-    Tile best{1, 64};
+// "<CTAs>x<BN>" in ONNXB_DENSE_TILE pins the shape for A/B measurements and tests
+bool pinned_tile(int mode, Tile &t) {
+    const char *e = getenv("ONNXB_DENSE_TILE");
+    if (!e) return false;
+    t = Tile{e[0] - '0', e[0] && e[1] == 'x' ? atoi(e + 2) : 0};
+    return (t.ctas == 1 || t.ctas == 2) && tile_allowed(mode, t);
+}
+double stage_cycles(Tile t) { return std::max(2.0 * t.BN, (128.0 + t.BN / t.ctas) * kRowBytes / 50.0) + 30.0; }
+double epilogue_cycles(Tile t) { return 1000.0 + 12.0 * t.BN; }
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+Tile pick_tile(const DenseProblem &d, int num_kb) {
+    Tile best{1, 64}, t;
+    if (pinned_tile(d.mode, t)) return t;
     double best_cost = 1e300;
-    for (int ctas = 1; ctas <= 2; ++ctas)
-        for (int bn = 32; bn <= kMaxBN; bn += 32) {
-            const Tile t{ctas, bn};
-            if (!tile_allowed(d, t)) continue;
-            const int out_cols = d.mode == kDenseGated ? bn / 2 : bn;
-            const long long tiles = (long long)((d.M + kBM * ctas - 1) / (kBM * ctas)) * ((d.N + out_cols - 1) / out_cols) * products;
-            const int units = ctas == 2 ? max_pairs() : tc_host::num_sms();
-            const double waves = (double)((tiles + units - 1) / units);
-            const double stage = std::max(2.0 * bn, (128.0 + bn / ctas) * kRowBytes / 50.0) + 30.0;
-            const double epilogue = 1000.0 + 12.0 * bn;
-            const double cost = waves * std::max(num_kb * stage, epilogue) + epilogue;
+    for (t.ctas = 1; t.ctas <= 2; ++t.ctas)
+        for (t.BN = 32; t.BN <= kMaxBN; t.BN += 32) {
+            if (!tile_allowed(d.mode, t)) continue;
+            const int out_cols = d.mode == kDenseGated ? t.BN / 2 : t.BN;
+            const long long tiles = ceil_div(d.M, kBM * t.ctas) * ceil_div(d.N, out_cols);
+            const double waves = (double)ceil_div(tiles, t.ctas == 2 ? max_pairs() : tc_host::num_sms());
+            const double cost = waves * std::max(num_kb * stage_cycles(t), epilogue_cycles(t)) + epilogue_cycles(t);
             if (cost < best_cost * (1 - 1e-9)) {
                 best_cost = cost;
                 best = t;
@@ -462,36 +502,117 @@ Tile pick_tile(const DenseProblem &d, int products, int num_kb) {
     return best;
 }
 
+// The gradients' tiles, and the parts of dX's reduction, each with an fp32 plane that sum_parts_kernel adds up.  From the sizes alone (as a B200
+// has 148 SMs), since the workspace depends on it.
+struct GradPlan {
+    Tile tile;
+    int parts;
+};
+constexpr int kGradTerms = kRowBytes / 2;
+GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
+    GradPlan best{{1, 64}, 1};
+    double best_cost = 1e300;
+    Tile pinned;
+    const bool pin = pinned_tile(kDenseGrad, pinned);
+    const char *pin_parts = getenv("ONNXB_DENSE_PARTS");
+    const double x_kb = 2.0 * ceil_div(channels, kGradTerms), w_kb = (double)ceil_div(tokens, kGradTerms);
+    for (int ctas = 1; ctas <= 2; ++ctas)
+        for (int bn = 64; bn <= kMaxBN; bn += 64)
+            for (int parts = 1; parts <= 8; parts *= 2) {
+                const Tile t{ctas, bn};
+                if (!tile_allowed(kDenseGrad, t) || (pin && (t.ctas != pinned.ctas || t.BN != pinned.BN))) continue;
+                if (parts > 1 && (!dX || x_kb < 8 * parts)) continue;
+                if (pin_parts && parts != atoi(pin_parts) && (parts > 1 || (dX && x_kb >= 8 * atoi(pin_parts)))) continue;
+                const double units = ctas == 2 ? 74 : 148, stage = stage_cycles(t), epilogue = epilogue_cycles(t);
+                const double x_tiles = dX ? (double)(ceil_div(tokens, kBM * ctas) * ceil_div(width, bn)) * parts : 0.0;
+                const double w_tiles = (double)(ceil_div(channels, kBM * ctas) * ceil_div(width, bn)) * weights;
+                const double x_cost = std::max(x_kb / parts * stage, epilogue), w_cost = std::max(w_kb * stage, epilogue);
+                double cost = std::ceil(x_tiles / units) * x_cost;
+                if (w_tiles > 0) cost = std::max(cost, x_tiles > 0 ? (x_tiles * x_cost + w_tiles * w_cost) / units + 0.5 * w_cost : std::ceil(w_tiles / units) * w_cost);
+                cost += epilogue;
+                // (a launch, and the planes out of L2)
+                if (parts > 1) cost += 4000.0 + (4.0 * parts + 2.0) * tokens * width / 4000.0;
+                if (cost < best_cost * (1 - 1e-9)) {
+                    best_cost = cost;
+                    best = GradPlan{t, parts};
+                }
+            }
+    return best;
+}
+// a part's plane: whole tiles of rows, rows of whole 16-byte pieces
+long long part_rows(int tokens, Tile t) { return ceil_div(tokens, kBM * t.ctas) * kBM * t.ctas; }
+long long part_pitch(int width) { return ceil_div(width, 4) * 4; }
+
+// A's and B's maps; their rows begin at multiples of 16 bytes.  K-major: (terms, rows) boxes of 128 bytes x `box` rows.  The gradients': 64 x 64.
+bool operand_map(CUtensorMap *m, const DenseOperand &o, int bytes, long long rows, long long cols, int box) {
+    const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows};
+    const uint64_t pitch = (uint64_t)(rows > 1 ? o.ld * bytes : (o.ld * bytes + 15) / 16 * 16);
+    const uint32_t boxes[2] = {(uint32_t)(kRowBytes / bytes), (uint32_t)box};
+    return tc_host::make_tmap_of(bytes, m, o.p, 2, dims, &pitch, boxes, tc_host::kTmapSwizzle128);
+}
+// A result's map, where TMA can store it by tiles of `out_cols`: Params' y_tma
+int result_map(CUtensorMap *m, void *y, long long ld, int bytes, long long rows, long long cols, int out_cols) {
+    const uint64_t pitch = (uint64_t)(rows > 1 ? ld * bytes : (ld * bytes + 15) / 16 * 16);
+    if (!y || pitch % 16 || reinterpret_cast<uintptr_t>(y) % 16 || out_cols * bytes % kRowBytes) return 0;
+    const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows};
+    const uint32_t box[2] = {(uint32_t)(kRowBytes / bytes), 32};
+    if (!tc_host::make_tmap_of(bytes, m, y, 2, dims, &pitch, box, tc_host::kTmapSwizzle128)) return 0;
+    return cols * bytes % 16 == 0 ? 2 : 1;
+}
+
 }  // namespace
+
+size_t tc_grad_workspace(int tokens, int channels, int width, bool dX, int weights) {
+    const GradPlan plan = grad_plan(tokens, channels, width, dX, weights);
+    return plan.parts > 1 ? (size_t)(plan.parts * part_rows(tokens, plan.tile) * part_pitch(width) * 4) : 0;
+}
 
 int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
     using namespace tc_host;
-    const bool int8 = d.type == ONNXB_INT8, gated = d.mode == kDenseGated;
-    const bool a_mn = d.mode == kDenseGradW, b_mn = a_mn || d.mode == kDenseGradX;
-    const int bytes = type_bytes(d.type), terms = kRowBytes / bytes, y_bytes = type_bytes(d.y_type);
+    const bool int8 = d.type == ONNXB_INT8, gated = d.mode == kDenseGated, grad = d.mode == kDenseGrad;
+    const int bytes = type_bytes(d.type), terms = kRowBytes / bytes;
+    const int weights = grad ? (d.Y[1] != nullptr) + (d.Y[2] != nullptr) : 0;
     Params p{};
     p.M = d.M; p.N = d.N;
-    p.seg_kb = (d.K + terms - 1) / terms;
-    p.num_kb = d.mode == kDenseGradX ? 2 * p.seg_kb : p.seg_kb;
-    p.first = a_mn && !d.Y[0] ? 1 : 0;
-    p.products = a_mn && d.Y[0] && d.Y[1] ? 2 : 1;
-    const Tile tile = pick_tile(d, p.products, p.num_kb);
+    p.num_kb = (int)ceil_div(d.K, terms);
+    const GradPlan plan = grad ? grad_plan(d.M, d.K, d.N, d.Y[0] != nullptr, weights) : GradPlan{pick_tile(d, p.num_kb), 1};
+    const Tile tile = plan.tile;
     p.BN = tile.BN;
     p.out_cols = gated ? p.BN / 2 : p.BN;
-    p.tiles_m = (d.M + kBM * tile.ctas - 1) / (kBM * tile.ctas);
-    p.tiles_n = (d.N + p.out_cols - 1) / p.out_cols;
+    p.tiles_m = (int)ceil_div(d.M, kBM * tile.ctas);
+    p.tiles_n = (int)ceil_div(d.N, p.out_cols);
     p.band = 8;
-    const long long total = (long long)p.tiles_m * p.tiles_n * p.products;
-    if (total > 0x7fffffffLL - 65536 || (long long)p.band * p.tiles_n > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
+    long long total = (long long)p.tiles_m * p.tiles_n, x_tiles = 0, w_tiles = 0;
+    if (grad) {
+        p.channels = d.K;
+        p.x_tiles_m = p.tiles_m;
+        p.x_kb = 2 * p.num_kb;
+        p.x_parts = plan.parts;
+        p.x_part_kb = (int)ceil_div(p.x_kb, plan.parts);
+        p.x_part_rows = (int)part_rows(d.M, tile);
+        x_tiles = d.Y[0] ? total * plan.parts : 0;
+        p.w_tiles_m = (int)ceil_div(d.K, kBM * tile.ctas);
+        p.w_kb = (int)ceil_div(d.M, terms);
+        p.w_first = d.Y[1] ? 0 : 1;
+        w_tiles = (long long)p.w_tiles_m * p.tiles_n * weights;
+        p.w_before = (int)(std::max(p.x_part_kb * stage_cycles(tile), epilogue_cycles(tile)) / std::max(p.w_kb * stage_cycles(tile), epilogue_cycles(tile)));
+        total = x_tiles + w_tiles;
+        if (plan.parts * (long long)p.x_part_rows > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
+    }
+    if (total > 0x7fffffffLL / 2 || (long long)p.band * p.tiles_n > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
     p.total = (int)total;
+    p.x_tiles = (int)x_tiles;
+    p.w_tiles = (int)w_tiles;
     const int bnh = p.BN / tile.ctas;
     // Few tokens: no more of A's rows than there are.  The tensor cores read 128 all the same, what lies behind being other operands'
     // (or the staging blocks'); those rows of the accumulator are nobody's, and the ring is as much deeper.
-    const int a_rows = tile.ctas == 1 && !a_mn && d.M <= 64 ? (d.M <= 16 ? 16 : d.M <= 32 ? 32 : 64) : kBM;
+    const int a_rows = tile.ctas == 1 && !grad && d.M <= 64 ? (d.M <= 16 ? 16 : d.M <= 32 ? 32 : 64) : kBM;
     p.a_bytes = (uint32_t)(a_rows * kRowBytes);
     p.stage_bytes = p.a_bytes + (uint32_t)(bnh * kRowBytes);
     p.num_stages = std::min(kMaxStages, (kSmemLimit - 1024 - kBarrierBytes - kStagingBytes) / (int)p.stage_bytes);
-    p.idesc = int8 ? make_idesc_s8(kBM * tile.ctas, p.BN) : make_idesc_f16(kBM * tile.ctas, p.BN, d.type == ONNXB_BFLOAT16, a_mn, b_mn);
+    const int bf16 = d.type == ONNXB_BFLOAT16;
+    p.idesc = int8 ? make_idesc_s8(kBM * tile.ctas, p.BN) : make_idesc_f16(kBM * tile.ctas, p.BN, bf16, grad, grad);
+    p.idesc_x = make_idesc_f16(kBM * tile.ctas, p.BN, bf16, 0, 1);
     p.a_scale = d.a_scale; p.b_scale0 = d.b_scale[0]; p.b_scale1 = d.b_scale[1]; p.bias = d.bias;
     p.relu = d.relu; p.activation = d.activation;
     p.y_type = d.y_type;
@@ -500,25 +621,28 @@ int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
     if (!p.err) return (int)cudaErrorUnknown;
 
     Maps maps;
-    // An operand: (terms, rows) boxes of 128 bytes x `box` rows, or MN-major (rows, terms) boxes of 64 x 64
-    auto operand = [&](CUtensorMap *m, const DenseOperand &o, bool mn, int rows, int box) {
-        const uint64_t dims[2] = {(uint64_t)(mn ? rows : d.K), (uint64_t)(mn ? d.K : rows)};
-        const uint64_t pitch = (uint64_t)((mn ? d.K : rows) > 1 ? o.ld * bytes : (o.ld * bytes + 15) / 16 * 16);
-        const uint32_t boxes[2] = {mn ? 64u : (uint32_t)terms, mn ? 64u : (uint32_t)box};
-        return make_tmap_of(bytes, m, o.p, 2, dims, &pitch, boxes, kTmapSwizzle128);
-    };
+    bool fine = true;
     for (int i = 0; i < 2; ++i) {
-        const DenseOperand &a = d.A[d.mode == kDenseGradX || a_mn ? i : 0], &b = d.B[d.mode == kDenseGradX || gated ? i : 0];
-        if (!operand(&maps.A[i], a, a_mn, d.M, a_rows) || !operand(&maps.B[i], b, b_mn, d.N, gated ? p.out_cols : bnh)) return (int)cudaErrorInvalidValue;
+        if (grad) {
+            fine = fine && operand_map(&maps.A[i], d.A[i], bytes, d.M, d.K, 64);
+            if (d.Y[0]) fine = fine && operand_map(&maps.B[i], d.B[i], bytes, d.K, d.N, 64);
+            else maps.B[i] = maps.A[0];                              // (nobody's)
+        } else {
+            fine = fine && operand_map(&maps.A[i], d.A[0], bytes, d.M, d.K, a_rows) &&
+                   operand_map(&maps.B[i], d.B[gated ? i : 0], bytes, d.N, d.K, gated ? p.out_cols : bnh);
+        }
     }
+    maps.B[2] = maps.A[0];
+    if (weights) fine = fine && operand_map(&maps.B[2], d.B[2], bytes, d.M, d.N, 64);
+    if (!fine) return (int)cudaErrorInvalidValue;
     for (int i = 0; i < 3; ++i) {
-        maps.Y[i] = maps.A[0];                     // (never used where y_tma is not set)
+        maps.Y[i] = maps.A[0];                                       // (nobody's, where y_tma is not set)
         p.Y[i] = d.Y[i]; p.y_ld[i] = d.y_ld[i];
-        const uint64_t pitch = (uint64_t)(d.M > 1 ? d.y_ld[i] * y_bytes : (d.y_ld[i] * y_bytes + 15) / 16 * 16);
-        if (!d.Y[i] || pitch % 16 || reinterpret_cast<uintptr_t>(d.Y[i]) % 16 || p.out_cols * y_bytes % kRowBytes) continue;
-        const uint64_t dims[2] = {(uint64_t)d.N, (uint64_t)d.M};
-        const uint32_t box[2] = {(uint32_t)(kRowBytes / y_bytes), 32};
-        if (make_tmap_of(y_bytes, &maps.Y[i], d.Y[i], 2, dims, &pitch, box, kTmapSwizzle128)) p.y_tma[i] = (long long)d.N * y_bytes % 16 == 0 ? 2 : 1;
+        p.y_tma[i] = result_map(&maps.Y[i], d.Y[i], d.y_ld[i], type_bytes(d.y_type), grad && i > 0 ? d.K : d.M, d.N, p.out_cols);
+    }
+    if (plan.parts > 1) {
+        p.y_tma[0] = result_map(&maps.Y[0], d.partial, part_pitch(d.N), 4, plan.parts * (long long)p.x_part_rows, part_pitch(d.N), p.out_cols);
+        if (p.y_tma[0] != 2) return (int)cudaErrorInvalidValue;
     }
     const size_t smem = smem_with_tmem(1024 + (size_t)p.num_stages * p.stage_bytes + kStagingBytes + kBarrierBytes, 512);
     const Kernel kernel = tile.ctas == 2 ? kernel_for<2>(d.mode, int8) : kernel_for<1>(d.mode, int8);
@@ -529,7 +653,9 @@ int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
     const cudaError_t e = tile.ctas == 2 ? launch_pdl_cluster(kernel, 2, dim3(grid), dim3(kThreads), smem, stream, maps, p)
                                          : launch_pdl(kernel, dim3(grid), dim3(kThreads), smem, stream, maps, p);
     count_launch();
-    return (int)e;
+    if (e != cudaSuccess || plan.parts == 1) return (int)e;
+    const SumPartsProblem sum{plan.parts, p.x_part_rows, d.M, d.N, d.y_type, static_cast<const float *>(d.partial), part_pitch(d.N), d.Y[0], d.y_ld[0]};
+    return launch_sum_parts(sum, stream);
 }
 
 }  // namespace onnxb
