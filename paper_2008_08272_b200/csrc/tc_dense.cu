@@ -15,6 +15,8 @@
 //   - dX = dG Wg + dU Wu is one sum: the reduction runs over dG's channels, then dU's, with the other tensor maps from there on.
 //   - dWg = dG^T X and dWu = dU^T X take their operands as they lie, the reduction (tokens) along the rows: MN-major, 64 x 64 boxes.
 //     The same for Wg and Wu in dX.  No transposed copy is made, and dG's map serves both uses: its boxes are 64 x 64 either way.
+//   - Few tiles with a long reduction share it: the CTAs of a cluster have a part each of one tile's, and every block of columns is
+//     added up by one of them, from what the others write into its shared memory, in the parts' order.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -22,6 +24,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstdlib>
+#include <cstring>
 
 #include "dense.h"
 #include "dense_math.cuh"
@@ -52,6 +55,7 @@ struct Params {
     int BN, out_cols;          // columns of an accumulator; of the output per tile (half of them for the gated block)
     int tiles_m, tiles_n, band, total;
     int num_kb;                // stages of the reduction
+    int split, part_kb;        // CTAs that share a tile's, and the stages of each
     // kDenseGrad.  dX: row tiles, all tiles (of all parts of the reduction), stages (half of them of the first of its two terms), parts,
     // stages of a part, rows of a part's plane.  dWg and dWu: row tiles, all tiles, stages, the first that is wanted, tiles that a
     // unit with one tile of dX less takes before the others.
@@ -89,9 +93,15 @@ __device__ __forceinline__ void place(const Params &p, int tiles_m, int t, TileA
     at.tm = b * p.band + rr - at.tn * rows;
 }
 // The n-th tile of a unit (a CTA or a pair) of `units`; false: there is none
-template <int kMode>
+template <int kMode, bool kSplit>
 __device__ __forceinline__ bool nth_tile(const Params &p, int unit, int units, int n, TileAt &at) {
     at.x = false;
+    if (kSplit) {              // a cluster has one
+        place(p, p.tiles_m, unit, at);
+        at.kb0 = (int)cluster_ctarank() * p.part_kb;
+        at.kb1 = min(at.kb0 + p.part_kb, p.num_kb);
+        return n == 0;
+    }
     at.kb0 = 0;
     at.kb1 = kMode == kDenseGrad ? p.w_kb : p.num_kb;
     if (kMode != kDenseGrad) {
@@ -131,7 +141,7 @@ __device__ __forceinline__ uint32_t pack<__nv_bfloat162>(float a, float b) {
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-template <int kCtas, bool kInt8, int kMode>
+template <int kCtas, bool kInt8, int kMode, bool kSplit = false>
 __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_constant__ Maps maps, const Params p) {
     constexpr bool kGrad = kMode == kDenseGrad;
     extern __shared__ uint8_t smem_raw[];
@@ -145,7 +155,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = kCtas == 2 ? (int)cluster_ctarank() : 0;
-    const int unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
+    const int unit = blockIdx.x / (kSplit ? p.split : kCtas), units = gridDim.x / kCtas;
     TileAt at;
 
     if (threadIdx.x == 0) {
@@ -172,6 +182,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_holder;
     if (kCtas == 2) cluster_sync_all();     // the peer's barriers exist before anything arrives on them
+    // (kSplit: what the other CTAs send goes where the ring was, once all of them are done with theirs)
+    const int part = kSplit ? (int)cluster_ctarank() : 0;
     pdl_launch_dependents();
 
     if (warp == 0) {
@@ -186,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
         const int piece = is_a ? lane : lane - na;
         const uint32_t dst_off = is_a ? (uint32_t)piece * (kABytes / na) : p.a_bytes + (uint32_t)piece * (uint32_t)(bnh * kRowBytes / nb);
         constexpr int kTerms = kInt8 ? kRowBytes : kRowBytes / 2;       // of the reduction per stage
-        for (int n = 0; nth_tile<kMode>(p, unit, units, n, at); ++n) {
+        for (int n = 0; nth_tile<kMode, kSplit>(p, unit, units, n, at); ++n) {
             // the first of the rows that this copy brings (along the output's rows or columns), and whether they lie along a row in memory
             int row = is_a ? (at.tm * kCtas + rank) * kBM : at.tn * p.BN + rank * bnh;
             if (kGrad) row += piece * 64;
@@ -222,6 +234,11 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                 if (++stage == p.num_stages) { stage = 0; phase ^= 1; }
             }
         }
+        if (kSplit) {
+            __syncwarp();
+            cluster_sync_all();
+            cluster_sync_all();
+        }
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer (of a pair: the even CTA)
         if ((kCtas == 1 || rank == 0) && elect_one()) {
@@ -235,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
             const uint32_t a_at = (smem_u32(stages) >> 4) & 0x3FFFu, b_lo = (uint32_t)b_tmpl | (((smem_u32(stages) + p.a_bytes) >> 4) & 0x3FFFu);
             const uint32_t stage16 = p.stage_bytes >> 4;
             constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kB16 = kGrad ? kMn16 : kK16;
-            for (int n = 0; nth_tile<kMode>(p, unit, units, n, at); ++n) {
+            for (int n = 0; nth_tile<kMode, kSplit>(p, unit, units, n, at); ++n) {
                 const bool a_mn = kGrad && !at.x;
                 const uint64_t a_tmpl = a_mn ? mn_tmpl : k_tmpl;
                 const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), a_lo = (uint32_t)a_tmpl | a_at, a16 = a_mn ? kMn16 : kK16;
@@ -270,6 +287,11 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                 if (acc == 0) acc_phase ^= 1;
             }
         }
+        if (kSplit) {
+            __syncwarp();
+            cluster_sync_all();
+            cluster_sync_all();
+        }
     } else {
         // ------------------------------------------------------------ epilogue
         pdl_wait();
@@ -278,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
         int acc = 0;
         uint32_t acc_phase = 0;
         const uint32_t peer_tmem_empty = kCtas == 2 ? map_to_cta(smem_u32(&tmem_empty[0]), 0) : 0u;
-        for (int n = 0; nth_tile<kMode>(p, unit, units, n, at); ++n) {
+        for (int n = 0; nth_tile<kMode, kSplit>(p, unit, units, n, at); ++n) {
             // 32-bit results: of 8-bit operands where asked for, and the parts of a dX whose reduction is shared
             const bool parts = kGrad && at.x && p.x_parts > 1, wide = kGrad ? parts : p.y_type == ONNXB_FLOAT;
             const int block_cols = wide ? 32 : 64;             // columns of 128 bytes
@@ -295,15 +317,59 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                 s0 = in ? __ldg(p.b_scale0 + n0 + col + lane) : 0.f;
                 s1 = !in ? 0.f : kMode == kDenseGated ? __ldg(p.b_scale1 + n0 + col + lane) : p.bias ? __ldg(p.bias + n0 + col + lane) : 0.f;
             };
-            if (kInt8) fetch(lo * block_cols);
+            if (kInt8 && !kSplit) fetch(lo * block_cols);
             mbar_wait(&tmem_full[acc], acc_phase, p.err, 4);
             tc_fence_after_sync();
+            const uint32_t tbase = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * kMaxBN);
+            // kSplit: 32 accumulator columns from `col` on are added up by the CTA that has their block of results (block b: CTA b % split),
+            // where each other CTA's 128 rows of them have a place of their own, a column's rows one after the other.
+            auto owner = [&](int col) { return col % p.out_cols / block_cols % p.split; };
+            auto place_of = [&](int col, int from, int to) {
+                const int in = col % p.out_cols, blk = in / block_cols, chunks = block_cols / 32, per = kMode == kDenseGated ? 2 : 1;
+                const int slot = (blk / p.split * chunks + in % block_cols / 32) * per + (col >= p.out_cols ? 1 : 0);
+                return (uint32_t)((slot * (p.split - 1) + from - (from > to ? 1 : 0)) * 32 * kBM * 4 + (q * 32 + lane) * 4);
+            };
+            if (kSplit) {
+                cluster_sync_all();
+                if (row0 < M) {
+#pragma unroll 1
+                    for (int col = half * 32; col < p.BN; col += 64) {
+                        const int to = owner(col);
+                        if (to == part || col % p.out_cols >= cols) continue;
+                        uint32_t v[32];
+                        tmem_ld_32x32(tbase + (uint32_t)col, v);
+                        tmem_ld_wait();
+                        const uint32_t at_peer = map_to_cta(smem_u32(stages) + place_of(col, part, to), (uint32_t)to);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) st_cluster_u32(at_peer + (uint32_t)(j * kBM * 4), v[j]);
+                    }
+                }
+                cluster_sync_all();
+            }
+            // 32 columns of the accumulator, of all parts
+            auto load = [&](int col, uint32_t (&v)[32]) {
+                tmem_ld_32x32(tbase + (uint32_t)col, v);
+                if (!kSplit) return;
+                tmem_ld_wait();
+                uint32_t sum[32] = {};
+#pragma unroll 1
+                for (int s = 0; s < p.split; ++s) {
+                    const uint8_t *from = stages + place_of(col, s, part);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const uint32_t x = s == part ? v[j] : *reinterpret_cast<const uint32_t *>(from + j * kBM * 4);
+                        sum[j] = kInt8 ? sum[j] + x : __float_as_uint(__uint_as_float(sum[j]) + __uint_as_float(x));
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = sum[j];
+            };
             if (row0 < M) {
-                const uint32_t tbase = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * kMaxBN);
                 for (int which = 0; which < p.outs; ++which) {
                     const int y = !kGrad ? which : at.x ? 0 : 1 + p.w_first + at.z;
 #pragma unroll 1
                     for (int b = lo; b < hi; ++b) {
+                        if (kSplit && b % p.split != part) continue;
                         // (TMA writes whole pieces of 16 bytes: not where the last columns fill none, since what follows is not Y's)
                         const bool by_tma = p.y_tma[y] == 2 || (p.y_tma[y] && (b + 1) * block_cols <= cols);
                         if (lane == 0) tma_store_wait_read<0>();                // the buffer's last block has gone
@@ -315,12 +381,13 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                             float f[32];
                             if (kMode == kDenseGated) {
                                 uint32_t w[32];
-                                tmem_ld_32x32(tbase + (uint32_t)(which == 2 ? p.out_cols + col : col), v);
-                                if (which == 0) tmem_ld_32x32(tbase + (uint32_t)(p.out_cols + col), w);
+                                if (kInt8 && kSplit) fetch(col);
+                                load(which == 2 ? p.out_cols + col : col, v);
+                                if (which == 0) load(p.out_cols + col, w);
                                 tmem_ld_wait();
                                 const float c0 = s0, c1 = s1;
                                 if (kInt8) {
-                                    fetch(col + 32);
+                                    if (!kSplit) fetch(col + 32);
                                     // (one factor after the other: the sum may be 0 where the factors' product is infinite)
 #pragma unroll
                                     for (int j = 0; j < 32; ++j) {
@@ -340,11 +407,12 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
 #undef ONNXB_GATE
                                 }
                             } else {
-                                tmem_ld_32x32(tbase + (uint32_t)col, v);
+                                if (kInt8 && kSplit) fetch(col);
+                                load(col, v);
                                 tmem_ld_wait();
                                 if (kInt8) {
                                     const float c0 = s0, c1 = s1;
-                                    fetch(col + 32);
+                                    if (!kSplit) fetch(col + 32);
 #pragma unroll
                                     for (int j = 0; j < 32; ++j) {
                                         f[j] = (float)(int)v[j] * sa * __shfl_sync(0xffffffffu, c0, j) + __shfl_sync(0xffffffffu, c1, j);
@@ -433,6 +501,10 @@ Kernel kernel_for(int mode, bool int8) {
     if (int8) return mode == kDenseGated ? tc_dense_kernel<kCtas, true, kDenseGated> : tc_dense_kernel<kCtas, true, kDensePlain>;
     return mode == kDenseGated ? tc_dense_kernel<kCtas, false, kDenseGated> : tc_dense_kernel<kCtas, false, kDenseGrad>;
 }
+Kernel split_kernel_for(int mode, bool int8) {
+    if (!int8) return tc_dense_kernel<1, false, kDenseGated, true>;
+    return mode == kDenseGated ? tc_dense_kernel<1, true, kDenseGated, true> : tc_dense_kernel<1, true, kDensePlain, true>;
+}
 
 // CTA pairs that run at once, asked of the device's occupancy once (as for tc_gemm_kernel, whose shared memory and threads are the same)
 int max_pairs() {
@@ -465,40 +537,62 @@ int max_pairs() {
 // tensor cores 2 BN cycles on either; its operands come out of L2 at some 50 bytes a cycle and SM, of which a pair needs (128 + BN/2) * 128
 // and a lone CTA (128 + BN) * 128.  On top of that a tile's epilogue, which the next tile's products hide but for the last one.
 struct Tile {
-    int ctas, BN;
+    int ctas, BN, split;       // (split: CTAs that share a tile's reduction, in a cluster)
 };
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 bool tile_allowed(int mode, Tile t) {
     if (t.BN < 32 * t.ctas || t.BN > kMaxBN || t.BN % (32 * t.ctas)) return false;
     if (mode == kDenseGated) return t.BN % 64 == 0 && (t.BN == 64 || t.BN % 128 == 0);
     return mode != kDenseGrad || t.BN % (64 * t.ctas) == 0;
 }
-// "<CTAs>x<BN>" in ONNXB_DENSE_TILE pins the shape for A/B measurements and tests
+int ring_bytes() { return kSmemLimit - 1024 - kBarrierBytes - kStagingBytes; }
+int stage_bytes_of(Tile t, int a_rows) { return (a_rows + t.BN / t.ctas) * kRowBytes; }
+// Few tokens: no more of A's rows than there are.  The tensor cores read 128 all the same, what lies behind being other operands'
+// (or the staging blocks'); those rows of the accumulator are nobody's, and the ring is as much deeper.
+int a_rows_of(const DenseProblem &d, Tile t) {
+    return t.ctas == 1 && d.mode != kDenseGrad && d.M <= 64 ? (d.M <= 16 ? 16 : d.M <= 32 ? 32 : 64) : kBM;
+}
+int stages_of(Tile t, int a_rows) { return std::min(kMaxStages, ring_bytes() / stage_bytes_of(t, a_rows)); }
+// A shared reduction: every CTA has a part of it, all tiles run at once (of 148 SMs not every eight are a cluster's), and what
+// the others send has room where the ring was
+bool split_allowed(const DenseProblem &d, Tile t, int num_kb) {
+    if (t.split == 1) return true;
+    if (t.ctas != 1 || d.mode == kDenseGrad || t.split > 8 || num_kb < 2 * t.split) return false;
+    const int out_cols = d.mode == kDenseGated ? t.BN / 2 : t.BN, block_cols = d.y_type == ONNXB_FLOAT ? 32 : 64;
+    const long long tiles = ceil_div(d.M, kBM) * ceil_div(d.N, out_cols), part = ceil_div(num_kb, t.split);
+    const long long places = ceil_div(ceil_div(out_cols, block_cols), t.split) * (block_cols / 32) * (d.mode == kDenseGated ? 2 : 1) * (t.split - 1);
+    const int a_rows = a_rows_of(d, t);
+    return tiles * t.split <= 128 && part * (t.split - 1) < num_kb && places * 32 * kBM * 4 <= stages_of(t, a_rows) * stage_bytes_of(t, a_rows);
+}
+// "<CTAs>x<BN>" or "1x<BN>/<split>" in ONNXB_DENSE_TILE pins the shape for A/B measurements and tests
 bool pinned_tile(int mode, Tile &t) {
     const char *e = getenv("ONNXB_DENSE_TILE");
     if (!e) return false;
-    t = Tile{e[0] - '0', e[0] && e[1] == 'x' ? atoi(e + 2) : 0};
-    return (t.ctas == 1 || t.ctas == 2) && tile_allowed(mode, t);
+    const char *slash = strchr(e, '/');
+    t = Tile{e[0] - '0', e[0] && e[1] == 'x' ? atoi(e + 2) : 0, slash ? atoi(slash + 1) : 1};
+    return (t.ctas == 1 || t.ctas == 2) && t.split >= 1 && tile_allowed(mode, t);
 }
 double stage_cycles(Tile t) { return std::max(2.0 * t.BN, (128.0 + t.BN / t.ctas) * kRowBytes / 50.0) + 30.0; }
 double epilogue_cycles(Tile t) { return 1000.0 + 12.0 * t.BN; }
-long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
 Tile pick_tile(const DenseProblem &d, int num_kb) {
-    Tile best{1, 64}, t;
-    if (pinned_tile(d.mode, t)) return t;
+    Tile best{1, 64, 1}, t;
+    if (pinned_tile(d.mode, t) && split_allowed(d, t, num_kb)) return t;
     double best_cost = 1e300;
     for (t.ctas = 1; t.ctas <= 2; ++t.ctas)
-        for (t.BN = 32; t.BN <= kMaxBN; t.BN += 32) {
-            if (!tile_allowed(d.mode, t)) continue;
-            const int out_cols = d.mode == kDenseGated ? t.BN / 2 : t.BN;
-            const long long tiles = ceil_div(d.M, kBM * t.ctas) * ceil_div(d.N, out_cols);
-            const double waves = (double)ceil_div(tiles, t.ctas == 2 ? max_pairs() : tc_host::num_sms());
-            const double cost = waves * std::max(num_kb * stage_cycles(t), epilogue_cycles(t)) + epilogue_cycles(t);
-            if (cost < best_cost * (1 - 1e-9)) {
-                best_cost = cost;
-                best = t;
+        for (t.BN = 32; t.BN <= kMaxBN; t.BN += 32)
+            for (t.split = 1; t.split <= 8; t.split *= 2) {
+                if (!tile_allowed(d.mode, t) || !split_allowed(d, t, num_kb)) continue;
+                const int out_cols = d.mode == kDenseGated ? t.BN / 2 : t.BN;
+                const long long tiles = ceil_div(d.M, kBM * t.ctas) * ceil_div(d.N, out_cols) * t.split;
+                const double waves = (double)ceil_div(tiles, t.ctas == 2 ? max_pairs() : tc_host::num_sms());
+                double cost = waves * std::max(ceil_div(num_kb, t.split) * stage_cycles(t), epilogue_cycles(t)) + epilogue_cycles(t);
+                if (t.split > 1) cost += 3000.0;
+                if (cost < best_cost * (1 - 1e-9)) {
+                    best_cost = cost;
+                    best = t;
+                }
             }
-        }
     return best;
 }
 
@@ -510,7 +604,7 @@ struct GradPlan {
 };
 constexpr int kGradTerms = kRowBytes / 2;
 GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
-    GradPlan best{{1, 64}, 1};
+    GradPlan best{{1, 64, 1}, 1};
     double best_cost = 1e300;
     Tile pinned;
     const bool pin = pinned_tile(kDenseGrad, pinned);
@@ -519,7 +613,7 @@ GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
     for (int ctas = 1; ctas <= 2; ++ctas)
         for (int bn = 64; bn <= kMaxBN; bn += 64)
             for (int parts = 1; parts <= 8; parts *= 2) {
-                const Tile t{ctas, bn};
+                const Tile t{ctas, bn, 1};
                 if (!tile_allowed(kDenseGrad, t) || (pin && (t.ctas != pinned.ctas || t.BN != pinned.BN))) continue;
                 if (parts > 1 && (!dX || x_kb < 8 * parts)) continue;
                 if (pin_parts && parts != atoi(pin_parts) && (parts > 1 || (dX && x_kb >= 8 * atoi(pin_parts)))) continue;
@@ -603,13 +697,12 @@ int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
     p.total = (int)total;
     p.x_tiles = (int)x_tiles;
     p.w_tiles = (int)w_tiles;
-    const int bnh = p.BN / tile.ctas;
-    // Few tokens: no more of A's rows than there are.  The tensor cores read 128 all the same, what lies behind being other operands'
-    // (or the staging blocks'); those rows of the accumulator are nobody's, and the ring is as much deeper.
-    const int a_rows = tile.ctas == 1 && !grad && d.M <= 64 ? (d.M <= 16 ? 16 : d.M <= 32 ? 32 : 64) : kBM;
+    const int bnh = p.BN / tile.ctas, a_rows = a_rows_of(d, tile);
     p.a_bytes = (uint32_t)(a_rows * kRowBytes);
-    p.stage_bytes = p.a_bytes + (uint32_t)(bnh * kRowBytes);
-    p.num_stages = std::min(kMaxStages, (kSmemLimit - 1024 - kBarrierBytes - kStagingBytes) / (int)p.stage_bytes);
+    p.stage_bytes = (uint32_t)stage_bytes_of(tile, a_rows);
+    p.num_stages = stages_of(tile, a_rows);
+    p.split = tile.split;
+    p.part_kb = (int)ceil_div(p.num_kb, tile.split);
     const int bf16 = d.type == ONNXB_BFLOAT16;
     p.idesc = int8 ? make_idesc_s8(kBM * tile.ctas, p.BN) : make_idesc_f16(kBM * tile.ctas, p.BN, bf16, grad, grad);
     p.idesc_x = make_idesc_f16(kBM * tile.ctas, p.BN, bf16, 0, 1);
@@ -645,12 +738,13 @@ int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
         if (p.y_tma[0] != 2) return (int)cudaErrorInvalidValue;
     }
     const size_t smem = smem_with_tmem(1024 + (size_t)p.num_stages * p.stage_bytes + kStagingBytes + kBarrierBytes, 512);
-    const Kernel kernel = tile.ctas == 2 ? kernel_for<2>(d.mode, int8) : kernel_for<1>(d.mode, int8);
+    const Kernel kernel = tile.split > 1 ? split_kernel_for(d.mode, int8) : tile.ctas == 2 ? kernel_for<2>(d.mode, int8) : kernel_for<1>(d.mode, int8);
     const cudaError_t attr_err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
     if (attr_err != cudaSuccess) return (int)attr_err;
     const int units = tile.ctas == 2 ? max_pairs() : num_sms();
-    const int grid = (int)std::min<long long>(total, units) * tile.ctas;
-    const cudaError_t e = tile.ctas == 2 ? launch_pdl_cluster(kernel, 2, dim3(grid), dim3(kThreads), smem, stream, maps, p)
+    const int cluster = std::max(tile.ctas, tile.split);
+    const int grid = (int)(tile.split > 1 ? total : std::min<long long>(total, units)) * cluster;
+    const cudaError_t e = cluster > 1 ? launch_pdl_cluster(kernel, (unsigned)cluster, dim3(grid), dim3(kThreads), smem, stream, maps, p)
                                          : launch_pdl(kernel, dim3(grid), dim3(kThreads), smem, stream, maps, p);
     count_launch();
     if (e != cudaSuccess || plan.parts == 1) return (int)e;

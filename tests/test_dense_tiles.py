@@ -18,6 +18,35 @@ def normal(g, *size):
     return torch.randn(*size, generator=g, device="cuda")
 
 
+def check_forward(size):
+    M, K, F = size
+    g = torch.Generator(device="cuda").manual_seed(23)
+    A, B, Bu = (torch.randint(-128, 128, (n, (K + 15) // 16 * 16), generator=g, device="cuda", dtype=torch.int8)[:, :K] for n in (M, F, F))
+    sa, sb, su = (torch.rand(n, generator=g, device="cuda") / 99 for n in (M, F, F))
+    for y_type in (torch.float32, torch.float16):
+        assert ref.worst(binding.onnx_gemm_int8(A, sa, B, sb, sb, dtype=y_type), ref.gemm_int8(A, sa, B, sb, sb, False, y_type)) <= 1
+        assert ref.worst(binding.onnx_gated_int8(A, sa, B, sb / 9, Bu, su, dtype=y_type), ref.gated_int8(A, sa, B, sb / 9, Bu, su, "silu", y_type)) <= 1
+    for t in (torch.bfloat16, torch.float16):
+        X, Wg, Wu = normal(g, M, K).to(t), (normal(g, F, K) / math.sqrt(K)).to(t), (normal(g, F, K) / math.sqrt(K)).to(t)
+        got = binding.onnx_gated(X, Wg, Wu, save=True)
+        for y, pair in zip(got, ref.gated(X, Wg, Wu, "silu")):
+            assert ref.worst(y, pair) <= 1
+        assert torch.equal(binding.onnx_gated(X, Wg, Wu), got[0])
+    assert binding.last_device_status() == 0
+
+
+# one reduction shared by a cluster: (tokens, width, channels) of few tiles, parts that are not equally long
+LONG = [(20, 5000, 33), (40, 2000, 70), (130, 3001, 200), (300, 4104, 130), (128, 2200, 256)]
+
+
+@pytest.mark.parametrize("size", LONG, ids=str)
+@pytest.mark.parametrize("split", [2, 4, 8])
+@pytest.mark.parametrize("tile", ["1x32", "1x64", "1x128", "1x256"])
+def test_shared_reductions(tile, split, size, monkeypatch):
+    monkeypatch.setenv("ONNXB_DENSE_TILE", f"{tile}/{split}")
+    check_forward(size)
+
+
 @pytest.mark.parametrize("size", SIZES, ids=str)
 @pytest.mark.parametrize("tile", TILES)
 def test_tile_shapes(tile, size, monkeypatch):
