@@ -2,7 +2,8 @@
 // operands) and the three products of its gradients (DenseMode in dense.h).
 //
 // The pipeline is that of tc_gemm.cu: a persistent CTA (or a pair of two on one tile) per SM, 320 threads,
-//   warp 0    TMA producer, a ring of stages of 128 bytes along the reduction (64 16-bit or 128 8-bit terms);
+//   warp 0    TMA producer, a ring of stages of 128 bytes along the reduction (64 16-bit or 128 8-bit terms), or of 2 or 4 times
+//             that where tiles are small, since a stage costs its two single threads some 270 cycles whatever it holds;
 //   warp 1    one thread issues tcgen05.mma kind::f16 or kind::i8 into one of two TMEM accumulators;
 //   warps 2-9 epilogue: tcgen05.ld, the mathematics, 32-row blocks of 128 bytes staged in swizzled shared memory, TMA stores (plain ones
 //             where Y's rows do not begin at multiples of 16 bytes).
@@ -15,8 +16,8 @@
 //   - dX = dG Wg + dU Wu is one sum: the reduction runs over dG's channels, then dU's, with the other tensor maps from there on.
 //   - dWg = dG^T X and dWu = dU^T X take their operands as they lie, the reduction (tokens) along the rows: MN-major, 64 x 64 boxes.
 //     The same for Wg and Wu in dX.  No transposed copy is made, and dG's map serves both uses: its boxes are 64 x 64 either way.
-//   - Few tiles with a long reduction share it: the CTAs of a cluster have a part each of one tile's, and every block of columns is
-//     added up by one of them, from what the others write into its shared memory, in the parts' order.
+//   - Few tiles with a long reduction share it: the CTAs of a cluster have a part each of one tile's, and every quarter of a block of
+//     columns is added up by one of them, from what the others write into its shared memory, in the parts' order.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -55,6 +56,7 @@ struct Params {
     int BN, out_cols;          // columns of an accumulator; of the output per tile (half of them for the gated block)
     int tiles_m, tiles_n, band, total;
     int num_kb;                // stages of the reduction
+    int ks, full_kb;           // K blocks of 128 bytes per stage; stages whose blocks all lie inside the reduction
     int split, part_kb;        // CTAs that share a tile's, and the stages of each
     // kDenseGrad.  dX: row tiles, all tiles (of all parts of the reduction), stages (half of them of the first of its two terms), parts,
     // stages of a part, rows of a part's plane.  dWg and dWu: row tiles, all tiles, stages, the first that is wanted, tiles that a
@@ -75,6 +77,7 @@ struct Params {
 
 struct Maps {
     CUtensorMap A[2], B[3], Y[3];
+    CUtensorMap A4, B4[2];     // (terms, rows, K block, 1) views for stages of several blocks, or (terms, 8 rows, K block, group of rows)
 };
 
 struct TileAt {
@@ -220,6 +223,33 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                 mbar_wait(&empty[stage], phase ^ 1, p.err, 1);
                 if (lane == 0 && rank == 0) mbar_arrive_expect_tx(&full[stage], p.stage_bytes * kCtas);
                 __syncwarp();
+                if (!kGrad && p.ks > 1) {
+                    // Several blocks: in one copy per operand, or at the end of the reduction, past which the view would go on into
+                    // the next row, block by block
+                    uint8_t *at_stage = stages + (size_t)stage * p.stage_bytes;
+                    const uint32_t bar = full_issuer + (uint32_t)stage * 8u;
+                    const bool whole = kb < p.full_kb;
+                    const int s = whole ? 0 : lane % p.ks, o = whole ? lane : lane / p.ks;       // block, operand
+                    if (o <= nb) {
+                        const bool a = o == 0;
+                        const int w = kMode == kDenseGated && !a ? (kCtas == 2 ? rank : o - 1) : 0, rows = a ? (int)p.a_bytes / kRowBytes : bnh / nb;
+                        uint8_t *to = at_stage + (a ? 0u : (uint32_t)p.ks * (p.a_bytes + (uint32_t)((o - 1) * rows * kRowBytes))) + (uint32_t)(s * rows * kRowBytes);
+                        const int first = a ? (at.tm * kCtas + rank) * kBM : kMode == kDenseGated ? at.tn * p.out_cols : at.tn * p.BN + rank * bnh;
+                        const int block = kb * p.ks + s;
+                        if (whole) {
+                            // (one instruction for all lanes: see tc_gemm.cu)
+                            const bool groups = kMode == kDenseGated && kCtas == 1 && !a;
+                            const int c1 = groups ? 0 : first, c3 = groups ? first / 8 : 0;
+                            if (kCtas == 2) tma_load_4d_pair(to, a ? &maps.A4 : &maps.B4[w], bar, 0, c1, block, c3);
+                            else tma_load_4d(to, a ? &maps.A4 : &maps.B4[w], &full[stage], 0, c1, block, c3);
+                        } else {
+                            if (kCtas == 2) tma_load_2d_pair(to, a ? &maps.A[0] : &maps.B[w], bar, block * kTerms, first);
+                            else tma_load_2d(to, a ? &maps.A[0] : &maps.B[w], &full[stage], block * kTerms, first);
+                        }
+                    }
+                    if (++stage == p.num_stages) { stage = 0; phase ^= 1; }
+                    continue;
+                }
                 if (kGrad && at.x && kb > at.kb0 && kb * 2 == p.x_kb) {
                     map += 1;
                     term = 0;
@@ -247,10 +277,13 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
             // K-major: 8-row groups 1024 bytes apart, an instruction 32 bytes further along the swizzled rows.  MN-major: blocks of 64
             // rows or columns 64 x 128 bytes apart, groups of 8 terms 1024 bytes apart, an instruction two of those further.
             const uint64_t k_tmpl = make_smem_desc(0, 16, 1024, kSwizzle128B), mn_tmpl = make_smem_desc(0, 64 * kRowBytes, 1024, kSwizzle128B);
-            const uint64_t b_tmpl = kGrad ? mn_tmpl : k_tmpl;
+            // (Both weights of the gated block in a lone CTA's stage of several blocks: a block's 8-row groups lie as far apart as all blocks'
+            // take, so that one weight's go on where the other's end)
+            const bool groups = kMode == kDenseGated && kCtas == 1;
+            const uint64_t b_tmpl = kGrad ? mn_tmpl : make_smem_desc(0, 16, groups ? 1024u * (uint32_t)p.ks : 1024u, kSwizzle128B);
             const uint32_t b_hi = (uint32_t)(b_tmpl >> 32);
-            const uint32_t a_at = (smem_u32(stages) >> 4) & 0x3FFFu, b_lo = (uint32_t)b_tmpl | (((smem_u32(stages) + p.a_bytes) >> 4) & 0x3FFFu);
-            const uint32_t stage16 = p.stage_bytes >> 4;
+            const uint32_t a_at = (smem_u32(stages) >> 4) & 0x3FFFu, b_lo = (uint32_t)b_tmpl | (((smem_u32(stages) + (uint32_t)p.ks * p.a_bytes) >> 4) & 0x3FFFu);
+            const uint32_t stage16 = p.stage_bytes >> 4, b_block16 = (groups ? 1024u : (uint32_t)(p.BN / kCtas * kRowBytes)) >> 4;
             constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kB16 = kGrad ? kMn16 : kK16;
             for (int n = 0; nth_tile<kMode, kSplit>(p, unit, units, n, at); ++n) {
                 const bool a_mn = kGrad && !at.x;
@@ -265,17 +298,22 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                 for (int kb = at.kb0; kb < at.kb1; ++kb) {
                     mbar_wait(&full[stage], phase, p.err, 3);
                     tc_fence_after_sync();
-                    const uint32_t al = a_lo + (uint32_t)stage * stage16, bl = b_lo + (uint32_t)stage * stage16;
+                    uint32_t al = a_lo + (uint32_t)stage * stage16, bl = b_lo + (uint32_t)stage * stage16;
+                    for (int s = 0; s < p.ks; ++s) {
+                        // a block's four instructions
 #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) {
-                        if (kInt8) {
-                            if (kCtas == 2) mma_i8_lohi_pair(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
-                            else mma_i8_lohi(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
-                        } else {
-                            if (kCtas == 2) mma_f16_lohi_pair(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
-                            else mma_f16_lohi(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
+                        for (uint32_t k = 0; k < 4; ++k) {
+                            if (kInt8) {
+                                if (kCtas == 2) mma_i8_lohi_pair(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
+                                else mma_i8_lohi(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
+                            } else {
+                                if (kCtas == 2) mma_f16_lohi_pair(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
+                                else mma_f16_lohi(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
+                            }
+                            accumulate = 1;
                         }
-                        accumulate = 1;
+                        al += p.a_bytes >> 4;
+                        bl += b_block16;
                     }
                     if (kCtas == 2) mma_commit_pair(&empty[stage]);
                     else mma_commit(&empty[stage]);
@@ -321,27 +359,27 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
             mbar_wait(&tmem_full[acc], acc_phase, p.err, 4);
             tc_fence_after_sync();
             const uint32_t tbase = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * kMaxBN);
-            // kSplit: 32 accumulator columns from `col` on are added up by the CTA that has their block of results (block b: CTA b % split),
-            // where each other CTA's 128 rows of them have a place of their own, a column's rows one after the other.
-            auto owner = [&](int col) { return col % p.out_cols / block_cols % p.split; };
+            // kSplit: a quarter (32 rows) of a block of results is added up by one CTA of the cluster, where each other CTA's 32 x 32 values
+            // of it have a place of their own: four columns of a row by 32 rows, eight times.
+            auto owner = [&](int blk) { return (blk * 4 + q) % p.split; };
             auto place_of = [&](int col, int from, int to) {
                 const int in = col % p.out_cols, blk = in / block_cols, chunks = block_cols / 32, per = kMode == kDenseGated ? 2 : 1;
-                const int slot = (blk / p.split * chunks + in % block_cols / 32) * per + (col >= p.out_cols ? 1 : 0);
-                return (uint32_t)((slot * (p.split - 1) + from - (from > to ? 1 : 0)) * 32 * kBM * 4 + (q * 32 + lane) * 4);
+                const int slot = ((blk * 4 + q) / p.split * chunks + in % block_cols / 32) * per + (col >= p.out_cols ? 1 : 0);
+                return (uint32_t)((slot * (p.split - 1) + from - (from > to ? 1 : 0)) * kBlockBytes + lane * 16);
             };
             if (kSplit) {
                 cluster_sync_all();
                 if (row0 < M) {
 #pragma unroll 1
                     for (int col = half * 32; col < p.BN; col += 64) {
-                        const int to = owner(col);
+                        const int to = owner(col % p.out_cols / block_cols);
                         if (to == part || col % p.out_cols >= cols) continue;
                         uint32_t v[32];
                         tmem_ld_32x32(tbase + (uint32_t)col, v);
                         tmem_ld_wait();
                         const uint32_t at_peer = map_to_cta(smem_u32(stages) + place_of(col, part, to), (uint32_t)to);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) st_cluster_u32(at_peer + (uint32_t)(j * kBM * 4), v[j]);
+                        for (int j = 0; j < 32; j += 4) st_cluster_v4(at_peer + (uint32_t)(j * 128), v[j], v[j + 1], v[j + 2], v[j + 3]);
                     }
                 }
                 cluster_sync_all();
@@ -356,9 +394,14 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                 for (int s = 0; s < p.split; ++s) {
                     const uint8_t *from = stages + place_of(col, s, part);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const uint32_t x = s == part ? v[j] : *reinterpret_cast<const uint32_t *>(from + j * kBM * 4);
-                        sum[j] = kInt8 ? sum[j] + x : __float_as_uint(__uint_as_float(sum[j]) + __uint_as_float(x));
+                    for (int j = 0; j < 32; j += 4) {
+                        uint4 x = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                        if (s != part) x = *reinterpret_cast<const uint4 *>(from + j * 128);
+                        auto add = [](uint32_t a, uint32_t b) { return kInt8 ? a + b : __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); };
+                        sum[j] = add(sum[j], x.x);
+                        sum[j + 1] = add(sum[j + 1], x.y);
+                        sum[j + 2] = add(sum[j + 2], x.z);
+                        sum[j + 3] = add(sum[j + 3], x.w);
                     }
                 }
 #pragma unroll
@@ -369,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                     const int y = !kGrad ? which : at.x ? 0 : 1 + p.w_first + at.z;
 #pragma unroll 1
                     for (int b = lo; b < hi; ++b) {
-                        if (kSplit && b % p.split != part) continue;
+                        if (kSplit && owner(b) != part) continue;
                         // (TMA writes whole pieces of 16 bytes: not where the last columns fill none, since what follows is not Y's)
                         const bool by_tma = p.y_tma[y] == 2 || (p.y_tma[y] && (b + 1) * block_cols <= cols);
                         if (lane == 0) tma_store_wait_read<0>();                // the buffer's last block has gone
@@ -533,11 +576,15 @@ int max_pairs() {
     return n;
 }
 
-// Tile shapes: one CTA with 128 rows or a pair with 256, and BN accumulator columns.  A stage (128 bytes of the reduction) takes the
-// tensor cores 2 BN cycles on either; its operands come out of L2 at some 50 bytes a cycle and SM, of which a pair needs (128 + BN/2) * 128
-// and a lone CTA (128 + BN) * 128.  On top of that a tile's epilogue, which the next tile's products hide but for the last one.
+// Tile shapes: one CTA with 128 rows or a pair with 256, BN accumulator columns, and for few tiles a reduction shared by a cluster.  The
+// estimate, in SM cycles, fitted to single waves of 8-bit products 128 x 1024 x 2048 and 12288 and gated blocks of 16-bit ones:
+//   - a stage of ks K blocks takes the tensor cores 2 BN ks + 50, its two single threads 240 + 170 ks (75 for each copy beyond two), and its
+//     operands' way out of L2 their bytes at 90 a cycle, or at what 8100 a cycle for all SMs leave each;
+//   - a tile's epilogue 1000 + 13 BN, which the next tile's products hide but for the last one;
+//   - a shared reduction 2500 + 28 BN for two CTAs, and a third and a half as much again for four and eight.
 struct Tile {
-    int ctas, BN, split;       // (split: CTAs that share a tile's reduction, in a cluster)
+    int ctas, BN;
+    int split;                 // CTAs that share a tile's reduction, in a cluster
 };
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 bool tile_allowed(int mode, Tile t) {
@@ -546,23 +593,33 @@ bool tile_allowed(int mode, Tile t) {
     return mode != kDenseGrad || t.BN % (64 * t.ctas) == 0;
 }
 int ring_bytes() { return kSmemLimit - 1024 - kBarrierBytes - kStagingBytes; }
-int stage_bytes_of(Tile t, int a_rows) { return (a_rows + t.BN / t.ctas) * kRowBytes; }
 // Few tokens: no more of A's rows than there are.  The tensor cores read 128 all the same, what lies behind being other operands'
 // (or the staging blocks'); those rows of the accumulator are nobody's, and the ring is as much deeper.
 int a_rows_of(const DenseProblem &d, Tile t) {
     return t.ctas == 1 && d.mode != kDenseGrad && d.M <= 64 ? (d.M <= 16 ? 16 : d.M <= 32 ? 32 : 64) : kBM;
 }
-int stages_of(Tile t, int a_rows) { return std::min(kMaxStages, ring_bytes() / stage_bytes_of(t, a_rows)); }
+int block_bytes_of(const DenseProblem &d, Tile t) { return (a_rows_of(d, t) + t.BN / t.ctas) * kRowBytes; }
+// K blocks per stage: as many as leave four stages in the ring.  (Both weights in one CTA's stage: where their view in groups of 8 rows
+// ends with the tensors.)  ONNXB_DENSE_KS pins it.
+int blocks_per_stage(const DenseProblem &d, Tile t) {
+    if (d.mode == kDenseGated && t.ctas == 1 && (d.N % 8 || d.K % (kRowBytes / type_bytes(d.type)))) return 1;
+    const int most = d.mode == kDenseGrad ? 1 : ring_bytes() / 4 / block_bytes_of(d, t), ks = most >= 4 ? 4 : most >= 2 ? 2 : 1;
+    if (const char *e = getenv("ONNXB_DENSE_KS")) return std::min(ks, std::max(1, atoi(e)) == 3 ? 2 : std::max(1, atoi(e)));
+    return ks;
+}
+int stages_of(const DenseProblem &d, Tile t) { return std::min(kMaxStages, ring_bytes() / (block_bytes_of(d, t) * blocks_per_stage(d, t))); }
+long long stages_along(const DenseProblem &d, Tile t) { return ceil_div(d.K, (long long)(kRowBytes / type_bytes(d.type)) * blocks_per_stage(d, t)); }
 // A shared reduction: every CTA has a part of it, all tiles run at once (of 148 SMs not every eight are a cluster's), and what
 // the others send has room where the ring was
-bool split_allowed(const DenseProblem &d, Tile t, int num_kb) {
+bool split_allowed(const DenseProblem &d, Tile t) {
     if (t.split == 1) return true;
+    const long long num_kb = stages_along(d, t);
     if (t.ctas != 1 || d.mode == kDenseGrad || t.split > 8 || num_kb < 2 * t.split) return false;
     const int out_cols = d.mode == kDenseGated ? t.BN / 2 : t.BN, block_cols = d.y_type == ONNXB_FLOAT ? 32 : 64;
     const long long tiles = ceil_div(d.M, kBM) * ceil_div(d.N, out_cols), part = ceil_div(num_kb, t.split);
-    const long long places = ceil_div(ceil_div(out_cols, block_cols), t.split) * (block_cols / 32) * (d.mode == kDenseGated ? 2 : 1) * (t.split - 1);
-    const int a_rows = a_rows_of(d, t);
-    return tiles * t.split <= 128 && part * (t.split - 1) < num_kb && places * 32 * kBM * 4 <= stages_of(t, a_rows) * stage_bytes_of(t, a_rows);
+    const long long places = ceil_div(ceil_div(out_cols, block_cols) * 4, t.split) * (block_cols / 32) * (d.mode == kDenseGated ? 2 : 1) * (t.split - 1);
+    return tiles * t.split <= 128 && part * (t.split - 1) < num_kb &&
+           places * kBlockBytes <= (long long)stages_of(d, t) * block_bytes_of(d, t) * blocks_per_stage(d, t);
 }
 // "<CTAs>x<BN>" or "1x<BN>/<split>" in ONNXB_DENSE_TILE pins the shape for A/B measurements and tests
 bool pinned_tile(int mode, Tile &t) {
@@ -572,22 +629,28 @@ bool pinned_tile(int mode, Tile &t) {
     t = Tile{e[0] - '0', e[0] && e[1] == 'x' ? atoi(e + 2) : 0, slash ? atoi(slash + 1) : 1};
     return (t.ctas == 1 || t.ctas == 2) && t.split >= 1 && tile_allowed(mode, t);
 }
-double stage_cycles(Tile t) { return std::max(2.0 * t.BN, (128.0 + t.BN / t.ctas) * kRowBytes / 50.0) + 30.0; }
-double epilogue_cycles(Tile t) { return 1000.0 + 12.0 * t.BN; }
+// (ctas: that run at once; bytes: of a K block of a CTA)
+double stage_cycles(Tile t, int mode, int ks, int bytes, double ctas) {
+    const int copies = mode == kDenseGrad ? 2 + t.BN / t.ctas / 64 : mode == kDenseGated && t.ctas == 1 ? 3 : 2;
+    const double from_l2 = bytes / std::min(90.0, 8100.0 / ctas);
+    return std::max({2.0 * t.BN * ks + 50.0, 240.0 + 170.0 * ks + 75.0 * (copies - 2), from_l2 * ks});
+}
+double epilogue_cycles(Tile t) { return 1000.0 + 13.0 * t.BN; }
 
-Tile pick_tile(const DenseProblem &d, int num_kb) {
+Tile pick_tile(const DenseProblem &d) {
     Tile best{1, 64, 1}, t;
-    if (pinned_tile(d.mode, t) && split_allowed(d, t, num_kb)) return t;
+    if (pinned_tile(d.mode, t) && split_allowed(d, t)) return t;
     double best_cost = 1e300;
     for (t.ctas = 1; t.ctas <= 2; ++t.ctas)
         for (t.BN = 32; t.BN <= kMaxBN; t.BN += 32)
             for (t.split = 1; t.split <= 8; t.split *= 2) {
-                if (!tile_allowed(d.mode, t) || !split_allowed(d, t, num_kb)) continue;
-                const int out_cols = d.mode == kDenseGated ? t.BN / 2 : t.BN;
-                const long long tiles = ceil_div(d.M, kBM * t.ctas) * ceil_div(d.N, out_cols) * t.split;
-                const double waves = (double)ceil_div(tiles, t.ctas == 2 ? max_pairs() : tc_host::num_sms());
-                double cost = waves * std::max(ceil_div(num_kb, t.split) * stage_cycles(t), epilogue_cycles(t)) + epilogue_cycles(t);
-                if (t.split > 1) cost += 3000.0;
+                if (!tile_allowed(d.mode, t) || !split_allowed(d, t)) continue;
+                const int out_cols = d.mode == kDenseGated ? t.BN / 2 : t.BN, units = t.ctas == 2 ? max_pairs() : tc_host::num_sms();
+                const long long tiles = ceil_div(d.M, kBM * t.ctas) * ceil_div(d.N, out_cols) * t.split, at_once = std::min<long long>(tiles, units);
+                const double stage = stage_cycles(t, d.mode, blocks_per_stage(d, t), block_bytes_of(d, t), (double)at_once * t.ctas);
+                const double main = ceil_div(stages_along(d, t), t.split) * stage, epilogue = epilogue_cycles(t);
+                double cost = (double)ceil_div(tiles, units) * std::max(main, epilogue) + epilogue;
+                if (t.split > 1) cost += (2500.0 + 28.0 * t.BN) * (t.split == 2 ? 1.0 : t.split == 4 ? 1.3 : 1.5);
                 if (cost < best_cost * (1 - 1e-9)) {
                     best_cost = cost;
                     best = t;
@@ -617,9 +680,10 @@ GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
                 if (!tile_allowed(kDenseGrad, t) || (pin && (t.ctas != pinned.ctas || t.BN != pinned.BN))) continue;
                 if (parts > 1 && (!dX || x_kb < 8 * parts)) continue;
                 if (pin_parts && parts != atoi(pin_parts) && (parts > 1 || (dX && x_kb >= 8 * atoi(pin_parts)))) continue;
-                const double units = ctas == 2 ? 74 : 148, stage = stage_cycles(t), epilogue = epilogue_cycles(t);
+                const double units = ctas == 2 ? 74 : 148, epilogue = epilogue_cycles(t);
                 const double x_tiles = dX ? (double)(ceil_div(tokens, kBM * ctas) * ceil_div(width, bn)) * parts : 0.0;
                 const double w_tiles = (double)(ceil_div(channels, kBM * ctas) * ceil_div(width, bn)) * weights;
+                const double stage = stage_cycles(t, kDenseGrad, 1, (kBM + bn / ctas) * kRowBytes, ctas * std::min(units, x_tiles + w_tiles));
                 const double x_cost = std::max(x_kb / parts * stage, epilogue), w_cost = std::max(w_kb * stage, epilogue);
                 double cost = std::ceil(x_tiles / units) * x_cost;
                 if (w_tiles > 0) cost = std::max(cost, x_tiles > 0 ? (x_tiles * x_cost + w_tiles * w_cost) / units + 0.5 * w_cost : std::ceil(w_tiles / units) * w_cost);
@@ -639,10 +703,19 @@ long long part_pitch(int width) { return ceil_div(width, 4) * 4; }
 
 // A's and B's maps; their rows begin at multiples of 16 bytes.  K-major: (terms, rows) boxes of 128 bytes x `box` rows.  The gradients': 64 x 64.
 bool operand_map(CUtensorMap *m, const DenseOperand &o, int bytes, long long rows, long long cols, int box) {
-    const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows};
     const uint64_t pitch = (uint64_t)(rows > 1 ? o.ld * bytes : (o.ld * bytes + 15) / 16 * 16);
+    const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows};
     const uint32_t boxes[2] = {(uint32_t)(kRowBytes / bytes), (uint32_t)box};
     return tc_host::make_tmap_of(bytes, m, o.p, 2, dims, &pitch, boxes, tc_host::kTmapSwizzle128);
+}
+// The views for stages of `blocks` K blocks: (terms of a block, rows, block, 1), or where `groups` (terms, 8 rows, block, group of 8 rows).  Of the
+// whole blocks alone: the elements behind a row's last are not the row's.
+bool blocks_map(CUtensorMap *m, const DenseOperand &o, int bytes, long long rows, long long cols, int box, int blocks, bool groups) {
+    const uint64_t pitch = (uint64_t)(rows > 1 ? o.ld * bytes : (o.ld * bytes + 15) / 16 * 16), terms = kRowBytes / bytes;
+    const uint64_t dims[4] = {terms, groups ? 8 : (uint64_t)rows, (uint64_t)cols / terms, groups ? (uint64_t)rows / 8 : 1};
+    const uint64_t pitches[3] = {pitch, kRowBytes, groups ? 8 * pitch : (uint64_t)rows * pitch};
+    const uint32_t boxes[4] = {(uint32_t)terms, groups ? 8u : (uint32_t)box, (uint32_t)blocks, groups ? (uint32_t)box / 8 : 1u};
+    return tc_host::make_tmap_of(bytes, m, o.p, 4, dims, pitches, boxes, tc_host::kTmapSwizzle128);
 }
 // A result's map, where TMA can store it by tiles of `out_cols`: Params' y_tma
 int result_map(CUtensorMap *m, void *y, long long ld, int bytes, long long rows, long long cols, int out_cols) {
@@ -668,9 +741,11 @@ int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
     const int weights = grad ? (d.Y[1] != nullptr) + (d.Y[2] != nullptr) : 0;
     Params p{};
     p.M = d.M; p.N = d.N;
-    p.num_kb = (int)ceil_div(d.K, terms);
-    const GradPlan plan = grad ? grad_plan(d.M, d.K, d.N, d.Y[0] != nullptr, weights) : GradPlan{pick_tile(d, p.num_kb), 1};
+    const GradPlan plan = grad ? grad_plan(d.M, d.K, d.N, d.Y[0] != nullptr, weights) : GradPlan{pick_tile(d), 1};
     const Tile tile = plan.tile;
+    p.ks = blocks_per_stage(d, tile);
+    p.num_kb = (int)stages_along(d, tile);
+    p.full_kb = d.K % terms == 0 ? p.num_kb : d.K / (terms * p.ks);      // (whole blocks past the end of the view are zeros)
     p.BN = tile.BN;
     p.out_cols = gated ? p.BN / 2 : p.BN;
     p.tiles_m = (int)ceil_div(d.M, kBM * tile.ctas);
@@ -689,7 +764,8 @@ int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
         p.w_kb = (int)ceil_div(d.M, terms);
         p.w_first = d.Y[1] ? 0 : 1;
         w_tiles = (long long)p.w_tiles_m * p.tiles_n * weights;
-        p.w_before = (int)(std::max(p.x_part_kb * stage_cycles(tile), epilogue_cycles(tile)) / std::max(p.w_kb * stage_cycles(tile), epilogue_cycles(tile)));
+        const double stage = stage_cycles(tile, kDenseGrad, 1, (kBM + p.BN / tile.ctas) * kRowBytes, 148), epilogue = epilogue_cycles(tile);
+        p.w_before = (int)(std::max(p.x_part_kb * stage, epilogue) / std::max(p.w_kb * stage, epilogue));
         total = x_tiles + w_tiles;
         if (plan.parts * (long long)p.x_part_rows > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
     }
@@ -699,8 +775,8 @@ int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
     p.w_tiles = (int)w_tiles;
     const int bnh = p.BN / tile.ctas, a_rows = a_rows_of(d, tile);
     p.a_bytes = (uint32_t)(a_rows * kRowBytes);
-    p.stage_bytes = (uint32_t)stage_bytes_of(tile, a_rows);
-    p.num_stages = stages_of(tile, a_rows);
+    p.stage_bytes = (uint32_t)(block_bytes_of(d, tile) * p.ks);
+    p.num_stages = stages_of(d, tile);
     p.split = tile.split;
     p.part_kb = (int)ceil_div(p.num_kb, tile.split);
     const int bf16 = d.type == ONNXB_BFLOAT16;
@@ -724,6 +800,13 @@ int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
             fine = fine && operand_map(&maps.A[i], d.A[0], bytes, d.M, d.K, a_rows) &&
                    operand_map(&maps.B[i], d.B[gated ? i : 0], bytes, d.N, d.K, gated ? p.out_cols : bnh);
         }
+    }
+    maps.A4 = maps.B4[0] = maps.B4[1] = maps.A[0];
+    if (p.full_kb > 0 && p.ks > 1) {
+        const int b_rows = gated ? p.out_cols : bnh;
+        const bool groups = gated && tile.ctas == 1;
+        fine = fine && blocks_map(&maps.A4, d.A[0], bytes, d.M, d.K, a_rows, p.ks, false);
+        for (int i = 0; i < 2; ++i) fine = fine && blocks_map(&maps.B4[i], d.B[gated ? i : 0], bytes, d.N, d.K, b_rows, p.ks, groups);
     }
     maps.B[2] = maps.A[0];
     if (weights) fine = fine && operand_map(&maps.B[2], d.B[2], bytes, d.M, d.N, 64);

@@ -36,7 +36,17 @@ def check_forward(size):
 
 
 # one reduction shared by a cluster: (tokens, width, channels) of few tiles, parts that are not equally long
-LONG = [(20, 5000, 33), (40, 2000, 70), (130, 3001, 200), (300, 4104, 130), (128, 2200, 256)]
+LONG = [(20, 5000, 33), (40, 2000, 70), (130, 3001, 200), (300, 4104, 130), (128, 2200, 256), (150, 4096, 200)]
+
+
+@pytest.mark.parametrize("size", LONG + [(70, 256, 100), (1000, 512, 640), (40, 2048, 72), (33, 704, 1000), (90, 320, 136)], ids=str)
+@pytest.mark.parametrize("ks", [1, 2, 4])
+@pytest.mark.parametrize("tile", ["1x32", "1x64", "1x128", "2x64", "2x128", "1x64/2"])
+def test_blocks_per_stage(tile, ks, size, monkeypatch):
+    """Stages of several K blocks, whole ones and the last of a reduction."""
+    monkeypatch.setenv("ONNXB_DENSE_TILE", tile)
+    monkeypatch.setenv("ONNXB_DENSE_KS", str(ks))
+    check_forward(size)
 
 
 @pytest.mark.parametrize("size", LONG, ids=str)
