@@ -12,33 +12,43 @@ namespace {
 
 using namespace dense;
 
-// Rows that TMA cannot address (they do not begin at multiples of 16 bytes) laid out so that it can, 16 bytes a thread: aligned 4-byte loads,
-// put together across their borders, except at a row's ends, where they would reach into what is not the row's.
-__global__ void __launch_bounds__(256) repack_rows_kernel(const uint8_t *src, long long src_pitch, long long chunks, long long total, long long row_bytes,
-                                                          uint8_t *dst, long long dst_pitch) {
-    for (long long e = blockIdx.x * 256ll + threadIdx.x; e < total; e += gridDim.x * 256ll) {
-        const long long row = e / chunks, at = (e - row * chunks) * 16;
-        const uint8_t *from = src + row * src_pitch + at;
-        uint32_t w[4] = {0, 0, 0, 0};
-        const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(from) & 3);
-        if (at + 16 <= row_bytes && off == 0) {
+// Rows that TMA cannot address (they do not begin at multiples of 16 bytes) laid out so that it can: a warp per row, 16 bytes a lane and
+// step, put together from the two aligned 16-byte pieces that hold them; byte by byte at a row's ends, where those pieces reach into
+// what is not the row's.  A block per 8 rows of a tensor, all tensors of a call in one launch.  2 x 105 MB of 10229-byte rows: see DESIGN.
+__global__ void __launch_bounds__(256) repack_rows_kernel(const RepackProblem p) {
+    tc::pdl_launch_dependents();
+    tc::pdl_wait();
+    const RepackJob &job = p.job[blockIdx.y];
+    const int lane = threadIdx.x % 32;
+    for (int row = blockIdx.x * 8 + threadIdx.x / 32; row < job.rows; row += gridDim.x * 8) {
+        const uint8_t *src = job.src + row * job.src_pitch;
+        uint8_t *dst = job.dst + row * job.dst_pitch;
+        const int off = (int)(reinterpret_cast<uintptr_t>(src) & 15), bits = (off & 3) * 8;
+        for (long long at = lane * 16; at < job.row_bytes; at += 32 * 16) {
+            uint32_t w[8] = {}, out[4];
+            if ((at > 0 || off == 0) && at + (off ? 32 - off : 16) <= job.row_bytes) {
+                const uint4 *pieces = reinterpret_cast<const uint4 *>(src + at - off);
+                const uint4 a = __ldg(pieces), b = off ? __ldg(pieces + 1) : make_uint4(0, 0, 0, 0);
+                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+                w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+                // (the same for the whole warp)
+                auto from = [&](int first) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = reinterpret_cast<const uint32_t *>(from)[i];
-        } else if (at > 0 && at + 20 <= row_bytes) {
-            const uint32_t *words = reinterpret_cast<const uint32_t *>(from - off);
-            uint32_t low = words[0];
+                    for (int i = 0; i < 4; ++i) out[i] = __funnelshift_r(w[first + i], first + i < 7 ? w[first + i + 1] : 0u, bits);
+                };
+                if (off < 4) from(0);
+                else if (off < 8) from(1);
+                else if (off < 12) from(2);
+                else from(3);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t high = words[i + 1];
-                w[i] = __funnelshift_r(low, high, off * 8);
-                low = high;
+                for (int i = 0; i < 16; ++i)
+                    if (at + i < job.row_bytes) w[i / 4] |= (uint32_t)src[at + i] << (i % 4 * 8);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[i] = w[i];
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (at + i < row_bytes) w[i / 4] |= (uint32_t)from[i] << (i % 4 * 8);
+            *reinterpret_cast<uint4 *>(dst + at) = make_uint4(out[0], out[1], out[2], out[3]);
         }
-        *reinterpret_cast<uint4 *>(dst + row * dst_pitch + at) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
@@ -107,12 +117,13 @@ int launch_slope(const GatedSlopeProblem &p, cudaStream_t stream) {
 
 int launch_dense(const DenseProblem &p, cudaStream_t stream) { return dense_few_fits(p) ? launch_dense_few(p, stream) : launch_tc_dense(p, stream); }
 
-int launch_repack_rows(const void *src, long long src_pitch, int rows, long long row_bytes, void *dst, long long dst_pitch, cudaStream_t stream) {
-    const long long chunks = dst_pitch / 16, total = chunks * rows;
-    const int grid = (int)std::min<long long>((total + 255) / 256, 148 * 8);
-    repack_rows_kernel<<<grid, 256, 0, stream>>>(static_cast<const uint8_t *>(src), src_pitch, chunks, total, row_bytes, static_cast<uint8_t *>(dst), dst_pitch);
+int launch_repack_rows(const RepackProblem &p, cudaStream_t stream) {
+    int rows = 1;
+    for (int i = 0; i < p.count; ++i) rows = std::max(rows, p.job[i].rows);
+    const dim3 grid(std::min((rows + 7) / 8, 148 * 8), p.count);
+    const cudaError_t e = tc_host::launch_pdl(repack_rows_kernel, grid, dim3(256), 0, stream, p);
     count_launch();
-    return (int)cudaGetLastError();
+    return (int)e;
 }
 
 int launch_sum_parts(const SumPartsProblem &p, cudaStream_t stream) {

@@ -64,7 +64,18 @@ int launch_gated_slope(const GatedSlopeProblem &p, cudaStream_t stream);
 
 int launch_quantize_rows(int type, int M, int K, const void *X, long long x_ld, int8_t *Q, long long q_ld, float *scale, cudaStream_t stream);
 
-// dst[r] = the first row_bytes bytes of src's row r, rows dst_pitch apart (a multiple of 16, as dst is)
-int launch_repack_rows(const void *src, long long src_pitch, int rows, long long row_bytes, void *dst, long long dst_pitch, cudaStream_t stream);
+// Up to three tensors' rows laid out anew: dst's row r = the row_bytes bytes of src's, rows dst_pitch apart (a multiple of 16, as dst is)
+struct RepackJob {
+    const uint8_t *src;
+    long long src_pitch, row_bytes;
+    int rows;
+    uint8_t *dst;
+    long long dst_pitch;
+};
+struct RepackProblem {
+    RepackJob job[3];
+    int count;
+};
+int launch_repack_rows(const RepackProblem &p, cudaStream_t stream);
 
 }  // namespace onnxb

@@ -13,6 +13,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cstdlib>
 
 #include "dense.h"
 #include "dense_math.cuh"
@@ -184,7 +185,17 @@ void (*kernel_for(int M))(const Params) {
 
 }  // namespace
 
-bool dense_few_fits(const DenseProblem &d) { return (d.mode == kDensePlain || d.mode == kDenseGated) && d.M <= 16; }
+// Where it is the faster kernel: up to 8 tokens, unless a few blocks would go through a long reduction that the other one's clusters share
+// (gated block of 16-bit weights 8192 -> 128, one token: 12.8 us here, 9.8 there; 8-bit 12288 -> 256 6.4 and 6.5; 10240 -> 4096 9.6 and
+// 12.7), and up to 16 where all blocks run at once (16 tokens: 8-bit 10240 -> 4096 11.7 us here, 12.8 there; 4096 -> 10240 14.4 and 10.8).
+// ONNXB_DENSE_FEW = the most tokens pins it for A/B measurements and tests.
+bool dense_few_fits(const DenseProblem &d) {
+    if (d.mode != kDensePlain && d.mode != kDenseGated) return false;
+    if (const char *e = getenv("ONNXB_DENSE_FEW")) return d.M <= std::min(16, atoi(e));
+    const long long blocks = (d.N + kChannels - 1) / kChannels, bytes = (long long)d.K * type_bytes(d.type) * (d.mode == kDenseGated ? 2 : 1);
+    if (d.M <= 8) return blocks > 32 || bytes <= 12288;
+    return d.M <= 16 && blocks <= per_sm(2) * tc_host::num_sms() && (blocks > 64 || bytes <= 8192);
+}
 
 int launch_dense_few(const DenseProblem &d, cudaStream_t stream) {
     const bool gated = d.mode == kDenseGated;
