@@ -13,8 +13,7 @@ namespace {
 using namespace dense;
 
 // Rows that TMA cannot address (they do not begin at multiples of 16 bytes) laid out so that it can: a warp per row, 16 bytes a lane and
-// step, put together from the two aligned 16-byte pieces that hold them; byte by byte at a row's ends, where those pieces reach into
-// what is not the row's.  A block per 8 rows of a tensor, all tensors of a call in one launch.  2 x 105 MB of 10229-byte rows: see DESIGN.
+// step.  A block per 8 rows of a tensor, all tensors of a call in one launch.
 __global__ void __launch_bounds__(256) repack_rows_kernel(const RepackProblem p) {
     tc::pdl_launch_dependents();
     tc::pdl_wait();
@@ -23,32 +22,7 @@ __global__ void __launch_bounds__(256) repack_rows_kernel(const RepackProblem p)
     for (int row = blockIdx.x * 8 + threadIdx.x / 32; row < job.rows; row += gridDim.x * 8) {
         const uint8_t *src = job.src + row * job.src_pitch;
         uint8_t *dst = job.dst + row * job.dst_pitch;
-        const int off = (int)(reinterpret_cast<uintptr_t>(src) & 15), bits = (off & 3) * 8;
-        for (long long at = lane * 16; at < job.row_bytes; at += 32 * 16) {
-            uint32_t w[8] = {}, out[4];
-            if ((at > 0 || off == 0) && at + (off ? 32 - off : 16) <= job.row_bytes) {
-                const uint4 *pieces = reinterpret_cast<const uint4 *>(src + at - off);
-                const uint4 a = __ldg(pieces), b = off ? __ldg(pieces + 1) : make_uint4(0, 0, 0, 0);
-                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-                w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-                // (the same for the whole warp)
-                auto from = [&](int first) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) out[i] = __funnelshift_r(w[first + i], first + i < 7 ? w[first + i + 1] : 0u, bits);
-                };
-                if (off < 4) from(0);
-                else if (off < 8) from(1);
-                else if (off < 12) from(2);
-                else from(3);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (at + i < job.row_bytes) w[i / 4] |= (uint32_t)src[at + i] << (i % 4 * 8);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) out[i] = w[i];
-            }
-            *reinterpret_cast<uint4 *>(dst + at) = make_uint4(out[0], out[1], out[2], out[3]);
-        }
+        for (long long at = lane * 16; at < job.row_bytes; at += 32 * 16) *reinterpret_cast<uint4 *>(dst + at) = job.element == 2 ? load16_anywhere<2>(src, at, job.row_bytes) : load16_anywhere<1>(src, at, job.row_bytes);
     }
 }
 

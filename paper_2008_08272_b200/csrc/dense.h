@@ -68,7 +68,7 @@ int launch_quantize_rows(int type, int M, int K, const void *X, long long x_ld, 
 struct RepackJob {
     const uint8_t *src;
     long long src_pitch, row_bytes;
-    int rows;
+    int rows, element;       // bytes of one
     uint8_t *dst;
     long long dst_pitch;
 };

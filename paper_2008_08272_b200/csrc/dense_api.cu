@@ -55,7 +55,7 @@ struct Placement {
         const size_t bytes = copy_bytes(m);
         if (bytes == 0) return operand(m);
         const int element = type_bytes(m->type);
-        repack.job[repack.count++] = RepackJob{static_cast<const uint8_t *>(m->data), operand(m).ld * element, m->cols * element, (int)m->rows,
+        repack.job[repack.count++] = RepackJob{static_cast<const uint8_t *>(m->data), operand(m).ld * element, m->cols * element, (int)m->rows, element,
                                                reinterpret_cast<uint8_t *>(workspace), copy_pitch(m)};
         const DenseOperand o{workspace, copy_pitch(m) / element};
         workspace += bytes;

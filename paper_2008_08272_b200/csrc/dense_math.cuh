@@ -21,6 +21,37 @@ __device__ __forceinline__ __half from_float<__half>(float v) { return __float2h
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// The 16 bytes at `at` (a multiple of 16) of a row of row_bytes that begins anywhere, zeros past its end: put together from the two
+// aligned 16-byte pieces that hold them, or element by element (of kElement bytes) at the row's ends, where those pieces reach into
+// what is not the row's.
+template <int kElement>
+__device__ __forceinline__ uint4 load16_anywhere(const uint8_t *row, long long at, long long row_bytes) {
+    const int off = (int)(reinterpret_cast<uintptr_t>(row) & 15), bits = (off & 3) * 8;
+    uint32_t w[8] = {};
+    if ((at > 0 || off == 0) && at + (off ? 32 - off : 16) <= row_bytes) {
+        const uint4 *pieces = reinterpret_cast<const uint4 *>(row + at - off);
+        const uint4 a = __ldg(pieces), b = off ? __ldg(pieces + 1) : make_uint4(0, 0, 0, 0);
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+        w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+        // (`off` is the same for all of a row)
+        auto from = [&](int first) {
+            uint32_t out[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[i] = __funnelshift_r(w[first + i], first + i < 7 ? w[first + i + 1] : 0u, bits);
+            return make_uint4(out[0], out[1], out[2], out[3]);
+        };
+        return off < 4 ? from(0) : off < 8 ? from(1) : off < 12 ? from(2) : from(3);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i += kElement)
+        if (at + i < row_bytes) {
+            const uint8_t *e = row + at + i;
+            const uint32_t v = kElement == 4 ? *reinterpret_cast<const uint32_t *>(e) : kElement == 2 ? *reinterpret_cast<const uint16_t *>(e) : *e;
+            w[i / 4] |= v << (i % 4 * 8);
+        }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // 1 / (1 + exp(-z)): exp(-z) is finite up to z = -88 and infinite below, where the quotient is 0 as it should be (to 1e-38)
 __device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
 // sqrt(8/pi) (g + 0.044715 g^3): tanh's argument in the approximation of gelu, twice, since (1 + tanh(y)) / 2 = logistic(2y).
