@@ -772,6 +772,8 @@ def onnx_gated_backward(dH, X, Wg, Wu, G, U, *, activation="silu", wanted=(True,
     v = _Views("onnx_gated_backward", stream)
     dh, g, u = v.matrix(dH, "dH", _HALVES), v.matrix(G, "G", _HALVES, dH), v.matrix(U, "U", _HALVES, dH)
     kind = str(dH.dtype)[6:]
+    if len(wanted) != 3:
+        raise ValueError("wanted: a truth value for each of dX, dWg and dWu")
     want = [w or given is not None for w, given in zip(wanted, (dX, dWg, dWu))]
     x = v.matrix(X, "X", _HALVES, dH) if want[1] or want[2] else None
     wg, wu = (v.matrix(Wg, "Wg", _HALVES, dH), v.matrix(Wu, "Wu", _HALVES, dH)) if want[0] else (None, None)

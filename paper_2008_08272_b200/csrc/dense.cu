@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const SumPartsProblem p)
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int s = 0; s < p.parts; ++s) {
-            const float4 w = __ldg(reinterpret_cast<const float4 *>(p.P + ((long long)s * p.part_rows + i) * p.p_ld + j));
+            const float4 w = *reinterpret_cast<const float4 *>(p.P + ((long long)s * p.part_rows + i) * p.p_ld + j);
             v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
         }
         T *y = static_cast<T *>(p.Y) + i * p.y_ld + j;

@@ -43,13 +43,14 @@ struct Params {
     long long y_ld[3];
 };
 
-// 16 bytes of a row, zeros past its end; weights, which nobody reads twice, not by way of L1
+// 16 bytes of a row, zeros past its end; weights, which nobody reads twice, not by way of L1.  (No read-only loads here or in the other
+// kernels of the dense layers: a kernel that starts before the previous one has finished may see its operands written.)
 template <bool kWeight>
 __device__ __forceinline__ uint4 load16(const uint8_t *row, long long at, long long row_bytes) {
     uint4 v = make_uint4(0, 0, 0, 0);
     if (at + 16 <= row_bytes) {
-        if (kWeight) asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + at));
-        else v = __ldg(reinterpret_cast<const uint4 *>(row + at));
+        if (kWeight) asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + at));
+        else v = *reinterpret_cast<const uint4 *>(row + at);
     } else if (at < row_bytes) {
         uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -119,10 +120,10 @@ __global__ void __launch_bounds__(kThreads, per_sm(kTiles)) dense_few_kernel(con
     const bool mine = m < p.M && n < p.N;
     float sa = 0.f, sb[kWeights] = {}, bias = 0.f;
     if (kType == ONNXB_INT8 && mine) {
-        sa = __ldg(p.a_scale + m);
+        sa = p.a_scale[m];
 #pragma unroll
-        for (int w = 0; w < kWeights; ++w) sb[w] = __ldg(p.b_scale[w] + n);
-        if (kWeights == 1 && p.bias) bias = __ldg(p.bias + n);
+        for (int w = 0; w < kWeights; ++w) sb[w] = p.b_scale[w][n];
+        if (kWeights == 1 && p.bias) bias = p.bias[n];
     }
     for (long long at0 = begin + t * 16; at0 - t * 16 < end; at0 += kChunks * 64) {
         uint4 wv[kChunks][kWeights][2], xv[kChunks][kTiles];

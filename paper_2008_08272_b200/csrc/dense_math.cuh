@@ -30,7 +30,7 @@ __device__ __forceinline__ uint4 load16_anywhere(const uint8_t *row, long long a
     uint32_t w[8] = {};
     if ((at > 0 || off == 0) && at + (off ? 32 - off : 16) <= row_bytes) {
         const uint4 *pieces = reinterpret_cast<const uint4 *>(row + at - off);
-        const uint4 a = __ldg(pieces), b = off ? __ldg(pieces + 1) : make_uint4(0, 0, 0, 0);
+        const uint4 a = pieces[0], b = off ? pieces[1] : make_uint4(0, 0, 0, 0);
         w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
         w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
         // (`off` is the same for all of a row)

@@ -83,7 +83,7 @@ struct Piece {
     uint4 bits;
     __device__ __forceinline__ void clear() { bits = make_uint4(0, 0, 0, 0); }
     __device__ __forceinline__ void load(const T *row, int K, int i) {
-        bits = kAligned ? __ldg(reinterpret_cast<const uint4 *>(row) + i)
+        bits = kAligned ? reinterpret_cast<const uint4 *>(row)[i]
                         : load16_anywhere<sizeof(T)>(reinterpret_cast<const uint8_t *>(row), i * 16ll, K * (long long)sizeof(T));
     }
     __device__ __forceinline__ float at(int e) const { return to_float(reinterpret_cast<const T *>(&bits)[e]); }

@@ -348,12 +348,12 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
             const int blocks = (cols + block_cols - 1) / block_cols;
             const int lo = half ? (blocks + 1) / 2 : 0, hi = half ? blocks : (blocks + 1) / 2;
             // Scales and addends: the row's, and this lane's column's of the chunk of 32 that comes next, asked for ahead of it
-            const float sa = kInt8 && row < M ? __ldg(p.a_scale + row) : 0.f;
+            const float sa = kInt8 && row < M ? p.a_scale[row] : 0.f;
             float s0 = 0.f, s1 = 0.f;                          // (s1: Wu's scale, or the plain product's addend)
             auto fetch = [&](int col) {
                 const bool in = col + lane < cols;
-                s0 = in ? __ldg(p.b_scale0 + n0 + col + lane) : 0.f;
-                s1 = !in ? 0.f : kMode == kDenseGated ? __ldg(p.b_scale1 + n0 + col + lane) : p.bias ? __ldg(p.bias + n0 + col + lane) : 0.f;
+                s0 = in ? p.b_scale0[n0 + col + lane] : 0.f;
+                s1 = !in ? 0.f : kMode == kDenseGated ? p.b_scale1[n0 + col + lane] : p.bias ? p.bias[n0 + col + lane] : 0.f;
             };
             if (kInt8 && !kSplit) fetch(lo * block_cols);
             mbar_wait(&tmem_full[acc], acc_phase, p.err, 4);
