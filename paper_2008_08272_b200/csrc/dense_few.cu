@@ -1,15 +1,14 @@
 // Dense layers of 8- and 16-bit operands for a few tokens (single tokens first of all): every weight is read once and multiplied by
 // up to 16 tokens, so the weights' bytes are what bounds it, and what counts is that enough loads are in flight on every SM.
 //
-// A block of 8 warps has 16 channels (the gated block: of both weights).  Its warps share the reduction, an eighth of each row a warp,
-// and add their sums in shared memory, in a fixed order.  The weights go from global memory straight into the registers of
+// A block has 16 channels (the gated block: of both weights).  Its warps share the reduction, a part of each row a warp, and add their
+// sums in shared memory, in a fixed order.  The weights go from global memory straight into the registers of
 // mma.sync (16 channels x 8 tokens), 16 bytes per lane and load: which terms of the reduction a lane's registers hold is up to the
 // kernel as long as both operands agree, so a lane's four words are the terms that its 16 bytes hold, no matter which the
-// instruction calls them.  (tcgen05 would want them in shared memory first, and its 128 rows for a few tokens: by tc_dense.cu,
-// with a ring of the tokens' rows alone, the three figures below are 18.8, 33.2 and 18.6 us.)
-// Measured, one call after another on weights out of HBM: one token, 10240 -> 4096 in 8 bits 9.5 us (4.4 TB/s); gated block 4096 ->
-// 10240 of 16-bit weights 29.3 us (5.7 TB/s, 6.8 TB/s at 40960), eight tokens of 8-bit ones 16.4 us (5.1 TB/s).  What is left is
-// the launch and the last blocks: more loads per warp (fewer blocks an SM) or more blocks (fewer loads) are both slower.
+// instruction calls them.  (tcgen05 would want them in shared memory first, and its 128 rows for a few tokens: see dense_few_fits.)
+// Measured, one call after another on weights out of HBM: one token, 8-bit 10240 -> 4096 9.6 us (4.4 TB/s), 4096 -> 10240 8.3 us (5.1
+// TB/s); gated block 4096 -> 10240 of 16-bit weights 29.3 us (5.7 TB/s; 40960 channels 99 us, 6.8 TB/s), eight tokens of 8-bit ones 14.2 us
+// (5.9 TB/s).  What is left is the launch and the first and last loads.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -26,9 +25,9 @@ namespace {
 
 using namespace dense;
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps, kChannels = 16;
-// blocks an SM (of 8 tokens: at 2 or 4 8-bit 4096 -> 5120 7.4 or 6.0 us, 5.0 at 3; of 16 the registers are two blocks')
-constexpr int per_sm(int tiles) { return tiles == 1 ? 3 : 2; }
+constexpr int kChannels = 16;
+// Blocks an SM: 24 warps of 8 tokens (with 16 or 32 of them 8-bit 4096 -> 5120 takes 7.4 or 6.0 us, 5.0 so), of 16 tokens 16
+constexpr int per_sm(int tiles, int warps) { return (tiles == 1 ? 24 : 16) / warps; }
 constexpr int kAhead = 256;              // bytes of its part of a row that a warp asks for ahead
 
 struct Params {
@@ -91,8 +90,8 @@ __device__ __forceinline__ void put(void *Y, int type, long long at, float v) {
 }
 
 // kTiles: of 8 tokens; kWeights: 2 for the gated block
-template <int kType, int kTiles, int kWeights>
-__global__ void __launch_bounds__(kThreads, per_sm(kTiles)) dense_few_kernel(const Params p) {
+template <int kType, int kTiles, int kWeights, int kWarps>
+__global__ void __launch_bounds__(32 * kWarps, per_sm(kTiles, kWarps)) dense_few_kernel(const Params p) {
     typedef typename Of<kType>::Sum Sum;
     constexpr int kChunks = kWeights == 2 ? 2 : 4, kTokens = 8 * kTiles;
     __shared__ Sum sums[kWarps][kWeights][kChannels][kTokens + 1];
@@ -116,11 +115,16 @@ __global__ void __launch_bounds__(kThreads, per_sm(kTiles)) dense_few_kernel(con
         asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row), "r"((uint32_t)min(end - begin, (long long)kAhead) / 16 * 16) : "memory");
     }
     tc::pdl_wait();
-    const int m = threadIdx.x / kChannels, r = threadIdx.x % kChannels, n = n0 + r;
-    const bool mine = m < p.M && n < p.N;
-    float sa = 0.f, sb[kWeights] = {}, bias = 0.f;
-    if (kType == ONNXB_INT8 && mine) {
-        sa = p.a_scale[m];
+    // The results that are this thread's, and their scales, asked for before the sums are there
+    constexpr int kResults = kTokens * kChannels / (32 * kWarps) > 0 ? kTokens * kChannels / (32 * kWarps) : 1;
+    const int r = threadIdx.x % kChannels, n = n0 + r;
+    float sa[kResults] = {}, sb[kWeights] = {}, bias = 0.f;
+    if (kType == ONNXB_INT8 && n < p.N) {
+#pragma unroll
+        for (int i = 0; i < kResults; ++i) {
+            const int m = threadIdx.x / kChannels + i * (2 * kWarps);
+            if (m < p.M) sa[i] = p.a_scale[m];
+        }
 #pragma unroll
         for (int w = 0; w < kWeights; ++w) sb[w] = p.b_scale[w][n];
         if (kWeights == 1 && p.bias) bias = p.bias[n];
@@ -155,47 +159,66 @@ __global__ void __launch_bounds__(kThreads, per_sm(kTiles)) dense_few_kernel(con
 #pragma unroll
             for (int e = 0; e < 4; ++e) sums[warp][w][g + e / 2 * 8][i * 8 + 2 * t + e % 2] = acc[w][i][e];
     __syncthreads();
-    if (!mine) return;
-    float v[kWeights];
+    if (n >= p.N) return;
 #pragma unroll
-    for (int w = 0; w < kWeights; ++w) {
-        Sum s = 0;
+    for (int i = 0; i < kResults; ++i) {
+        const int m = threadIdx.x / kChannels + i * (2 * kWarps);
+        if (m >= p.M) return;
+        float v[kWeights];
 #pragma unroll
-        for (int k = 0; k < kWarps; ++k) s += sums[k][w][r][m];
-        // (one factor after the other: the sum may be 0 where the factors' product is infinite)
-        v[w] = kType == ONNXB_INT8 ? (float)s * sa * sb[w] : (float)s;
-    }
-    float y = v[0];
-    if (kWeights == 2) {
-        if (p.Y[1]) {
-            put(p.Y[1], p.y_type, m * p.y_ld[1] + n, v[0]);
-            put(p.Y[2], p.y_type, m * p.y_ld[2] + n, v[kWeights - 1]);
+        for (int w = 0; w < kWeights; ++w) {
+            Sum s = 0;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) s += sums[k][w][r][m];
+            // (one factor after the other: the sum may be 0 where the factors' product is infinite)
+            v[w] = kType == ONNXB_INT8 ? (float)s * sa[i] * sb[w] : (float)s;
         }
-        y = activate(p.activation, v[0]) * v[kWeights - 1];
-    } else {
-        y += bias;
-        if (p.relu) y = fmaxf(y, 0.f);
+        float y = v[0];
+        if (kWeights == 2) {
+            if (p.Y[1]) {
+                put(p.Y[1], p.y_type, m * p.y_ld[1] + n, v[0]);
+                put(p.Y[2], p.y_type, m * p.y_ld[2] + n, v[kWeights - 1]);
+            }
+            y = activate(p.activation, v[0]) * v[kWeights - 1];
+        } else {
+            y += bias;
+            if (p.relu) y = fmaxf(y, 0.f);
+        }
+        put(p.Y[0], p.y_type, m * p.y_ld[0] + n, y);
     }
-    put(p.Y[0], p.y_type, m * p.y_ld[0] + n, y);
 }
 
-template <int kType, int kWeights>
+template <int kType, int kWeights, int kWarps>
 void (*kernel_for(int M))(const Params) {
-    return M <= 8 ? dense_few_kernel<kType, 1, kWeights> : dense_few_kernel<kType, 2, kWeights>;
+    return M <= 8 ? dense_few_kernel<kType, 1, kWeights, kWarps> : dense_few_kernel<kType, 2, kWeights, kWarps>;
+}
+template <int kWarps>
+void (*kernel_for(const DenseProblem &d))(const Params) {
+    if (d.type == ONNXB_INT8) return d.mode == kDenseGated ? kernel_for<ONNXB_INT8, 2, kWarps>(d.M) : kernel_for<ONNXB_INT8, 1, kWarps>(d.M);
+    return d.type == ONNXB_FLOAT16 ? kernel_for<ONNXB_FLOAT16, 2, kWarps>(d.M) : kernel_for<ONNXB_BFLOAT16, 2, kWarps>(d.M);
+}
+// Warps a block: as many as let all blocks run at once, or 8 where no number does.  (16, 8 and 4: gated block 8192 -> 1024 11.5, 17.8 and 30
+// us; 8-bit 10240 -> 4096 11.6, 9.6 and 15.2; 4096 -> 10240 11.8, 9.4 and 8.3.)  ONNXB_DENSE_FEW_WARPS pins it.
+int warps_of(const DenseProblem &d) {
+    if (const char *e = getenv("ONNXB_DENSE_FEW_WARPS")) return atoi(e) == 4 ? 4 : atoi(e) == 16 ? 16 : 8;
+    const int tiles = d.M <= 8 ? 1 : 2;
+    const long long blocks = (d.N + kChannels - 1) / kChannels, bytes = (long long)d.K * type_bytes(d.type), turn = d.mode == kDenseGated ? 128 : 256;
+    for (int warps = 16; warps >= 4; warps /= 2)
+        if (blocks <= per_sm(tiles, warps) * tc_host::num_sms() && (warps <= 4 || bytes >= warps * turn)) return warps;
+    return 8;
 }
 
 }  // namespace
 
-// Where it is the faster kernel: up to 8 tokens, unless a few blocks would go through a long reduction that the other one's clusters share
-// (gated block of 16-bit weights 8192 -> 128, one token: 12.8 us here, 9.8 there; 8-bit 12288 -> 256 6.4 and 6.5; 10240 -> 4096 9.6 and
-// 12.7), and up to 16 where all blocks run at once (16 tokens: 8-bit 10240 -> 4096 11.7 us here, 12.8 there; 4096 -> 10240 14.4 and 10.8).
+// Where it is the faster kernel: up to 8 tokens (gated block of 16-bit weights 4096 -> 10240 29 us here, 33 there; 8192 -> 128 8.9 and
+// 10.7; 8-bit 10240 -> 4096 9.6 and 12.7), and up to 16 where two blocks an SM are all there are (16 tokens: 8-bit 10240 -> 4096 11.9 us
+// here, 12.8 there; 4096 -> 10240 14.7 and 10.9) or the weights are few (gated block of 8-bit ones 512 -> 8192 3.8 and 4.9).
 // ONNXB_DENSE_FEW = the most tokens pins it for A/B measurements and tests.
 bool dense_few_fits(const DenseProblem &d) {
     if (d.mode != kDensePlain && d.mode != kDenseGated) return false;
     if (const char *e = getenv("ONNXB_DENSE_FEW")) return d.M <= std::min(16, atoi(e));
-    const long long blocks = (d.N + kChannels - 1) / kChannels, bytes = (long long)d.K * type_bytes(d.type) * (d.mode == kDenseGated ? 2 : 1);
-    if (d.M <= 8) return blocks > 32 || bytes <= 12288;
-    return d.M <= 16 && blocks <= per_sm(2) * tc_host::num_sms() && (blocks > 64 || bytes <= 8192);
+    const long long blocks = (d.N + kChannels - 1) / kChannels, bytes = (long long)d.K * type_bytes(d.type) * d.N * (d.mode == kDenseGated ? 2 : 1);
+    return d.M <= 8 || (d.M <= 16 && (blocks <= 2 * tc_host::num_sms() || bytes <= 10000000));
 }
 
 int launch_dense_few(const DenseProblem &d, cudaStream_t stream) {
@@ -210,13 +233,13 @@ int launch_dense_few(const DenseProblem &d, cudaStream_t stream) {
         p.b_pitch[w] = d.B[w].ld * bytes;
         p.b_scale[w] = d.b_scale[w];
     }
-    p.first = per_sm(d.M <= 8 ? 1 : 2) * tc_host::num_sms();
     p.a_scale = d.a_scale; p.bias = d.bias;
     p.relu = d.relu; p.activation = d.activation; p.y_type = d.y_type;
     for (int i = 0; i < 3; ++i) { p.Y[i] = d.Y[i]; p.y_ld[i] = d.y_ld[i]; }
-    auto kernel = d.type == ONNXB_INT8 ? (gated ? kernel_for<ONNXB_INT8, 2>(d.M) : kernel_for<ONNXB_INT8, 1>(d.M))
-                  : d.type == ONNXB_FLOAT16 ? kernel_for<ONNXB_FLOAT16, 2>(d.M) : kernel_for<ONNXB_BFLOAT16, 2>(d.M);
-    const cudaError_t e = tc_host::launch_pdl(kernel, dim3((d.N + kChannels - 1) / kChannels), dim3(kThreads), 0, stream, p);
+    const int warps = warps_of(d);
+    p.first = per_sm(d.M <= 8 ? 1 : 2, warps) * tc_host::num_sms();
+    auto kernel = warps == 4 ? kernel_for<4>(d) : warps == 8 ? kernel_for<8>(d) : kernel_for<16>(d);
+    const cudaError_t e = tc_host::launch_pdl(kernel, dim3((d.N + kChannels - 1) / kChannels), dim3(32 * warps), 0, stream, p);
     count_launch();
     return (int)e;
 }

@@ -99,3 +99,14 @@ def test_parts_of_the_reduction(tile, parts, size, monkeypatch):
         assert ref.worst(y, pair) <= 1
     assert torch.equal(alone, got[0]) and all(torch.equal(a, b) for a, b in zip(weights, got[1:]))
     assert binding.last_device_status() == 0
+
+
+@pytest.mark.parametrize("size", [(1, 4096, 700), (3, 200, 33), (8, 1030, 257), (9, 520, 100), (16, 2056, 300), (12, 24, 40)], ids=str)
+@pytest.mark.parametrize("warps", [4, 8, 16])
+def test_few_tokens_by_warps(warps, size, monkeypatch):
+    """Every number of warps that a block of the kernel for a few tokens may have; and the other kernel for the same tokens."""
+    monkeypatch.setenv("ONNXB_DENSE_FEW_WARPS", str(warps))
+    monkeypatch.setenv("ONNXB_DENSE_FEW", "16")
+    check_forward(size)
+    monkeypatch.setenv("ONNXB_DENSE_FEW", "0")
+    check_forward(size)
