@@ -413,8 +413,9 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
 #pragma unroll 1
                     for (int b = lo; b < hi; ++b) {
                         if (kSplit && owner(b) != part) continue;
-                        // (TMA writes whole pieces of 16 bytes: not where the last columns fill none, since what follows is not Y's)
-                        const bool by_tma = p.y_tma[y] == 2 || (p.y_tma[y] && (b + 1) * block_cols <= cols);
+                        // (TMA writes whole blocks, and of those at Y's end whole pieces of 16 bytes: not where the tile ends inside a block, or
+                        // the last columns fill no piece, since what follows is another tile's or not Y's)
+                        const bool by_tma = p.y_tma[y] && (b + 1) * block_cols <= (p.y_tma[y] == 2 ? p.out_cols : cols);
                         if (lane == 0) tma_store_wait_read<0>();                // the buffer's last block has gone
                         __syncwarp();
 #pragma unroll 1
@@ -609,7 +610,7 @@ struct Tile {
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 bool tile_allowed(int mode, Tile t) {
     if (t.BN < 32 * t.ctas || t.BN > kMaxBN || t.BN % (32 * t.ctas)) return false;
-    if (mode == kDenseGated) return t.BN % 64 == 0 && (t.BN == 64 || t.BN % 128 == 0);
+    if (mode == kDenseGated) return t.BN % 64 == 0;
     return mode != kDenseGrad || t.BN % (64 * t.ctas) == 0;
 }
 int ring_bytes() { return kSmemLimit - 1024 - kBarrierBytes - kStagingBytes; }
@@ -737,10 +738,10 @@ bool blocks_map(CUtensorMap *m, const DenseOperand &o, int bytes, long long rows
     const uint32_t boxes[4] = {(uint32_t)terms, groups ? 8u : (uint32_t)box, (uint32_t)blocks, groups ? (uint32_t)box / 8 : 1u};
     return tc_host::make_tmap_of(bytes, m, o.p, 4, dims, pitches, boxes, tc_host::kTmapSwizzle128);
 }
-// A result's map, where TMA can store it by tiles of `out_cols`: Params' y_tma
-int result_map(CUtensorMap *m, void *y, long long ld, int bytes, long long rows, long long cols, int out_cols) {
+// A result's map, where TMA can store it: Params' y_tma
+int result_map(CUtensorMap *m, void *y, long long ld, int bytes, long long rows, long long cols) {
     const uint64_t pitch = (uint64_t)(rows > 1 ? ld * bytes : (ld * bytes + 15) / 16 * 16);
-    if (!y || pitch % 16 || reinterpret_cast<uintptr_t>(y) % 16 || out_cols * bytes % kRowBytes) return 0;
+    if (!y || pitch % 16 || reinterpret_cast<uintptr_t>(y) % 16) return 0;
     const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows};
     const uint32_t box[2] = {(uint32_t)(kRowBytes / bytes), 32};
     if (!tc_host::make_tmap_of(bytes, m, y, 2, dims, &pitch, box, tc_host::kTmapSwizzle128)) return 0;
@@ -837,10 +838,10 @@ int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
     for (int i = 0; i < 3; ++i) {
         maps.Y[i] = maps.A[0];
         p.Y[i] = d.Y[i]; p.y_ld[i] = d.y_ld[i];
-        p.y_tma[i] = result_map(&maps.Y[i], d.Y[i], d.y_ld[i], type_bytes(d.y_type), grad && i > 0 ? d.K : d.M, d.N, p.out_cols);
+        p.y_tma[i] = result_map(&maps.Y[i], d.Y[i], d.y_ld[i], type_bytes(d.y_type), grad && i > 0 ? d.K : d.M, d.N);
     }
     if (plan.parts > 1) {
-        p.y_tma[0] = result_map(&maps.Y[0], d.partial, part_pitch(d.N), 4, plan.parts * (long long)p.x_part_rows, part_pitch(d.N), p.out_cols);
+        p.y_tma[0] = result_map(&maps.Y[0], d.partial, part_pitch(d.N), 4, plan.parts * (long long)p.x_part_rows, part_pitch(d.N));
         if (p.y_tma[0] != 2) return (int)cudaErrorInvalidValue;
     }
     const size_t smem = smem_with_tmem(1024 + (size_t)p.num_stages * p.stage_bytes + kStagingBytes + kBarrierBytes, 512);
