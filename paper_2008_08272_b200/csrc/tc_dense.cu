@@ -616,23 +616,30 @@ bool tile_allowed(int mode, Tile t) {
 int ring_bytes() { return kSmemLimit - 1024 - kBarrierBytes - kStagingBytes; }
 // Few tokens: no more of A's rows than there are.  The tensor cores read 128 all the same, what lies behind being other operands'
 // (or the staging blocks'); those rows of the accumulator are nobody's, and the ring is as much deeper.
-int a_rows_of(const DenseProblem &d, Tile t) {
+// (`most_ks`: the most K blocks per stage, which ONNXB_DENSE_KS = 1 or 2 pins; read once a call, since looking through the environment for
+// every shape costs more host time than the rest of the choice)
+struct Shape : DenseProblem {
+    int most_ks;
+    explicit Shape(const DenseProblem &d) : DenseProblem(d), most_ks(4) {
+        if (const char *e = getenv("ONNXB_DENSE_KS")) most_ks = e[0] == '1' ? 1 : e[0] == '2' ? 2 : 4;
+    }
+};
+int a_rows_of(const Shape &d, Tile t) {
     return t.ctas == 1 && d.mode != kDenseGrad && d.M <= 64 ? (d.M <= 16 ? 16 : d.M <= 32 ? 32 : 64) : kBM;
 }
-int block_bytes_of(const DenseProblem &d, Tile t) { return (a_rows_of(d, t) + t.BN / t.ctas) * kRowBytes; }
+int block_bytes_of(const Shape &d, Tile t) { return (a_rows_of(d, t) + t.BN / t.ctas) * kRowBytes; }
 // K blocks per stage: as many as leave four stages in the ring.  (Both weights in one CTA's stage: where their view in groups of 8 rows
-// ends with the tensors.)  ONNXB_DENSE_KS pins it.
-int blocks_per_stage(const DenseProblem &d, Tile t) {
+// ends with the tensors.)
+int blocks_per_stage(const Shape &d, Tile t) {
     if (d.mode == kDenseGated && t.ctas == 1 && (d.N % 8 || d.K % (kRowBytes / type_bytes(d.type)))) return 1;
-    const int most = d.mode == kDenseGrad ? 1 : ring_bytes() / 4 / block_bytes_of(d, t), ks = most >= 4 ? 4 : most >= 2 ? 2 : 1;
-    if (const char *e = getenv("ONNXB_DENSE_KS")) return std::min(ks, std::max(1, atoi(e)) == 3 ? 2 : std::max(1, atoi(e)));
-    return ks;
+    const int most = d.mode == kDenseGrad ? 1 : std::min(d.most_ks, ring_bytes() / 4 / block_bytes_of(d, t));
+    return most >= 4 ? 4 : most >= 2 ? 2 : 1;
 }
-int stages_of(const DenseProblem &d, Tile t) { return std::min(kMaxStages, ring_bytes() / (block_bytes_of(d, t) * blocks_per_stage(d, t))); }
-long long stages_along(const DenseProblem &d, Tile t) { return ceil_div(d.K, (long long)(kRowBytes / type_bytes(d.type)) * blocks_per_stage(d, t)); }
+int stages_of(const Shape &d, Tile t) { return std::min(kMaxStages, ring_bytes() / (block_bytes_of(d, t) * blocks_per_stage(d, t))); }
+long long stages_along(const Shape &d, Tile t) { return ceil_div(d.K, (long long)(kRowBytes / type_bytes(d.type)) * blocks_per_stage(d, t)); }
 // A shared reduction: every CTA has a part of it, all tiles run at once (of 148 SMs not every eight are a cluster's), and what
 // the others send has room where the ring was
-bool split_allowed(const DenseProblem &d, Tile t) {
+bool split_allowed(const Shape &d, Tile t) {
     if (t.split == 1) return true;
     const long long num_kb = stages_along(d, t);
     if (t.ctas != 1 || d.mode == kDenseGrad || t.split > 8 || num_kb < 2 * t.split) return false;
@@ -658,7 +665,7 @@ double stage_cycles(Tile t, int mode, int ks, int bytes, double ctas) {
 }
 double epilogue_cycles(Tile t) { return 1000.0 + 13.0 * t.BN; }
 
-Tile pick_tile(const DenseProblem &d) {
+Tile pick_tile(const Shape &d) {
     Tile best{1, 64, 1}, t;
     if (pinned_tile(d.mode, t) && split_allowed(d, t)) return t;
     double best_cost = 1e300;
@@ -755,8 +762,9 @@ size_t tc_grad_workspace(int tokens, int channels, int width, bool dX, int weigh
     return plan.parts > 1 ? (size_t)(plan.parts * part_rows(tokens, plan.tile) * part_pitch(width) * 4) : 0;
 }
 
-int launch_tc_dense(const DenseProblem &d, cudaStream_t stream) {
+int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
     using namespace tc_host;
+    const Shape d(problem);
     const bool int8 = d.type == ONNXB_INT8, gated = d.mode == kDenseGated, grad = d.mode == kDenseGrad;
     const int bytes = type_bytes(d.type), terms = kRowBytes / bytes;
     const int weights = grad ? (d.Y[1] != nullptr) + (d.Y[2] != nullptr) : 0;
