@@ -1,5 +1,6 @@
 /*
- * onnx_b200.h - C ABI of the ONNX Conv / Gemm library for NVIDIA B200 (sm_100a).
+ * onnx_b200.h - C ABI of the ONNX Conv / Gemm library for NVIDIA B200 (sm_100a), with the dense layers
+ * of language models in 16 and 8 bits beside Gemm.
  *
  * The library computes the two operators at the centre of the inference code an
  * ONNX compiler emits for MNIST- and ResNet-50-class models (the paper's Sec. 4.1
@@ -11,7 +12,8 @@
  * Sec. 3.4.2, restricted to static shapes.
  *
  * General conventions
- *   - All tensors are dense, row-major, 32-bit float.  Conv tensors are NCHW.
+ *   - All tensors are dense, row-major, 32-bit float.  Conv tensors are NCHW.  (The dense layers of 8- and
+ *     16-bit operands, onnx_quantize_rows_run to onnx_gated_backward_run, have types, rows and sizes of their own.)
  *   - Pointers named X, W, B, A, C, Y and `workspace` are DEVICE pointers owned
  *     by the caller.  Attribute structs, dims arrays and out-parameters are HOST
  *     memory.  `cuda_stream` is a cudaStream_t passed as void* (NULL = the
