@@ -26,31 +26,59 @@ __global__ void __launch_bounds__(256) repack_rows_kernel(const RepackProblem p)
     }
 }
 
+// What a 16-bit number leaves of v, as one; nothing where there is no such number
+template <typename T>
+__device__ __forceinline__ T remainder_of(float v, T nearest) {
+    const float left = v - to_float(nearest);
+    return from_float<T>(isfinite(left) ? left : 0.f);
+}
+
 // dG = dH U act'(G), dU = dH act(G): five tensors' bytes, and about 40 instructions an element.  A block has 8 rows by 32 pieces of 8
-// elements (of 1 where rows do not begin at multiples of 16 bytes), so that nothing is divided to find a place.  4096 x 10240 of 16-bit floats: see
-// launch_gated_slope.
-template <typename T, int kCount>
-__global__ void __launch_bounds__(256) gated_slope_kernel(const GatedSlopeProblem p) {
+// elements (of 1 where rows do not begin at multiples of 16 bytes), so that nothing is divided to find a place.  4096 x 10240 of bf16: 65 us (6.5
+// TB/s).  kTwins: see GatedSlopeProblem; the blocks from x_blocks on copy X.
+template <typename T, int kCount, bool kTwins>
+__global__ void __launch_bounds__(256) gated_slope_kernel(const GatedSlopeProblem p, int x_blocks) {
     struct alignas(kCount * sizeof(T)) Piece { T v[kCount]; };
-    const long long j = ((long long)blockIdx.x * 32 + threadIdx.x % 32) * kCount;
     tc::pdl_launch_dependents();
     tc::pdl_wait();
+    if (kTwins && (int)blockIdx.x >= x_blocks) {
+        const long long j = ((long long)blockIdx.x - x_blocks) * 32 + threadIdx.x % 32;
+        if (j >= p.K) return;
+        for (int i = blockIdx.y * 8 + threadIdx.x / 32; i < p.M; i += gridDim.y * 8) {
+            const T x = static_cast<const T *>(p.X.p)[i * p.X.ld + j];
+            T *to = static_cast<T *>(p.twice) + i * p.twice_ld + j;
+            to[0] = x;
+            to[p.M * p.twice_ld] = x;
+        }
+        return;
+    }
+    const long long j = ((long long)blockIdx.x * 32 + threadIdx.x % 32) * kCount;
     if (j >= p.F) return;
     for (int i = blockIdx.y * 8 + threadIdx.x / 32; i < p.M; i += gridDim.y * 8) {
         const Piece dh = *reinterpret_cast<const Piece *>(static_cast<const T *>(p.dH.p) + i * p.dH.ld + j);
         const Piece g = *reinterpret_cast<const Piece *>(static_cast<const T *>(p.G.p) + i * p.G.ld + j);
         const Piece u = *reinterpret_cast<const Piece *>(static_cast<const T *>(p.U.p) + i * p.U.ld + j);
-        Piece dg, du;
+        Piece dg, du, dg_rest, du_rest;
 #pragma unroll
         for (int e = 0; e < kCount; ++e) {
             float value, slope;
             const float d = to_float(dh.v[e]);
             activate_with_slope(p.activation, to_float(g.v[e]), value, slope);
-            dg.v[e] = from_float<T>(d * to_float(u.v[e]) * slope);
-            du.v[e] = from_float<T>(d * value);
+            const float a = d * to_float(u.v[e]) * slope, b = d * value;
+            dg.v[e] = from_float<T>(a);
+            du.v[e] = from_float<T>(b);
+            if (kTwins) {
+                dg_rest.v[e] = remainder_of(a, dg.v[e]);
+                du_rest.v[e] = remainder_of(b, du.v[e]);
+            }
         }
-        *reinterpret_cast<Piece *>(static_cast<T *>(p.dG) + i * p.d_ld + j) = dg;
-        *reinterpret_cast<Piece *>(static_cast<T *>(p.dU) + i * p.d_ld + j) = du;
+        T *to_g = static_cast<T *>(p.dG) + i * p.d_ld + j, *to_u = static_cast<T *>(p.dU) + i * p.d_ld + j;
+        *reinterpret_cast<Piece *>(to_g) = dg;
+        *reinterpret_cast<Piece *>(to_u) = du;
+        if (kTwins) {
+            *reinterpret_cast<Piece *>(to_g + p.M * p.d_ld) = dg_rest;
+            *reinterpret_cast<Piece *>(to_u + p.M * p.d_ld) = du_rest;
+        }
     }
 }
 
@@ -65,8 +93,10 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const SumPartsProblem p)
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int s = 0; s < p.parts; ++s) {
-            const float4 w = *reinterpret_cast<const float4 *>(p.P + ((long long)s * p.part_rows + i) * p.p_ld + j);
-            v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
+            const float *from = p.P + ((long long)s * p.part_rows + i) * p.p_ld + j;
+            const float4 w = *reinterpret_cast<const float4 *>(from);
+            const float4 rest = p.twins ? *reinterpret_cast<const float4 *>(from + p.M * p.p_ld) : make_float4(0.f, 0.f, 0.f, 0.f);
+            v = make_float4(v.x + w.x + rest.x, v.y + w.y + rest.y, v.z + w.z + rest.z, v.w + w.w + rest.w);
         }
         T *y = static_cast<T *>(p.Y) + i * p.y_ld + j;
         alignas(8) const T out[4] = {from_float<T>(v.x), from_float<T>(v.y), from_float<T>(v.z), from_float<T>(v.w)};
@@ -82,9 +112,10 @@ int launch_slope(const GatedSlopeProblem &p, cudaStream_t stream) {
     auto aligned = [&](const DenseOperand &o) { return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && (p.M == 1 || o.ld % 8 == 0); };
     const bool pieces = p.F % 8 == 0 && aligned(p.dH) && aligned(p.G) && aligned(p.U);
     const int count = pieces ? 8 : 1, across = (p.F + 32 * count - 1) / (32 * count);
-    const dim3 grid(across, std::min(65535, (p.M + 7) / 8));
-    return (int)(pieces ? tc_host::launch_pdl(gated_slope_kernel<T, 8>, grid, dim3(256), 0, stream, p)
-                        : tc_host::launch_pdl(gated_slope_kernel<T, 1>, grid, dim3(256), 0, stream, p));
+    const dim3 grid(across + (p.twins && p.X.p ? (p.K + 31) / 32 : 0), std::min(65535, (p.M + 7) / 8));
+    auto kernel = pieces ? (p.twins ? gated_slope_kernel<T, 8, true> : gated_slope_kernel<T, 8, false>)
+                         : (p.twins ? gated_slope_kernel<T, 1, true> : gated_slope_kernel<T, 1, false>);
+    return (int)tc_host::launch_pdl(kernel, grid, dim3(256), 0, stream, p, across);
 }
 
 }  // namespace

@@ -30,6 +30,9 @@ struct DenseProblem {
     void *Y[3];
     long long y_ld[3];
     void *partial;       // kDenseGrad: tc_grad_workspace bytes
+    // kDenseGrad of a few tokens: A[0] and A[1] hold every token twice, the 16-bit numbers nearest to dG and dU and, M/2 rows on, those nearest
+    // to what these leave of them; B[2] holds X twice; Y[0] is the sum of both.  (M: rows of A)
+    int twins;
 };
 
 inline int type_bytes(int type) { return type == ONNXB_FLOAT ? 4 : type == ONNXB_INT8 ? 1 : 2; }
@@ -41,11 +44,12 @@ int launch_dense_few(const DenseProblem &p, cudaStream_t stream);
 // On the tensor cores (tc_dense.cu).  Operands' rows begin at multiples of 16 bytes.
 int launch_tc_dense(const DenseProblem &p, cudaStream_t stream);
 // Scratch that the gradients' products need (dX in parts of its long reduction, where there would be few tiles)
-size_t tc_grad_workspace(int tokens, int channels, int width, bool dX, int weights);
+size_t tc_grad_workspace(int rows, int channels, int width, bool dX, int weights, bool twins);
 
-// Y[i,j] = the sum over s < parts of P[s * part_rows + i][j], in that order, rounded to `type`; P's rows p_ld floats apart (a multiple of 4)
+// Y[i,j] = the sum over s < parts of P[s * part_rows + i][j], in that order, and of twins that of P[s * part_rows + M + i][j] after each,
+// rounded to `type`; P's rows p_ld floats apart (a multiple of 4)
 struct SumPartsProblem {
-    int parts, part_rows, M, N, type;
+    int parts, part_rows, M, N, type, twins;
     const float *P;
     long long p_ld;
     void *Y;
@@ -53,12 +57,17 @@ struct SumPartsProblem {
 };
 int launch_sum_parts(const SumPartsProblem &p, cudaStream_t stream);
 
-// dG = dH U act'(G), dU = dH act(G), each [M,F]; all of one 16-bit type
+// dG = dH U act'(G), dU = dH act(G), each [M,F]; all of one 16-bit type.  twins: what rounding leaves of them as well, M rows on, and X [M,K]
+// (its p NULL where there is none) copied to `twice`, and again M rows on.
 struct GatedSlopeProblem {
     int type, activation, M, F;
     DenseOperand dH, G, U;
     void *dG, *dU;
     long long d_ld;
+    int twins, K;
+    DenseOperand X;
+    void *twice;
+    long long twice_ld;
 };
 int launch_gated_slope(const GatedSlopeProblem &p, cudaStream_t stream);
 

@@ -191,17 +191,29 @@ extern "C" onnxb_status onnx_gated_int8_run(const onnxb_matrix *A, const float *
     return run_gated(d, A, Wg, Wu, workspace, workspace_bytes, (cudaStream_t)cuda_stream);
 }
 
-// The gradients' workspace: dG and dU, their rows at multiples of 16 bytes.
-static int64_t slope_pitch(int64_t F) { return (F + 7) / 8 * 8; }
-static size_t slope_bytes(int64_t M, int64_t F) { return (size_t)(M * slope_pitch(F) * 2); }
+// The gradients' workspace: dG and dU, their rows at multiples of 16 bytes; for few tokens all of these rows twice, and X twice.
+// Rounding dG and dU to 16 bits makes the gradients' error 1.4 times that of rounding them alone, but of single tokens up to twice it,
+// since so few roundings do not average.  Up to kMostTwins tokens what is left of them goes along as tokens of its own: the tensor
+// cores have room for these rows anyway (64 of a K block, 128 of a tile), and what it costs is dX's sum of both in a launch of its own
+// (16 tokens, 4096 x 10240: 73.7 -> 75.3 us; one, 64 x 64: 3.7 -> 4.9).
+constexpr int64_t kMostTwins = 32;
+static int64_t padded_pitch(int64_t cols) { return (cols + 7) / 8 * 8; }
+static bool has_twins(int64_t M) { return M <= kMostTwins; }
+static int64_t slope_rows(int64_t M) { return has_twins(M) ? 2 * M : M; }
+static size_t slope_bytes(int64_t M, int64_t F) { return (size_t)(slope_rows(M) * padded_pitch(F) * 2); }
+// X for dWg and dWu
+static size_t tokens_bytes(const onnxb_matrix *X) {
+    if (!X || X->rows < 1 || X->cols < 1 || X->rows > kMostSize || X->cols > kMostSize) return 0;
+    return has_twins(X->rows) ? slope_bytes(X->rows, X->cols) : copy_bytes(X);
+}
 
 extern "C" size_t onnx_gated_backward_workspace_bytes(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
                                                       const onnxb_matrix *dX, const onnxb_matrix *dWg, const onnxb_matrix *dWu) {
     if (!dH || dH->rows < 1 || dH->cols < 1 || dH->rows > kMostSize || dH->cols > kMostSize) return 0;
     const onnxb_matrix *one = dX ? dX : dWg ? dWg : dWu;
     if (!one || one->cols < 1 || one->cols > kMostSize) return 0;
-    return 2 * slope_bytes(dH->rows, dH->cols) + (dX ? copy_bytes(Wg) + copy_bytes(Wu) : 0) + (dWg || dWu ? copy_bytes(X) : 0) +
-           tc_grad_workspace((int)dH->rows, (int)dH->cols, (int)one->cols, dX != nullptr, (dWg != nullptr) + (dWu != nullptr));
+    return 2 * slope_bytes(dH->rows, dH->cols) + (dX ? copy_bytes(Wg) + copy_bytes(Wu) : 0) + (dWg || dWu ? tokens_bytes(X) : 0) +
+           tc_grad_workspace((int)slope_rows(dH->rows), (int)dH->cols, (int)one->cols, dX != nullptr, (dWg != nullptr) + (dWu != nullptr), has_twins(dH->rows));
 }
 
 extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
@@ -248,16 +260,25 @@ extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const on
     s.type = dH->type; s.activation = activation;
     s.M = (int)M; s.F = (int)F;
     s.dH = operand(dH); s.G = operand(G); s.U = operand(U);
-    s.d_ld = slope_pitch(F);
+    s.d_ld = padded_pitch(F);
     char *ws = static_cast<char *>(workspace);
     s.dG = ws;
     s.dU = ws + slope_bytes(M, F);
     ws += 2 * slope_bytes(M, F);
+    s.twins = has_twins(M);
+    s.K = (int)K;
+    if (s.twins && weights) {
+        s.X = operand(X);
+        s.twice = ws;
+        s.twice_ld = padded_pitch(K);
+        ws += tokens_bytes(X);
+    }
     int err = launch_gated_slope(s, stream);
     DenseProblem d{};
     d.mode = kDenseGrad;
     d.type = d.y_type = dH->type;
-    d.M = (int)M; d.N = (int)K; d.K = (int)F;
+    d.M = (int)slope_rows(M); d.N = (int)K; d.K = (int)F;
+    d.twins = s.twins;
     d.A[0] = DenseOperand{s.dG, s.d_ld};
     d.A[1] = DenseOperand{s.dU, s.d_ld};
     Placement placed(ws);
@@ -265,7 +286,7 @@ extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const on
         d.B[0] = placed(Wg);
         d.B[1] = placed(Wu);
     }
-    if (weights) d.B[2] = placed(X);
+    if (weights) d.B[2] = s.twins ? DenseOperand{s.twice, s.twice_ld} : placed(X);
     if (err == 0) err = placed.run(stream);
     for (int i = 0; i < 3; ++i) {
         d.Y[i] = outs[i] ? outs[i]->data : nullptr;

@@ -59,9 +59,9 @@ struct Params {
     int ks, full_kb;           // K blocks of 128 bytes per stage; stages whose blocks all lie inside the reduction
     int split, part_kb;        // CTAs that share a tile's, and the stages of each
     // kDenseGrad.  dX: row tiles, all tiles (of all parts of the reduction), stages (half of them of the first of its two terms), parts,
-    // stages of a part, rows of a part's plane.  dWg and dWu: row tiles, all tiles, stages, the first that is wanted, tiles that a
+    // stages of a part, rows of a part's plane, whether dX's tiles go to planes of fp32.  dWg and dWu: row tiles, all tiles, stages, the first that is wanted, tiles that a
     // unit with one tile of dX less takes before the others.
-    int x_tiles_m, x_tiles, x_kb, x_parts, x_part_kb, x_part_rows;
+    int x_tiles_m, x_tiles, x_kb, x_parts, x_part_kb, x_part_rows, x_planes;
     int channels, w_tiles_m, w_tiles, w_kb, w_first, w_before;
     uint32_t idesc_x;
     int num_stages;
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
         const uint32_t peer_tmem_empty = kCtas == 2 ? map_to_cta(smem_u32(&tmem_empty[0]), 0) : 0u;
         for (int n = 0; nth_tile<kMode, kSplit>(p, unit, units, n, at); ++n) {
             // 32-bit results: of 8-bit operands where asked for, and the parts of a dX whose reduction is shared
-            const bool parts = kGrad && at.x && p.x_parts > 1, wide = kGrad ? parts : p.y_type == ONNXB_FLOAT;
+            const bool parts = kGrad && at.x && p.x_planes, wide = kGrad ? parts : p.y_type == ONNXB_FLOAT;
             const int block_cols = wide ? 32 : 64;             // columns of 128 bytes
             const int M = kGrad && !at.x ? p.channels : p.M;
             const int row0 = (at.tm * kCtas + rank) * kBM + q * 32, row = row0 + lane;
@@ -757,9 +757,9 @@ int result_map(CUtensorMap *m, void *y, long long ld, int bytes, long long rows,
 
 }  // namespace
 
-size_t tc_grad_workspace(int tokens, int channels, int width, bool dX, int weights) {
-    const GradPlan plan = grad_plan(tokens, channels, width, dX, weights);
-    return plan.parts > 1 ? (size_t)(plan.parts * part_rows(tokens, plan.tile) * part_pitch(width) * 4) : 0;
+size_t tc_grad_workspace(int rows, int channels, int width, bool dX, int weights, bool twins) {
+    const GradPlan plan = grad_plan(rows, channels, width, dX, weights);
+    return plan.parts > 1 || (dX && twins) ? (size_t)(plan.parts * part_rows(rows, plan.tile) * part_pitch(width) * 4) : 0;
 }
 
 int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
@@ -768,6 +768,7 @@ int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
     const bool int8 = d.type == ONNXB_INT8, gated = d.mode == kDenseGated, grad = d.mode == kDenseGrad;
     const int bytes = type_bytes(d.type), terms = kRowBytes / bytes;
     const int weights = grad ? (d.Y[1] != nullptr) + (d.Y[2] != nullptr) : 0;
+    const int tokens = d.twins ? d.M / 2 : d.M;
     Params p{};
     p.M = d.M; p.N = d.N;
     const GradPlan plan = grad ? grad_plan(d.M, d.K, d.N, d.Y[0] != nullptr, weights) : GradPlan{pick_tile(d), 1};
@@ -788,6 +789,7 @@ int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
         p.x_parts = plan.parts;
         p.x_part_kb = (int)ceil_div(p.x_kb, plan.parts);
         p.x_part_rows = (int)part_rows(d.M, tile);
+        p.x_planes = d.Y[0] && (plan.parts > 1 || d.twins);
         x_tiles = d.Y[0] ? total * plan.parts : 0;
         p.w_tiles_m = (int)ceil_div(d.K, kBM * tile.ctas);
         p.w_kb = (int)ceil_div(d.M, terms);
@@ -846,9 +848,9 @@ int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
     for (int i = 0; i < 3; ++i) {
         maps.Y[i] = maps.A[0];
         p.Y[i] = d.Y[i]; p.y_ld[i] = d.y_ld[i];
-        p.y_tma[i] = result_map(&maps.Y[i], d.Y[i], d.y_ld[i], type_bytes(d.y_type), grad && i > 0 ? d.K : d.M, d.N);
+        p.y_tma[i] = result_map(&maps.Y[i], d.Y[i], d.y_ld[i], type_bytes(d.y_type), grad && i > 0 ? d.K : tokens, d.N);
     }
-    if (plan.parts > 1) {
+    if (p.x_planes) {
         p.y_tma[0] = result_map(&maps.Y[0], d.partial, part_pitch(d.N), 4, plan.parts * (long long)p.x_part_rows, part_pitch(d.N));
         if (p.y_tma[0] != 2) return (int)cudaErrorInvalidValue;
     }
@@ -862,8 +864,8 @@ int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
     const cudaError_t e = cluster > 1 ? launch_pdl_cluster(kernel, (unsigned)cluster, dim3(grid), dim3(kThreads), smem, stream, maps, p)
                                          : launch_pdl(kernel, dim3(grid), dim3(kThreads), smem, stream, maps, p);
     count_launch();
-    if (e != cudaSuccess || plan.parts == 1) return (int)e;
-    const SumPartsProblem sum{plan.parts, p.x_part_rows, d.M, d.N, d.y_type, static_cast<const float *>(d.partial), part_pitch(d.N), d.Y[0], d.y_ld[0]};
+    if (e != cudaSuccess || !p.x_planes) return (int)e;
+    const SumPartsProblem sum{plan.parts, p.x_part_rows, tokens, d.N, d.y_type, d.twins, static_cast<const float *>(d.partial), part_pitch(d.N), d.Y[0], d.y_ld[0]};
     return launch_sum_parts(sum, stream);
 }
 

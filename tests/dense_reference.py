@@ -78,15 +78,19 @@ def gated_int8(A, a_scale, Wg, g_scale, Wu, u_scale, kind, t):
     return _gate(kind, g, 4 * STEP * g.abs(), u, 4 * STEP * u.abs(), t)
 
 
-def gated_backward(dH, X, Wg, Wu, G, U, kind):
-    """((dX, tolerance), (dWg, tolerance), (dWu, tolerance)); dG and dU are rounded to the type on the way."""
+def gated_backward(dH, X, Wg, Wu, G, U, kind, twice=False):
+    """((dX, tolerance), (dWg, tolerance), (dWu, tolerance)); dG and dU are rounded to the type on the way, or (`twice`) what that leaves
+    of them is, which is half a step at most."""
     t = dH.dtype
     dh, g, u, x, wg, wu = (v.double() for v in (dH, G, U, X, Wg, Wu))
     value, slope = act(kind, g)
     dg, du = dh * u * slope, dh * value
     off_g = SLOPE * (dh * u).abs() + 3 * STEP * dg.abs()
     off_u = ACT * du.abs() + STEP * du.abs()
-    off_g, off_u = off_g + half_step(t, dg.abs() + off_g), off_u + half_step(t, du.abs() + off_u)
+    rest_g, rest_u = half_step(t, dg.abs() + off_g), half_step(t, du.abs() + off_u)
+    if twice:
+        rest_g, rest_u = half_step(t, rest_g), half_step(t, rest_u)
+    off_g, off_u = off_g + rest_g, off_u + rest_u
     F, M = dH.shape[1], dH.shape[0]
 
     def product(terms, n):
@@ -95,8 +99,9 @@ def gated_backward(dH, X, Wg, Wu, G, U, kind):
         off = sum(o @ b.abs() for _, o, b in terms) + n * STEP * size
         return y, off + half_step(t, y.abs() + off)
 
-    return (product([(dg, off_g, wg), (du, off_u, wu)], 2 * F),
-            product([(dg.T, off_g.T, x)], M), product([(du.T, off_u.T, x)], M))
+    n = 2 if twice else 1
+    return (product([(dg, off_g, wg), (du, off_u, wu)], 2 * n * F),
+            product([(dg.T, off_g.T, x)], n * M), product([(du.T, off_u.T, x)], n * M))
 
 
 def worst(got, pair):

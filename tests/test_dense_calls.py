@@ -105,6 +105,26 @@ def test_non_finite_values_stay_where_they_belong(M, value):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("size", [(1, 64, 69), (1, 368, 192), (2, 33, 1100), (5, 200, 64), (17, 96, 256), (31, 520, 77), (32, 64, 64)], ids=str)
+def test_gradients_of_few_tokens_round_once(size, t):
+    """Up to 32 tokens dG and dU keep what rounding leaves of them: the gradients are as near as rounding the results lets them be."""
+    M, K, F = size
+    X, Wg, Wu, dH = operands(M, K, F, t, 51)
+    H, G, U = binding.onnx_gated(X, Wg, Wu, activation="gelu_tanh", save=True)
+    dense = binding.onnx_gated_backward(dH, X, Wg, Wu, G, U, activation="gelu_tanh")
+    odd = torch.full((M, K + 3), 7.0, dtype=t, device="cuda")
+    odd[:, 1:K + 1] = X
+    strided = binding.onnx_gated_backward(dH, odd[:, 1:K + 1], Wg, Wu, G, U, activation="gelu_tanh")
+    want = ref.gated_backward(dH, X, Wg, Wu, G, U, "gelu_tanh", twice=True)
+    for y, z, pair in zip(dense, strided, want):
+        assert ref.worst(y, pair) <= 1 and torch.equal(y, z)
+        once = float((pair[0].to(t).double() - pair[0]).norm())
+        # (the products' sums in 32 bits and the activation's 2^-15 besides)
+        assert float((y.double() - pair[0]).norm()) <= 1.1 * once + 2.0 ** -13 * float(pair[0].norm())
+
+
+@pytest.mark.gpu
 def test_what_the_binding_refuses():
     X, Wg, Wu, dH = operands(6)
     Q, s = binding.onnx_quantize_rows(X)
