@@ -12,17 +12,19 @@ namespace {
 
 using namespace dense;
 
-// Rows that TMA cannot address (they do not begin at multiples of 16 bytes) laid out so that it can: a warp per row, 16 bytes a lane and
-// step.  A block per 8 rows of a tensor, all tensors of a call in one launch.
+// Rows that TMA cannot address (they do not begin at multiples of 16 bytes) laid out so that it can, zeros up to the next one: 16 bytes a lane
+// and step, a warp per row, several where rows are few and long, or one for several rows of less than 32 steps.  All tensors of a call in
+// one launch.
 __global__ void __launch_bounds__(256) repack_rows_kernel(const RepackProblem p) {
     tc::pdl_launch_dependents();
     tc::pdl_wait();
     const RepackJob &job = p.job[blockIdx.y];
-    const int lane = threadIdx.x % 32;
-    for (int row = blockIdx.x * 8 + threadIdx.x / 32; row < job.rows; row += gridDim.x * 8) {
+    const int per_row = job.dst_pitch >= 512 ? 32 : job.dst_pitch >= 256 ? 16 : 8, rows = 256 / per_row, lane = threadIdx.x % per_row;
+    for (int row = blockIdx.x * rows + threadIdx.x / per_row; row < job.rows; row += gridDim.x * rows) {
         const uint8_t *src = job.src + row * job.src_pitch;
         uint8_t *dst = job.dst + row * job.dst_pitch;
-        for (long long at = lane * 16; at < job.row_bytes; at += 32 * 16) *reinterpret_cast<uint4 *>(dst + at) = job.element == 2 ? load16_anywhere<2>(src, at, job.row_bytes) : load16_anywhere<1>(src, at, job.row_bytes);
+        for (long long at = (long long)(blockIdx.z * per_row + lane) * 16; at < job.dst_pitch; at += (long long)gridDim.z * per_row * 16)
+            *reinterpret_cast<uint4 *>(dst + at) = job.element == 2 ? load16_anywhere<2>(src, at, job.row_bytes) : load16_anywhere<1>(src, at, job.row_bytes);
     }
 }
 
@@ -123,9 +125,15 @@ int launch_slope(const GatedSlopeProblem &p, cudaStream_t stream) {
 int launch_dense(const DenseProblem &p, cudaStream_t stream) { return dense_few_fits(p) ? launch_dense_few(p, stream) : launch_tc_dense(p, stream); }
 
 int launch_repack_rows(const RepackProblem &p, cudaStream_t stream) {
-    int rows = 1;
-    for (int i = 0; i < p.count; ++i) rows = std::max(rows, p.job[i].rows);
-    const dim3 grid(std::min((rows + 7) / 8, 148 * 8), p.count);
+    int blocks = 1;
+    long long parts = 1;
+    for (int i = 0; i < p.count; ++i) {
+        parts = std::max(parts, (p.job[i].dst_pitch + 511) / 512);
+        const int rows = p.job[i].dst_pitch >= 512 ? 8 : p.job[i].dst_pitch >= 256 ? 16 : 32;        // a block
+        blocks = std::max(blocks, (p.job[i].rows + rows - 1) / rows);
+    }
+    blocks = std::min(blocks, 148 * 8);
+    const dim3 grid(blocks, p.count, (unsigned)std::max(1ll, std::min(parts, 148ll * 16 / (blocks * p.count))));
     const cudaError_t e = tc_host::launch_pdl(repack_rows_kernel, grid, dim3(256), 0, stream, p);
     count_launch();
     return (int)e;

@@ -61,6 +61,11 @@ struct Placement {
         workspace += bytes;
         return o;
     }
+    // The reduction's length for `operands` that all run along it: where every one is a copy, that with the zeros behind its rows, so that
+    // the kernels have whole blocks of it.
+    int reduction(int64_t K, int operands, int type) const {
+        return repack.count == operands ? (int)((K * type_bytes(type) + 127) / 128 * 128 / type_bytes(type)) : (int)K;
+    }
     int run(cudaStream_t stream) const { return repack.count ? launch_repack_rows(repack, stream) : 0; }
 };
 
@@ -115,6 +120,7 @@ extern "C" onnxb_status onnx_gemm_int8_run(const onnxb_matrix *A, const float *a
     Placement placed(workspace);
     d.A[0] = placed(A);
     d.B[0] = placed(B);
+    d.K = placed.reduction(K, 2, ONNXB_INT8);
     const int err = placed.run((cudaStream_t)cuda_stream);
     return status_of(err ? err : launch_dense(d, (cudaStream_t)cuda_stream));
 }
@@ -152,6 +158,7 @@ static onnxb_status run_gated(DenseProblem &d, const onnxb_matrix *X, const onnx
     d.A[0] = placed(X);
     d.B[0] = placed(Wg);
     d.B[1] = placed(Wu);
+    d.K = placed.reduction(X->cols, 3, X->type);
     const int err = placed.run(stream);
     return status_of(err ? err : launch_dense(d, stream));
 }

@@ -45,7 +45,7 @@ __device__ __forceinline__ uint4 load16_anywhere(const uint8_t *row, long long a
 #pragma unroll
     for (int i = 0; i < 16; i += kElement)
         if (at + i < row_bytes) {
-            const uint8_t *e = row + at + i;
+            const uint8_t *e = row + at + i;                     // (nothing is read past the row)
             const uint32_t v = kElement == 4 ? *reinterpret_cast<const uint32_t *>(e) : kElement == 2 ? *reinterpret_cast<const uint16_t *>(e) : *e;
             w[i / 4] |= v << (i % 4 * 8);
         }

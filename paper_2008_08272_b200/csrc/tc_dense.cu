@@ -408,10 +408,13 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                 for (int j = 0; j < 32; ++j) v[j] = sum[j];
             };
             if (row0 < M) {
-                for (int which = 0; which < p.outs; ++which) {
-                    const int y = !kGrad ? which : at.x ? 0 : 1 + p.w_first + at.z;
+                {
+                    // The two warps of a quarter share its blocks of all results in turns; of 8-bit operands, whose scales are fetched from
+                    // one to the next, a half each
 #pragma unroll 1
-                    for (int b = lo; b < hi; ++b) {
+                    for (int item = kInt8 ? lo : half, items = kInt8 ? hi : blocks * p.outs; item < items; item += kInt8 ? 1 : 2) {
+                        const int which = kInt8 || item < blocks ? 0 : item < 2 * blocks ? 1 : 2, b = item - which * blocks;
+                        const int y = !kGrad ? which : at.x ? 0 : 1 + p.w_first + at.z;
                         if (kSplit && owner(b) != part) continue;
                         // (TMA writes whole blocks, and of those at Y's end whole pieces of 16 bytes: not where the tile ends inside a block, or
                         // the last columns fill no piece, since what follows is another tile's or not Y's)
@@ -665,18 +668,20 @@ double stage_cycles(Tile t, int mode, int ks, int bytes, double ctas) {
 }
 double epilogue_cycles(Tile t) { return 1000.0 + 13.0 * t.BN; }
 
-Tile pick_tile(const Shape &d) {
+// `outs`: results that a tile's epilogue stores, the further ones at twice the first one's time in all; most_split: the most CTAs to share a reduction
+Tile pick_tile(const Shape &d, int outs, int most_split) {
     Tile best{1, 64, 1}, t;
-    if (pinned_tile(d.mode, t) && split_allowed(d, t)) return t;
     double best_cost = 1e300;
     for (t.ctas = 1; t.ctas <= 2; ++t.ctas)
         for (t.BN = 32; t.BN <= kMaxBN; t.BN += 32)
-            for (t.split = 1; t.split <= 8; t.split *= 2) {
+            for (t.split = 1; t.split <= most_split; t.split *= 2) {
                 if (!tile_allowed(d.mode, t) || !split_allowed(d, t)) continue;
                 const int out_cols = d.mode == kDenseGated ? t.BN / 2 : t.BN, units = t.ctas == 2 ? max_pairs() : tc_host::num_sms();
                 const long long tiles = ceil_div(d.M, kBM * t.ctas) * ceil_div(d.N, out_cols) * t.split, at_once = std::min<long long>(tiles, units);
                 const double stage = stage_cycles(t, d.mode, blocks_per_stage(d, t), block_bytes_of(d, t), (double)at_once * t.ctas);
-                const double main = ceil_div(stages_along(d, t), t.split) * stage, epilogue = epilogue_cycles(t);
+                // (columns that fill no blocks are stored plainly)
+                const double main = ceil_div(stages_along(d, t), t.split) * stage, whole = out_cols * type_bytes(d.y_type) % kRowBytes ? 2.0 : 1.0;
+                const double epilogue = epilogue_cycles(t) * whole * (outs > 1 ? 2.0 : 1.0);
                 double cost = (double)ceil_div(tiles, units) * std::max(main, epilogue) + epilogue;
                 if (t.split > 1) cost += (2500.0 + 28.0 * t.BN) * (t.split == 2 ? 1.0 : t.split == 4 ? 1.3 : 1.5);
                 if (cost < best_cost * (1 - 1e-9)) {
@@ -685,6 +690,13 @@ Tile pick_tile(const Shape &d) {
                 }
             }
     return best;
+}
+Tile pick_tile(const Shape &d) {
+    Tile t;
+    if (pinned_tile(d.mode, t) && split_allowed(d, t)) return t;
+    // Whether and how a reduction is shared does not go by what else is stored: the gated block's H is the same bit by bit with G and U and without
+    t = pick_tile(d, 1, 8);
+    return t.split == 1 && d.mode == kDenseGated && d.Y[1] ? pick_tile(d, 3, 1) : t;
 }
 
 // The gradients' tiles, and the parts of dX's reduction, each with an fp32 plane that sum_parts_kernel adds up.  From the sizes alone (as a B200
