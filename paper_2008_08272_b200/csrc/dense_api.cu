@@ -175,7 +175,9 @@ extern "C" onnxb_status onnx_gated_run(const onnxb_matrix *X, const onnxb_matrix
         CHECK(check_view(U));
         if (G->type != X->type || U->type != X->type) return ONNXB_ERR_ATTR;
         if (!has_size(G, H->rows, H->cols) || !has_size(U, H->rows, H->cols)) return ONNXB_ERR_SHAPE;
-        if (same_place(G, U) || same_place(G, H) || same_place(U, H) || same_place(G, X) || same_place(U, X)) return ONNXB_ERR_UNSUPPORTED;
+        if (same_place(G, U) || same_place(G, H) || same_place(U, H)) return ONNXB_ERR_UNSUPPORTED;
+        for (const onnxb_matrix *in : {X, Wg, Wu})
+            if (same_place(G, in) || same_place(U, in)) return ONNXB_ERR_UNSUPPORTED;
         d.Y[1] = G->data; d.y_ld[1] = operand(G).ld;
         d.Y[2] = U->data; d.y_ld[2] = operand(U).ld;
     }

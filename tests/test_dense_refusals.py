@@ -97,7 +97,7 @@ def test_gated():
     assert call(good, activation=4) == ATTR and call(good, activation=-1) == ATTR
     for name, size in (("X", (5, 40)), ("Wg", (30, 41)), ("Wu", (31, 40)), ("H", (4, 31)), ("G", (3, 30)), ("U", (4, 29))):
         assert call({**good, name: mat(*size, BF16)}) == SHAPE
-    for a, b in (("G", "U"), ("G", "H"), ("U", "H"), ("H", "X"), ("G", "X"), ("H", "Wg")):
+    for a, b in (("G", "U"), ("G", "H"), ("U", "H"), ("H", "X"), ("G", "X"), ("H", "Wg"), ("G", "Wg"), ("U", "Wu")):
         assert call({**good, a: change(good[a], data=good[b].data)}) == UNSUPPORTED
     assert call({**good, "H": change(good["H"], data=good["H"].data + 1)}) == UNSUPPORTED
 
