@@ -35,7 +35,7 @@ __device__ __forceinline__ T remainder_of(float v, T nearest) {
     return from_float<T>(isfinite(left) ? left : 0.f);
 }
 
-// dG = dH U act'(G), dU = dH act(G): five tensors' bytes, and about 40 instructions an element.  A block has 8 rows by 32 pieces of 8
+// dG = dH U act'(G), dU = dH act(G), in 32 bits and rounded once, to what the tensor cores take: five tensors' bytes, and about 40 instructions an element.  A block has 8 rows by 32 pieces of 8
 // elements (of 1 where rows do not begin at multiples of 16 bytes), so that nothing is divided to find a place.  4096 x 10240 of bf16: 65 us (6.5
 // TB/s).  kTwins: see GatedSlopeProblem; the blocks from x_blocks on copy X.
 template <typename T, int kCount, bool kTwins>

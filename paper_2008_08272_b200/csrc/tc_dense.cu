@@ -14,10 +14,15 @@
 //   - The gradients are one launch: dX's tiles, which are few and long, then those of dWg and dWu, handed out so that the units that got
 //     one tile of dX less get as many more of the others as that one takes.
 //   - dX = dG Wg + dU Wu is one sum: the reduction runs over dG's channels, then dU's, with the other tensor maps from there on.
-//   - dWg = dG^T X and dWu = dU^T X take their operands as they lie, the reduction (tokens) along the rows: MN-major, 64 x 64 boxes.
-//     The same for Wg and Wu in dX.  No transposed copy is made, and dG's map serves both uses: its boxes are 64 x 64 either way.
+//   - dWg = dG^T X and dWu = dU^T X take their operands as they lie, the reduction (tokens) along the rows: MN-major, boxes of 64
+//     by 64 or, two K blocks a stage, 128.  The same for Wg and Wu in dX.  No transposed copy is made, and dG's map serves both uses: its
+//     boxes are 64 terms by so many tokens, or 64 channels by so many terms.
 //   - Few tiles with a long reduction share it: the CTAs of a cluster have a part each of one tile's, and every quarter of a block of
 //     columns is added up by one of them, from what the others write into its shared memory, in the parts' order.
+// Measured (a burst; under the power cap of a long run in brackets): gated block 4096 x 4096 x 10240 in bf16 with G and U kept 450 us, 1.53
+// PFLOP/s (535), of 8-bit operands 203 us, 3.4 POP/s (247); 8-bit Gemm 4096 x 10240 x 4096 110 us, 3.1 POP/s (130); the three products of
+// the gradients at the first size 880 us, 1.56 PFLOP/s: the tensor pipe is 90 to 96 % busy.  Small tiles are bound by a stage's
+// 410 cycles, short reductions by the epilogue's latencies (two warps a scheduler), few tokens by the weights' bytes.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -199,15 +204,18 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
         const int nb = kGrad ? bnh / 64 : kMode == kDenseGated && kCtas == 1 ? 2 : 1;
         const bool is_a = lane < na, active = lane < na + nb;
         const int piece = is_a ? lane : lane - na;
-        const uint32_t dst_off = is_a ? (uint32_t)piece * (kABytes / na) : p.a_bytes + (uint32_t)piece * (uint32_t)(bnh * kRowBytes / nb);
+        // (a piece of 64 columns has a block of the reduction after the other; the two pieces of dG are such, or for dX its rows')
+        const uint32_t dst_off = is_a ? (uint32_t)(piece * p.ks) * (kABytes / na)
+                                      : (uint32_t)p.ks * (p.a_bytes + (uint32_t)piece * (uint32_t)(bnh * kRowBytes / nb));
         constexpr int kTerms = kInt8 ? kRowBytes : kRowBytes / 2;       // of the reduction per stage
         for (int n = 0; nth_tile<kMode, kSplit>(p, unit, units, n, at); ++n) {
             // the first of the rows that this copy brings (along the output's rows or columns), and whether they lie along a row in memory
             int row = is_a ? (at.tm * kCtas + rank) * kBM : at.tn * p.BN + rank * bnh;
-            if (kGrad) row += piece * 64;
             const bool mn = kGrad && !(is_a && at.x);
+            if (kGrad && (mn || p.ks == 1)) row += piece * 64;
             const CUtensorMap *map = is_a ? &maps.A[0] : &maps.B[0];
-            int term = at.kb0 * kTerms;
+            int term = at.kb0 * kTerms * p.ks;
+            const int ahead = kGrad && p.ks == 2 && !mn ? piece * kTerms : 0;          // (dX's two pieces of dG: a block each)
             if (kMode == kDenseGated && !is_a) {
                 // a pair's CTA has one of the two weights, a lone CTA both
                 row = at.tn * p.out_cols;
@@ -216,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
             if (kGrad && !at.x) map = is_a ? &maps.A[p.w_first + at.z] : &maps.B[2];
             if (kGrad && at.x && at.kb0 * 2 >= p.x_kb) {
                 map += 1;
-                term -= p.x_kb / 2 * kTerms;
+                term -= p.x_kb / 2 * kTerms * p.ks;
             }
             if (n == 0) pdl_wait();
             for (int kb = at.kb0; kb < at.kb1; ++kb) {
@@ -256,11 +264,11 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                 }
                 uint8_t *dst = stages + (size_t)stage * p.stage_bytes + dst_off;
                 if (active) {
-                    const int c0 = mn ? row : term, c1 = mn ? term : row;
+                    const int c0 = mn ? row : term + ahead, c1 = mn ? term : row;
                     if (kCtas == 2) tma_load_2d_pair(dst, map, full_issuer + (uint32_t)stage * 8u, c0, c1);
                     else tma_load_2d(dst, map, &full[stage], c0, c1);
                 }
-                term += kTerms;
+                term += kTerms * p.ks;
                 if (++stage == p.num_stages) { stage = 0; phase ^= 1; }
             }
         }
@@ -275,21 +283,21 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
             int stage = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0;
             // K-major: 8-row groups 1024 bytes apart, an instruction 32 bytes further along the swizzled rows.  MN-major: blocks of 64
-            // rows or columns 64 x 128 bytes apart, groups of 8 terms 1024 bytes apart, an instruction two of those further.
-            const uint64_t k_tmpl = make_smem_desc(0, 16, 1024, kSwizzle128B), mn_tmpl = make_smem_desc(0, 64 * kRowBytes, 1024, kSwizzle128B);
+            // rows or columns a stage's 64 or 128 terms of 128 bytes apart, groups of 8 terms 1024 bytes apart, an instruction two of those further.
+            const uint64_t k_tmpl = make_smem_desc(0, 16, 1024, kSwizzle128B), mn_tmpl = make_smem_desc(0, 64u * kRowBytes * (uint32_t)p.ks, 1024, kSwizzle128B);
             // (Both weights of the gated block in a lone CTA's stage of several blocks: a block's 8-row groups lie as far apart as all blocks'
             // take, so that one weight's go on where the other's end)
             const bool groups = kMode == kDenseGated && kCtas == 1;
             const uint64_t b_tmpl = kGrad ? mn_tmpl : make_smem_desc(0, 16, groups ? 1024u * (uint32_t)p.ks : 1024u, kSwizzle128B);
             const uint32_t b_hi = (uint32_t)(b_tmpl >> 32);
             const uint32_t a_at = (smem_u32(stages) >> 4) & 0x3FFFu, b_lo = (uint32_t)b_tmpl | (((smem_u32(stages) + (uint32_t)p.ks * p.a_bytes) >> 4) & 0x3FFFu);
-            const uint32_t stage16 = p.stage_bytes >> 4, b_block16 = (groups ? 1024u : (uint32_t)(p.BN / kCtas * kRowBytes)) >> 4;
+            const uint32_t stage16 = p.stage_bytes >> 4, b_block16 = (kGrad ? 64u * kRowBytes : groups ? 1024u : (uint32_t)(p.BN / kCtas * kRowBytes)) >> 4;
             constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kB16 = kGrad ? kMn16 : kK16;
             for (int n = 0; nth_tile<kMode, kSplit>(p, unit, units, n, at); ++n) {
                 const bool a_mn = kGrad && !at.x;
                 const uint64_t a_tmpl = a_mn ? mn_tmpl : k_tmpl;
                 const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), a_lo = (uint32_t)a_tmpl | a_at, a16 = a_mn ? kMn16 : kK16;
-                const uint32_t idesc = kGrad && at.x ? p.idesc_x : p.idesc;
+                const uint32_t idesc = kGrad && at.x ? p.idesc_x : p.idesc, a_block16 = (a_mn ? 64u * kRowBytes : p.a_bytes) >> 4;
                 if (kCtas == 2) mbar_wait_cluster(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 else mbar_wait(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 tc_fence_after_sync();
@@ -312,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                             }
                             accumulate = 1;
                         }
-                        al += p.a_bytes >> 4;
+                        al += a_block16;
                         bl += b_block16;
                     }
                     if (kCtas == 2) mma_commit_pair(&empty[stage]);
@@ -635,8 +643,8 @@ int block_bytes_of(const Shape &d, Tile t) { return (a_rows_of(d, t) + t.BN / t.
 // ends with the tensors.)
 int blocks_per_stage(const Shape &d, Tile t) {
     if (d.mode == kDenseGated && t.ctas == 1 && (d.N % 8 || d.K % (kRowBytes / type_bytes(d.type)))) return 1;
-    const int most = d.mode == kDenseGrad ? 1 : std::min(d.most_ks, ring_bytes() / 4 / block_bytes_of(d, t));
-    return most >= 4 ? 4 : most >= 2 ? 2 : 1;
+    const int most = std::min(d.most_ks, ring_bytes() / 4 / block_bytes_of(d, t));
+    return most >= 4 && d.mode != kDenseGrad ? 4 : most >= 2 ? 2 : 1;
 }
 int stages_of(const Shape &d, Tile t) { return std::min(kMaxStages, ring_bytes() / (block_bytes_of(d, t) * blocks_per_stage(d, t))); }
 long long stages_along(const Shape &d, Tile t) { return ceil_div(d.K, (long long)(kRowBytes / type_bytes(d.type)) * blocks_per_stage(d, t)); }
@@ -707,23 +715,29 @@ struct GradPlan {
 };
 constexpr int kGradTerms = kRowBytes / 2;
 GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
+    DenseProblem sizes{};
+    sizes.mode = kDenseGrad;
+    sizes.type = ONNXB_BFLOAT16;
+    sizes.M = tokens; sizes.N = width; sizes.K = channels;
+    const Shape shape(sizes);
     GradPlan best{{1, 64, 1}, 1};
     double best_cost = 1e300;
     Tile pinned;
     const bool pin = pinned_tile(kDenseGrad, pinned);
     const char *pin_parts = getenv("ONNXB_DENSE_PARTS");
-    const double x_kb = 2.0 * ceil_div(channels, kGradTerms), w_kb = (double)ceil_div(tokens, kGradTerms);
     for (int ctas = 1; ctas <= 2; ++ctas)
         for (int bn = 64; bn <= kMaxBN; bn += 64)
             for (int parts = 1; parts <= 8; parts *= 2) {
                 const Tile t{ctas, bn, 1};
                 if (!tile_allowed(kDenseGrad, t) || (pin && (t.ctas != pinned.ctas || t.BN != pinned.BN))) continue;
+                const int ks = blocks_per_stage(shape, t);
+                const double x_kb = 2.0 * ceil_div(channels, kGradTerms * ks), w_kb = (double)ceil_div(tokens, kGradTerms * ks);
                 if (parts > 1 && (!dX || x_kb < 8 * parts)) continue;
                 if (pin_parts && parts != atoi(pin_parts) && (parts > 1 || (dX && x_kb >= 8 * atoi(pin_parts)))) continue;
                 const double units = ctas == 2 ? 74 : 148, epilogue = epilogue_cycles(t);
                 const double x_tiles = dX ? (double)(ceil_div(tokens, kBM * ctas) * ceil_div(width, bn)) * parts : 0.0;
                 const double w_tiles = (double)(ceil_div(channels, kBM * ctas) * ceil_div(width, bn)) * weights;
-                const double stage = stage_cycles(t, kDenseGrad, 1, (kBM + bn / ctas) * kRowBytes, ctas * std::min(units, x_tiles + w_tiles));
+                const double stage = stage_cycles(t, kDenseGrad, ks, block_bytes_of(shape, t), ctas * std::min(units, x_tiles + w_tiles));
                 const double x_cost = std::max(x_kb / parts * stage, epilogue), w_cost = std::max(w_kb * stage, epilogue);
                 double cost = std::ceil(x_tiles / units) * x_cost;
                 if (w_tiles > 0) cost = std::max(cost, x_tiles > 0 ? (x_tiles * x_cost + w_tiles * w_cost) / units + 0.5 * w_cost : std::ceil(w_tiles / units) * w_cost);
@@ -741,7 +755,7 @@ GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
 long long part_rows(int tokens, Tile t) { return ceil_div(tokens, kBM * t.ctas) * kBM * t.ctas; }
 long long part_pitch(int width) { return ceil_div(width, 4) * 4; }
 
-// A's and B's maps; their rows begin at multiples of 16 bytes.  K-major: (terms, rows) boxes of 128 bytes x `box` rows.  The gradients': 64 x 64.
+// A's and B's maps; their rows begin at multiples of 16 bytes.  K-major: (terms, rows) boxes of 128 bytes x `box` rows.  The gradients': 64 x 64 ks.
 bool operand_map(CUtensorMap *m, const DenseOperand &o, int bytes, long long rows, long long cols, int box) {
     const uint64_t pitch = (uint64_t)(rows > 1 ? o.ld * bytes : (o.ld * bytes + 15) / 16 * 16);
     const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows};
@@ -804,10 +818,10 @@ int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
         p.x_planes = d.Y[0] && (plan.parts > 1 || d.twins);
         x_tiles = d.Y[0] ? total * plan.parts : 0;
         p.w_tiles_m = (int)ceil_div(d.K, kBM * tile.ctas);
-        p.w_kb = (int)ceil_div(d.M, terms);
+        p.w_kb = (int)ceil_div(d.M, terms * p.ks);
         p.w_first = d.Y[1] ? 0 : 1;
         w_tiles = (long long)p.w_tiles_m * p.tiles_n * weights;
-        const double stage = stage_cycles(tile, kDenseGrad, 1, (kBM + p.BN / tile.ctas) * kRowBytes, 148), epilogue = epilogue_cycles(tile);
+        const double stage = stage_cycles(tile, kDenseGrad, p.ks, block_bytes_of(d, tile), 148), epilogue = epilogue_cycles(tile);
         p.w_before = (int)(std::max(p.x_part_kb * stage, epilogue) / std::max(p.w_kb * stage, epilogue));
         total = x_tiles + w_tiles;
         if (plan.parts * (long long)p.x_part_rows > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
@@ -837,8 +851,8 @@ int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
     // (a map that nobody uses is a copy of one that is there)
     if (grad) {
         for (int i = 0; i < 2; ++i) {
-            fine = fine && operand_map(&maps.A[i], d.A[i], bytes, d.M, d.K, 64);
-            if (d.Y[0]) fine = fine && operand_map(&maps.B[i], d.B[i], bytes, d.K, d.N, 64);
+            fine = fine && operand_map(&maps.A[i], d.A[i], bytes, d.M, d.K, 64 * p.ks);
+            if (d.Y[0]) fine = fine && operand_map(&maps.B[i], d.B[i], bytes, d.K, d.N, 64 * p.ks);
             else maps.B[i] = maps.A[0];
         }
     } else {
@@ -848,14 +862,14 @@ int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
         else maps.B[1] = maps.B[0];
     }
     maps.A4 = maps.B4[0] = maps.B4[1] = maps.A[0];
-    if (p.full_kb > 0 && p.ks > 1) {
+    if (!grad && p.full_kb > 0 && p.ks > 1) {
         const int b_rows = gated ? p.out_cols : bnh;
         const bool groups = gated && tile.ctas == 1;
         fine = fine && blocks_map(&maps.A4, d.A[0], bytes, d.M, d.K, a_rows, p.ks, false);
         for (int i = 0; i < (gated ? 2 : 1); ++i) fine = fine && blocks_map(&maps.B4[i], d.B[i], bytes, d.N, d.K, b_rows, p.ks, groups);
     }
     maps.B[2] = maps.A[0];
-    if (weights) fine = fine && operand_map(&maps.B[2], d.B[2], bytes, d.M, d.N, 64);
+    if (weights) fine = fine && operand_map(&maps.B[2], d.B[2], bytes, d.M, d.N, 64 * p.ks);
     if (!fine) return (int)cudaErrorInvalidValue;
     for (int i = 0; i < 3; ++i) {
         maps.Y[i] = maps.A[0];

@@ -101,6 +101,25 @@ def test_parts_of_the_reduction(tile, parts, size, monkeypatch):
     assert binding.last_device_status() == 0
 
 
+@pytest.mark.parametrize("size", [(40, 200, 70), (300, 520, 700), (129, 77, 1030), (700, 136, 64), (64, 64, 2056)], ids=str)
+@pytest.mark.parametrize("ks", [1, 2])
+@pytest.mark.parametrize("tile", ["1x64", "1x128", "2x128", "2x256"])
+def test_gradients_by_blocks_per_stage(tile, ks, size, monkeypatch):
+    monkeypatch.setenv("ONNXB_DENSE_TILE", tile)
+    monkeypatch.setenv("ONNXB_DENSE_KS", str(ks))
+    M, K, F = size
+    g = torch.Generator(device="cuda").manual_seed(24)
+    t = torch.bfloat16
+    X, Wg, Wu = normal(g, M, K).to(t), (normal(g, F, K) / math.sqrt(K)).to(t), (normal(g, F, K) / math.sqrt(K)).to(t)
+    dH, G, U = normal(g, M, F).to(t), normal(g, M, F).to(t), normal(g, M, F).to(t)
+    want = ref.gated_backward(dH, X, Wg, Wu, G, U, "relu")
+    for parts in ("1", "4"):
+        monkeypatch.setenv("ONNXB_DENSE_PARTS", parts)
+        for y, pair in zip(binding.onnx_gated_backward(dH, X, Wg, Wu, G, U, activation="relu"), want):
+            assert ref.worst(y, pair) <= 1
+    assert binding.last_device_status() == 0
+
+
 @pytest.mark.parametrize("size", [(1, 4096, 700), (3, 200, 33), (8, 1030, 257), (9, 520, 100), (16, 2056, 300), (12, 24, 40)], ids=str)
 @pytest.mark.parametrize("warps", [4, 8, 16])
 def test_few_tokens_by_warps(warps, size, monkeypatch):
