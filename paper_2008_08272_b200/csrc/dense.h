@@ -19,6 +19,10 @@ struct DenseOperand {
     long long ld;        // elements between rows of the tensor as it is stored
 };
 
+struct GradChoice {      // tile shape, and parts of dX's reduction
+    int ctas, BN, parts;
+};
+
 struct DenseProblem {
     int mode;
     int type;            // of the operands
@@ -29,7 +33,8 @@ struct DenseProblem {
     int y_type;
     void *Y[3];
     long long y_ld[3];
-    void *partial;       // kDenseGrad: tc_grad_workspace bytes
+    GradChoice grad;     // kDenseGrad: tc_grad_choice's
+    void *partial;       // tc_grad_workspace bytes
     // kDenseGrad of a few tokens: A[0] and A[1] hold every token twice, the 16-bit numbers nearest to dG and dU and, M/2 rows on, those nearest
     // to what these leave of them; B[2] holds X twice; Y[0] is the sum of both.  (M: rows of A)
     int twins;
@@ -44,7 +49,8 @@ int launch_dense_few(const DenseProblem &p, cudaStream_t stream);
 // On the tensor cores (tc_dense.cu).  Operands' rows begin at multiples of 16 bytes.
 int launch_tc_dense(const DenseProblem &p, cudaStream_t stream);
 // Scratch that the gradients' products need (dX in parts of its long reduction, where there would be few tiles)
-size_t tc_grad_workspace(int rows, int channels, int width, bool dX, int weights, bool twins);
+GradChoice tc_grad_choice(int rows, int channels, int width, bool dX, int weights);
+size_t tc_grad_workspace(const GradChoice &choice, int rows, int width, bool dX, bool twins);
 
 // Y[i,j] = the sum over s < parts of P[s * part_rows + i][j], in that order, and of twins that of P[s * part_rows + M + i][j] after each,
 // rounded to `type`; P's rows p_ld floats apart (a multiple of 4)

@@ -216,13 +216,21 @@ static size_t tokens_bytes(const onnxb_matrix *X) {
     return has_twins(X->rows) ? slope_bytes(X->rows, X->cols) : copy_bytes(X);
 }
 
-extern "C" size_t onnx_gated_backward_workspace_bytes(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
-                                                      const onnxb_matrix *dX, const onnxb_matrix *dWg, const onnxb_matrix *dWu) {
+static size_t backward_bytes(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu, const onnxb_matrix *dX,
+                             const onnxb_matrix *dWg, const onnxb_matrix *dWu, GradChoice &choice) {
     if (!dH || dH->rows < 1 || dH->cols < 1 || dH->rows > kMostSize || dH->cols > kMostSize) return 0;
     const onnxb_matrix *one = dX ? dX : dWg ? dWg : dWu;
     if (!one || one->cols < 1 || one->cols > kMostSize) return 0;
+    const int rows = (int)slope_rows(dH->rows), width = (int)one->cols;
+    choice = tc_grad_choice(rows, (int)dH->cols, width, dX != nullptr, (dWg != nullptr) + (dWu != nullptr));
     return 2 * slope_bytes(dH->rows, dH->cols) + (dX ? copy_bytes(Wg) + copy_bytes(Wu) : 0) + (dWg || dWu ? tokens_bytes(X) : 0) +
-           tc_grad_workspace((int)slope_rows(dH->rows), (int)dH->cols, (int)one->cols, dX != nullptr, (dWg != nullptr) + (dWu != nullptr), has_twins(dH->rows));
+           tc_grad_workspace(choice, rows, width, dX != nullptr, has_twins(dH->rows));
+}
+
+extern "C" size_t onnx_gated_backward_workspace_bytes(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
+                                                      const onnxb_matrix *dX, const onnxb_matrix *dWg, const onnxb_matrix *dWu) {
+    GradChoice choice;
+    return backward_bytes(dH, X, Wg, Wu, dX, dWg, dWu, choice);
 }
 
 extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
@@ -264,7 +272,8 @@ extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const on
                 return ONNXB_ERR_CUDA;
         return ONNXB_OK;
     }
-    CHECK(check_workspace(workspace, workspace_bytes, onnx_gated_backward_workspace_bytes(dH, X, Wg, Wu, dX, dWg, dWu)));
+    DenseProblem d{};
+    CHECK(check_workspace(workspace, workspace_bytes, backward_bytes(dH, X, Wg, Wu, dX, dWg, dWu, d.grad)));
     GatedSlopeProblem s{};
     s.type = dH->type; s.activation = activation;
     s.M = (int)M; s.F = (int)F;
@@ -283,7 +292,6 @@ extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const on
         ws += tokens_bytes(X);
     }
     int err = launch_gated_slope(s, stream);
-    DenseProblem d{};
     d.mode = kDenseGrad;
     d.type = d.y_type = dH->type;
     d.M = (int)slope_rows(M); d.N = (int)K; d.K = (int)F;

@@ -176,9 +176,11 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
             mbar_init(&tmem_empty[a], kEpiWarps * kCtas);
         }
         mbar_fence_init();
-        prefetch_tmap(&maps.A[0]);
-        prefetch_tmap(&maps.B[0]);
-        if (kMode == kDenseGated) prefetch_tmap(&maps.B[1]);
+        // (of those that there are)
+        const bool blocks = !kGrad && p.ks > 1 && p.full_kb > 0;
+        prefetch_tmap(blocks ? &maps.A4 : &maps.A[0]);
+        if (!kGrad || p.x_tiles) prefetch_tmap(blocks ? &maps.B4[0] : &maps.B[0]);
+        if (kMode == kDenseGated) prefetch_tmap(blocks ? &maps.B4[1] : &maps.B[1]);
         if (p.y_tma[0]) prefetch_tmap(&maps.Y[0]);
     }
     if (warp == 1) {
@@ -581,6 +583,19 @@ Kernel split_kernel_for(int mode, bool int8) {
     return mode == kDenseGated ? tc_dense_kernel<1, true, kDenseGated, true> : tc_dense_kernel<1, true, kDensePlain, true>;
 }
 
+// The kernel's shared memory allowed for, once a device (`index`: the kernel's, below 12)
+cudaError_t allow_shared_memory(Kernel kernel, int index) {
+    static std::atomic<uint64_t> done[12];
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (done[index].load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+    if (set == cudaSuccess && dev < 64) done[index].fetch_or(bit, std::memory_order_release);
+    return set;
+}
+
 // CTA pairs that run at once, asked of the device's occupancy once (as for tc_gemm_kernel, whose shared memory and threads are the same)
 int max_pairs() {
     static std::atomic<int> cached{-1};
@@ -619,6 +634,7 @@ struct Tile {
     int split;                 // CTAs that share a tile's reduction, in a cluster
 };
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+int ceil_int(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }      // (32 bits: a choice makes dozens)
 bool tile_allowed(int mode, Tile t) {
     if (t.BN < 32 * t.ctas || t.BN > kMaxBN || t.BN % (32 * t.ctas)) return false;
     if (mode == kDenseGated) return t.BN % 64 == 0;
@@ -648,8 +664,9 @@ int blocks_per_stage(const Shape &d, Tile t) {
 }
 int stages_of(const Shape &d, Tile t) { return std::min(kMaxStages, ring_bytes() / (block_bytes_of(d, t) * blocks_per_stage(d, t))); }
 long long stages_along(const Shape &d, Tile t) { return ceil_div(d.K, (long long)(kRowBytes / type_bytes(d.type)) * blocks_per_stage(d, t)); }
-// A shared reduction: every CTA has a part of it, all tiles run at once (of 148 SMs not every eight are a cluster's), and what
+// A shared reduction: every CTA has a part of it, all tiles run at once (of 148 SMs not every eight are a cluster's: 128), and what
 // the others send has room where the ring was
+constexpr long long kMostShared = 128;
 bool split_allowed(const Shape &d, Tile t) {
     if (t.split == 1) return true;
     const long long num_kb = stages_along(d, t);
@@ -657,7 +674,7 @@ bool split_allowed(const Shape &d, Tile t) {
     const int out_cols = d.mode == kDenseGated ? t.BN / 2 : t.BN, block_cols = d.y_type == ONNXB_FLOAT ? 32 : 64;
     const long long tiles = ceil_div(d.M, kBM) * ceil_div(d.N, out_cols), part = ceil_div(num_kb, t.split);
     const long long places = ceil_div(ceil_div(out_cols, block_cols) * 4, t.split) * (block_cols / 32) * (d.mode == kDenseGated ? 2 : 1) * (t.split - 1);
-    return tiles * t.split <= 128 && part * (t.split - 1) < num_kb &&
+    return tiles * t.split <= kMostShared && part * (t.split - 1) < num_kb &&
            places * kBlockBytes <= (long long)stages_of(d, t) * block_bytes_of(d, t) * blocks_per_stage(d, t);
 }
 // "<CTAs>x<BN>" or "1x<BN>/<split>" in ONNXB_DENSE_TILE pins the shape for A/B measurements and tests
@@ -680,23 +697,31 @@ double epilogue_cycles(Tile t) { return 1000.0 + 13.0 * t.BN; }
 Tile pick_tile(const Shape &d, int outs, int most_split) {
     Tile best{1, 64, 1}, t;
     double best_cost = 1e300;
-    for (t.ctas = 1; t.ctas <= 2; ++t.ctas)
-        for (t.BN = 32; t.BN <= kMaxBN; t.BN += 32)
+    const int terms = kRowBytes / type_bytes(d.type), y_bytes = type_bytes(d.y_type);
+    for (t.ctas = 1; t.ctas <= 2; ++t.ctas) {
+        const int units = t.ctas == 2 ? max_pairs() : tc_host::num_sms(), tiles_m = ceil_int(d.M, kBM * t.ctas);
+        for (t.BN = 32 * t.ctas; t.BN <= kMaxBN; t.BN += 32) {
+            if (!tile_allowed(d.mode, t)) continue;
+            const int out_cols = d.mode == kDenseGated ? t.BN / 2 : t.BN, ks = blocks_per_stage(d, t), bytes = block_bytes_of(d, t);
+            const long long tiles = (long long)tiles_m * ceil_int(d.N, out_cols);
+            const int stages = ceil_int(d.K, terms * ks);
+            // (columns that fill no blocks are stored plainly)
+            const double epilogue = epilogue_cycles(t) * (out_cols * y_bytes % kRowBytes ? 2.0 : 1.0) * (outs > 1 ? 2.0 : 1.0);
             for (t.split = 1; t.split <= most_split; t.split *= 2) {
-                if (!tile_allowed(d.mode, t) || !split_allowed(d, t)) continue;
-                const int out_cols = d.mode == kDenseGated ? t.BN / 2 : t.BN, units = t.ctas == 2 ? max_pairs() : tc_host::num_sms();
-                const long long tiles = ceil_div(d.M, kBM * t.ctas) * ceil_div(d.N, out_cols) * t.split, at_once = std::min<long long>(tiles, units);
-                const double stage = stage_cycles(t, d.mode, blocks_per_stage(d, t), block_bytes_of(d, t), (double)at_once * t.ctas);
-                // (columns that fill no blocks are stored plainly)
-                const double main = ceil_div(stages_along(d, t), t.split) * stage, whole = out_cols * type_bytes(d.y_type) % kRowBytes ? 2.0 : 1.0;
-                const double epilogue = epilogue_cycles(t) * whole * (outs > 1 ? 2.0 : 1.0);
-                double cost = (double)ceil_div(tiles, units) * std::max(main, epilogue) + epilogue;
+                if (t.split > 1 && tiles * t.split > kMostShared) break;
+                if (t.split > 1 && !split_allowed(d, t)) continue;
+                const long long at_once = std::min<long long>(tiles * t.split, units);
+                const double stage = stage_cycles(t, d.mode, ks, bytes, (double)(at_once * t.ctas));
+                const double main = (t.split == 1 ? stages : ceil_int(stages, t.split)) * stage;
+                double cost = (double)(tiles * t.split <= units ? 1 : ceil_div(tiles, units)) * std::max(main, epilogue) + epilogue;
                 if (t.split > 1) cost += (2500.0 + 28.0 * t.BN) * (t.split == 2 ? 1.0 : t.split == 4 ? 1.3 : 1.5);
                 if (cost < best_cost * (1 - 1e-9)) {
                     best_cost = cost;
                     best = t;
                 }
             }
+        }
+    }
     return best;
 }
 Tile pick_tile(const Shape &d) {
@@ -725,20 +750,20 @@ GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
     Tile pinned;
     const bool pin = pinned_tile(kDenseGrad, pinned);
     const char *pin_parts = getenv("ONNXB_DENSE_PARTS");
-    for (int ctas = 1; ctas <= 2; ++ctas)
-        for (int bn = 64; bn <= kMaxBN; bn += 64)
+    const int only = pin_parts ? atoi(pin_parts) : 0;
+    for (int ctas = 1; ctas <= 2; ++ctas) {
+        const int units = ctas == 2 ? 74 : 148, tiles_x = ceil_int(tokens, kBM * ctas), tiles_w = ceil_int(channels, kBM * ctas) * weights;
+        for (int bn = 64 * ctas; bn <= kMaxBN; bn += 64 * ctas) {
+            const Tile t{ctas, bn, 1};
+            if (pin && (t.ctas != pinned.ctas || t.BN != pinned.BN)) continue;
+            const int ks = blocks_per_stage(shape, t), x_kb = 2 * ceil_int(channels, kGradTerms * ks), w_kb = ceil_int(tokens, kGradTerms * ks);
+            const double across = ceil_int(width, bn), epilogue = epilogue_cycles(t), w_tiles = tiles_w * across;
             for (int parts = 1; parts <= 8; parts *= 2) {
-                const Tile t{ctas, bn, 1};
-                if (!tile_allowed(kDenseGrad, t) || (pin && (t.ctas != pinned.ctas || t.BN != pinned.BN))) continue;
-                const int ks = blocks_per_stage(shape, t);
-                const double x_kb = 2.0 * ceil_div(channels, kGradTerms * ks), w_kb = (double)ceil_div(tokens, kGradTerms * ks);
-                if (parts > 1 && (!dX || x_kb < 8 * parts)) continue;
-                if (pin_parts && parts != atoi(pin_parts) && (parts > 1 || (dX && x_kb >= 8 * atoi(pin_parts)))) continue;
-                const double units = ctas == 2 ? 74 : 148, epilogue = epilogue_cycles(t);
-                const double x_tiles = dX ? (double)(ceil_div(tokens, kBM * ctas) * ceil_div(width, bn)) * parts : 0.0;
-                const double w_tiles = (double)(ceil_div(channels, kBM * ctas) * ceil_div(width, bn)) * weights;
-                const double stage = stage_cycles(t, kDenseGrad, ks, block_bytes_of(shape, t), ctas * std::min(units, x_tiles + w_tiles));
-                const double x_cost = std::max(x_kb / parts * stage, epilogue), w_cost = std::max(w_kb * stage, epilogue);
+                if (parts > 1 && (!dX || x_kb < 8 * parts)) break;
+                if (only && parts != only && (parts > 1 || (dX && x_kb >= 8 * only))) continue;
+                const double x_tiles = dX ? tiles_x * across * parts : 0.0;
+                const double stage = stage_cycles(t, kDenseGrad, ks, block_bytes_of(shape, t), ctas * std::min((double)units, x_tiles + w_tiles));
+                const double x_cost = std::max(x_kb * stage / parts, epilogue), w_cost = std::max(w_kb * stage, epilogue);
                 double cost = std::ceil(x_tiles / units) * x_cost;
                 if (w_tiles > 0) cost = std::max(cost, x_tiles > 0 ? (x_tiles * x_cost + w_tiles * w_cost) / units + 0.5 * w_cost : std::ceil(w_tiles / units) * w_cost);
                 cost += epilogue;
@@ -748,7 +773,10 @@ GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
                     best_cost = cost;
                     best = GradPlan{t, parts};
                 }
+                if (x_tiles >= 4 * units) break;       // (enough tiles: parts are for few)
             }
+        }
+    }
     return best;
 }
 // a part's plane: whole tiles of rows, rows of whole 16-byte pieces
@@ -783,8 +811,12 @@ int result_map(CUtensorMap *m, void *y, long long ld, int bytes, long long rows,
 
 }  // namespace
 
-size_t tc_grad_workspace(int rows, int channels, int width, bool dX, int weights, bool twins) {
+GradChoice tc_grad_choice(int rows, int channels, int width, bool dX, int weights) {
     const GradPlan plan = grad_plan(rows, channels, width, dX, weights);
+    return GradChoice{plan.tile.ctas, plan.tile.BN, plan.parts};
+}
+size_t tc_grad_workspace(const GradChoice &c, int rows, int width, bool dX, bool twins) {
+    const GradPlan plan{{c.ctas, c.BN, 1}, c.parts};
     return plan.parts > 1 || (dX && twins) ? (size_t)(plan.parts * part_rows(rows, plan.tile) * part_pitch(width) * 4) : 0;
 }
 
@@ -797,7 +829,7 @@ int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
     const int tokens = d.twins ? d.M / 2 : d.M;
     Params p{};
     p.M = d.M; p.N = d.N;
-    const GradPlan plan = grad ? grad_plan(d.M, d.K, d.N, d.Y[0] != nullptr, weights) : GradPlan{pick_tile(d), 1};
+    const GradPlan plan = grad ? GradPlan{{d.grad.ctas, d.grad.BN, 1}, d.grad.parts} : GradPlan{pick_tile(d), 1};
     const Tile tile = plan.tile;
     p.ks = blocks_per_stage(d, tile);
     p.num_kb = (int)stages_along(d, tile);
@@ -846,33 +878,29 @@ int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
     p.err = device_status_ptr();
     if (!p.err) return (int)cudaErrorUnknown;
 
-    Maps maps;
+    Maps maps{};
     bool fine = true;
-    // (a map that nobody uses is a copy of one that is there)
+    // (maps that nobody uses are left as they are: zeros)
     if (grad) {
         for (int i = 0; i < 2; ++i) {
             fine = fine && operand_map(&maps.A[i], d.A[i], bytes, d.M, d.K, 64 * p.ks);
             if (d.Y[0]) fine = fine && operand_map(&maps.B[i], d.B[i], bytes, d.K, d.N, 64 * p.ks);
-            else maps.B[i] = maps.A[0];
         }
     } else {
-        fine = operand_map(&maps.A[0], d.A[0], bytes, d.M, d.K, a_rows) && operand_map(&maps.B[0], d.B[0], bytes, d.N, d.K, gated ? p.out_cols : bnh);
-        maps.A[1] = maps.A[0];
-        if (gated) fine = fine && operand_map(&maps.B[1], d.B[1], bytes, d.N, d.K, p.out_cols);
-        else maps.B[1] = maps.B[0];
+        // (block by block, and by stages of several; each where there is such a stage, since a map costs 0.4 us of host time)
+        const int b_rows = gated ? p.out_cols : bnh, count = gated ? 2 : 1;
+        if (p.ks == 1 || p.full_kb < p.num_kb) {
+            fine = operand_map(&maps.A[0], d.A[0], bytes, d.M, d.K, a_rows);
+            for (int i = 0; i < count; ++i) fine = fine && operand_map(&maps.B[i], d.B[i], bytes, d.N, d.K, b_rows);
+        }
+        if (p.ks > 1 && p.full_kb > 0) {
+            fine = fine && blocks_map(&maps.A4, d.A[0], bytes, d.M, d.K, a_rows, p.ks, false);
+            for (int i = 0; i < count; ++i) fine = fine && blocks_map(&maps.B4[i], d.B[i], bytes, d.N, d.K, b_rows, p.ks, gated && tile.ctas == 1);
+        }
     }
-    maps.A4 = maps.B4[0] = maps.B4[1] = maps.A[0];
-    if (!grad && p.full_kb > 0 && p.ks > 1) {
-        const int b_rows = gated ? p.out_cols : bnh;
-        const bool groups = gated && tile.ctas == 1;
-        fine = fine && blocks_map(&maps.A4, d.A[0], bytes, d.M, d.K, a_rows, p.ks, false);
-        for (int i = 0; i < (gated ? 2 : 1); ++i) fine = fine && blocks_map(&maps.B4[i], d.B[i], bytes, d.N, d.K, b_rows, p.ks, groups);
-    }
-    maps.B[2] = maps.A[0];
     if (weights) fine = fine && operand_map(&maps.B[2], d.B[2], bytes, d.M, d.N, 64 * p.ks);
     if (!fine) return (int)cudaErrorInvalidValue;
     for (int i = 0; i < 3; ++i) {
-        maps.Y[i] = maps.A[0];
         p.Y[i] = d.Y[i]; p.y_ld[i] = d.y_ld[i];
         p.y_tma[i] = result_map(&maps.Y[i], d.Y[i], d.y_ld[i], type_bytes(d.y_type), grad && i > 0 ? d.K : tokens, d.N);
     }
@@ -882,7 +910,7 @@ int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
     }
     const size_t smem = smem_with_tmem(1024 + (size_t)p.num_stages * p.stage_bytes + kStagingBytes + kBarrierBytes, 512);
     const Kernel kernel = tile.split > 1 ? split_kernel_for(d.mode, int8) : tile.ctas == 2 ? kernel_for<2>(d.mode, int8) : kernel_for<1>(d.mode, int8);
-    const cudaError_t attr_err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+    const cudaError_t attr_err = allow_shared_memory(kernel, (tile.split > 1 ? 2 : tile.ctas - 1) * 4 + (int8 ? 2 : 0) + (gated ? 1 : 0));
     if (attr_err != cudaSuccess) return (int)attr_err;
     const int units = tile.ctas == 2 ? max_pairs() : num_sms();
     const int cluster = std::max(tile.ctas, tile.split);
