@@ -58,10 +58,31 @@ __device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f 
 // (As tanh the factor would lose all its digits where it is small.)
 __device__ __forceinline__ float gelu_argument(float g) { return 1.5957691216057308f * fmaf(0.044715f * g * g, g, g); }
 
+// The normal distribution's value at g, and exp(-g^2 / 2).  Its tail beyond |g| is exp(-g^2 / 2) t P(t), t = 1 / (1 + 0.3 |g|), P of degree 7 fitted
+// to it for |g| < 14.5 (largest relative error 1.7e-7, by reweighted least squares on Chebyshev points; in 32 bits 4e-6 at |g| = 13, where g^2 / 2 is
+// rounded, 1.3e-6 below 6).  erfcf's 50 instructions an element were most of the epilogue: gated block 1597 x 384 x 1088 17.8 us with it.
+__device__ __forceinline__ float normal_at(float g, float &density) {
+    const float t = __fdividef(1.f, fmaf(0.3f, fabsf(g), 1.f));
+    float p = 0.03542385995388031f;
+    p = fmaf(p, t, -0.1561589390039444f);
+    p = fmaf(p, t, 0.20455756783485413f);
+    p = fmaf(p, t, -0.052034683525562286f);
+    p = fmaf(p, t, 0.1276920884847641f);
+    p = fmaf(p, t, 0.10017585754394531f);
+    p = fmaf(p, t, 0.12071214616298676f);
+    p = fmaf(p, t, 0.11963200569152832f);
+    density = __expf(-0.5f * g * g);
+    const float tail = density * t * p;
+    return g >= 0.f ? 1.f - tail : tail;
+}
+
 // act(g)
 __device__ __forceinline__ float activate(int kind, float g) {
     if (kind == ONNXB_SILU) return g * logistic(g);
-    if (kind == ONNXB_GELU) return 0.5f * g * erfcf(-0.70710678118654752f * g);      // (1 + erf would lose its digits for negative g)
+    if (kind == ONNXB_GELU) {
+        float density;
+        return g * normal_at(g, density);
+    }
     if (kind == ONNXB_GELU_TANH) return g * logistic(gelu_argument(g));
     return g > 0.f ? g : 0.f;
 }
@@ -73,9 +94,10 @@ __device__ __forceinline__ void activate_with_slope(int kind, float g, float &va
         value = g * p;
         slope = fmaf(value, 1.f - p, p);
     } else if (kind == ONNXB_GELU) {
-        const float p = 0.5f * erfcf(-0.70710678118654752f * g);
+        float density;
+        const float p = normal_at(g, density);
         value = g * p;
-        slope = fmaf(g * 0.39894228040143268f, __expf(-0.5f * g * g), p);
+        slope = fmaf(g * 0.39894228040143268f, density, p);
     } else if (kind == ONNXB_GELU_TANH) {
         const float p = logistic(gelu_argument(g));
         value = g * p;

@@ -3,8 +3,8 @@
 Tolerances, all from the formats: a rounding to a type t is off by at most half a step, eps(t)/2 of the value (and half the smallest number
 where that is more); a sum of n products that are exact in 32 bits, taken in 32 bits in any order, with every addition off by as much as
 a whole step, by n 2^-23 sum|products|; the activation in 32 bits by 2^-15 of its value (an exponential with its argument rounded in
-32 bits is off by about |argument| 2^-23, the argument at most 100 where the value counts; four units in the last place of erfc and
-a quotient besides), its slope, which is a sum, by 2^-15 of 1.2, its largest value.  Two numbers given to 64-bit functions are exact.
+32 bits is off by about |argument| 2^-23, the argument at most 100 where the value counts; a polynomial of the normal distribution's tail by
+2^-22 and a quotient besides), its slope, which is a sum, by 2^-15 of 1.2, its largest value.  Two numbers given to 64-bit functions are exact.
 """
 import math
 
