@@ -91,7 +91,7 @@ struct TileAt {
     bool x;                    // a tile of dX
 };
 // Tiles of one product lie in bands of `band` row tiles, a band's columns one after the other, so that the tiles in flight share
-// their operands in L2 (of 148 SMs' 74 pairs at band 8: 8 row tiles and 9 column tiles).
+// their operands in L2 (of 148 SMs' 74 pairs at band 8: 8 row tiles and 9 column tiles), and a band's rows stay there.
 __device__ __forceinline__ void place(const Params &p, int tiles_m, int t, TileAt &at) {
     const int per = tiles_m * p.tiles_n;
     at.z = t / per;
@@ -838,7 +838,10 @@ int launch_tc_dense(const DenseProblem &problem, cudaStream_t stream) {
     p.out_cols = gated ? p.BN / 2 : p.BN;
     p.tiles_m = (int)ceil_div(d.M, kBM * tile.ctas);
     p.tiles_n = (int)ceil_div(d.N, p.out_cols);
-    p.band = 8;
+    // Bands of at most a third of L2 of A's rows, all alike.  (4, 8, 16 and 32 tiles a band: gated block 4096 x 4096 x 10240 in bf16 548, 515,
+    // 511 and 508 us under the power cap; the gradients, whose operands are larger, 1125, 1125, 1139 and 1155.)
+    const int most = (int)std::max(4LL, std::min(32LL, 40000000LL / ((long long)kBM * tile.ctas * d.K * bytes)));
+    p.band = grad ? 8 : ceil_int(p.tiles_m, ceil_int(p.tiles_m, most));
     long long total = (long long)p.tiles_m * p.tiles_n, x_tiles = 0, w_tiles = 0;
     if (grad) {
         p.channels = d.K;
