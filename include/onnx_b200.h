@@ -426,7 +426,7 @@ onnxb_status onnx_gated_int8_run(const onnxb_matrix *A, const float *a_scale, co
  * them); X is not read (and may be NULL) without dWg and dWu, Wg and Wu neither without dX.  dG and dU are rounded to the
  * type between the two steps (the tensor cores take 16-bit operands; up to 32 tokens, where few roundings would not average, what
  * that leaves of them is kept as well), sums are in 32 bits, dX is one sum over both terms, and each result is rounded once.
- * Deterministic: no atomics.
+ * Deterministic: no atomics; and a result is the same bit by bit whichever others are wanted with it.
  */
 size_t onnx_gated_backward_workspace_bytes(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,
                                            const onnxb_matrix *dX, const onnxb_matrix *dWg, const onnxb_matrix *dWu);      /* host only */

@@ -739,7 +739,8 @@ struct GradPlan {
     int parts;
 };
 constexpr int kGradTerms = kRowBytes / 2;
-GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
+// `like`: a plan whose parts this one has to have, with their borders (which lie at whole stages)
+GradPlan search_grad_plan(int tokens, int channels, int width, bool dX, int weights, const GradPlan *like) {
     DenseProblem sizes{};
     sizes.mode = kDenseGrad;
     sizes.type = ONNXB_BFLOAT16;
@@ -756,10 +757,13 @@ GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
         for (int bn = 64 * ctas; bn <= kMaxBN; bn += 64 * ctas) {
             const Tile t{ctas, bn, 1};
             if (pin && (t.ctas != pinned.ctas || t.BN != pinned.BN)) continue;
-            const int ks = blocks_per_stage(shape, t), x_kb = 2 * ceil_int(channels, kGradTerms * ks), w_kb = ceil_int(tokens, kGradTerms * ks);
+            const int ks = blocks_per_stage(shape, t);
+            if (like && like->parts > 1 && ks != blocks_per_stage(shape, like->tile)) continue;
+            const int x_kb = 2 * ceil_int(channels, kGradTerms * ks), w_kb = ceil_int(tokens, kGradTerms * ks);
             const double across = ceil_int(width, bn), epilogue = epilogue_cycles(t), w_tiles = tiles_w * across;
             for (int parts = 1; parts <= 8; parts *= 2) {
                 if (parts > 1 && (!dX || x_kb < 8 * parts)) break;
+                if (like && parts != like->parts) continue;
                 if (only && parts != only && (parts > 1 || (dX && x_kb >= 8 * only))) continue;
                 const double x_tiles = dX ? tiles_x * across * parts : 0.0;
                 const double stage = stage_cycles(t, kDenseGrad, ks, block_bytes_of(shape, t), ctas * std::min((double)units, x_tiles + w_tiles));
@@ -778,6 +782,14 @@ GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
         }
     }
     return best;
+}
+// dX is the same bit by bit whichever weights' gradients are wanted with it: its parts are those of the call that wants both, the tiles' shape
+// that of the call.  (By itself dX of 256 x 10240 x 4096 would take 63 us in four parts and takes 82 in two, of 2048 x 10240 x 4096 310 in four and
+// 250 in one; of 512 x 2816 x 1024 25.6 either way.)
+GradPlan grad_plan(int tokens, int channels, int width, bool dX, int weights) {
+    if (!dX || weights == 2) return search_grad_plan(tokens, channels, width, dX, weights, nullptr);
+    const GradPlan both = search_grad_plan(tokens, channels, width, true, 2, nullptr);
+    return search_grad_plan(tokens, channels, width, true, weights, &both);
 }
 // a part's plane: whole tiles of rows, rows of whole 16-byte pieces
 long long part_rows(int tokens, Tile t) { return ceil_div(tokens, kBM * t.ctas) * kBM * t.ctas; }

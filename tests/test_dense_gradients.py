@@ -1,0 +1,57 @@
+"""The gated block's gradients where what one call computes must not go by what it does besides: which results are wanted, how many tokens
+there are."""
+import itertools
+import math
+
+import pytest
+import torch
+
+from paper_2008_08272_b200 import binding
+from paper_2008_08272_b200.binding import Matrix
+
+# (tokens, width, channels), dX's long reduction in parts by the rule: short and long rows, whole K blocks and odd ones
+IN_PARTS = [(64, 4096, 10240), (96, 264, 3001), (128, 512, 1024), (200, 1024, 2816), (512, 1024, 4096), (512, 512, 1090), (1024, 1024, 4096)]
+FORMS = [w for w in itertools.product((True, False), repeat=3) if w[0]]
+
+
+def normal(g, *size):
+    return torch.randn(*size, generator=g, device="cuda")
+
+
+def views(*sizes):
+    """bfloat16 views at addresses of their own, rows at multiples of 16 bytes (nothing is launched on them)."""
+    return [Matrix((i + 1) << 24, rows, cols, (cols + 7) // 8 * 8, 16, 0) for i, (rows, cols) in enumerate(sizes)]
+
+
+@pytest.mark.parametrize("size", IN_PARTS, ids=str)
+def test_parts_of_dX_do_not_go_by_what_else_is_wanted(size):
+    """Each part has a plane of fp32 in the workspace, whole tiles of 128 or 256 rows: as many parts in every form (no GPU needed)."""
+    M, K, F = size
+    dH, X, W, dX, dW = views((M, F), (M, K), (F, K), (M, K), (F, K))
+    lib, found = binding.load(), set()
+    for _, g, u in FORMS:
+        need = lib.onnx_gated_backward_workspace_bytes(dH, X if g or u else None, W, W, dX, dW if g else None, dW if u else None)
+        planes = (need - 2 * M * dH.ld * 2) / ((K + 3) // 4 * 4 * 4)
+        fits = {planes / rows for rows in (-(-M // 128) * 128, -(-M // 256) * 256)} & {2.0, 4.0, 8.0}
+        assert fits, (size, planes)
+        found.add(frozenset(fits))
+    assert frozenset.intersection(*found), found
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("size", IN_PARTS + [(2048, 1024, 4096)], ids=str)
+def test_dX_is_the_same_whatever_else_is_wanted(size, t):
+    """Bit by bit, with nothing pinned: a weight that is frozen does not change the other gradients."""
+    g = torch.Generator(device="cuda").manual_seed(61)
+    M, K, F = size
+    X, Wg, Wu = normal(g, M, K).to(t), (normal(g, F, K) / math.sqrt(K)).to(t), (normal(g, F, K) / math.sqrt(K)).to(t)
+    dH, G, U = normal(g, M, F).to(t), normal(g, M, F).to(t), normal(g, M, F).to(t)
+    every = binding.onnx_gated_backward(dH, X, Wg, Wu, G, U)
+    for wanted in itertools.product((True, False), repeat=3):
+        if not any(wanted):
+            continue
+        some = binding.onnx_gated_backward(dH, X, Wg, Wu, G, U, wanted=wanted)
+        for w, a, b in zip(wanted, some, every):
+            assert (a is None) == (not w) and (a is None or torch.equal(a, b)), wanted
+    assert binding.last_device_status() == 0
