@@ -425,7 +425,7 @@ onnxb_status onnx_gated_int8_run(const onnxb_matrix *A, const float *a_scale, co
  * All of one type, 16-bit floats; shapes as the forward call's.  dX, dWg, dWu: each may be NULL where it is not wanted (not all of
  * them); X is not read (and may be NULL) without dWg and dWu, Wg and Wu neither without dX.  dG and dU are rounded to the
  * type between the two steps (the tensor cores take 16-bit operands; up to 32 tokens, where few roundings would not average, what
- * that leaves of them is kept as well), sums are in 32 bits, dX is one sum over both terms, and each result is rounded once.
+ * that leaves of them is kept as well, but for X or weights that are not finite), sums are in 32 bits, dX is one sum over both terms, and each result is rounded once.
  * Deterministic: no atomics; and a result is the same bit by bit whichever others are wanted with it.
  */
 size_t onnx_gated_backward_workspace_bytes(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu,

@@ -50,7 +50,8 @@ __global__ void __launch_bounds__(256) gated_slope_kernel(const GatedSlopeProble
             const T x = static_cast<const T *>(p.X.p)[i * p.X.ld + j];
             T *to = static_cast<T *>(p.twice) + i * p.twice_ld + j;
             to[0] = x;
-            to[p.M * p.twice_ld] = x;
+            // (what is left of dG and dU adds nothing to an infinity or a NaN, and would make a NaN of an infinity)
+            to[p.M * p.twice_ld] = isfinite(to_float(x)) ? x : from_float<T>(0.f);
         }
         return;
     }
@@ -98,7 +99,9 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const SumPartsProblem p)
             const float *from = p.P + ((long long)s * p.part_rows + i) * p.p_ld + j;
             const float4 w = *reinterpret_cast<const float4 *>(from);
             const float4 rest = p.twins ? *reinterpret_cast<const float4 *>(from + p.M * p.p_ld) : make_float4(0.f, 0.f, 0.f, 0.f);
-            v = make_float4(v.x + w.x + rest.x, v.y + w.y + rest.y, v.z + w.z + rest.z, v.w + w.w + rest.w);
+            // (of infinite weights the twins' sum is the opposite infinity or NaN, where there is nothing to add any more)
+            auto both = [](float sum, float own, float twin) { return sum + own + (isfinite(own) ? twin : 0.f); };
+            v = make_float4(both(v.x, w.x, rest.x), both(v.y, w.y, rest.y), both(v.z, w.z, rest.z), both(v.w, w.w, rest.w));
         }
         T *y = static_cast<T *>(p.Y) + i * p.y_ld + j;
         alignas(8) const T out[4] = {from_float<T>(v.x), from_float<T>(v.y), from_float<T>(v.z), from_float<T>(v.w)};

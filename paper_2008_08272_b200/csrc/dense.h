@@ -52,8 +52,8 @@ int launch_tc_dense(const DenseProblem &p, cudaStream_t stream);
 GradChoice tc_grad_choice(int rows, int channels, int width, bool dX, int weights);
 size_t tc_grad_workspace(const GradChoice &choice, int rows, int width, bool dX, bool twins);
 
-// Y[i,j] = the sum over s < parts of P[s * part_rows + i][j], in that order, and of twins that of P[s * part_rows + M + i][j] after each,
-// rounded to `type`; P's rows p_ld floats apart (a multiple of 4)
+// Y[i,j] = the sum over s < parts of P[s * part_rows + i][j], in that order, and of twins that of P[s * part_rows + M + i][j] after each finite
+// one, rounded to `type`; P's rows p_ld floats apart (a multiple of 4)
 struct SumPartsProblem {
     int parts, part_rows, M, N, type, twins;
     const float *P;
@@ -64,7 +64,7 @@ struct SumPartsProblem {
 int launch_sum_parts(const SumPartsProblem &p, cudaStream_t stream);
 
 // dG = dH U act'(G), dU = dH act(G), each [M,F]; all of one 16-bit type.  twins: what rounding leaves of them as well, M rows on, and X [M,K]
-// (its p NULL where there is none) copied to `twice`, and again M rows on.
+// (its p NULL where there is none) copied to `twice`, and again M rows on, zeros there where it is not finite.
 struct GatedSlopeProblem {
     int type, activation, M, F;
     DenseOperand dH, G, U;

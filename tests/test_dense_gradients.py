@@ -6,6 +6,7 @@ import math
 import pytest
 import torch
 
+import dense_reference as ref
 from paper_2008_08272_b200 import binding
 from paper_2008_08272_b200.binding import Matrix
 
@@ -55,3 +56,33 @@ def test_dX_is_the_same_whatever_else_is_wanted(size, t):
         for w, a, b in zip(wanted, some, every):
             assert (a is None) == (not w) and (a is None or torch.equal(a, b)), wanted
     assert binding.last_device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("M", [1, 5, 32, 33, 150])
+def test_infinite_operands_give_what_the_sums_give(M, t):
+    """An infinity (or NaN) among X or the weights: the results it goes into are infinite with the sign of dG or dU, or NaN, as the definition
+    has it, up to 32 tokens as above; all others are as they were."""
+    g = torch.Generator(device="cuda").manual_seed(62)
+    K, F = 72, 200
+    X, Wg, Wu = normal(g, M, K).to(t), (normal(g, F, K) / 9).to(t), (normal(g, F, K) / 9).to(t)
+    dH, G, U = ((1 + torch.rand(M, F, generator=g, device="cuda")).to(t) * normal(g, M, F).sign().to(t) for _ in range(3))
+    clean = binding.onnx_gated_backward(dH, X, Wg, Wu, G, U, activation="gelu")
+    value, slope = ref.act("gelu", G.double())
+    dG, dU = dH.double() * U.double() * slope, dH.double() * value       # none of them 0
+    for where, at, v in (("X", (0, 7), math.inf), ("X", (M - 1, 71), -math.inf), ("X", (M // 2, 0), math.nan), ("Wg", (9, 3), math.inf),
+                         ("Wu", (199, 64), -math.inf), ("Wg", (100, 70), math.nan)):
+        own = {"X": X, "Wg": Wg, "Wu": Wu}
+        own[where] = own[where].clone()
+        own[where][at] = v
+        got = binding.onnx_gated_backward(dH, own["X"], own["Wg"], own["Wu"], G, U, activation="gelu")
+        torch.cuda.synchronize()
+        column, factor = at[1], {"X": None, "Wg": dG[:, at[0]], "Wu": dU[:, at[0]]}[where]
+        want = [c.double() for c in clean]
+        if where == "X":
+            want[1][:, column], want[2][:, column] = dG[at[0]] * v, dU[at[0]] * v
+        else:
+            want[0][:, column] = factor * v
+        for y, w in zip(got, want):
+            assert torch.equal(y.double().nan_to_num(7.0, 3e38, -3e38), w.nan_to_num(7.0, 3e38, -3e38)) and torch.equal(y.isnan(), w.isnan()), (where, at, v)
