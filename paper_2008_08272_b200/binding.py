@@ -633,6 +633,11 @@ class _Views:
         rows, cols = t.shape
         return Matrix(t.data_ptr() or None, rows, cols, t.stride(0) if rows > 1 else cols, TYPE_CODES[kind], 0)
 
+    def given(self, t, name, types, like=None):
+        """A result that the caller may give: refused, where it cannot be taken, before anything is made for the call."""
+        if t is not None:
+            self.matrix(t, name, types, like)
+
     def vector(self, t, name, size, allow_none=False):
         if t is None and allow_none:
             return None
@@ -648,15 +653,18 @@ class _Views:
     def new(self, rows, cols, dtype, kept=True):
         return _new((rows, cols), self.device, self.stream, dtype, kept)
 
+    def given_workspace(self, given):
+        if given is not None:
+            self._on_device(given, "workspace")
+            if not given.is_contiguous():
+                raise TypeError("workspace must be contiguous")
+
     def workspace(self, given, need):
         """(tensor, pointer, bytes): the caller's, or one of ``need`` bytes."""
         if given is None and need:
             given = _new(need, self.device, self.stream, "uint8", kept=False)
         if given is None:
             return None, None, 0
-        self._on_device(given, "workspace")
-        if not given.is_contiguous():
-            raise TypeError("workspace must be contiguous")
         return given, ctypes.c_void_p(given.data_ptr()), given.numel() * given.element_size()
 
     def call(self, function, *args):
@@ -687,6 +695,8 @@ def onnx_quantize_rows(X, *, Q=None, scale=None, stream=None):
     lib = load()
     v = _Views("onnx_quantize_rows", stream)
     x = v.matrix(X, "X", _FLOATS)
+    v.given(Q, "Q", _INT8)
+    v.vector(scale, "scale", x.rows, allow_none=True)
     if Q is None:
         Q = v.new(x.rows, (x.cols + 15) // 16 * 16, "int8")
         Q = Q if Q.shape[1] == x.cols else Q[:, :x.cols]
@@ -713,12 +723,14 @@ def onnx_gemm_int8(A, a_scale, B, b_scale, C=None, *, fuse_relu=False, dtype="fl
     lib = load()
     v = _Views("onnx_gemm_int8", stream)
     a, b = v.matrix(A, "A", _INT8), v.matrix(B, "B", _INT8)
+    sa, sb, c = v.vector(a_scale, "a_scale", a.rows), v.vector(b_scale, "b_scale", b.rows), v.vector(C, "C", b.rows, allow_none=True)
+    v.given(Y, "Y", _FLOATS)
+    v.given_workspace(workspace)
     if Y is None:
         Y = v.new(a.rows, b.rows, _float_name(dtype))
     y = v.matrix(Y, "Y", _FLOATS)
     held, ws, ws_len = v.workspace(workspace, lib.onnx_gemm_int8_workspace_bytes(a, b))
-    v.call(lib.onnx_gemm_int8_run, a, v.vector(a_scale, "a_scale", a.rows), b, v.vector(b_scale, "b_scale", b.rows),
-           v.vector(C, "C", b.rows, allow_none=True), int(bool(fuse_relu)), y, ws, ws_len)
+    v.call(lib.onnx_gemm_int8_run, a, sa, b, sb, c, int(bool(fuse_relu)), y, ws, ws_len)
     return Y
 
 
@@ -732,6 +744,10 @@ def onnx_gated(X, Wg, Wu, *, activation="silu", save=False, H=None, G=None, U=No
     v = _Views("onnx_gated", stream)
     x, wg, wu = v.matrix(X, "X", _HALVES), v.matrix(Wg, "Wg", _HALVES, X), v.matrix(Wu, "Wu", _HALVES, X)
     save = save or G is not None or U is not None
+    for result, name in ((H, "H"), (G, "G"), (U, "U")):
+        v.given(result, name, _HALVES, X)
+    v.given_workspace(workspace)
+    activation = _activation(activation)
     kind = str(X.dtype)[6:]
     H = v.new(x.rows, wg.rows, kind) if H is None else H
     if save:
@@ -740,7 +756,7 @@ def onnx_gated(X, Wg, Wu, *, activation="silu", save=False, H=None, G=None, U=No
     h = v.matrix(H, "H", _HALVES, X)
     g, u = (v.matrix(G, "G", _HALVES, X), v.matrix(U, "U", _HALVES, X)) if save else (None, None)
     held, ws, ws_len = v.workspace(workspace, lib.onnx_gated_workspace_bytes(x, wg, wu))
-    v.call(lib.onnx_gated_run, x, wg, wu, _activation(activation), h, _ref(g), _ref(u), ws, ws_len)
+    v.call(lib.onnx_gated_run, x, wg, wu, activation, h, _ref(g), _ref(u), ws, ws_len)
     return (H, G, U) if save else H
 
 
@@ -752,12 +768,15 @@ def onnx_gated_int8(A, a_scale, Wg, g_scale, Wu, u_scale, *, activation="silu", 
     lib = load()
     v = _Views("onnx_gated_int8", stream)
     a, wg, wu = v.matrix(A, "A", _INT8), v.matrix(Wg, "Wg", _INT8), v.matrix(Wu, "Wu", _INT8)
+    sa, sg, su = v.vector(a_scale, "a_scale", a.rows), v.vector(g_scale, "g_scale", wg.rows), v.vector(u_scale, "u_scale", wu.rows)
+    activation = _activation(activation)
+    v.given(H, "H", _FLOATS)
+    v.given_workspace(workspace)
     if H is None:
         H = v.new(a.rows, wg.rows, _float_name(dtype))
     h = v.matrix(H, "H", _FLOATS)
     held, ws, ws_len = v.workspace(workspace, lib.onnx_gated_workspace_bytes(a, wg, wu))
-    v.call(lib.onnx_gated_int8_run, a, v.vector(a_scale, "a_scale", a.rows), wg, v.vector(g_scale, "g_scale", wg.rows), wu,
-           v.vector(u_scale, "u_scale", wu.rows), _activation(activation), h, ws, ws_len)
+    v.call(lib.onnx_gated_int8_run, a, sa, wg, sg, wu, su, activation, h, ws, ws_len)
     return H
 
 
@@ -779,12 +798,15 @@ def onnx_gated_backward(dH, X, Wg, Wu, G, U, *, activation="silu", wanted=(True,
     wg, wu = (v.matrix(Wg, "Wg", _HALVES, dH), v.matrix(Wu, "Wu", _HALVES, dH)) if want[0] else (None, None)
     if not any(want):
         raise OnnxB200Error(1, "onnx_gated_backward: no gradient is wanted")
+    for result, name in ((dX, "dX"), (dWg, "dWg"), (dWu, "dWu")):
+        v.given(result, name, _HALVES, dH)
+    v.given_workspace(workspace)
+    activation = _activation(activation)
     width = x.cols if x else wg.cols
     outs = [None if not w else v.new(rows, width, kind) if given is None else given
             for w, given, rows in zip(want, (dX, dWg, dWu), (dh.rows, dh.cols, dh.cols))]
     dx, dwg, dwu = (None if o is None else v.matrix(o, name, _HALVES, dH) for o, name in zip(outs, ("dX", "dWg", "dWu")))
     held, ws, ws_len = v.workspace(workspace, lib.onnx_gated_backward_workspace_bytes(
         _ref(dh), _ref(x), _ref(wg), _ref(wu), _ref(dx), _ref(dwg), _ref(dwu)))
-    v.call(lib.onnx_gated_backward_run, dh, _ref(x), _ref(wg), _ref(wu), g, u, _activation(activation), _ref(dx), _ref(dwg), _ref(dwu), ws,
-           ws_len)
+    v.call(lib.onnx_gated_backward_run, dh, _ref(x), _ref(wg), _ref(wu), g, u, activation, _ref(dx), _ref(dwg), _ref(dwu), ws, ws_len)
     return tuple(outs)

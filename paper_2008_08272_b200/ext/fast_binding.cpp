@@ -346,6 +346,16 @@ struct Views {
     at::Tensor made(at::IntArrayRef size, at::ScalarType type, bool is_result = true) {
         return new_tensor(size, type, at::Device(at::kCUDA, device), given_stream, stream, is_result);
     }
+    // Whether the results and the workspace that the caller gives can be taken; asked before anything is made for the call
+    bool takes(std::initializer_list<PyObject *> results, PyObject *workspace) {
+        onnxb_matrix m{};
+        for (PyObject *o : results) matrix(o, m);
+        if (workspace != Py_None) {
+            const at::Tensor *t = on_device(workspace);
+            if (t && !t->is_contiguous()) fine = false;
+        }
+        return fine;
+    }
     // a result: the caller's, or one made here
     onnxb_matrix *result(PyObject *given, int64_t rows, int64_t cols, int32_t type, at::Tensor &t, onnxb_matrix &m) {
         if (given != Py_None) return matrix(given, m);
@@ -358,7 +368,7 @@ struct Views {
         bytes = 0;
         if (given != Py_None) {
             const at::Tensor *g = on_device(given);
-            if (!g || !g->is_contiguous()) { fine = false; return nullptr; }
+            if (!g) return nullptr;
             bytes = g->nbytes();
             return g->data_ptr();
         }
@@ -392,18 +402,18 @@ inline int32_t float_type_of(PyObject *o) {
 PyObject *py_quantize_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (n != 4) return slow_path();
     Views v(a[3]);
-    onnxb_matrix x, q;
+    onnxb_matrix x{}, q{};
     if (!v.matrix(a[0], x) || !v.fine || x.rows < 1) return slow_path();
     at::Tensor qt, st;
-    if (a[1] != Py_None) v.matrix(a[1], q);
-    else {
+    float *scale = v.vector(a[2], x.rows);
+    v.matrix(a[1], q);
+    if (!v.fine) return slow_path();
+    if (a[1] == Py_None) {
         const int64_t pitch = (x.cols + 15) / 16 * 16;
         qt = v.made({x.rows, pitch}, at::kChar);
         if (pitch != x.cols) qt = qt.narrow(1, 0, x.cols);
         v.take(qt, q);
     }
-    float *scale = v.vector(a[2], x.rows);
-    if (!v.fine) return slow_path();
     if (!scale) {
         st = v.made({x.rows}, at::kFloat);
         scale = static_cast<float *>(st.data_ptr());
@@ -416,18 +426,18 @@ PyObject *py_quantize_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyObject *py_gemm_int8(PyObject *, PyObject *const *o, Py_ssize_t n) {
     if (n != 10) return slow_path();
     Views v(o[9]);
-    onnxb_matrix a, b, y;
+    onnxb_matrix a{}, b{}, y{};
     if (!v.matrix(o[0], a) || !v.matrix(o[2], b) || !v.fine) return slow_path();
     const float *sa = v.vector(o[1], a.rows), *sb = v.vector(o[3], b.rows), *c = v.vector(o[4], b.rows);
     const int relu = PyObject_IsTrue(o[5]);
     const int32_t type = o[7] == Py_None ? float_type_of(o[6]) : ONNXB_FLOAT;
     if (PyErr_Occurred()) { PyErr_Clear(); return slow_path(); }
-    if (!v.fine || !type) return slow_path();
+    if (!type || !v.takes({o[7]}, o[8])) return slow_path();
     at::Tensor yt, wt;
     size_t ws_bytes;
     v.result(o[7], a.rows, b.rows, type, yt, y);
     void *ws = v.workspace(o[8], abi.gemm_int8_workspace_bytes(&a, &b), wt, ws_bytes);
-    if (!v.fine || abi.gemm_int8_run(&a, sa, &b, sb, c, relu, &y, ws, ws_bytes, v.stream) != ONNXB_OK) return slow_path();
+    if (abi.gemm_int8_run(&a, sa, &b, sb, c, relu, &y, ws, ws_bytes, v.stream) != ONNXB_OK) return slow_path();
     return result(o[7], yt);
 }
 
@@ -435,11 +445,11 @@ PyObject *py_gemm_int8(PyObject *, PyObject *const *o, Py_ssize_t n) {
 PyObject *py_gated(PyObject *, PyObject *const *o, Py_ssize_t n) {
     if (n != 10) return slow_path();
     Views v(o[9]);
-    onnxb_matrix x, wg, wu, h, g, u;
+    onnxb_matrix x{}, wg{}, wu{}, h{}, g{}, u{};
     if (!v.matrix(o[0], x) || !v.matrix(o[1], wg) || !v.matrix(o[2], wu) || !v.fine) return slow_path();
     const int activation = activation_of(o[3]), asked = PyObject_IsTrue(o[4]);
     if (PyErr_Occurred()) { PyErr_Clear(); return slow_path(); }
-    if (activation < 0 || (x.type != ONNXB_FLOAT16 && x.type != ONNXB_BFLOAT16)) return slow_path();
+    if (activation < 0 || (x.type != ONNXB_FLOAT16 && x.type != ONNXB_BFLOAT16) || !v.takes({o[5], o[6], o[7]}, o[8])) return slow_path();
     const bool save = asked || o[6] != Py_None || o[7] != Py_None;
     at::Tensor ht, gt, ut, wt;
     size_t ws_bytes;
@@ -449,7 +459,7 @@ PyObject *py_gated(PyObject *, PyObject *const *o, Py_ssize_t n) {
         v.result(o[7], x.rows, wg.rows, x.type, ut, u);
     }
     void *ws = v.workspace(o[8], abi.gated_workspace_bytes(&x, &wg, &wu), wt, ws_bytes);
-    if (!v.fine || abi.gated_run(&x, &wg, &wu, activation, &h, save ? &g : nullptr, save ? &u : nullptr, ws, ws_bytes, v.stream) != ONNXB_OK)
+    if (abi.gated_run(&x, &wg, &wu, activation, &h, save ? &g : nullptr, save ? &u : nullptr, ws, ws_bytes, v.stream) != ONNXB_OK)
         return slow_path();
     if (!save) return result(o[5], ht);
     return Py_BuildValue("(NNN)", result(o[5], ht), result(o[6], gt), result(o[7], ut));
@@ -459,17 +469,17 @@ PyObject *py_gated(PyObject *, PyObject *const *o, Py_ssize_t n) {
 PyObject *py_gated_int8(PyObject *, PyObject *const *o, Py_ssize_t n) {
     if (n != 11) return slow_path();
     Views v(o[10]);
-    onnxb_matrix a, wg, wu, h;
+    onnxb_matrix a{}, wg{}, wu{}, h{};
     if (!v.matrix(o[0], a) || !v.matrix(o[2], wg) || !v.matrix(o[4], wu) || !v.fine) return slow_path();
     const float *sa = v.vector(o[1], a.rows), *sg = v.vector(o[3], wg.rows), *su = v.vector(o[5], wu.rows);
     const int activation = activation_of(o[6]);
     const int32_t type = o[8] == Py_None ? float_type_of(o[7]) : ONNXB_FLOAT;
-    if (!v.fine || activation < 0 || !type) return slow_path();
+    if (activation < 0 || !type || !v.takes({o[8]}, o[9])) return slow_path();
     at::Tensor ht, wt;
     size_t ws_bytes;
     v.result(o[8], a.rows, wg.rows, type, ht, h);
     void *ws = v.workspace(o[9], abi.gated_workspace_bytes(&a, &wg, &wu), wt, ws_bytes);
-    if (!v.fine || abi.gated_int8_run(&a, sa, &wg, sg, &wu, su, activation, &h, ws, ws_bytes, v.stream) != ONNXB_OK) return slow_path();
+    if (abi.gated_int8_run(&a, sa, &wg, sg, &wu, su, activation, &h, ws, ws_bytes, v.stream) != ONNXB_OK) return slow_path();
     return result(o[8], ht);
 }
 
@@ -477,7 +487,7 @@ PyObject *py_gated_int8(PyObject *, PyObject *const *o, Py_ssize_t n) {
 PyObject *py_gated_backward(PyObject *, PyObject *const *o, Py_ssize_t n) {
     if (n != 15) return slow_path();
     Views v(o[14]);
-    onnxb_matrix in[6], out[3];
+    onnxb_matrix in[6] = {}, out[3] = {};
     onnxb_matrix *ins[6], *outs[3] = {nullptr, nullptr, nullptr};
     const int activation = activation_of(o[6]);
     bool want[3];
@@ -489,13 +499,14 @@ PyObject *py_gated_backward(PyObject *, PyObject *const *o, Py_ssize_t n) {
         if (used && !ins[i]) return slow_path();
     }
     if (!v.fine || activation < 0 || !(want[0] || want[1] || want[2]) || (in[0].type != ONNXB_FLOAT16 && in[0].type != ONNXB_BFLOAT16)) return slow_path();
+    if (!v.takes({o[10], o[11], o[12]}, o[13])) return slow_path();
     const int64_t width = ins[1] ? in[1].cols : in[2].cols;
     at::Tensor ts[3], wt;
     for (int i = 0; i < 3; ++i)
         if (want[i]) outs[i] = v.result(o[10 + i], i == 0 ? in[0].rows : in[0].cols, width, in[0].type, ts[i], out[i]);
     size_t ws_bytes;
     void *ws = v.workspace(o[13], abi.gated_backward_workspace_bytes(ins[0], ins[1], ins[2], ins[3], outs[0], outs[1], outs[2]), wt, ws_bytes);
-    if (!v.fine || abi.gated_backward_run(ins[0], ins[1], ins[2], ins[3], ins[4], ins[5], activation, outs[0], outs[1], outs[2], ws, ws_bytes,
+    if (abi.gated_backward_run(ins[0], ins[1], ins[2], ins[3], ins[4], ins[5], activation, outs[0], outs[1], outs[2], ws, ws_bytes,
                                           v.stream) != ONNXB_OK)
         return slow_path();
     PyObject *got[3];
