@@ -351,7 +351,8 @@ onnxb_status onnx_global_average_pool_channel_major_run(const int64_t x_dims[4],
  * best kept with rows at such multiples.  What lies between a view's rows is neither read as a value nor written.
  * Sizes: rows may be 0 where they are tokens (nothing is launched, but for gradients of weights, which are then zeros);
  * each size at most 2^30, `ld` at most 2^31-1, and at least `cols` where there are two rows and more (no rows that overlap).  Tensors
- * of more than 2^31-1 elements are taken.  Outputs must not overlap inputs or each other (those that begin at the same address are refused).
+ * of more than 2^31-1 elements are taken.  Outputs (a scale that is written among them) must not overlap inputs or each other, nor the
+ * workspace any of them; those that begin at the same address are refused.
  * Calls that may overlap in time need workspaces of their own; what a workspace holds is undefined after a call.
  * scale: one 32-bit float a row.  Errors common to these calls: ERR_NULL (a required view, its data or a scale); ERR_SHAPE (sizes that do not fit
  * together or a row pitch below the width); ERR_ATTR (a type or an activation that the call does not take); ERR_UNSUPPORTED (sizes

@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <initializer_list>
 
 #include "dense.h"
 
@@ -30,6 +31,12 @@ bool has_size(const onnxb_matrix *m, int64_t rows, int64_t cols) { return m->row
 // (a single row has no pitch: its own length stands for it)
 DenseOperand operand(const onnxb_matrix *m) { return DenseOperand{m->data, m->rows > 1 ? (long long)m->ld : (long long)m->cols}; }
 bool same_place(const onnxb_matrix *a, const onnxb_matrix *b) { return a && b && a->rows > 0 && a->data == b->data; }
+// Whether a vector (or NULL), or the workspace, begins where a view does that has rows
+bool begins_at(const void *p, std::initializer_list<const onnxb_matrix *> views) {
+    for (const onnxb_matrix *m : views)
+        if (p && m && m->rows > 0 && m->data == p) return true;
+    return false;
+}
 
 // Whether TMA can address a view's rows; what its copy in the workspace takes otherwise, rows at multiples of 128 bytes (of 16 would do, but
 // 8-bit 1001 x 1536 x 777 then takes 7.0 us, 5.8 so).
@@ -41,10 +48,10 @@ size_t copy_bytes(const onnxb_matrix *m) {
     if (!m || m->rows < 1 || m->cols < 1 || m->rows > kMostSize || m->cols > kMostSize || in_place(m)) return 0;
     return (size_t)(copy_pitch(m) * m->rows);
 }
-onnxb_status check_workspace(const void *workspace, size_t bytes, size_t need) {
+onnxb_status check_workspace(const void *workspace, size_t bytes, size_t need, std::initializer_list<const onnxb_matrix *> views) {
     if (need == 0) return ONNXB_OK;
     if (!workspace || bytes < need) return ONNXB_ERR_WORKSPACE;
-    return reinterpret_cast<uintptr_t>(workspace) % 16 ? ONNXB_ERR_UNSUPPORTED : ONNXB_OK;
+    return reinterpret_cast<uintptr_t>(workspace) % 16 || begins_at(workspace, views) ? ONNXB_ERR_UNSUPPORTED : ONNXB_OK;
 }
 // Operands as the kernels read them: where they lie, or copied to the workspace, all in one launch (run(), before their first use).
 struct Placement {
@@ -86,7 +93,7 @@ extern "C" onnxb_status onnx_quantize_rows_run(const onnxb_matrix *X, const onnx
     if (!has_size(Q, X->rows, X->cols)) return ONNXB_ERR_SHAPE;
     if (X->rows == 0) return ONNXB_OK;
     if (!scale) return ONNXB_ERR_NULL;
-    if (reinterpret_cast<uintptr_t>(scale) % 4 || same_place(X, Q)) return ONNXB_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(scale) % 4 || same_place(X, Q) || begins_at(scale, {X, Q})) return ONNXB_ERR_UNSUPPORTED;
     const DenseOperand x = operand(X), q = operand(Q);
     return status_of(launch_quantize_rows(X->type, (int)X->rows, (int)X->cols, x.p, x.ld, static_cast<int8_t *>(const_cast<void *>(q.p)), q.ld,
                                           scale, (cudaStream_t)cuda_stream));
@@ -108,7 +115,7 @@ extern "C" onnxb_status onnx_gemm_int8_run(const onnxb_matrix *A, const float *a
     if (M == 0) return ONNXB_OK;
     if (!a_scale || !b_scale) return ONNXB_ERR_NULL;
     if ((reinterpret_cast<uintptr_t>(a_scale) | reinterpret_cast<uintptr_t>(b_scale) | reinterpret_cast<uintptr_t>(C)) % 4) return ONNXB_ERR_UNSUPPORTED;
-    if (same_place(Y, A) || same_place(Y, B)) return ONNXB_ERR_UNSUPPORTED;
+    if (same_place(Y, A) || same_place(Y, B) || begins_at(a_scale, {Y}) || begins_at(b_scale, {Y}) || begins_at(C, {Y})) return ONNXB_ERR_UNSUPPORTED;
     DenseProblem d{};
     d.mode = kDensePlain;
     d.type = ONNXB_INT8;
@@ -116,7 +123,7 @@ extern "C" onnxb_status onnx_gemm_int8_run(const onnxb_matrix *A, const float *a
     d.a_scale = a_scale; d.b_scale[0] = b_scale; d.bias = C; d.relu = fuse_relu != 0;
     d.y_type = Y->type;
     d.Y[0] = Y->data; d.y_ld[0] = operand(Y).ld;
-    CHECK(check_workspace(workspace, workspace_bytes, onnx_gemm_int8_workspace_bytes(A, B)));
+    CHECK(check_workspace(workspace, workspace_bytes, onnx_gemm_int8_workspace_bytes(A, B), {A, B, Y}));
     Placement placed(workspace);
     d.A[0] = placed(A);
     d.B[0] = placed(B);
@@ -151,9 +158,9 @@ static onnxb_status gated_problem(const onnxb_matrix *X, const onnxb_matrix *Wg,
     return ONNXB_OK;
 }
 
-static onnxb_status run_gated(DenseProblem &d, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu, void *workspace,
-                              size_t workspace_bytes, cudaStream_t stream) {
-    CHECK(check_workspace(workspace, workspace_bytes, onnx_gated_workspace_bytes(X, Wg, Wu)));
+static onnxb_status run_gated(DenseProblem &d, const onnxb_matrix *X, const onnxb_matrix *Wg, const onnxb_matrix *Wu, const onnxb_matrix *H,
+                              const onnxb_matrix *G, const onnxb_matrix *U, void *workspace, size_t workspace_bytes, cudaStream_t stream) {
+    CHECK(check_workspace(workspace, workspace_bytes, onnx_gated_workspace_bytes(X, Wg, Wu), {X, Wg, Wu, H, G, U}));
     Placement placed(workspace);
     d.A[0] = placed(X);
     d.B[0] = placed(Wg);
@@ -182,7 +189,7 @@ extern "C" onnxb_status onnx_gated_run(const onnxb_matrix *X, const onnxb_matrix
         d.Y[2] = U->data; d.y_ld[2] = operand(U).ld;
     }
     if (done) return ONNXB_OK;
-    return run_gated(d, X, Wg, Wu, workspace, workspace_bytes, (cudaStream_t)cuda_stream);
+    return run_gated(d, X, Wg, Wu, H, G, U, workspace, workspace_bytes, (cudaStream_t)cuda_stream);
 }
 
 extern "C" onnxb_status onnx_gated_int8_run(const onnxb_matrix *A, const float *a_scale, const onnxb_matrix *Wg, const float *g_scale,
@@ -196,8 +203,9 @@ extern "C" onnxb_status onnx_gated_int8_run(const onnxb_matrix *A, const float *
     if (done) return ONNXB_OK;
     if (!a_scale || !g_scale || !u_scale) return ONNXB_ERR_NULL;
     if ((reinterpret_cast<uintptr_t>(a_scale) | reinterpret_cast<uintptr_t>(g_scale) | reinterpret_cast<uintptr_t>(u_scale)) % 4) return ONNXB_ERR_UNSUPPORTED;
+    if (begins_at(a_scale, {H}) || begins_at(g_scale, {H}) || begins_at(u_scale, {H})) return ONNXB_ERR_UNSUPPORTED;
     d.a_scale = a_scale; d.b_scale[0] = g_scale; d.b_scale[1] = u_scale;
-    return run_gated(d, A, Wg, Wu, workspace, workspace_bytes, (cudaStream_t)cuda_stream);
+    return run_gated(d, A, Wg, Wu, H, nullptr, nullptr, workspace, workspace_bytes, (cudaStream_t)cuda_stream);
 }
 
 // The gradients' workspace: dG and dU, their rows at multiples of 16 bytes; for few tokens all of these rows twice, and X twice.
@@ -273,7 +281,8 @@ extern "C" onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const on
         return ONNXB_OK;
     }
     DenseProblem d{};
-    CHECK(check_workspace(workspace, workspace_bytes, backward_bytes(dH, X, Wg, Wu, dX, dWg, dWu, d.grad)));
+    CHECK(check_workspace(workspace, workspace_bytes, backward_bytes(dH, X, Wg, Wu, dX, dWg, dWu, d.grad),
+                          {dX, dWg, dWu, dH, G, U, ins[0], ins[1], ins[2]}));
     GatedSlopeProblem s{};
     s.type = dH->type; s.activation = activation;
     s.M = (int)M; s.F = (int)F;
