@@ -382,7 +382,8 @@ typedef enum {
  *   Q[i,k]   = the nearest integer to X[i,k] / scale[i] (of the exact quotient, ties to even), at most 127 in magnitude
  *
  * X [M,K] of 32- or 16-bit floats, Q [M,K] of 8-bit integers, scale [M].  A row whose scale is 0 becomes zeros.  A row with a NaN
- * or an infinity becomes zeros with a scale of NaN: whatever is computed from it is NaN, not a number that looks right.
+ * or an infinity becomes zeros with a scale of NaN: onnx_gemm_int8_run and onnx_gated_int8_run make NaN of it, not a number that looks
+ * right, and so does quantising that again; but for fuse_relu, which makes 0 of NaN as it does everywhere in this library.
  */
 onnxb_status onnx_quantize_rows_run(const onnxb_matrix *X, const onnxb_matrix *Q, float *scale, void *cuda_stream);
 
