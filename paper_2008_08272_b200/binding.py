@@ -736,7 +736,8 @@ def onnx_gemm_int8(A, a_scale, B, b_scale, C=None, *, fuse_relu=False, dtype="fl
 
 def onnx_gated(X, Wg, Wu, *, activation="silu", save=False, H=None, G=None, U=None, workspace=None, stream=None):
     """``onnx_gated_run``: H = act(X Wg^T) * (X Wu^T), X [M,K], Wg and Wu [F,K], all float16 or all bfloat16.  ``save`` (or a G and a U to
-    write to): (H, G, U) with the two projections, which ``onnx_gated_backward`` takes."""
+    write to): (H, G, U) with the two projections, which ``onnx_gated_backward`` takes.  As all calls here, it leaves torch's autograd alone: the results have
+    no graph, whether or not the inputs require gradients, and the gradients are those that ``onnx_gated_backward`` is asked for."""
     h = (_fast_mod or _fast()).gated(X, Wg, Wu, activation, save, H, G, U, workspace, stream)
     if h is not None:
         return h
@@ -783,7 +784,8 @@ def onnx_gated_int8(A, a_scale, Wg, g_scale, Wu, u_scale, *, activation="silu", 
 def onnx_gated_backward(dH, X, Wg, Wu, G, U, *, activation="silu", wanted=(True, True, True), dX=None, dWg=None, dWu=None, workspace=None,
                         stream=None):
     """``onnx_gated_backward_run``: (dX, dWg, dWu) of ``onnx_gated``, from its G and U.  ``wanted``: which of the three (None in the
-    place of the others; weights that are not needed for them, or X, may be None)."""
+    place of the others; weights that are not needed for them, or X, may be None).  dG and dU are held in the operands' type in between: in
+    float16 what is above 65504 there becomes infinite, with the dX of that token and the weights' gradients of that channel."""
     done = (_fast_mod or _fast()).gated_backward(dH, X, Wg, Wu, G, U, activation, *wanted, dX, dWg, dWu, workspace, stream)
     if done is not None:
         return done

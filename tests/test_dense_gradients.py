@@ -86,3 +86,58 @@ def test_infinite_operands_give_what_the_sums_give(M, t):
             want[0][:, column] = factor * v
         for y, w in zip(got, want):
             assert torch.equal(y.double().nan_to_num(7.0, 3e38, -3e38), w.nan_to_num(7.0, 3e38, -3e38)) and torch.equal(y.isnan(), w.isnan()), (where, at, v)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [4, 40])
+def test_dG_beyond_the_types_range(M):
+    """dG and dU are held in the operands' type: one above float16's largest number is infinite, and so is what it goes into (dX of its token,
+    dWg of its channel), no more than that; bfloat16 takes it."""
+    g = torch.Generator(device="cuda").manual_seed(63)
+    K, F = 64, 96
+    X, Wg, Wu, dH, G, U = (normal(g, *s) for s in ((M, K), (F, K), (F, K), (M, F), (M, F), (M, F)))
+    large, G[2, 9], U[2, 9] = dH.clone(), 8.0, 4.0
+    large[2, 9] = 30000.0
+    rows, channels = [i for i in range(M) if i != 2], [j for j in range(F) if j != 9]
+    for t in (torch.float16, torch.bfloat16):
+        clean, got = ([y.float() for y in binding.onnx_gated_backward(*(v.to(t) for v in (d, X, Wg, Wu, G, U)))] for d in (dH, large))
+        torch.cuda.synchronize()
+        assert torch.equal(got[0][rows], clean[0][rows]) and all(torch.equal(a[channels], b[channels]) for a, b in zip(got[1:], clean[1:]))
+        if t == torch.bfloat16:
+            assert all(bool(y.isfinite().all()) for y in got)
+        else:
+            assert not bool(got[0][2].isfinite().any()) and not bool(got[1][9].isfinite().any())
+
+
+class Gated(torch.autograd.Function):
+    """The gated block with its gradients, as a training program has them."""
+
+    @staticmethod
+    def forward(ctx, X, Wg, Wu):
+        H, G, U = binding.onnx_gated(X, Wg, Wu, save=True)
+        ctx.save_for_backward(X, Wg, Wu, G, U)
+        return H
+
+    @staticmethod
+    def backward(ctx, dH):
+        return binding.onnx_gated_backward(dH.contiguous(), *ctx.saved_tensors, wanted=ctx.needs_input_grad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [7, 90])
+def test_within_autograd(M):
+    """The calls leave autograd alone (no graph, of parameters neither), and serve as a function of it, a frozen weight among the inputs."""
+    g = torch.Generator(device="cuda").manual_seed(64)
+    X, Wg, Wu, dH = (normal(g, *s).bfloat16() for s in ((M, 72), (96, 72), (96, 72), (M, 96)))
+    leaves = [torch.nn.Parameter(v) for v in (X, Wg, Wu)]
+    assert not any(y.requires_grad for y in binding.onnx_gated(*leaves, save=True))
+    H, G, U = binding.onnx_gated(X, Wg, Wu, save=True)
+    for frozen, dH in ((None, dH), (1, dH), (None, torch.ones_like(dH[:1, :1]).expand(M, 96))):
+        want = binding.onnx_gated_backward(dH.contiguous(), X, Wg, Wu, G, U)
+        for i, leaf in enumerate(leaves):
+            leaf.grad = None
+            leaf.requires_grad_(i != frozen)
+        y = Gated.apply(*leaves)
+        y.backward(dH)
+        torch.cuda.synchronize()
+        assert torch.equal(y, H) and all(leaf.grad is None if i == frozen else torch.equal(leaf.grad, w) for i, (leaf, w) in enumerate(zip(leaves, want)))
