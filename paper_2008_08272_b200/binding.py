@@ -786,6 +786,9 @@ def onnx_gated_backward(dH, X, Wg, Wu, G, U, *, activation="silu", wanted=(True,
     """``onnx_gated_backward_run``: (dX, dWg, dWu) of ``onnx_gated``, from its G and U.  ``wanted``: which of the three (None in the
     place of the others; weights that are not needed for them, or X, may be None).  dG and dU are held in the operands' type in between: in
     float16 what is above 65504 there becomes infinite, with the dX of that token and the weights' gradients of that channel."""
+    wanted = tuple(wanted)
+    if len(wanted) != 3:
+        raise ValueError("wanted: a truth value for each of dX, dWg and dWu")
     done = (_fast_mod or _fast()).gated_backward(dH, X, Wg, Wu, G, U, activation, *wanted, dX, dWg, dWu, workspace, stream)
     if done is not None:
         return done
@@ -793,8 +796,6 @@ def onnx_gated_backward(dH, X, Wg, Wu, G, U, *, activation="silu", wanted=(True,
     v = _Views("onnx_gated_backward", stream)
     dh, g, u = v.matrix(dH, "dH", _HALVES), v.matrix(G, "G", _HALVES, dH), v.matrix(U, "U", _HALVES, dH)
     kind = str(dH.dtype)[6:]
-    if len(wanted) != 3:
-        raise ValueError("wanted: a truth value for each of dX, dWg and dWu")
     want = [w or given is not None for w, given in zip(wanted, (dX, dWg, dWu))]
     x = v.matrix(X, "X", _HALVES, dH) if want[1] or want[2] else None
     wg, wu = (v.matrix(Wg, "Wg", _HALVES, dH), v.matrix(Wu, "Wu", _HALVES, dH)) if want[0] else (None, None)

@@ -49,3 +49,16 @@ def test_refused_before_anything_is_made(native, monkeypatch):
             call(**{name: bad})
         assert torch.cuda.max_memory_allocated() == before, (name, bad.shape, bad.dtype)
     assert binding.launch_count() == launches
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("native", [True, False])
+def test_wanted_is_three_truth_values(native, monkeypatch):
+    X, Wg, Wu, G = zeros(M, K), zeros(F, K), zeros(F, K), zeros(M, F)
+    if not native:
+        monkeypatch.setattr(binding, "_fast_mod", binding._Declined())
+    for wanted in ((True,) * 2, (True,) * 4, (True,) * 11, ()):
+        with pytest.raises(ValueError):
+            binding.onnx_gated_backward(G, X, Wg, Wu, G, G, wanted=wanted)
+    some = binding.onnx_gated_backward(G, X, Wg, Wu, G, G, wanted=(w for w in (1, 0, True)))
+    assert [y is None for y in some] == [False, True, False]
