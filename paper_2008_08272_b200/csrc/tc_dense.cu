@@ -418,134 +418,132 @@ __global__ void __launch_bounds__(kThreads, 1) tc_dense_kernel(const __grid_cons
                 for (int j = 0; j < 32; ++j) v[j] = sum[j];
             };
             if (row0 < M) {
-                {
-                    // The two warps of a quarter share its blocks of all results in turns; of 8-bit operands, whose scales are fetched from
-                    // one to the next, a half each
+                // The two warps of a quarter share its blocks of all results in turns; of 8-bit operands, whose scales are fetched from
+                // one to the next, a half each
 #pragma unroll 1
-                    for (int item = kInt8 ? lo : half, items = kInt8 ? hi : blocks * p.outs; item < items; item += kInt8 ? 1 : 2) {
-                        const int which = kInt8 || item < blocks ? 0 : item < 2 * blocks ? 1 : 2, b = item - which * blocks;
-                        const int y = !kGrad ? which : at.x ? 0 : 1 + p.w_first + at.z;
-                        if (kSplit && owner(b) != part) continue;
-                        // (TMA writes whole blocks, and of those at Y's end whole pieces of 16 bytes: not where the tile ends inside a block, or
-                        // the last columns fill no piece, since what follows is another tile's or not Y's)
-                        const bool by_tma = p.y_tma[y] && (b + 1) * block_cols <= (p.y_tma[y] == 2 ? p.out_cols : cols);
-                        if (lane == 0) tma_store_wait_read<0>();                // the buffer's last block has gone
-                        __syncwarp();
+                for (int item = kInt8 ? lo : half, items = kInt8 ? hi : blocks * p.outs; item < items; item += kInt8 ? 1 : 2) {
+                    const int which = kInt8 || item < blocks ? 0 : item < 2 * blocks ? 1 : 2, b = item - which * blocks;
+                    const int y = !kGrad ? which : at.x ? 0 : 1 + p.w_first + at.z;
+                    if (kSplit && owner(b) != part) continue;
+                    // (TMA writes whole blocks, and of those at Y's end whole pieces of 16 bytes: not where the tile ends inside a block, or
+                    // the last columns fill no piece, since what follows is another tile's or not Y's)
+                    const bool by_tma = p.y_tma[y] && (b + 1) * block_cols <= (p.y_tma[y] == 2 ? p.out_cols : cols);
+                    if (lane == 0) tma_store_wait_read<0>();                // the buffer's last block has gone
+                    __syncwarp();
 #pragma unroll 1
-                        for (int c = 0; c < block_cols && b * block_cols + c < p.out_cols; c += 32) {
-                            const int col = b * block_cols + c;
-                            uint32_t v[32];
-                            float f[32];
-                            if (kMode == kDenseGated) {
-                                uint32_t w[32];
-                                if (kInt8 && kSplit) fetch(col);
-                                load(which == 2 ? p.out_cols + col : col, v);
-                                if (which == 0) load(p.out_cols + col, w);
-                                tmem_ld_wait();
-                                const float c0 = s0, c1 = s1;
-                                if (kInt8) {
-                                    if (!kSplit) fetch(col + 32);
-                                    // (one factor after the other: the sum may be 0 where the factors' product is infinite)
+                    for (int c = 0; c < block_cols && b * block_cols + c < p.out_cols; c += 32) {
+                        const int col = b * block_cols + c;
+                        uint32_t v[32];
+                        float f[32];
+                        if (kMode == kDenseGated) {
+                            uint32_t w[32];
+                            if (kInt8 && kSplit) fetch(col);
+                            load(which == 2 ? p.out_cols + col : col, v);
+                            if (which == 0) load(p.out_cols + col, w);
+                            tmem_ld_wait();
+                            const float c0 = s0, c1 = s1;
+                            if (kInt8) {
+                                if (!kSplit) fetch(col + 32);
+                                // (one factor after the other: the sum may be 0 where the factors' product is infinite)
 #pragma unroll
-                                    for (int j = 0; j < 32; ++j) {
-                                        f[j] = (float)(int)v[j] * sa * __shfl_sync(0xffffffffu, c0, j);
-                                        w[j] = __float_as_uint((float)(int)w[j] * sa * __shfl_sync(0xffffffffu, c1, j));
-                                    }
-                                } else {
-#pragma unroll
-                                    for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+                                for (int j = 0; j < 32; ++j) {
+                                    f[j] = (float)(int)v[j] * sa * __shfl_sync(0xffffffffu, c0, j);
+                                    w[j] = __float_as_uint((float)(int)w[j] * sa * __shfl_sync(0xffffffffu, c1, j));
                                 }
-                                if (which == 0) {
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+                            }
+                            if (which == 0) {
 #define ONNXB_GATE(kind) _Pragma("unroll") for (int j = 0; j < 32; ++j) f[j] = activate(kind, f[j]) * __uint_as_float(w[j])
-                                    if (p.activation == ONNXB_SILU) { ONNXB_GATE(ONNXB_SILU); }
-                                    else if (p.activation == ONNXB_GELU) { ONNXB_GATE(ONNXB_GELU); }
-                                    else if (p.activation == ONNXB_GELU_TANH) { ONNXB_GATE(ONNXB_GELU_TANH); }
-                                    else { ONNXB_GATE(ONNXB_RELU); }
+                                if (p.activation == ONNXB_SILU) { ONNXB_GATE(ONNXB_SILU); }
+                                else if (p.activation == ONNXB_GELU) { ONNXB_GATE(ONNXB_GELU); }
+                                else if (p.activation == ONNXB_GELU_TANH) { ONNXB_GATE(ONNXB_GELU_TANH); }
+                                else { ONNXB_GATE(ONNXB_RELU); }
 #undef ONNXB_GATE
-                                }
-                            } else {
-                                if (kInt8 && kSplit) fetch(col);
-                                load(col, v);
-                                tmem_ld_wait();
-                                if (kInt8) {
-                                    const float c0 = s0, c1 = s1;
-                                    if (!kSplit) fetch(col + 32);
-#pragma unroll
-                                    for (int j = 0; j < 32; ++j) {
-                                        f[j] = (float)(int)v[j] * sa * __shfl_sync(0xffffffffu, c0, j) + __shfl_sync(0xffffffffu, c1, j);
-                                        if (p.relu) f[j] = fmaxf(f[j], 0.f);
-                                    }
-                                } else {
-#pragma unroll
-                                    for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
-                                }
-                            }
-                            // the lane's row of the block, 16-byte piece i at position i ^ (lane % 8): the 128-byte swizzle
-                            if (wide) {
-#pragma unroll
-                                for (int i = 0; i < 8; ++i)
-                                    *reinterpret_cast<float4 *>(buf + lane * kRowBytes + ((i ^ (lane & 7)) << 4)) =
-                                        make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-                            } else {
-                                uint32_t h[16];
-                                if (p.y_type == ONNXB_FLOAT16) {
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i) h[i] = pack<__half2>(f[2 * i], f[2 * i + 1]);
-                                } else {
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i) h[i] = pack<__nv_bfloat162>(f[2 * i], f[2 * i + 1]);
-                                }
-#pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    *reinterpret_cast<uint4 *>(buf + lane * kRowBytes + (((c / 8 + i) ^ (lane & 7)) << 4)) =
-                                        make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
-                            }
-                        }
-                        const int col0 = n0 + b * block_cols;
-                        if (by_tma) {
-                            fence_proxy_async_smem();
-                            __syncwarp();
-                            if (lane == 0) {
-                                tma_store_2d(&maps.Y[y], buf, col0, parts ? at.z * p.x_part_rows + row0 : row0);
-                                tma_store_commit();
                             }
                         } else {
-                            // Rows that TMA cannot address: read back row by row, 8 bytes a lane and two rows at a time where they begin at
-                            // multiples of 8, else 4 bytes a lane.  Short loops: most launches run this once or twice, out of cold
-                            // instruction memory (with four rows' reads first and odd 16-bit rows shifted to whole words gated block
-                            // 333 x 1000 x 2741 takes 12.9 us, 11.7 so; 2736 channels, by TMA, 10.6).
-                            __syncwarp();
-                            const int rows = min(32, M - row0), element = wide ? 4 : 2, left = (cols - b * block_cols) * element;
-                            char *out = static_cast<char *>(p.Y[y]) + ((long long)row0 * p.y_ld[y] + col0) * element;
-                            const long long pitch = p.y_ld[y] * element;
-                            if (((reinterpret_cast<uintptr_t>(out) | (unsigned long long)pitch) & 7) == 0) {
-                                const int at = lane % 16 * 8;
-#pragma unroll 4
-                                for (int r = lane / 16; r < rows; r += 2) {
-                                    const uint2 v = *reinterpret_cast<const uint2 *>(buf + r * kRowBytes + (((at >> 4) ^ (r & 7)) << 4 | (at & 8)));
-                                    char *to = out + r * pitch + at;
-                                    if (at + 8 <= left) *reinterpret_cast<uint2 *>(to) = v;
-                                    else if (at < left) {
-                                        if (at + 4 <= left) *reinterpret_cast<uint32_t *>(to) = v.x;
-                                        if (left & 2) *reinterpret_cast<uint16_t *>(to + (left & 4)) = (uint16_t)(left & 4 ? v.y : v.x);
-                                    }
+                            if (kInt8 && kSplit) fetch(col);
+                            load(col, v);
+                            tmem_ld_wait();
+                            if (kInt8) {
+                                const float c0 = s0, c1 = s1;
+                                if (!kSplit) fetch(col + 32);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) {
+                                    f[j] = (float)(int)v[j] * sa * __shfl_sync(0xffffffffu, c0, j) + __shfl_sync(0xffffffffu, c1, j);
+                                    if (p.relu) f[j] = fmaxf(f[j], 0.f);
                                 }
                             } else {
-                                const int at = lane * 4;
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+                            }
+                        }
+                        // the lane's row of the block, 16-byte piece i at position i ^ (lane % 8): the 128-byte swizzle
+                        if (wide) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                *reinterpret_cast<float4 *>(buf + lane * kRowBytes + ((i ^ (lane & 7)) << 4)) =
+                                    make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+                        } else {
+                            uint32_t h[16];
+                            if (p.y_type == ONNXB_FLOAT16) {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) h[i] = pack<__half2>(f[2 * i], f[2 * i + 1]);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) h[i] = pack<__nv_bfloat162>(f[2 * i], f[2 * i + 1]);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                *reinterpret_cast<uint4 *>(buf + lane * kRowBytes + (((c / 8 + i) ^ (lane & 7)) << 4)) =
+                                    make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
+                        }
+                    }
+                    const int col0 = n0 + b * block_cols;
+                    if (by_tma) {
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tma_store_2d(&maps.Y[y], buf, col0, parts ? at.z * p.x_part_rows + row0 : row0);
+                            tma_store_commit();
+                        }
+                    } else {
+                        // Rows that TMA cannot address: read back row by row, 8 bytes a lane and two rows at a time where they begin at
+                        // multiples of 8, else 4 bytes a lane.  Short loops: most launches run this once or twice, out of cold
+                        // instruction memory (with four rows' reads first and odd 16-bit rows shifted to whole words gated block
+                        // 333 x 1000 x 2741 takes 12.9 us, 11.7 so; 2736 channels, by TMA, 10.6).
+                        __syncwarp();
+                        const int rows = min(32, M - row0), element = wide ? 4 : 2, left = (cols - b * block_cols) * element;
+                        char *out = static_cast<char *>(p.Y[y]) + ((long long)row0 * p.y_ld[y] + col0) * element;
+                        const long long pitch = p.y_ld[y] * element;
+                        if (((reinterpret_cast<uintptr_t>(out) | (unsigned long long)pitch) & 7) == 0) {
+                            const int at = lane % 16 * 8;
 #pragma unroll 4
-                                for (int r = 0; r < rows; ++r) {
-                                    const uint32_t v = *reinterpret_cast<const uint32_t *>(buf + r * kRowBytes + (((at >> 4) ^ (r & 7)) << 4 | (at & 12)));
-                                    char *to = out + r * pitch + at;
-                                    if (wide) {
-                                        if (at < left) *reinterpret_cast<uint32_t *>(to) = v;
-                                    } else {
-                                        if (at < left) *reinterpret_cast<uint16_t *>(to) = (uint16_t)v;
-                                        if (at + 2 < left) *reinterpret_cast<uint16_t *>(to + 2) = (uint16_t)(v >> 16);
-                                    }
+                            for (int r = lane / 16; r < rows; r += 2) {
+                                const uint2 v = *reinterpret_cast<const uint2 *>(buf + r * kRowBytes + (((at >> 4) ^ (r & 7)) << 4 | (at & 8)));
+                                char *to = out + r * pitch + at;
+                                if (at + 8 <= left) *reinterpret_cast<uint2 *>(to) = v;
+                                else if (at < left) {
+                                    if (at + 4 <= left) *reinterpret_cast<uint32_t *>(to) = v.x;
+                                    if (left & 2) *reinterpret_cast<uint16_t *>(to + (left & 4)) = (uint16_t)(left & 4 ? v.y : v.x);
                                 }
                             }
-                            __syncwarp();
+                        } else {
+                            const int at = lane * 4;
+#pragma unroll 4
+                            for (int r = 0; r < rows; ++r) {
+                                const uint32_t v = *reinterpret_cast<const uint32_t *>(buf + r * kRowBytes + (((at >> 4) ^ (r & 7)) << 4 | (at & 12)));
+                                char *to = out + r * pitch + at;
+                                if (wide) {
+                                    if (at < left) *reinterpret_cast<uint32_t *>(to) = v;
+                                } else {
+                                    if (at < left) *reinterpret_cast<uint16_t *>(to) = (uint16_t)v;
+                                    if (at + 2 < left) *reinterpret_cast<uint16_t *>(to + 2) = (uint16_t)(v >> 16);
+                                }
+                            }
                         }
+                        __syncwarp();
                     }
                 }
             }
