@@ -3,7 +3,7 @@
 //
 // The pipeline is that of tc_gemm.cu: a persistent CTA (or a pair of two on one tile) per SM, 320 threads,
 //   warp 0    TMA producer, a ring of stages of 128 bytes along the reduction (64 16-bit or 128 8-bit terms), or of 2 or 4 times
-//             that where tiles are small, since a stage costs its two single threads some 270 cycles whatever it holds;
+//             that where tiles are small, since a stage costs its two single threads 240 cycles, and 170 more for each block;
 //   warp 1    one thread issues tcgen05.mma kind::f16 or kind::i8 into one of two TMEM accumulators;
 //   warps 2-9 epilogue: tcgen05.ld, the mathematics, 32-row blocks of 128 bytes staged in swizzled shared memory, TMA stores (plain ones
 //             where Y's rows do not begin at multiples of 16 bytes).
@@ -22,7 +22,7 @@
 // Measured (a burst; under the power cap of a long run in brackets): gated block 4096 x 4096 x 10240 in bf16 with G and U kept 450 us, 1.53
 // PFLOP/s (535), of 8-bit operands 203 us, 3.4 POP/s (247); 8-bit Gemm 4096 x 10240 x 4096 110 us, 3.1 POP/s (130); the three products of
 // the gradients at the first size 880 us, 1.56 PFLOP/s: the tensor pipe is 90 to 96 % busy.  Small tiles are bound by a stage's
-// 410 cycles, short reductions by the epilogue's latencies (two warps a scheduler), few tokens by the weights' bytes.
+// 410 cycles (of one block), short reductions by the epilogue's latencies (two warps a scheduler), few tokens by the weights' bytes.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
