@@ -41,7 +41,7 @@ def test_parts_of_dX_do_not_go_by_what_else_is_wanted(size):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("t", [torch.bfloat16, torch.float16], ids=str)
-@pytest.mark.parametrize("size", IN_PARTS + [(2048, 1024, 4096)], ids=str)
+@pytest.mark.parametrize("size", IN_PARTS + [(2048, 1024, 4096), (1, 4096, 10240), (20, 1024, 4096), (32, 512, 2816)], ids=str)
 def test_dX_is_the_same_whatever_else_is_wanted(size, t):
     """Bit by bit, with nothing pinned: a weight that is frozen does not change the other gradients."""
     g = torch.Generator(device="cuda").manual_seed(61)
