@@ -427,9 +427,10 @@ onnxb_status onnx_gated_int8_run(const onnxb_matrix *A, const float *a_scale, co
  * All of one type, 16-bit floats; shapes as the forward call's.  dX, dWg, dWu: each may be NULL where it is not wanted (not all of
  * them); X is not read (and may be NULL) without dWg and dWu, Wg and Wu neither without dX.  dG and dU are rounded to the
  * type between the two steps (the tensor cores take 16-bit operands; up to 32 tokens, where few roundings would not average, what
- * that leaves of them is kept as well, but for X or weights that are not finite), sums are in 32 bits, dX is one sum over both terms, and each result is rounded once.
- * In float16 a dG or dU above 65504 in magnitude is therefore infinite, whatever the number of tokens, and so is all that it goes into (dX of its token,
- * the weights' gradients of its channel), even where these would have fitted: loss scaling as for any training in float16, or bfloat16.
+ * that leaves of them is kept as well, but for X or weights that are not finite), sums are in 32 bits, dX is one sum over both terms,
+ * and each result is rounded once.  In float16 a dG or dU above 65504 in magnitude is therefore infinite, whatever the number of tokens, and
+ * what it goes into (dX of its token, the weights' gradients of its channel) is infinite or NaN, even where that would have fitted:
+ * scale the loss as for any training in float16, or use bfloat16.
  * Rounding dG and dU makes the results' error 1.4 times that of rounding the results alone, from 33 tokens on.
  * Deterministic: no atomics; and a result is the same bit by bit whichever others are wanted with it.
  */

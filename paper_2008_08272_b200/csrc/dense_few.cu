@@ -198,9 +198,9 @@ void (*kernel_for(const DenseProblem &d))(const Params) {
     return d.type == ONNXB_FLOAT16 ? kernel_for<ONNXB_FLOAT16, 2, kWarps>(d.M) : kernel_for<ONNXB_BFLOAT16, 2, kWarps>(d.M);
 }
 // Warps a block: as many as let all blocks run at once, or 8 where no number does.  (16, 8 and 4: gated block 8192 -> 1024 11.5, 17.8 and 30
-// us; 8-bit 10240 -> 4096 11.6, 9.6 and 15.2; 4096 -> 10240 11.8, 9.4 and 8.3.)  That makes a step where 4 warps no longer do: one token, 8-bit 4096 -> 14208, 888 blocks, 9.4 us; -> 14224
-// 11.2 of 8 warps (12.3 of 4; 9.0 are the weights' bytes); gated block of 16-bit weights 40.5 on both sides, of 8 warps 36.0 and 39.8.
-// ONNXB_DENSE_FEW_WARPS pins it.
+// us; 8-bit 10240 -> 4096 11.6, 9.6 and 15.2; 4096 -> 10240 11.8, 9.4 and 8.3.)  That
+// makes a step where 4 warps no longer do: one token, 8-bit 4096 -> 14208, 888 blocks, 9.4 us; -> 14224 11.2 of 8 warps (12.3 of 4; 9.0 are the
+// weights' bytes); gated block of 16-bit weights 40.5 and 39.8, of 8 warps 36.0 and 39.8.  ONNXB_DENSE_FEW_WARPS pins it.
 int warps_of(const DenseProblem &d) {
     if (const char *e = getenv("ONNXB_DENSE_FEW_WARPS")) return atoi(e) == 4 ? 4 : atoi(e) == 16 ? 16 : 8;
     const int tiles = d.M <= 8 ? 1 : 2;
