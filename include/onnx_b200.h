@@ -441,6 +441,37 @@ onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const onnxb_matrix 
                                      const onnxb_matrix *dWg, const onnxb_matrix *dWu, void *workspace, size_t workspace_bytes,
                                      void *cuda_stream);
 
+/*
+ * onnx_layer_normalization_run - ONNX LayerNormalization over the rows of a two-dimensional view (a tensor of more dimensions: its rows, of all the
+ * dimensions from `axis` on):
+ *
+ *   mean[i] = sum_k X[i,k] / K,  inv_std[i] = 1 / sqrt(sum_k (X[i,k] - mean[i])^2 / K + epsilon)
+ *   Y[i,k] = (X[i,k] - mean[i]) * inv_std[i] * scale[k] + bias[k]
+ *
+ * X and Y [M,K] of one type, 32- or 16-bit floats; scale and bias views of one row of K, of X's type or of 32-bit floats (both of one type);
+ * bias may be NULL.  mean and inv_std: 32-bit floats [M], ONNX's Mean and InvStdDev, which the gradients want; both NULL where they are
+ * not kept.  epsilon: finite, not negative.  Computed in 32 bits, the mean taken away before the squares are added up; each result is rounded once.
+ * What the tensors may be is said above at onnxb_matrix; errors are those of that list (ERR_ATTR also: epsilon).
+ */
+onnxb_status onnx_layer_normalization_run(const onnxb_matrix *X, const onnxb_matrix *scale, const onnxb_matrix *bias, float epsilon,
+                                          const onnxb_matrix *Y, float *mean, float *inv_std, void *cuda_stream);
+
+/*
+ * onnx_layer_normalization_backward_run - the gradients of onnx_layer_normalization_run, from dY, X and the mean and inv_std that it kept:
+ *
+ *   n[i,k] = (X[i,k] - mean[i]) * inv_std[i],  d[i,k] = dY[i,k] * scale[k]
+ *   dX[i,k] = inv_std[i] * (d[i,k] - mean_k(d[i,:]) - n[i,k] * mean_k(d[i,:] * n[i,:]))
+ *   dScale[k] = sum_i dY[i,k] * n[i,k],  dBias[k] = sum_i dY[i,k]
+ *
+ * dY, X and dX [M,K] of one type; scale, dScale and dBias one row of K each, of that type or of 32-bit floats (all of one type).  dX, dScale and dBias:
+ * each may be NULL where it is not wanted (not all of them); scale may be NULL without dX.  Sums are in 32 bits, in an order that the
+ * sizes fix: results are the same bit by bit from call to call, and whichever others are wanted.  No rows: dScale and dBias are zeros.
+ */
+size_t onnx_layer_normalization_backward_workspace_bytes(const onnxb_matrix *X, const onnxb_matrix *dScale, const onnxb_matrix *dBias);   /* host only */
+onnxb_status onnx_layer_normalization_backward_run(const onnxb_matrix *dY, const onnxb_matrix *X, const onnxb_matrix *scale, const float *mean,
+                                                   const float *inv_std, const onnxb_matrix *dX, const onnxb_matrix *dScale,
+                                                   const onnxb_matrix *dBias, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 /* Human-readable name of a status code (static storage, never NULL). */
 const char *onnxb_status_string(onnxb_status status);
 

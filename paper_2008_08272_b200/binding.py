@@ -37,6 +37,7 @@ EXPORTS = [
     "onnxb_probe_wait_timeout",
     "onnx_quantize_rows_run", "onnx_gemm_int8_workspace_bytes", "onnx_gemm_int8_run", "onnx_gated_workspace_bytes", "onnx_gated_run",
     "onnx_gated_int8_run", "onnx_gated_backward_workspace_bytes", "onnx_gated_backward_run",
+    "onnx_layer_normalization_run", "onnx_layer_normalization_backward_workspace_bytes", "onnx_layer_normalization_backward_run",
 ]
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
 TYPE_CODES = {"float32": 1, "int8": 3, "float16": 10, "bfloat16": 16}      # ONNX's
@@ -184,11 +185,13 @@ def load(build_if_missing: bool = True):
                        ("onnx_gemm_int8_run", [mp, vp, mp, vp, vp, ctypes.c_int, mp, vp, sz, vp]),
                        ("onnx_gated_run", [mp, mp, mp, ctypes.c_int, mp, mp, mp, vp, sz, vp]),
                        ("onnx_gated_int8_run", [mp, vp, mp, vp, mp, vp, ctypes.c_int, mp, vp, sz, vp]),
-                       ("onnx_gated_backward_run", [mp] * 6 + [ctypes.c_int] + [mp] * 3 + [vp, sz, vp])):
+                       ("onnx_gated_backward_run", [mp] * 6 + [ctypes.c_int] + [mp] * 3 + [vp, sz, vp]),
+                       ("onnx_layer_normalization_run", [mp] * 3 + [ctypes.c_float, mp, vp, vp, vp]),
+                       ("onnx_layer_normalization_backward_run", [mp] * 3 + [vp, vp] + [mp] * 3 + [vp, sz, vp])):
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = args
     for name, args in (("onnx_gemm_int8_workspace_bytes", [mp, mp]), ("onnx_gated_workspace_bytes", [mp] * 3),
-                       ("onnx_gated_backward_workspace_bytes", [mp] * 7)):
+                       ("onnx_gated_backward_workspace_bytes", [mp] * 7), ("onnx_layer_normalization_backward_workspace_bytes", [mp] * 3)):
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = args
     _lib = lib
@@ -638,6 +641,20 @@ class _Views:
         if t is not None:
             self.matrix(t, name, types, like)
 
+    def row(self, t, name, types, size, like=None):
+        """A vector of weights, as a matrix of one row."""
+        if t is None:
+            raise OnnxB200Error(1, f"{name} is None")
+        self._on_device(t, name)
+        kind = str(t.dtype)[6:]
+        if kind not in types or (like is not None and t.dtype != like.dtype):
+            raise TypeError(f"{name} must be {' or '.join(types)}" + ("" if like is None else ", all weights of one type"))
+        if t.dim() != 1 or not t.is_contiguous():
+            raise TypeError(f"{name} must have one dimension and be contiguous")
+        if t.numel() != size:
+            raise OnnxB200Error(3, f"{self.where}: {name} has {t.numel()} values, not {size}")
+        return Matrix(t.data_ptr() or None, 1, size, size, TYPE_CODES[kind], 0)
+
     def vector(self, t, name, size, allow_none=False):
         if t is None and allow_none:
             return None
@@ -813,3 +830,71 @@ def onnx_gated_backward(dH, X, Wg, Wu, G, U, *, activation="silu", wanted=(True,
         _ref(dh), _ref(x), _ref(wg), _ref(wu), _ref(dx), _ref(dwg), _ref(dwu)))
     v.call(lib.onnx_gated_backward_run, dh, _ref(x), _ref(wg), _ref(wu), g, u, activation, _ref(dx), _ref(dwg), _ref(dwu), ws, ws_len)
     return tuple(outs)
+
+
+# --------------------------------------------------------------------- layer normalisation
+def onnx_layer_normalization(X, scale, B=None, *, epsilon=1e-5, save=False, Y=None, mean=None, inv_std=None, stream=None):
+    """``onnx_layer_normalization_run``: Y = (X - mean) * inv_std * scale + B of each row of X [M,K] (ONNX LayerNormalization over the last axis;
+    rows of more dimensions: a view of them).  X float32, float16 or bfloat16; scale and B [K] of X's type or float32.  ``save`` (or a mean and an
+    inv_std to write to): (Y, mean, inv_std), which ``onnx_layer_normalization_backward`` takes."""
+    done = (_fast_mod or _fast()).layer_norm(X, scale, B, epsilon, save, Y, mean, inv_std, stream)
+    if done is not None:
+        return done
+    lib = load()
+    v = _Views("onnx_layer_normalization", stream)
+    x = v.matrix(X, "X", _FLOATS)
+    kind = str(X.dtype)[6:]
+    weights = (kind, "float32") if kind != "float32" else ("float32",)
+    s = v.row(scale, "scale", weights, x.cols)
+    b = None if B is None else v.row(B, "B", weights, x.cols, scale)
+    v.given(Y, "Y", _FLOATS, X)
+    save = save or mean is not None or inv_std is not None
+    for given, name in ((mean, "mean"), (inv_std, "inv_std")):
+        v.vector(given, name, x.rows, allow_none=True)
+    Y = v.new(x.rows, x.cols, kind) if Y is None else Y
+    if save:
+        mean = _new(x.rows, v.device, stream) if mean is None else mean
+        inv_std = _new(x.rows, v.device, stream) if inv_std is None else inv_std
+    m, r = (v.vector(mean, "mean", x.rows), v.vector(inv_std, "inv_std", x.rows)) if save else (None, None)
+    v.call(lib.onnx_layer_normalization_run, x, s, _ref(b), float(epsilon), v.matrix(Y, "Y", _FLOATS, X), m, r)
+    return (Y, mean, inv_std) if save else Y
+
+
+def onnx_layer_normalization_backward(dY, X, scale, mean, inv_std, *, wanted=(True, True, True), dX=None, dScale=None, dB=None, workspace=None,
+                                      stream=None):
+    """``onnx_layer_normalization_backward_run``: (dX, dScale, dB) of ``onnx_layer_normalization``, from its mean and inv_std.  ``wanted``: which of
+    the three (None in the place of the others).  dScale and dB are of scale's type; without scale (which dX alone needs) of X's, or of that of
+    those that are given."""
+    wanted = tuple(wanted)
+    if len(wanted) != 3:
+        raise ValueError("wanted: a truth value for each of dX, dScale and dB")
+    done = (_fast_mod or _fast()).layer_norm_backward(dY, X, scale, mean, inv_std, *wanted, dX, dScale, dB, workspace, stream)
+    if done is not None:
+        return done
+    lib = load()
+    v = _Views("onnx_layer_normalization_backward", stream)
+    dy, x = v.matrix(dY, "dY", _FLOATS), v.matrix(X, "X", _FLOATS, dY)
+    kind = str(X.dtype)[6:]
+    weights = (kind, "float32") if kind != "float32" else ("float32",)
+    want = [w or given is not None for w, given in zip(wanted, (dX, dScale, dB))]
+    if not any(want):
+        raise OnnxB200Error(1, "onnx_layer_normalization_backward: no gradient is wanted")
+    like = next((t for t in (scale, dScale, dB) if t is not None), None)
+    s = v.row(scale, "scale", weights, x.cols) if want[0] or scale is not None else None
+    m, r = v.vector(mean, "mean", x.rows), v.vector(inv_std, "inv_std", x.rows)
+    v.given(dX, "dX", _FLOATS, X)
+    for given, name in ((dScale, "dScale"), (dB, "dB")):
+        if given is not None:
+            v.row(given, name, weights, x.cols, like)
+    v.given_workspace(workspace)
+    if want[0] and dX is None:
+        dX = v.new(x.rows, x.cols, kind)
+    of_weights = kind if like is None else str(like.dtype)[6:]
+    dScale = _new(x.cols, v.device, stream, of_weights) if want[1] and dScale is None else dScale
+    dB = _new(x.cols, v.device, stream, of_weights) if want[2] and dB is None else dB
+    dx = v.matrix(dX, "dX", _FLOATS, X) if want[0] else None
+    ds = v.row(dScale, "dScale", weights, x.cols, like) if want[1] else None
+    db = v.row(dB, "dB", weights, x.cols, like) if want[2] else None
+    held, ws, ws_len = v.workspace(workspace, lib.onnx_layer_normalization_backward_workspace_bytes(x, _ref(ds), _ref(db)))
+    v.call(lib.onnx_layer_normalization_backward_run, dy, x, _ref(s) if want[0] else None, m, r, _ref(dx), _ref(ds), _ref(db), ws, ws_len)
+    return dX, dScale, dB

@@ -21,7 +21,8 @@ __global__ void __launch_bounds__(256) repack_rows_kernel(const RepackProblem p)
     const RepackJob &job = p.job[blockIdx.y];
     const int per_row = job.dst_pitch >= 512 ? 32 : job.dst_pitch >= 256 ? 16 : 8, rows = 256 / per_row, lane = threadIdx.x % per_row;
     for (int row = blockIdx.x * rows + threadIdx.x / per_row; row < job.rows; row += gridDim.x * rows) {
-        const uint8_t *src = job.src + row * job.src_pitch;
+        const int group = job.group_rows ? row / job.group_rows : 0;
+        const uint8_t *src = job.src + group * job.group_pitch + (row - group * job.group_rows) * job.src_pitch;
         uint8_t *dst = job.dst + row * job.dst_pitch;
         for (long long at = (long long)(blockIdx.z * per_row + lane) * 16; at < job.dst_pitch; at += (long long)gridDim.z * per_row * 16)
             *reinterpret_cast<uint4 *>(dst + at) = job.element == 2 ? load16_anywhere<2>(src, at, job.row_bytes) : load16_anywhere<1>(src, at, job.row_bytes);

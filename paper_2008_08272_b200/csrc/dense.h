@@ -86,6 +86,8 @@ struct RepackJob {
     int rows, element;       // bytes of one
     uint8_t *dst;
     long long dst_pitch;
+    int group_rows;          // src's rows lie in groups of so many, group_pitch apart (0: in one)
+    long long group_pitch;
 };
 struct RepackProblem {
     RepackJob job[3];

@@ -43,6 +43,9 @@ struct Abi {
     decltype(&onnx_gated_int8_run) gated_int8_run;
     decltype(&onnx_gated_backward_workspace_bytes) gated_backward_workspace_bytes;
     decltype(&onnx_gated_backward_run) gated_backward_run;
+    decltype(&onnx_layer_normalization_run) layer_norm_run;
+    decltype(&onnx_layer_normalization_backward_workspace_bytes) layer_norm_backward_workspace_bytes;
+    decltype(&onnx_layer_normalization_backward_run) layer_norm_backward_run;
 } abi;
 
 struct Plan {                    // what a convolution descriptor resolved to
@@ -145,6 +148,9 @@ PyObject *py_bind(PyObject *, PyObject *arg) {
     get(abi.gated_int8_run, "onnx_gated_int8_run");
     get(abi.gated_backward_workspace_bytes, "onnx_gated_backward_workspace_bytes");
     get(abi.gated_backward_run, "onnx_gated_backward_run");
+    get(abi.layer_norm_run, "onnx_layer_normalization_run");
+    get(abi.layer_norm_backward_workspace_bytes, "onnx_layer_normalization_backward_workspace_bytes");
+    get(abi.layer_norm_backward_run, "onnx_layer_normalization_backward_run");
     if (!ok) { PyErr_SetString(PyExc_OSError, "a symbol of the C ABI is missing"); return nullptr; }
     Py_RETURN_NONE;
 }
@@ -320,9 +326,11 @@ struct Views {
         if (t.device().index() != device) fine = false;
         return &t;
     }
+    static int32_t code_of(at::ScalarType type) {
+        return type == at::kFloat ? ONNXB_FLOAT : type == at::kChar ? ONNXB_INT8 : type == at::kHalf ? ONNXB_FLOAT16 : type == at::kBFloat16 ? ONNXB_BFLOAT16 : 0;
+    }
     void take(const at::Tensor &t, onnxb_matrix &m) {
-        const at::ScalarType type = t.scalar_type();
-        m.type = type == at::kFloat ? ONNXB_FLOAT : type == at::kChar ? ONNXB_INT8 : type == at::kHalf ? ONNXB_FLOAT16 : type == at::kBFloat16 ? ONNXB_BFLOAT16 : 0;
+        m.type = code_of(t.scalar_type());
         if (!m.type || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) { fine = false; return; }
         m.data = t.data_ptr();
         m.rows = t.size(0);
@@ -335,6 +343,15 @@ struct Views {
         if (o == Py_None) return nullptr;
         const at::Tensor *t = on_device(o);
         if (t) take(*t, m);
+        return &m;
+    }
+    // a vector of floats of any type as a matrix of one row, or nullptr for None
+    onnxb_matrix *row(PyObject *o, int64_t size, onnxb_matrix &m) {
+        if (o == Py_None) return nullptr;
+        const at::Tensor *t = on_device(o);
+        if (!t || t->dim() != 1 || !t->is_contiguous() || t->numel() != size) { fine = false; return &m; }
+        m = onnxb_matrix{t->data_ptr(), 1, size, size, code_of(t->scalar_type()), 0};
+        if (!m.type || m.type == ONNXB_INT8) fine = false;
         return &m;
     }
     float *vector(PyObject *o, int64_t size) {
@@ -517,6 +534,70 @@ PyObject *py_gated_backward(PyObject *, PyObject *const *o, Py_ssize_t n) {
     return Py_BuildValue("(NNN)", got[0], got[1], got[2]);
 }
 
+// layer_norm(X, scale, B, epsilon, save, Y, mean, inv_std, stream) -> Y, or (Y, mean, inv_std)
+PyObject *py_layer_norm(PyObject *, PyObject *const *o, Py_ssize_t n) {
+    if (n != 9) return slow_path();
+    Views v(o[8]);
+    onnxb_matrix x{}, s{}, b{}, y{};
+    if (!v.matrix(o[0], x) || !v.fine || x.rows < 1 || x.type == ONNXB_INT8 || !v.row(o[1], x.cols, s)) return slow_path();
+    const onnxb_matrix *bias = v.row(o[2], x.cols, b);
+    const double epsilon = PyFloat_AsDouble(o[3]);
+    const int asked = PyObject_IsTrue(o[4]);
+    if (PyErr_Occurred()) { PyErr_Clear(); return slow_path(); }
+    const bool save = asked || o[6] != Py_None || o[7] != Py_None;
+    float *mean = v.vector(o[6], x.rows), *inv_std = v.vector(o[7], x.rows);
+    if (!v.fine || !v.takes({o[5]}, Py_None)) return slow_path();
+    at::Tensor yt, mt, rt;
+    v.result(o[5], x.rows, x.cols, x.type, yt, y);
+    if (save && !mean) {
+        mt = v.made({x.rows}, at::kFloat);
+        mean = static_cast<float *>(mt.data_ptr());
+    }
+    if (save && !inv_std) {
+        rt = v.made({x.rows}, at::kFloat);
+        inv_std = static_cast<float *>(rt.data_ptr());
+    }
+    if (abi.layer_norm_run(&x, &s, bias, (float)epsilon, &y, mean, inv_std, v.stream) != ONNXB_OK) return slow_path();
+    if (!save) return result(o[5], yt);
+    return Py_BuildValue("(NNN)", result(o[5], yt), result(o[6], mt), result(o[7], rt));
+}
+
+// layer_norm_backward(dY, X, scale, mean, inv_std, dX wanted, dScale wanted, dB wanted, dX, dScale, dB, workspace, stream) -> (dX, dScale, dB)
+PyObject *py_layer_norm_backward(PyObject *, PyObject *const *o, Py_ssize_t n) {
+    if (n != 13) return slow_path();
+    Views v(o[12]);
+    onnxb_matrix dy{}, x{}, s{}, out[3] = {};
+    onnxb_matrix *outs[3] = {nullptr, nullptr, nullptr};
+    bool want[3];
+    for (int i = 0; i < 3; ++i) want[i] = o[8 + i] != Py_None || PyObject_IsTrue(o[5 + i]) == 1;
+    if (PyErr_Occurred()) { PyErr_Clear(); return slow_path(); }
+    if (!v.matrix(o[0], dy) || !v.matrix(o[1], x) || !v.fine || x.rows < 1 || x.type == ONNXB_INT8 || !(want[0] || want[1] || want[2])) return slow_path();
+    // (without scale the weights' type is another's: the checked path's)
+    if (!v.row(o[2], x.cols, s)) return slow_path();
+    const float *mean = v.vector(o[3], x.rows), *inv_std = v.vector(o[4], x.rows);
+    if (!v.fine || !v.takes({o[8]}, o[11])) return slow_path();
+    for (int i = 1; i < 3; ++i) outs[i] = v.row(o[8 + i], x.cols, out[i]);
+    if (!v.fine) return slow_path();
+    at::Tensor ts[3], wt;
+    if (want[0]) outs[0] = v.result(o[8], x.rows, x.cols, x.type, ts[0], out[0]);
+    for (int i = 1; i < 3; ++i)
+        if (want[i] && !outs[i]) {
+            ts[i] = v.made({x.cols}, s.type == ONNXB_FLOAT ? at::kFloat : s.type == ONNXB_FLOAT16 ? at::kHalf : at::kBFloat16);
+            out[i] = onnxb_matrix{ts[i].data_ptr(), 1, x.cols, x.cols, s.type, 0};
+            outs[i] = &out[i];
+        }
+    size_t ws_bytes;
+    void *ws = v.workspace(o[11], abi.layer_norm_backward_workspace_bytes(&x, outs[1], outs[2]), wt, ws_bytes);
+    if (abi.layer_norm_backward_run(&dy, &x, want[0] ? &s : nullptr, mean, inv_std, outs[0], outs[1], outs[2], ws, ws_bytes, v.stream) != ONNXB_OK)
+        return slow_path();
+    PyObject *got[3];
+    for (int i = 0; i < 3; ++i) {
+        got[i] = want[i] ? result(o[8 + i], ts[i]) : Py_None;
+        if (!want[i]) Py_INCREF(Py_None);
+    }
+    return Py_BuildValue("(NNN)", got[0], got[1], got[2]);
+}
+
 // Address, type, sizes and strides of a tensor, or of those in a tuple or a dict (whose entry "input" is left out); false for anything else
 bool add_state(PyObject *o, std::vector<int64_t> &out) {
     if (THPVariable_CheckExact(o)) {
@@ -573,6 +654,8 @@ PyMethodDef methods[] = {
     {"gated", reinterpret_cast<PyCFunction>(&guarded<py_gated>), METH_FASTCALL, nullptr},
     {"gated_int8", reinterpret_cast<PyCFunction>(&guarded<py_gated_int8>), METH_FASTCALL, nullptr},
     {"gated_backward", reinterpret_cast<PyCFunction>(&guarded<py_gated_backward>), METH_FASTCALL, nullptr},
+    {"layer_norm", reinterpret_cast<PyCFunction>(&guarded<py_layer_norm>), METH_FASTCALL, nullptr},
+    {"layer_norm_backward", reinterpret_cast<PyCFunction>(&guarded<py_layer_norm_backward>), METH_FASTCALL, nullptr},
     {"state", reinterpret_cast<PyCFunction>(&guarded<py_state>), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_onnxb_fast", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
