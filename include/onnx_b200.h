@@ -472,6 +472,75 @@ onnxb_status onnx_layer_normalization_backward_run(const onnxb_matrix *dY, const
                                                    const float *inv_std, const onnxb_matrix *dX, const onnxb_matrix *dScale,
                                                    const onnxb_matrix *dBias, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
+/*
+ * Products of rows that belong to groups, each group with weights of its own: the layers of experts of a language model.  (They stand beside
+ * onnx_gated_run, whose block they compute, and whose weights all rows share.)
+ *
+ * The rows of a group lie one after the other.  `offsets`: 32-bit integers [groups + 1] on the device; group g has rows offsets[g] to offsets[g+1] - 1, and
+ * may have none.  Rows before offsets[0] and from offsets[groups] on belong to no group: they are not read as values, and rows of results there are left
+ * as they were.  The host never reads the offsets, so no call waits for the device, and a captured call is replayed with whatever they hold then.  They
+ * should rise from 0 to the rows; what is outside of that counts as the nearest end, and an offset below the one before it as that.
+ *
+ * onnxb_matrices: `count` views of [rows, cols] each, the weights of one group after the other, `stride` elements apart.  Their order in memory is
+ * free (all groups' first rows may come first), but none of their rows overlap (ERR_SHAPE).  At most 1024 groups, count * rows at most 2^31-1,
+ * and `stride` at most 2^36 (ERR_UNSUPPORTED).  All else is as said above at onnxb_matrix, alignment among it: what TMA cannot address, rows or
+ * groups that do not begin at multiples of 16 bytes, is laid out in the workspace first, weights as a whole.
+ */
+typedef struct {
+    void *data;              /* device (inputs are only read) */
+    int64_t count;           /* groups */
+    int64_t rows, cols;      /* of each */
+    int64_t ld;              /* elements from one row to the next */
+    int64_t stride;          /* elements from one group's first row to the next's */
+    int32_t type;            /* onnxb_type */
+    int32_t reserved;        /* must be 0 */
+} onnxb_matrices;
+
+/*
+ * onnx_grouped_gemm_run - Y[i,:] = W[g] X[i,:] for the rows i of each group g: X [R,K], W groups of [N,K] (a row for each channel), Y [R,N],
+ * all of one type, 16-bit floats.  Sums are in 32 bits, each result is rounded once.
+ */
+size_t onnx_grouped_gemm_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *W);      /* host only */
+onnxb_status onnx_grouped_gemm_run(const onnxb_matrix *X, const onnxb_matrices *W, const int32_t *offsets, const onnxb_matrix *Y, void *workspace,
+                                   size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * onnx_grouped_gated_run - the gated block of onnx_gated_run with weights of the row's group: G[i,:] = Wg[g] X[i,:], U[i,:] = Wu[g] X[i,:],
+ * H = act(G) * U.  G and U: both NULL where they are not kept.
+ */
+size_t onnx_grouped_gated_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu);      /* host only */
+onnxb_status onnx_grouped_gated_run(const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu, const int32_t *offsets, int activation,
+                                    const onnxb_matrix *H, const onnxb_matrix *G, const onnxb_matrix *U, void *workspace, size_t workspace_bytes,
+                                    void *cuda_stream);
+
+/*
+ * onnx_grouped_gemm_backward_run - the gradients of onnx_grouped_gemm_run: dX[i,:] = sum_n dY[i,n] W[g][n,:], dW[g] = sum over the group's rows of
+ * dY[i,:]^T X[i,:] (zeros for a group without rows).  Each may be NULL where it is not wanted (not both); X is not read (and may be NULL) without
+ * dW, nor W without dX.  Sums are in 32 bits, in an order that goes by the sizes and offsets alone; each result is rounded once.
+ */
+size_t onnx_grouped_gemm_backward_workspace_bytes(const onnxb_matrix *dY, const onnxb_matrix *X, const onnxb_matrices *W, const onnxb_matrix *dX,
+                                                  const onnxb_matrices *dW);      /* host only */
+onnxb_status onnx_grouped_gemm_backward_run(const onnxb_matrix *dY, const onnxb_matrix *X, const onnxb_matrices *W, const int32_t *offsets,
+                                            const onnxb_matrix *dX, const onnxb_matrices *dW, void *workspace, size_t workspace_bytes,
+                                            void *cuda_stream);
+
+/*
+ * onnx_grouped_gated_backward_run - the gradients of onnx_grouped_gated_run, from dH and the G and U that it kept:
+ *
+ *   dG = dH * U * act'(G),  dU = dH * act(G)
+ *   dX[i,:] = dG[i,:] Wg[g] + dU[i,:] Wu[g],  dWg[g] = sum over the group's rows of dG[i,:]^T X[i,:],  dWu[g] of dU[i,:]^T X[i,:]
+ *
+ * dX, dWg, dWu: each may be NULL where it is not wanted (not all of them); X is not read without dWg and dWu, Wg and Wu not without dX.  dG and dU
+ * are rounded to the type between the two steps, as the tensor cores take them, for any number of rows: the results' error is 1.4 times that of rounding them
+ * alone, and in float16 a dG or dU above 65504 in magnitude is infinite (see onnx_gated_backward_run).
+ */
+size_t onnx_grouped_gated_backward_workspace_bytes(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu,
+                                                   const onnxb_matrix *dX, const onnxb_matrices *dWg, const onnxb_matrices *dWu);      /* host only */
+onnxb_status onnx_grouped_gated_backward_run(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu,
+                                             const onnxb_matrix *G, const onnxb_matrix *U, const int32_t *offsets, int activation,
+                                             const onnxb_matrix *dX, const onnxb_matrices *dWg, const onnxb_matrices *dWu, void *workspace,
+                                             size_t workspace_bytes, void *cuda_stream);
+
 /* Human-readable name of a status code (static storage, never NULL). */
 const char *onnxb_status_string(onnxb_status status);
 

@@ -38,6 +38,9 @@ EXPORTS = [
     "onnx_quantize_rows_run", "onnx_gemm_int8_workspace_bytes", "onnx_gemm_int8_run", "onnx_gated_workspace_bytes", "onnx_gated_run",
     "onnx_gated_int8_run", "onnx_gated_backward_workspace_bytes", "onnx_gated_backward_run",
     "onnx_layer_normalization_run", "onnx_layer_normalization_backward_workspace_bytes", "onnx_layer_normalization_backward_run",
+    "onnx_grouped_gemm_workspace_bytes", "onnx_grouped_gemm_run", "onnx_grouped_gated_workspace_bytes", "onnx_grouped_gated_run",
+    "onnx_grouped_gemm_backward_workspace_bytes", "onnx_grouped_gemm_backward_run", "onnx_grouped_gated_backward_workspace_bytes",
+    "onnx_grouped_gated_backward_run",
 ]
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
 TYPE_CODES = {"float32": 1, "int8": 3, "float16": 10, "bfloat16": 16}      # ONNX's
@@ -64,6 +67,12 @@ class Matrix(ctypes.Structure):
     """``onnxb_matrix``: a two-dimensional view."""
     _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64),
                 ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class Matrices(ctypes.Structure):
+    """``onnxb_matrices``: a view of each group's weights."""
+    _fields_ = [("data", ctypes.c_void_p), ("count", ctypes.c_int64), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("stride", ctypes.c_int64), ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -180,18 +189,25 @@ def load(build_if_missing: bool = True):
     lib.onnxb_probe_tf32_mma_rate.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_double), vp]
     lib.onnxb_probe_wait_timeout.restype = ctypes.c_int
     lib.onnxb_probe_wait_timeout.argtypes = [ctypes.c_longlong, vp]
-    mp = ctypes.POINTER(Matrix)
+    mp, gp = ctypes.POINTER(Matrix), ctypes.POINTER(Matrices)
     for name, args in (("onnx_quantize_rows_run", [mp, mp, vp, vp]),
                        ("onnx_gemm_int8_run", [mp, vp, mp, vp, vp, ctypes.c_int, mp, vp, sz, vp]),
                        ("onnx_gated_run", [mp, mp, mp, ctypes.c_int, mp, mp, mp, vp, sz, vp]),
                        ("onnx_gated_int8_run", [mp, vp, mp, vp, mp, vp, ctypes.c_int, mp, vp, sz, vp]),
                        ("onnx_gated_backward_run", [mp] * 6 + [ctypes.c_int] + [mp] * 3 + [vp, sz, vp]),
                        ("onnx_layer_normalization_run", [mp] * 3 + [ctypes.c_float, mp, vp, vp, vp]),
-                       ("onnx_layer_normalization_backward_run", [mp] * 3 + [vp, vp] + [mp] * 3 + [vp, sz, vp])):
+                       ("onnx_layer_normalization_backward_run", [mp] * 3 + [vp, vp] + [mp] * 3 + [vp, sz, vp]),
+                       ("onnx_grouped_gemm_run", [mp, gp, vp, mp, vp, sz, vp]),
+                       ("onnx_grouped_gated_run", [mp, gp, gp, vp, ctypes.c_int, mp, mp, mp, vp, sz, vp]),
+                       ("onnx_grouped_gemm_backward_run", [mp, mp, gp, vp, mp, gp, vp, sz, vp]),
+                       ("onnx_grouped_gated_backward_run", [mp, mp, gp, gp, mp, mp, vp, ctypes.c_int, mp, gp, gp, vp, sz, vp])):
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = args
     for name, args in (("onnx_gemm_int8_workspace_bytes", [mp, mp]), ("onnx_gated_workspace_bytes", [mp] * 3),
-                       ("onnx_gated_backward_workspace_bytes", [mp] * 7), ("onnx_layer_normalization_backward_workspace_bytes", [mp] * 3)):
+                       ("onnx_gated_backward_workspace_bytes", [mp] * 7), ("onnx_layer_normalization_backward_workspace_bytes", [mp] * 3),
+                       ("onnx_grouped_gemm_workspace_bytes", [mp, gp]), ("onnx_grouped_gated_workspace_bytes", [mp, gp, gp]),
+                       ("onnx_grouped_gemm_backward_workspace_bytes", [mp, mp, gp, mp, gp]),
+                       ("onnx_grouped_gated_backward_workspace_bytes", [mp, mp, gp, gp, mp, gp, gp])):
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = args
     _lib = lib
@@ -641,6 +657,29 @@ class _Views:
         if t is not None:
             self.matrix(t, name, types, like)
 
+    def groups(self, t, name, like):
+        """Each group's weights, of ``like``'s type."""
+        if t is None:
+            raise OnnxB200Error(1, f"{name} is None")
+        self._on_device(t, name)
+        if t.dtype != like.dtype:
+            raise TypeError(f"{name} must be {' or '.join(_HALVES)}, all of one type")
+        if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+            raise TypeError(f"{name} must have three dimensions, the elements of a row one right after the other")
+        count, rows, cols = t.shape
+        ld = t.stride(1) if rows > 1 else cols
+        return Matrices(t.data_ptr() or None, count, rows, cols, ld, t.stride(0) if count > 1 else rows * ld, TYPE_CODES[str(t.dtype)[6:]], 0)
+
+    def offsets(self, t, groups):
+        if t is None:
+            raise OnnxB200Error(1, "offsets is None")
+        self._on_device(t, "offsets")
+        if str(t.dtype) != "torch.int32" or t.dim() != 1 or not t.is_contiguous():
+            raise TypeError("offsets must be contiguous int32 of one dimension")
+        if t.numel() != groups + 1:
+            raise OnnxB200Error(3, f"{self.where}: offsets has {t.numel()} values, not {groups + 1}")
+        return ctypes.c_void_p(t.data_ptr())
+
     def row(self, t, name, types, size, like=None):
         """A vector of weights, as a matrix of one row."""
         if t is None:
@@ -898,3 +937,129 @@ def onnx_layer_normalization_backward(dY, X, scale, mean, inv_std, *, wanted=(Tr
     held, ws, ws_len = v.workspace(workspace, lib.onnx_layer_normalization_backward_workspace_bytes(x, _ref(ds), _ref(db)))
     v.call(lib.onnx_layer_normalization_backward_run, dy, x, _ref(s) if want[0] else None, m, r, _ref(dx), _ref(ds), _ref(db), ws, ws_len)
     return dX, dScale, dB
+
+
+# --------------------------------------------------------------------- products whose weights go by the row's group (expert)
+def _new_groups(v, w, kind):
+    """Weights' gradients: of all groups, one after the other."""
+    return _new((w.count, w.rows, w.cols), v.device, v.stream, kind)
+
+
+def onnx_grouped_gemm(X, W, offsets, *, Y=None, workspace=None, stream=None):
+    """``onnx_grouped_gemm_run``: Y[i] = W[g] X[i] for the rows i of each group g, offsets[g] to offsets[g + 1] - 1.  X [R,K], W [groups,N,K], all float16 or
+    all bfloat16; offsets int32 [groups + 1] on the device, which the host never reads.  Rows of no group are left as they were (in a Y made
+    here: unspecified)."""
+    y = (_fast_mod or _fast()).grouped_gemm(X, W, offsets, Y, workspace, stream)
+    if y is not None:
+        return y
+    lib = load()
+    v = _Views("onnx_grouped_gemm", stream)
+    x, w = v.matrix(X, "X", _HALVES), v.groups(W, "W", X)
+    at = v.offsets(offsets, w.count)
+    v.given(Y, "Y", _HALVES, X)
+    v.given_workspace(workspace)
+    Y = v.new(x.rows, w.rows, str(X.dtype)[6:]) if Y is None else Y
+    y = v.matrix(Y, "Y", _HALVES, X)
+    held, ws, ws_len = v.workspace(workspace, lib.onnx_grouped_gemm_workspace_bytes(x, w))
+    v.call(lib.onnx_grouped_gemm_run, x, w, at, y, ws, ws_len)
+    return Y
+
+
+def onnx_grouped_gated(X, Wg, Wu, offsets, *, activation="silu", save=False, H=None, G=None, U=None, workspace=None, stream=None):
+    """``onnx_grouped_gated_run``: ``onnx_gated`` with weights [groups,F,K] of the row's group (see ``onnx_grouped_gemm``): H, or (H, G, U) with the two
+    projections where ``save`` is true or a G or a U is given, which ``onnx_grouped_gated_backward`` takes."""
+    h = (_fast_mod or _fast()).grouped_gated(X, Wg, Wu, offsets, activation, save, H, G, U, workspace, stream)
+    if h is not None:
+        return h
+    lib = load()
+    v = _Views("onnx_grouped_gated", stream)
+    x, wg, wu = v.matrix(X, "X", _HALVES), v.groups(Wg, "Wg", X), v.groups(Wu, "Wu", X)
+    at = v.offsets(offsets, wg.count)
+    save = save or G is not None or U is not None
+    for result, name in ((H, "H"), (G, "G"), (U, "U")):
+        v.given(result, name, _HALVES, X)
+    v.given_workspace(workspace)
+    activation = _activation(activation)
+    kind = str(X.dtype)[6:]
+    H = v.new(x.rows, wg.rows, kind) if H is None else H
+    if save:
+        G = v.new(x.rows, wg.rows, kind) if G is None else G
+        U = v.new(x.rows, wg.rows, kind) if U is None else U
+    h = v.matrix(H, "H", _HALVES, X)
+    g, u = (v.matrix(G, "G", _HALVES, X), v.matrix(U, "U", _HALVES, X)) if save else (None, None)
+    held, ws, ws_len = v.workspace(workspace, lib.onnx_grouped_gated_workspace_bytes(x, wg, wu))
+    v.call(lib.onnx_grouped_gated_run, x, wg, wu, at, activation, h, _ref(g), _ref(u), ws, ws_len)
+    return (H, G, U) if save else H
+
+
+def onnx_grouped_gemm_backward(dY, X, W, offsets, *, wanted=(True, True), dX=None, dW=None, workspace=None, stream=None):
+    """``onnx_grouped_gemm_backward_run``: (dX, dW) of ``onnx_grouped_gemm``.  ``wanted``: which of them (None in the place of the other; X is not needed
+    for dX, nor W for dW if that is given).  dW is zeros for a group without rows; dX's rows of no group are left as they were."""
+    wanted = tuple(wanted)
+    if len(wanted) != 2:
+        raise ValueError("wanted: a truth value for each of dX and dW")
+    done = (_fast_mod or _fast()).grouped_gemm_backward(dY, X, W, offsets, *wanted, dX, dW, workspace, stream)
+    if done is not None:
+        return done
+    lib = load()
+    v = _Views("onnx_grouped_gemm_backward", stream)
+    dy = v.matrix(dY, "dY", _HALVES)
+    want = [w or given is not None for w, given in zip(wanted, (dX, dW))]
+    if not any(want):
+        raise OnnxB200Error(1, "onnx_grouped_gemm_backward: no gradient is wanted")
+    x = v.matrix(X, "X", _HALVES, dY) if want[1] else None
+    w = v.groups(W, "W", dY) if want[0] or dW is None else None
+    like = w if w is not None else v.groups(dW, "dW", dY)
+    at = v.offsets(offsets, like.count)
+    v.given(dX, "dX", _HALVES, dY)
+    if dW is not None:
+        v.groups(dW, "dW", dY)
+    v.given_workspace(workspace)
+    kind = str(dY.dtype)[6:]
+    dX = v.new(dy.rows, like.cols, kind) if want[0] and dX is None else dX
+    dW = _new_groups(v, like, kind) if want[1] and dW is None else dW
+    dx = v.matrix(dX, "dX", _HALVES, dY) if want[0] else None
+    dw = v.groups(dW, "dW", dY) if want[1] else None
+    w = w if want[0] else None
+    held, ws, ws_len = v.workspace(workspace, lib.onnx_grouped_gemm_backward_workspace_bytes(_ref(dy), _ref(x), _ref(w), _ref(dx), _ref(dw)))
+    v.call(lib.onnx_grouped_gemm_backward_run, dy, _ref(x), _ref(w), at, _ref(dx), _ref(dw), ws, ws_len)
+    return dX, dW
+
+
+def onnx_grouped_gated_backward(dH, X, Wg, Wu, G, U, offsets, *, activation="silu", wanted=(True, True, True), dX=None, dWg=None, dWu=None,
+                                workspace=None, stream=None):
+    """``onnx_grouped_gated_backward_run``: (dX, dWg, dWu) of ``onnx_grouped_gated``, from its G and U.  ``wanted`` as for ``onnx_gated_backward``; both weights
+    are asked for in any case but where all gradients of weights that are wanted are given (their sizes say the groups and the width)."""
+    wanted = tuple(wanted)
+    if len(wanted) != 3:
+        raise ValueError("wanted: a truth value for each of dX, dWg and dWu")
+    done = (_fast_mod or _fast()).grouped_gated_backward(dH, X, Wg, Wu, G, U, offsets, activation, *wanted, dX, dWg, dWu, workspace, stream)
+    if done is not None:
+        return done
+    lib = load()
+    v = _Views("onnx_grouped_gated_backward", stream)
+    dh, g, u = v.matrix(dH, "dH", _HALVES), v.matrix(G, "G", _HALVES, dH), v.matrix(U, "U", _HALVES, dH)
+    kind = str(dH.dtype)[6:]
+    want = [w or given is not None for w, given in zip(wanted, (dX, dWg, dWu))]
+    if not any(want):
+        raise OnnxB200Error(1, "onnx_grouped_gated_backward: no gradient is wanted")
+    x = v.matrix(X, "X", _HALVES, dH) if want[1] or want[2] else None
+    needed = want[0] or any(w and given is None for w, given in zip(want[1:], (dWg, dWu)))
+    wg, wu = (v.groups(Wg, "Wg", dH), v.groups(Wu, "Wu", dH)) if needed else (None, None)
+    given = [None if t is None else v.groups(t, name, dH) for t, name in ((dWg, "dWg"), (dWu, "dWu"))]
+    like = wg if wg is not None else given[0] or given[1]
+    at = v.offsets(offsets, like.count)
+    v.given(dX, "dX", _HALVES, dH)
+    v.given_workspace(workspace)
+    activation = _activation(activation)
+    dX = v.new(dh.rows, like.cols, kind) if want[0] and dX is None else dX
+    dWg = _new_groups(v, like, kind) if want[1] and dWg is None else dWg
+    dWu = _new_groups(v, like, kind) if want[2] and dWu is None else dWu
+    dx = v.matrix(dX, "dX", _HALVES, dH) if want[0] else None
+    dwg = v.groups(dWg, "dWg", dH) if want[1] else None
+    dwu = v.groups(dWu, "dWu", dH) if want[2] else None
+    wg, wu = (wg, wu) if want[0] else (None, None)
+    held, ws, ws_len = v.workspace(workspace, lib.onnx_grouped_gated_backward_workspace_bytes(
+        _ref(dh), _ref(x), _ref(wg), _ref(wu), _ref(dx), _ref(dwg), _ref(dwu)))
+    v.call(lib.onnx_grouped_gated_backward_run, dh, _ref(x), _ref(wg), _ref(wu), g, u, at, activation, _ref(dx), _ref(dwg), _ref(dwu), ws, ws_len)
+    return dX, dWg, dWu

@@ -46,6 +46,14 @@ struct Abi {
     decltype(&onnx_layer_normalization_run) layer_norm_run;
     decltype(&onnx_layer_normalization_backward_workspace_bytes) layer_norm_backward_workspace_bytes;
     decltype(&onnx_layer_normalization_backward_run) layer_norm_backward_run;
+    decltype(&onnx_grouped_gemm_workspace_bytes) grouped_gemm_workspace_bytes;
+    decltype(&onnx_grouped_gemm_run) grouped_gemm_run;
+    decltype(&onnx_grouped_gated_workspace_bytes) grouped_gated_workspace_bytes;
+    decltype(&onnx_grouped_gated_run) grouped_gated_run;
+    decltype(&onnx_grouped_gemm_backward_workspace_bytes) grouped_gemm_backward_workspace_bytes;
+    decltype(&onnx_grouped_gemm_backward_run) grouped_gemm_backward_run;
+    decltype(&onnx_grouped_gated_backward_workspace_bytes) grouped_gated_backward_workspace_bytes;
+    decltype(&onnx_grouped_gated_backward_run) grouped_gated_backward_run;
 } abi;
 
 struct Plan {                    // what a convolution descriptor resolved to
@@ -151,6 +159,14 @@ PyObject *py_bind(PyObject *, PyObject *arg) {
     get(abi.layer_norm_run, "onnx_layer_normalization_run");
     get(abi.layer_norm_backward_workspace_bytes, "onnx_layer_normalization_backward_workspace_bytes");
     get(abi.layer_norm_backward_run, "onnx_layer_normalization_backward_run");
+    get(abi.grouped_gemm_workspace_bytes, "onnx_grouped_gemm_workspace_bytes");
+    get(abi.grouped_gemm_run, "onnx_grouped_gemm_run");
+    get(abi.grouped_gated_workspace_bytes, "onnx_grouped_gated_workspace_bytes");
+    get(abi.grouped_gated_run, "onnx_grouped_gated_run");
+    get(abi.grouped_gemm_backward_workspace_bytes, "onnx_grouped_gemm_backward_workspace_bytes");
+    get(abi.grouped_gemm_backward_run, "onnx_grouped_gemm_backward_run");
+    get(abi.grouped_gated_backward_workspace_bytes, "onnx_grouped_gated_backward_workspace_bytes");
+    get(abi.grouped_gated_backward_run, "onnx_grouped_gated_backward_run");
     if (!ok) { PyErr_SetString(PyExc_OSError, "a symbol of the C ABI is missing"); return nullptr; }
     Py_RETURN_NONE;
 }
@@ -343,6 +359,34 @@ struct Views {
         if (o == Py_None) return nullptr;
         const at::Tensor *t = on_device(o);
         if (t) take(*t, m);
+        return &m;
+    }
+    // each group's weights, 16-bit floats, or nullptr for None
+    onnxb_matrices *groups(PyObject *o, onnxb_matrices &m) {
+        if (o == Py_None) return nullptr;
+        const at::Tensor *t = on_device(o);
+        if (!t || t->dim() != 3 || (t->size(2) > 1 && t->stride(2) != 1)) { fine = false; return &m; }
+        m.type = code_of(t->scalar_type());
+        if (m.type != ONNXB_FLOAT16 && m.type != ONNXB_BFLOAT16) { fine = false; return &m; }
+        m.data = t->data_ptr();
+        m.count = t->size(0);
+        m.rows = t->size(1);
+        m.cols = t->size(2);
+        m.ld = m.rows > 1 ? t->stride(1) : m.cols;
+        m.stride = m.count > 1 ? t->stride(0) : m.rows * m.ld;
+        m.reserved = 0;
+        return &m;
+    }
+    const int32_t *offsets(PyObject *o, int64_t groups) {
+        const at::Tensor *t = on_device(o);
+        if (!t || t->scalar_type() != at::kInt || t->dim() != 1 || !t->is_contiguous() || t->numel() != groups + 1) { fine = false; return nullptr; }
+        return static_cast<const int32_t *>(t->data_ptr());
+    }
+    // gradients of weights: the caller's, or made here
+    onnxb_matrices *result(PyObject *given, const onnxb_matrices &like, at::Tensor &t, onnxb_matrices &m) {
+        if (given != Py_None) return groups(given, m);
+        t = made({like.count, like.rows, like.cols}, like.type == ONNXB_FLOAT16 ? at::kHalf : at::kBFloat16);
+        m = onnxb_matrices{t.data_ptr(), like.count, like.rows, like.cols, like.cols, like.rows * like.cols, like.type, 0};
         return &m;
     }
     // a vector of floats of any type as a matrix of one row, or nullptr for None
@@ -598,6 +642,116 @@ PyObject *py_layer_norm_backward(PyObject *, PyObject *const *o, Py_ssize_t n) {
     return Py_BuildValue("(NNN)", got[0], got[1], got[2]);
 }
 
+// grouped_gemm(X, W, offsets, Y, workspace, stream)
+PyObject *py_grouped_gemm(PyObject *, PyObject *const *o, Py_ssize_t n) {
+    if (n != 6) return slow_path();
+    Views v(o[5]);
+    onnxb_matrix x{}, y{};
+    onnxb_matrices w{};
+    if (!v.matrix(o[0], x) || !v.groups(o[1], w) || !v.fine || x.rows < 1 || x.type != w.type) return slow_path();
+    const int32_t *offsets = v.offsets(o[2], w.count);
+    if (!v.fine || !v.takes({o[3]}, o[4])) return slow_path();
+    at::Tensor yt, wt;
+    size_t ws_bytes;
+    v.result(o[3], x.rows, w.rows, x.type, yt, y);
+    void *ws = v.workspace(o[4], abi.grouped_gemm_workspace_bytes(&x, &w), wt, ws_bytes);
+    if (abi.grouped_gemm_run(&x, &w, offsets, &y, ws, ws_bytes, v.stream) != ONNXB_OK) return slow_path();
+    return result(o[3], yt);
+}
+
+// grouped_gated(X, Wg, Wu, offsets, activation, save, H, G, U, workspace, stream) -> H, or (H, G, U)
+PyObject *py_grouped_gated(PyObject *, PyObject *const *o, Py_ssize_t n) {
+    if (n != 11) return slow_path();
+    Views v(o[10]);
+    onnxb_matrix x{}, h{}, g{}, u{};
+    onnxb_matrices wg{}, wu{};
+    if (!v.matrix(o[0], x) || !v.groups(o[1], wg) || !v.groups(o[2], wu) || !v.fine || x.rows < 1 || x.type != wg.type) return slow_path();
+    const int32_t *offsets = v.offsets(o[3], wg.count);
+    const int activation = activation_of(o[4]), asked = PyObject_IsTrue(o[5]);
+    if (PyErr_Occurred()) { PyErr_Clear(); return slow_path(); }
+    if (activation < 0 || !v.fine || !v.takes({o[6], o[7], o[8]}, o[9])) return slow_path();
+    const bool save = asked || o[7] != Py_None || o[8] != Py_None;
+    at::Tensor ht, gt, ut, wt;
+    size_t ws_bytes;
+    v.result(o[6], x.rows, wg.rows, x.type, ht, h);
+    if (save) {
+        v.result(o[7], x.rows, wg.rows, x.type, gt, g);
+        v.result(o[8], x.rows, wg.rows, x.type, ut, u);
+    }
+    void *ws = v.workspace(o[9], abi.grouped_gated_workspace_bytes(&x, &wg, &wu), wt, ws_bytes);
+    if (abi.grouped_gated_run(&x, &wg, &wu, offsets, activation, &h, save ? &g : nullptr, save ? &u : nullptr, ws, ws_bytes, v.stream) != ONNXB_OK)
+        return slow_path();
+    if (!save) return result(o[6], ht);
+    return Py_BuildValue("(NNN)", result(o[6], ht), result(o[7], gt), result(o[8], ut));
+}
+
+// grouped_gemm_backward(dY, X, W, offsets, dX wanted, dW wanted, dX, dW, workspace, stream) -> (dX, dW)
+PyObject *py_grouped_gemm_backward(PyObject *, PyObject *const *o, Py_ssize_t n) {
+    if (n != 10) return slow_path();
+    Views v(o[9]);
+    onnxb_matrix dy{}, x{}, dx{};
+    onnxb_matrices w{}, dw{};
+    bool want[2];
+    for (int i = 0; i < 2; ++i) want[i] = o[6 + i] != Py_None || PyObject_IsTrue(o[4 + i]) == 1;
+    if (PyErr_Occurred()) { PyErr_Clear(); return slow_path(); }
+    // (without W its sizes are dW's: the checked path's)
+    if (!v.matrix(o[0], dy) || !v.groups(o[2], w) || !v.fine || dy.rows < 1 || dy.type != w.type || !(want[0] || want[1])) return slow_path();
+    if (want[1] && !v.matrix(o[1], x)) return slow_path();
+    const int32_t *offsets = v.offsets(o[3], w.count);
+    if (!v.fine || !v.takes({o[6]}, o[8])) return slow_path();
+    v.groups(o[7], dw);
+    if (!v.fine) return slow_path();
+    at::Tensor xt, dt, wt;
+    size_t ws_bytes;
+    onnxb_matrix *to_x = want[0] ? v.result(o[6], dy.rows, w.cols, dy.type, xt, dx) : nullptr;
+    onnxb_matrices *to_w = want[1] ? v.result(o[7], w, dt, dw) : nullptr;
+    const onnxb_matrix *from = want[1] ? &x : nullptr;
+    const onnxb_matrices *weights = want[0] ? &w : nullptr;
+    void *ws = v.workspace(o[8], abi.grouped_gemm_backward_workspace_bytes(&dy, from, weights, to_x, to_w), wt, ws_bytes);
+    if (abi.grouped_gemm_backward_run(&dy, from, weights, offsets, to_x, to_w, ws, ws_bytes, v.stream) != ONNXB_OK) return slow_path();
+    PyObject *none = Py_None;
+    if (!want[0] || !want[1]) Py_INCREF(none);
+    return Py_BuildValue("(NN)", want[0] ? result(o[6], xt) : none, want[1] ? result(o[7], dt) : none);
+}
+
+// grouped_gated_backward(dH, X, Wg, Wu, G, U, offsets, activation, dX wanted, dWg wanted, dWu wanted, dX, dWg, dWu, workspace, stream)
+// -> (dX, dWg, dWu)
+PyObject *py_grouped_gated_backward(PyObject *, PyObject *const *o, Py_ssize_t n) {
+    if (n != 16) return slow_path();
+    Views v(o[15]);
+    onnxb_matrix dh{}, x{}, g{}, u{}, dx{};
+    onnxb_matrices w[2] = {}, d[2] = {};
+    const int activation = activation_of(o[7]);
+    bool want[3];
+    for (int i = 0; i < 3; ++i) want[i] = o[11 + i] != Py_None || PyObject_IsTrue(o[8 + i]) == 1;
+    if (PyErr_Occurred()) { PyErr_Clear(); return slow_path(); }
+    if (!v.matrix(o[0], dh) || !v.groups(o[2], w[0]) || !v.groups(o[3], w[1]) || !v.matrix(o[4], g) || !v.matrix(o[5], u)) return slow_path();
+    if (!v.fine || dh.rows < 1 || dh.type != w[0].type || activation < 0 || !(want[0] || want[1] || want[2])) return slow_path();
+    const bool of_weights = want[1] || want[2];
+    if (of_weights && !v.matrix(o[1], x)) return slow_path();
+    const int32_t *offsets = v.offsets(o[6], w[0].count);
+    if (!v.fine || !v.takes({o[11]}, o[14])) return slow_path();
+    for (int i = 0; i < 2; ++i) v.groups(o[12 + i], d[i]);
+    if (!v.fine) return slow_path();
+    at::Tensor ts[3], wt;
+    onnxb_matrices *to_w[2] = {nullptr, nullptr};
+    onnxb_matrix *to_x = want[0] ? v.result(o[11], dh.rows, w[0].cols, dh.type, ts[0], dx) : nullptr;
+    for (int i = 0; i < 2; ++i)
+        if (want[1 + i]) to_w[i] = v.result(o[12 + i], w[0], ts[1 + i], d[i]);
+    const onnxb_matrix *from = of_weights ? &x : nullptr;
+    const onnxb_matrices *wg = want[0] ? &w[0] : nullptr, *wu = want[0] ? &w[1] : nullptr;
+    size_t ws_bytes;
+    void *ws = v.workspace(o[14], abi.grouped_gated_backward_workspace_bytes(&dh, from, wg, wu, to_x, to_w[0], to_w[1]), wt, ws_bytes);
+    if (abi.grouped_gated_backward_run(&dh, from, wg, wu, &g, &u, offsets, activation, to_x, to_w[0], to_w[1], ws, ws_bytes, v.stream) != ONNXB_OK)
+        return slow_path();
+    PyObject *got[3];
+    for (int i = 0; i < 3; ++i) {
+        got[i] = want[i] ? result(o[11 + i], ts[i]) : Py_None;
+        if (!want[i]) Py_INCREF(Py_None);
+    }
+    return Py_BuildValue("(NNN)", got[0], got[1], got[2]);
+}
+
 // Address, type, sizes and strides of a tensor, or of those in a tuple or a dict (whose entry "input" is left out); false for anything else
 bool add_state(PyObject *o, std::vector<int64_t> &out) {
     if (THPVariable_CheckExact(o)) {
@@ -656,6 +810,10 @@ PyMethodDef methods[] = {
     {"gated_backward", reinterpret_cast<PyCFunction>(&guarded<py_gated_backward>), METH_FASTCALL, nullptr},
     {"layer_norm", reinterpret_cast<PyCFunction>(&guarded<py_layer_norm>), METH_FASTCALL, nullptr},
     {"layer_norm_backward", reinterpret_cast<PyCFunction>(&guarded<py_layer_norm_backward>), METH_FASTCALL, nullptr},
+    {"grouped_gemm", reinterpret_cast<PyCFunction>(&guarded<py_grouped_gemm>), METH_FASTCALL, nullptr},
+    {"grouped_gated", reinterpret_cast<PyCFunction>(&guarded<py_grouped_gated>), METH_FASTCALL, nullptr},
+    {"grouped_gemm_backward", reinterpret_cast<PyCFunction>(&guarded<py_grouped_gemm_backward>), METH_FASTCALL, nullptr},
+    {"grouped_gated_backward", reinterpret_cast<PyCFunction>(&guarded<py_grouped_gated_backward>), METH_FASTCALL, nullptr},
     {"state", reinterpret_cast<PyCFunction>(&guarded<py_state>), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_onnxb_fast", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
