@@ -2,15 +2,20 @@
 // onnx_grouped_gated_run, and the products of their gradients.
 //
 // The pipeline is that of tc_dense.cu: a persistent CTA (or a pair of two on one tile) per SM,
-//   warp 0    TMA producer, a ring of stages of 64 terms of the reduction, in boxes of 64 terms by 64 rows (8 KB) that are one lane's copy each;
+//   warp 0    TMA producer, a ring of stages of 64 terms of the reduction;
 //   warp 1    one thread issues tcgen05.mma kind::f16 into one of two TMEM accumulators;
-//   warps 2-9 epilogue: tcgen05.ld, the mathematics, 32 x 64 blocks laid out in shared memory and stored by whole 128-byte rows;
+//   warps 2-9 epilogue: tcgen05.ld, the mathematics, stores;
 //   warp 10   clears what a stage holds of the next group's rows (below).
 // What is its own:
-//   - Where the groups lie only the device knows: every CTA reads the offsets, makes them rise, and counts the groups' row tiles, in shared
-//     memory; a tile's number is looked up there.  The grid is what the host knows to be enough, at most one CTA an SM, and the call waits for nothing.
-//   - A tile has rows of one group.  Its copies may bring the next group's rows too: they are rows of the accumulator that nobody stores.  Weights
-//     are three-dimensional tensors to TMA, so that what lies behind a group's last channel is zeros.
+//   - Where the groups lie only the device knows: every CTA reads the offsets, makes them rise, and counts the groups' tiles, in shared memory; a tile's
+//     number is looked up there.  The grid is what the host knows to be enough, at most one CTA an SM, and the call waits for nothing.
+//   - Products of rows (the forward ones and dX) have the weights as the instruction's 128 or 256 rows and the group's rows as its columns, of which there
+//     may be any multiple of 16 up to 256: a group's last tile then costs what it has, where 256 rows a tile would be half empty in groups of some
+//     hundred.  A group's tiles are made as alike as multiples of 16 allow.  The accumulator is the result's transpose: a lane has a channel of 32 rows, and
+//     trades every other one with its neighbour, so that both store two channels of 16 rows, 64 bytes of each row a warp.  The gated block has two such
+//     products of the same rows, of up to 128, side by side in the accumulator.
+//   - A copy of a group's last rows may bring the next group's too: they are columns of the accumulator that nobody stores.  Weights are three-dimensional
+//     tensors to TMA, so that what lies behind a group's last channel is zeros.
 //   - The gradients of the weights sum over a group's rows, which end inside a stage.  There, rows of the next group would be terms of the sum, and if
 //     they are not finite zeros on the other side would not help: warp 10 clears them on both sides, up to the next multiple of 16 rows, and the
 //     stage's instructions end there.  Such a stage's copies complete on a barrier of this CTA's own, since of a pair each CTA clears what it holds.
@@ -44,7 +49,9 @@ constexpr int kMaxStages = 24;
 constexpr int kThreads = 352;
 constexpr int kEpiWarps = 8;
 constexpr int kBlockBytes = 32 * kRowBytes;        // what an epilogue warp lays out: 32 rows of 128 bytes
-constexpr int kStagingBytes = kEpiWarps * kBlockBytes;
+constexpr int kStagingBytes = kEpiWarps * kBlockBytes;         // (of gradients of weights alone)
+constexpr int kABytes = kBM * kRowBytes;           // of one of the weights, or of a CTA's rows, in a stage
+constexpr int kGatedAt = 128;                      // where the second product's columns are in an accumulator
 constexpr int kBarrierBytes = 1024;
 constexpr int kSmemLimit = 232448;
 static_assert((4 * kMaxStages + 5) * 8 <= kBarrierBytes, "barriers");
@@ -53,47 +60,55 @@ struct Params {
     int rows, groups;
     const int *offsets;
     int channels, width;
-    int N;                         // columns of the output (of both products of the gradients: the width)
-    int BN, out_cols;              // columns of an accumulator; of the output per tile (half of them for the gated block)
-    int tiles_n, band;
+    int most_rows;                 // of a tile of rows: columns of an accumulator (of the gated block: of one of its two)
+    int tiles_n, band;             // of the results' columns, 128 or 256 of them a tile
     int num_kb;                    // stages of the reduction; of one term of dX's
-    int a_rows, b_box;             // rows of A in a stage; of a box of B
+    int b_box;                     // rows of a small copy of rows
     int terms, with_x;             // kGroupedGrad: terms; dX is wanted
-    int w_tiles_m, w_total;        // row tiles of one weights' gradient; tiles of all of them
+    int BN;                        // columns of a tile of the weights' gradients
+    int w_tiles_m, w_tiles_n, w_total;     // row and column tiles of one weights' gradient; tiles of all of them
     int w_first, w_count;          // the first that is wanted; how many are
     int num_stages;
-    uint32_t idesc, idesc_x, stage_bytes, a_bytes;
+    uint32_t idesc_x, idesc_w;     // (of tiles of rows without their columns)
+    uint32_t stage_bytes, b_at;    // where B begins in a stage
     int bf16, activation, outs;    // outs: results of a tile (the gated block: H alone, or H, G and U)
     void *Y[3];
     long long y_ld[3];
-    int y_wide[3];                 // rows begin at multiples of 16 bytes
+    int y_pairs[3];                // rows begin at multiples of 4 bytes
     void *D[2];
     long long d_ld[2], d_stride[2];
-    int d_wide[2];
+    int d_wide[2];                 // rows begin at multiples of 16 bytes
     unsigned int *err;
 };
 
 struct Maps {
-    CUtensorMap A[2], W[2], X;
+    CUtensorMap W[2];              // weights, boxes of 128 channels (for dX of 64)
+    CUtensorMap R[2], R_small[2];  // rows (X, or dY or dG and dU), boxes of 128 and of b_box rows
+    CUtensorMap D[2], X;           // rows as terms of the weights' gradients, boxes of 64
 };
 
-// The groups, in shared memory: the first row of each and behind the last, and how many row tiles the groups before each have
+// The groups, in shared memory: the first row of each and behind the last, and how many tiles of rows the groups before each have
 struct Groups {
     int *first, *tiles;
 };
+// Rows of a tile of a group that has so many: as alike as multiples of 16 allow
+__device__ __forceinline__ int rows_per_tile(int rows, int most) {
+    const int tiles = (rows + most - 1) / most;
+    return tiles > 0 ? ((rows + tiles - 1) / tiles + 15) / 16 * 16 : 16;
+}
 struct TileAt {
     int g, tm, tn, z;          // z: which of the weights' gradients
-    int row0, row_end;         // the tile's first row, and where its group ends (gradients of weights: the group's first row)
+    int row0, rows;            // the tile's rows (gradients of weights: the group's)
     int kb;                    // stages
     bool x;                    // of rows: the forward products and dX
 };
-// Of `tiles_m` by tiles_n tiles the r-th, in bands of `band` row tiles, a band's columns one after the other: the tiles in flight share operands in L2
-__device__ __forceinline__ void place(const Params &p, int tiles_m, int r, TileAt &at) {
-    const int b = r / (p.band * p.tiles_n), rr = r - b * p.band * p.tiles_n, rows = min(p.band, tiles_m - b * p.band);
+// Of `tiles_m` by `tiles_n` tiles the r-th, in bands of `band` row tiles, a band's columns one after the other: the tiles in flight share operands in L2
+__device__ __forceinline__ void place(int band, int tiles_m, int tiles_n, int r, TileAt &at) {
+    const int b = r / (band * tiles_n), rr = r - b * band * tiles_n, rows = min(band, tiles_m - b * band);
     at.tn = rr / rows;
-    at.tm = b * p.band + rr - at.tn * rows;
+    at.tm = b * band + rr - at.tn * rows;
 }
-template <int kCtas, int kMode>
+template <int kMode>
 __device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t, TileAt &at) {
     constexpr bool kGrad = kMode == kGroupedGrad;
     const int of_rows = !kGrad || p.with_x ? s.tiles[p.groups] * p.tiles_n : 0;
@@ -108,22 +123,23 @@ __device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t,
             else hi = mid;
         }
         at.g = lo;
-        place(p, s.tiles[lo + 1] - s.tiles[lo], t - s.tiles[lo] * p.tiles_n, at);
-        at.row0 = s.first[lo] + at.tm * kBM * kCtas;
-        at.row_end = s.first[lo + 1];
+        place(p.band, s.tiles[lo + 1] - s.tiles[lo], p.tiles_n, t - s.tiles[lo] * p.tiles_n, at);
+        const int all = s.first[lo + 1] - s.first[lo], per = rows_per_tile(all, p.most_rows);
+        at.row0 = s.first[lo] + at.tm * per;
+        at.rows = min(per, all - at.tm * per);
         at.kb = kGrad ? p.terms * p.num_kb : p.num_kb;
         return true;
     }
     t -= of_rows;
     if (!kGrad || t >= p.w_total) return false;
-    const int per = p.w_tiles_m * p.tiles_n;
+    const int per = p.w_tiles_m * p.w_tiles_n;
     at.g = t / (per * p.w_count);
     const int r = t - at.g * per * p.w_count;
     at.z = r / per;
-    place(p, p.w_tiles_m, r - at.z * per, at);
+    place(p.band, p.w_tiles_m, p.w_tiles_n, r - at.z * per, at);
     at.row0 = s.first[at.g];
-    at.row_end = s.first[at.g + 1];
-    at.kb = (at.row_end - at.row0 + kTerms - 1) / kTerms;
+    at.rows = s.first[at.g + 1] - at.row0;
+    at.kb = (at.rows + kTerms - 1) / kTerms;
     return true;
 }
 
@@ -147,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t *stages = smem;
     uint8_t *staging = smem + (size_t)p.num_stages * p.stage_bytes;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + kStagingBytes);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + (kGrad ? kStagingBytes : 0));
     uint64_t *full = bars, *empty = bars + kMaxStages, *tail_full = bars + 2 * kMaxStages, *cleared = bars + 3 * kMaxStages;
     uint64_t *tmem_full = bars + 4 * kMaxStages, *tmem_empty = tmem_full + 2;
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(tmem_empty + 2);
@@ -172,7 +188,6 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             mbar_init(&tmem_empty[a], kEpiWarps * kCtas);
         }
         mbar_fence_init();
-        prefetch_tmap(&maps.A[0]);
         prefetch_tmap(kGrad && !p.with_x ? &maps.X : &maps.W[0]);
         if (kGated) prefetch_tmap(&maps.W[1]);
     }
@@ -199,7 +214,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             end = max(end, most);
             int before = __shfl_up_sync(0xffffffffu, end, 1);
             if (lane == 0) before = most;
-            int tiles = i < p.groups ? (end - before + kBM * kCtas - 1) / (kBM * kCtas) : 0;
+            const int per = rows_per_tile(end - before, p.most_rows);
+            int tiles = i < p.groups ? (end - before + per - 1) / per : 0;
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
                 const int other = __shfl_up_sync(0xffffffffu, tiles, o);
@@ -220,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
     if (kCtas == 2) cluster_sync_all();     // the peer's barriers exist before anything arrives on them
 
     // Whether a tile's last stage ends inside the next group's rows, where it is not by 16 rows that it does
-    auto has_tail = [&](const TileAt &t) { return kGrad && !t.x && ((t.row_end - t.row0) & 15) != 0; };
+    auto has_tail = [&](const TileAt &t) { return kGrad && !t.x && (t.rows & 15) != 0; };
 
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer: every lane with a copy of its own per stage
@@ -228,34 +244,28 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
         uint32_t phase = 0;
         const uint32_t full_issuer = kCtas == 2 ? map_to_cta(smem_u32(&full[0]), 0) : 0u;
         const uint32_t tail_own = kCtas == 2 ? map_to_cta(smem_u32(&tail_full[0]), (uint32_t)rank) : 0u;
-        const int bnh = p.BN / kCtas, nb = bnh / p.b_box;                  // B's rows that this CTA stages, and their boxes
-        for (int n = unit; tile_at<kCtas, kMode>(p, groups, n, at); n += units) {
-            // Boxes of A: those that hold a row of the group's (gradients of weights: both)
-            const int a_box = min(kBox, p.a_rows);
-            auto boxes_of = [&](int r) { return !at.x ? 2 : min(max((at.row_end - at.row0 - r * kBM + a_box - 1) / a_box, 0), p.a_rows / a_box); };
-            const int na = boxes_of(rank);
-            uint32_t bytes = (uint32_t)(boxes_of(0) * a_box + nb * p.b_box) * kRowBytes;
-            const uint32_t own_bytes = (uint32_t)(na * a_box + nb * p.b_box) * kRowBytes;
-            if (kCtas == 2) bytes += (uint32_t)(boxes_of(1) * a_box + nb * p.b_box) * kRowBytes;
+        const int bnh = p.BN / kCtas;
+        for (int n = unit; tile_at<kMode>(p, groups, n, at); n += units) {
+            // Tiles of rows: the weights in one copy (each of the gated block's two), for dX in two of 64 columns; then this CTA's rows, in one copy or
+            // where they are few in one or two small ones.  Gradients of weights: copies of 64 channels and 64 columns by 64 rows.
+            const int half_rows = ((at.rows + 15) / 16 * 16) / kCtas;
+            const bool small = at.x && half_rows <= 2 * p.b_box;
+            const int na = kMode == kGroupedPlain ? 1 : 2;
+            const int nb = !at.x ? bnh / kBox : small ? (half_rows + p.b_box - 1) / p.b_box : 1;
+            const int a_box_bytes = kGrad ? kBoxBytes : kABytes, b_box_bytes = !at.x ? kBoxBytes : (small ? p.b_box : kBM) * kRowBytes;
+            const uint32_t bytes = (uint32_t)(na * a_box_bytes + nb * b_box_bytes);
             const bool is_a = lane < na, active = lane < na + nb;
             const int piece = is_a ? lane : lane - na;
-            const uint32_t dst_off = is_a ? (uint32_t)(piece * a_box) * kRowBytes : p.a_bytes + (uint32_t)(piece * p.b_box) * kRowBytes;
-            const CUtensorMap *map = is_a ? &maps.A[0] : &maps.W[0];
-            // where the copy begins: along the tile (rows, channels or columns), and along the reduction
+            const uint32_t dst_off = is_a ? (uint32_t)(piece * a_box_bytes) : p.b_at + (uint32_t)(piece * b_box_bytes);
+            // the map, and where the copy begins along the tile (channels, columns or rows); along the reduction: `term`
+            const CUtensorMap *map;
             int along;
             if (at.x) {
-                if (is_a) along = at.row0 + rank * kBM + piece * a_box;
-                else if (kGated) {
-                    // a pair's CTA has one of the two weights, a lone CTA both, each with half of the boxes
-                    const int per = kCtas == 2 ? nb : nb / 2, w = kCtas == 2 ? rank : piece / per;
-                    map = &maps.W[w];
-                    along = at.tn * p.out_cols + (piece - (kCtas == 2 ? 0 : w * per)) * p.b_box;
-                } else {
-                    along = at.tn * p.BN + rank * bnh + piece * p.b_box;
-                }
+                map = !is_a ? (small ? &maps.R_small[0] : &maps.R[0]) : kGated ? &maps.W[piece & 1] : &maps.W[0];
+                along = !is_a ? at.row0 + rank * half_rows + piece * p.b_box : (at.tn * kCtas + rank) * kBM + (kGrad ? piece * kBox : 0);
             } else {
+                map = is_a ? &maps.D[p.w_first + at.z] : &maps.X;
                 along = is_a ? (at.tm * kCtas + rank) * kBM + piece * kBox : at.tn * p.BN + rank * bnh + piece * kBox;
-                map = is_a ? &maps.A[p.w_first + at.z] : &maps.X;
             }
             const bool tail = has_tail(at);
             int term = at.x ? 0 : at.row0;
@@ -264,10 +274,10 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 const bool to_clear = tail && kb == at.kb - 1;
                 if (lane == 0) {
                     if (to_clear) {
-                        mbar_arrive_expect_tx(&tail_full[stage], own_bytes);
+                        mbar_arrive_expect_tx(&tail_full[stage], bytes);
                         if (rank == 0) mbar_arrive(&full[stage]);
                     } else if (rank == 0) {
-                        mbar_arrive_expect_tx(&full[stage], bytes);
+                        mbar_arrive_expect_tx(&full[stage], bytes * kCtas);
                     }
                 }
                 __syncwarp();
@@ -279,15 +289,16 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                     uint8_t *dst = stages + (size_t)stage * p.stage_bytes + dst_off;
                     const uint32_t bar = kCtas == 2 ? (to_clear ? tail_own : full_issuer) + (uint32_t)stage * 8u : 0u;
                     uint64_t *own = to_clear ? &tail_full[stage] : &full[stage];
-                    // A K-major: (term, row); MN-major: (row, term).  Weights: (term, channel, group), or for dX (column, channel, group).
-                    if (!at.x || is_a) {
-                        const int c0 = at.x ? term : along, c1 = at.x ? along : term;
-                        if (kCtas == 2) tma_load_2d_pair(dst, map, bar, c0, c1);
-                        else tma_load_2d(dst, map, own, c0, c1);
-                    } else {
+                    if (at.x && is_a) {
+                        // weights: (term, channel, group), or for dX (column, channel, group)
                         const int c0 = kGrad ? along : term, c1 = kGrad ? term : along;
                         if (kCtas == 2) tma_load_3d_pair(dst, map, bar, c0, c1, at.g);
                         else tma_load_3d(dst, map, own, c0, c1, at.g);
+                    } else {
+                        // rows: (term, row); as terms themselves: (channel or column, row)
+                        const int c0 = at.x ? term : along, c1 = at.x ? along : term;
+                        if (kCtas == 2) tma_load_2d_pair(dst, map, bar, c0, c1);
+                        else tma_load_2d(dst, map, own, c0, c1);
                     }
                 }
                 term += kTerms;
@@ -302,19 +313,18 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             // K-major: 8-row groups 1024 bytes apart, an instruction 32 bytes further along the swizzled rows.  MN-major: blocks of 64 rows or
             // columns a box apart, groups of 8 terms 1024 bytes apart, an instruction two of those further.
             const uint64_t k_tmpl = make_smem_desc(0, 16, 1024, kSwizzle128B), mn_tmpl = make_smem_desc(0, kBoxBytes, 1024, kSwizzle128B);
-            const uint64_t b_tmpl = kGrad ? mn_tmpl : k_tmpl;
-            const uint32_t b_hi = (uint32_t)(b_tmpl >> 32);
-            const uint32_t a_at = (smem_u32(stages) >> 4) & 0x3FFFu, b_lo = (uint32_t)b_tmpl | (((smem_u32(stages) + p.a_bytes) >> 4) & 0x3FFFu);
-            const uint32_t stage16 = p.stage_bytes >> 4;
-            constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kB16 = kGrad ? kMn16 : kK16;
-            for (int n = unit; tile_at<kCtas, kMode>(p, groups, n, at); n += units) {
+            const uint64_t a_tmpl = kGrad ? mn_tmpl : k_tmpl;
+            const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), a_lo = (uint32_t)a_tmpl | ((smem_u32(stages) >> 4) & 0x3FFFu);
+            const uint32_t b_base = ((smem_u32(stages) + p.b_at) >> 4) & 0x3FFFu, stage16 = p.stage_bytes >> 4;
+            constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kA16 = kGrad ? kMn16 : kK16;
+            for (int n = unit; tile_at<kMode>(p, groups, n, at); n += units) {
                 if (at.kb == 0) continue;              // a group without rows
-                const bool a_mn = kGrad && !at.x, tail = has_tail(at);
-                const uint64_t a_tmpl = a_mn ? mn_tmpl : k_tmpl;
-                const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), a_lo = (uint32_t)a_tmpl | a_at, a16 = a_mn ? kMn16 : kK16;
-                const uint32_t idesc = kGrad && at.x ? p.idesc_x : p.idesc;
+                const bool b_mn = kGrad && !at.x, tail = has_tail(at);
+                const uint64_t b_tmpl = b_mn ? mn_tmpl : k_tmpl;
+                const uint32_t b_hi = (uint32_t)(b_tmpl >> 32), b_lo = (uint32_t)b_tmpl | b_base, b16 = b_mn ? kMn16 : kK16;
+                const uint32_t idesc = b_mn ? p.idesc_w : p.idesc_x | ((uint32_t)((at.rows + 15) / 16 * 2) << 17);
                 // instructions of the last stage
-                const int last = a_mn ? (at.row_end - at.row0 - (at.kb - 1) * kTerms + 15) / 16 : 4;
+                const int last = b_mn ? (at.rows - (at.kb - 1) * kTerms + 15) / 16 : 4;
                 if (kCtas == 2) mbar_wait_cluster(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 else mbar_wait(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 tc_fence_after_sync();
@@ -333,8 +343,12 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
 #pragma unroll
                     for (uint32_t k = 0; k < 4; ++k) {
                         if (kGrad && (int)k >= instructions) break;
-                        if (kCtas == 2) mma_f16_lohi_pair(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
-                        else mma_f16_lohi(d_tmem, al + k * a16, a_hi, bl + k * kB16, b_hi, idesc, accumulate);
+#pragma unroll
+                        for (uint32_t w = 0; w < (kGated ? 2u : 1u); ++w) {
+                            const uint32_t a = al + w * (kABytes >> 4) + k * kA16, d = d_tmem + w * kGatedAt;
+                            if (kCtas == 2) mma_f16_lohi_pair(d, a, a_hi, bl + k * b16, b_hi, idesc, accumulate);
+                            else mma_f16_lohi(d, a, a_hi, bl + k * b16, b_hi, idesc, accumulate);
+                        }
                         accumulate = 1;
                     }
                     if (kCtas == 2) mma_commit_pair(&empty[stage]);
@@ -353,8 +367,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             int stage = 0;
             uint32_t clear_phase = 0;
             const uint32_t cleared_issuer = kCtas == 2 ? map_to_cta(smem_u32(&cleared[0]), 0) : 0u;
-            const int boxes = (int)(p.stage_bytes / kBoxBytes);
-            for (int n = unit; tile_at<kCtas, kMode>(p, groups, n, at); n += units) {
+            const int boxes = kBM / kBox + p.BN / kCtas / kBox;
+            for (int n = unit; tile_at<kMode>(p, groups, n, at); n += units) {
                 if (at.kb == 0) continue;
                 stage += at.kb - 1;
                 stage %= p.num_stages;
@@ -362,10 +376,12 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                     mbar_wait(&tail_full[stage], (clear_phase >> stage) & 1u, p.err, 6);
                     clear_phase ^= 1u << stage;
                     // a box has a row of the group's, 64 columns of it, in 128 bytes (the swizzle moves pieces within them)
-                    const int from = (at.row_end - at.row0) - (at.kb - 1) * kTerms, pieces = ((from + 15) / 16 * 16 - from) * 8;
+                    const int from = at.rows - (at.kb - 1) * kTerms, pieces = ((from + 15) / 16 * 16 - from) * 8;
                     uint8_t *first = stages + (size_t)stage * p.stage_bytes + from * kRowBytes;
-                    for (int b = 0; b < boxes; ++b)
-                        for (int i = lane; i < pieces; i += 32) *reinterpret_cast<uint4 *>(first + b * kBoxBytes + i * 16) = make_uint4(0, 0, 0, 0);
+                    for (int b = 0; b < boxes; ++b) {
+                        uint8_t *box = first + (b < kBM / kBox ? b * kBoxBytes : (int)p.b_at + (b - kBM / kBox) * kBoxBytes);
+                        for (int i = lane; i < pieces; i += 32) *reinterpret_cast<uint4 *>(box + i * 16) = make_uint4(0, 0, 0, 0);
+                    }
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
@@ -383,58 +399,94 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
         int acc = 0;
         uint32_t acc_phase = 0;
         const uint32_t peer_tmem_empty = kCtas == 2 ? map_to_cta(smem_u32(&tmem_empty[0]), 0) : 0u;
-        for (int n = unit; tile_at<kCtas, kMode>(p, groups, n, at); n += units) {
-            const int n0 = at.tn * p.out_cols, cols = min(p.out_cols, p.N - n0), blocks = (cols + 63) / 64;
-            // the first row of this warp's quarter, in its output, and how many of its 32 are the group's (gradients of weights: channels)
-            const int quarter = rank * kBM + q * 32;
-            const int row0 = at.x ? at.row0 + quarter : at.tm * kCtas * kBM + quarter;
-            const int rows = min(32, (at.x ? at.row_end : p.channels) - row0);
+        for (int n = unit; tile_at<kMode>(p, groups, n, at); n += units) {
             const bool some = at.kb > 0;
             if (some) {
                 mbar_wait(&tmem_full[acc], acc_phase, p.err, 4);
                 tc_fence_after_sync();
             }
             const uint32_t tbase = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * kMaxBN);
-            if (rows > 0) {
-                // the two warps of a quarter share its blocks of all results in turns
+            auto words_of = [&](const float (&lo)[16], const float (&hi)[16], uint32_t (&h)[16]) {
+                if (p.bf16) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) h[i] = pack<__nv_bfloat162>(lo[i], hi[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) h[i] = pack<__half2>(lo[i], hi[i]);
+                }
+            };
+            if (!kGrad || at.x) {
+                // Lanes are channels (columns of the result), columns rows.  The two warps of a quarter share blocks of 32 rows of all results in turns.
+                const int all = kGrad ? p.width : p.channels, channel0 = (at.tn * kCtas + rank) * kBM + q * 32, mine = channel0 + (lane & ~1);
+                const int blocks = channel0 < all ? (at.rows + 31) / 32 : 0, odd = lane & 1;
 #pragma unroll 1
                 for (int item = half; item < blocks * p.outs; item += 2) {
-                    const int which = item < blocks ? 0 : item < 2 * blocks ? 1 : 2, b = item - which * blocks;
-#pragma unroll 1
-                    for (int c = 0; c < 64 && b * 64 + c < p.out_cols; c += 32) {
-                        const int col = b * 64 + c;
-                        uint32_t v[32];
-                        float f[32];
-                        if (some) {
-                            tmem_ld_32x32(tbase + (uint32_t)(which == 2 ? p.out_cols + col : col), v);
-                            if (kGated && which == 0) {
-                                uint32_t w[32];
-                                tmem_ld_32x32(tbase + (uint32_t)(p.out_cols + col), w);
-                                tmem_ld_wait();
-#define ONNXB_GATE(kind) _Pragma("unroll") for (int j = 0; j < 32; ++j) f[j] = activate(kind, __uint_as_float(v[j])) * __uint_as_float(w[j])
-                                if (p.activation == ONNXB_SILU) { ONNXB_GATE(ONNXB_SILU); }
-                                else if (p.activation == ONNXB_GELU) { ONNXB_GATE(ONNXB_GELU); }
-                                else if (p.activation == ONNXB_GELU_TANH) { ONNXB_GATE(ONNXB_GELU_TANH); }
-                                else { ONNXB_GATE(ONNXB_RELU); }
+                    const int which = item < blocks ? 0 : item < 2 * blocks ? 1 : 2, first = (item - which * blocks) * 32;
+                    uint32_t v[32];
+                    tmem_ld_32x32(tbase + (uint32_t)(which == 2 ? kGatedAt + first : first), v);
+                    if (kGated && which == 0) {
+                        uint32_t w[32];
+                        tmem_ld_32x32(tbase + (uint32_t)(kGatedAt + first), w);
+                        tmem_ld_wait();
+#define ONNXB_GATE(kind) _Pragma("unroll") for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(activate(kind, __uint_as_float(v[j])) * __uint_as_float(w[j]))
+                        if (p.activation == ONNXB_SILU) { ONNXB_GATE(ONNXB_SILU); }
+                        else if (p.activation == ONNXB_GELU) { ONNXB_GATE(ONNXB_GELU); }
+                        else if (p.activation == ONNXB_GELU_TANH) { ONNXB_GATE(ONNXB_GELU_TANH); }
+                        else { ONNXB_GATE(ONNXB_RELU); }
 #undef ONNXB_GATE
-                            } else {
-                                tmem_ld_wait();
+                    } else {
+                        tmem_ld_wait();
+                    }
+                    // of rows 2 i and 2 i + 1 an even lane keeps the first and an odd one the second, each of its own channel and its neighbour's
+                    float lo[16], hi[16];
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? v[2 * i] : v[2 * i + 1], 1);
+                        lo[i] = __uint_as_float(odd ? other : v[2 * i]);
+                        hi[i] = __uint_as_float(odd ? v[2 * i + 1] : other);
+                    }
+                    uint32_t h[16];
+                    words_of(lo, hi, h);
+                    const int rows = at.rows - first - odd;                // (of those from this lane's first on)
+                    const long long ld = p.y_ld[which];
+                    uint16_t *out = static_cast<uint16_t *>(p.Y[which]) + (at.row0 + first + odd) * ld + mine;
+                    if (p.y_pairs[which] && mine + 2 <= all) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (2 * i < rows) *reinterpret_cast<uint32_t *>(out + 2 * i * ld) = h[i];
+                    } else if (mine < all) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (2 * i < rows) {
+                                out[2 * i * ld] = (uint16_t)h[i];
+                                if (mine + 1 < all) out[2 * i * ld + 1] = (uint16_t)(h[i] >> 16);
                             }
+                    }
+                }
+            } else {
+                // Lanes are channels (rows of the gradient), columns its columns.  The two warps of a quarter share its blocks of 64 columns in turns.
+                const int row0 = (at.tm * kCtas + rank) * kBM + q * 32, rows = min(32, p.channels - row0), n0 = at.tn * p.BN;
+                const int blocks = rows > 0 ? (min(p.BN, p.width - n0) + 63) / 64 : 0;
+#pragma unroll 1
+                for (int b = half; b < blocks; b += 2) {
+#pragma unroll 1
+                    for (int c = 0; c < 64; c += 32) {
+                        uint32_t v[32], h[16];
+                        if (some) {
+                            tmem_ld_32x32(tbase + (uint32_t)(b * 64 + c), v);
+                            tmem_ld_wait();
                         } else {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) f[j] = 0.f;
+                            for (int j = 0; j < 32; ++j) v[j] = 0u;
                         }
+                        float lo[16], hi[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            lo[i] = __uint_as_float(v[2 * i]);
+                            hi[i] = __uint_as_float(v[2 * i + 1]);
+                        }
+                        words_of(lo, hi, h);
                         // the lane's row of the block, 16-byte piece i at position i ^ (lane % 8)
-                        uint32_t h[16];
-                        if (p.bf16) {
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) h[i] = pack<__nv_bfloat162>(f[2 * i], f[2 * i + 1]);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) h[i] = pack<__half2>(f[2 * i], f[2 * i + 1]);
-                        }
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             *reinterpret_cast<uint4 *>(buf + lane * kRowBytes + (((c / 8 + i) ^ (lane & 7)) << 4)) =
@@ -442,11 +494,10 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                     }
                     __syncwarp();
                     // Stored by rows, four at a time in pieces of 16 bytes, or one in pairs of elements
-                    const int w = p.w_first + at.z, left = min(64, cols - b * 64);
-                    const bool of_weights = kGrad && !at.x;
-                    const long long ld = of_weights ? p.d_ld[w] : p.y_ld[which];
-                    uint16_t *out = static_cast<uint16_t *>(of_weights ? p.D[w] : p.Y[which]) + (of_weights ? at.g * p.d_stride[w] : 0) + row0 * ld + n0 + b * 64;
-                    if (of_weights ? p.d_wide[w] : p.y_wide[which]) {
+                    const int w = p.w_first + at.z, left = min(64, p.width - n0 - b * 64);
+                    const long long ld = p.d_ld[w];
+                    uint16_t *out = static_cast<uint16_t *>(p.D[w]) + at.g * p.d_stride[w] + row0 * ld + n0 + b * 64;
+                    if (p.d_wide[w]) {
                         const int piece = lane & 7, mine = left - piece * 8;
 #pragma unroll 4
                         for (int r = lane >> 3; r < rows; r += 4) {
@@ -515,13 +566,12 @@ cudaError_t allow_shared_memory(Kernel kernel, int index) {
 
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
+// CTAs of a tile, and the most rows of one of rows
 struct Tile {
-    int ctas, BN;
+    int ctas, rows;
 };
 bool tile_allowed(int mode, Tile t) {
-    if (t.BN < 64 || t.BN > kMaxBN || t.BN % 64) return false;
-    // boxes of 64 rows of B in each CTA, or of both weights of the gated block in a lone one (of 32 where these are few)
-    return t.ctas == 2 ? t.BN % 128 == 0 : mode != kGroupedGated || t.BN != 192;
+    return (t.ctas == 1 || t.ctas == 2) && t.rows >= 16 && t.rows % 16 == 0 && t.rows <= (mode == kGroupedGated ? 128 : 128 * t.ctas);
 }
 // CTA pairs that run at once, asked of the device's occupancy once
 int max_pairs() {
@@ -550,13 +600,14 @@ int max_pairs() {
     return n;
 }
 Tile pick_tile(const GroupedProblem &d) {
+    // "<CTAs>x<rows>" in ONNXB_GROUPED_TILE pins the shape for A/B measurements and tests
     if (const char *e = getenv("ONNXB_GROUPED_TILE")) {
         const Tile t{e[0] - '0', e[0] && e[1] == 'x' ? atoi(e + 2) : 0};
-        if ((t.ctas == 1 || t.ctas == 2) && tile_allowed(d.mode, t)) return t;
+        if (tile_allowed(d.mode, t)) return t;
     }
     const long long per_group = d.rows / std::min(d.rows, d.groups);
-    if (per_group > 128) return Tile{2, 256};
-    return Tile{1, per_group >= 32 ? 256 : 128};
+    const int ctas = per_group > 64 ? 2 : 1;
+    return Tile{ctas, std::min(d.mode == kGroupedGated ? 128 : 128 * ctas, (d.rows + 15) / 16 * 16)};
 }
 
 // Rows that begin at multiples of 16 bytes, as (terms, rows) in boxes of 64 by `box`
@@ -584,36 +635,38 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     Params p{};
     p.rows = d.rows; p.groups = d.groups; p.offsets = d.offsets;
     p.channels = d.channels; p.width = d.width;
-    p.N = grad ? d.width : d.channels;
-    p.BN = tile.BN;
-    p.out_cols = gated ? p.BN / 2 : p.BN;
-    p.tiles_n = (int)ceil_div(p.N, p.out_cols);
+    p.most_rows = tile.rows;
+    const int columns = kBM * tile.ctas;                   // of a tile of rows
+    p.tiles_n = (int)ceil_div(grad ? d.width : d.channels, columns);
     p.band = 8;
     p.num_kb = (int)ceil_div(grad ? d.channels : d.width, kTerms);
-    // Few rows: no more of A's than there are.  The tensor cores read 128 all the same, what lies behind being other operands'; those rows of the accumulator are nobody's.
-    p.a_rows = tile.ctas == 1 && !grad && d.rows <= 64 ? (d.rows <= 16 ? 16 : d.rows <= 32 ? 32 : 64) : kBM;
-    p.b_box = gated && tile.BN / 2 < kBox && tile.ctas == 1 ? 32 : kBox;
+    // small copies of rows: no more than all the rows that there are
+    p.b_box = d.rows <= 16 ? 16 : 32;
     p.terms = d.terms;
     p.with_x = grad && d.Y[0] ? 1 : 0;
     p.w_first = d.D[0].p ? 0 : 1;
     p.w_count = grad ? (d.D[0].p != nullptr) + (d.D[1].p != nullptr) : 0;
+    p.BN = kBM * tile.ctas;
     p.w_tiles_m = (int)ceil_div(d.channels, kBM * tile.ctas);
-    const long long w_total = (long long)d.groups * p.w_count * p.w_tiles_m * p.tiles_n;
-    // row tiles: at most one of each group is not whole
-    const long long row_tiles = grad && !p.with_x ? 0 : d.rows / (kBM * tile.ctas) + std::min(d.groups, d.rows), most = row_tiles * p.tiles_n + w_total;
-    if (most > 0x7fffffffLL / 2 || (long long)p.band * p.tiles_n > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
+    p.w_tiles_n = (int)ceil_div(d.width, p.BN);
+    const long long w_total = (long long)d.groups * p.w_count * p.w_tiles_m * p.w_tiles_n;
+    // tiles of rows: at most one more for each group than whole ones
+    const long long row_tiles = grad && !p.with_x ? 0 : d.rows / tile.rows + std::min(d.groups, d.rows), most = row_tiles * p.tiles_n + w_total;
+    if (most > 0x7fffffffLL / 2 || (long long)p.band * std::max(p.tiles_n, p.w_tiles_n) > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
     p.w_total = (int)w_total;
-    p.a_bytes = (uint32_t)(p.a_rows * kRowBytes);
-    p.stage_bytes = p.a_bytes + (uint32_t)(p.BN / tile.ctas * kRowBytes);
-    const int table = ((2 * d.groups + 2) * 4 + 15) / 16 * 16;
-    p.num_stages = std::min(kMaxStages, (kSmemLimit - 1024 - kBarrierBytes - kStagingBytes - table) / (int)p.stage_bytes);
+    p.b_at = (uint32_t)(gated ? 2 * kABytes : kABytes);
+    // (B: the rows of a CTA's part of a tile, or of the gradients of weights its columns)
+    const int b_rows = grad ? kBM : std::max(tile.rows / tile.ctas > 2 * p.b_box ? kBM : 0, 2 * p.b_box);
+    p.stage_bytes = p.b_at + (uint32_t)(b_rows * kRowBytes);
+    const int table = ((2 * d.groups + 2) * 4 + 15) / 16 * 16, staging = grad ? kStagingBytes : 0;
+    p.num_stages = std::min(kMaxStages, (kSmemLimit - 1024 - kBarrierBytes - staging - table) / (int)p.stage_bytes);
     const int bf16 = d.type == ONNXB_BFLOAT16;
-    p.idesc = make_idesc_f16(kBM * tile.ctas, p.BN, bf16, grad, grad);
-    p.idesc_x = make_idesc_f16(kBM * tile.ctas, p.BN, bf16, 0, 1);
+    p.idesc_x = make_idesc_f16(kBM * tile.ctas, 0, bf16, grad, 0);
+    p.idesc_w = make_idesc_f16(kBM * tile.ctas, p.BN, bf16, 1, 1);
     p.bf16 = bf16;
     p.activation = d.activation;
     p.outs = gated && d.Y[1] ? 3 : 1;
-    for (int i = 0; i < 3; ++i) { p.Y[i] = d.Y[i]; p.y_ld[i] = d.y_ld[i]; p.y_wide[i] = by_16(d.Y[i], d.y_ld[i]); }
+    for (int i = 0; i < 3; ++i) { p.Y[i] = d.Y[i]; p.y_ld[i] = d.y_ld[i]; p.y_pairs[i] = reinterpret_cast<uintptr_t>(d.Y[i]) % 4 == 0 && d.y_ld[i] % 2 == 0; }
     for (int i = 0; i < 2; ++i) {
         p.D[i] = const_cast<void *>(d.D[i].p); p.d_ld[i] = d.D[i].ld; p.d_stride[i] = d.D[i].stride;
         p.d_wide[i] = by_16(d.D[i].p, d.D[i].ld) && d.D[i].stride % 8 == 0;
@@ -623,13 +676,19 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
 
     Maps maps{};
     bool fine = true;
-    for (int i = 0; i < (grad ? d.terms : 1); ++i) fine = fine && rows_map(&maps.A[i], d.A[i], d.rows, grad ? d.channels : d.width, std::min(kBox, p.a_rows));
-    for (int i = 0; i < (gated ? 2 : grad ? d.terms : 1); ++i)
-        if (!grad || p.with_x) fine = fine && weights_map(&maps.W[i], d.W[i], d.groups, d.channels, d.width, p.b_box);
-    if (p.w_count) fine = fine && rows_map(&maps.X, d.X, d.rows, d.width, kBox);
+    const int terms = grad ? d.terms : 1, along = grad ? d.channels : d.width;
+    if (!grad || p.with_x) {
+        for (int i = 0; i < terms; ++i)
+            fine = fine && rows_map(&maps.R[i], d.A[i], d.rows, along, kBM) && rows_map(&maps.R_small[i], d.A[i], d.rows, along, p.b_box);
+        for (int i = 0; i < (gated ? 2 : terms); ++i) fine = fine && weights_map(&maps.W[i], d.W[i], d.groups, d.channels, d.width, grad ? kBox : kBM);
+    }
+    if (p.w_count) {
+        for (int i = 0; i < terms; ++i) fine = fine && rows_map(&maps.D[i], d.A[i], d.rows, d.channels, kBox);
+        fine = fine && rows_map(&maps.X, d.X, d.rows, d.width, kBox);
+    }
     if (!fine) return (int)cudaErrorInvalidValue;
 
-    const size_t smem = smem_with_tmem(1024 + (size_t)p.num_stages * p.stage_bytes + kStagingBytes + kBarrierBytes + table, 512);
+    const size_t smem = smem_with_tmem(1024 + (size_t)p.num_stages * p.stage_bytes + staging + kBarrierBytes + table, 512);
     const Kernel kernel = tile.ctas == 2 ? kernel_for<2>(d.mode) : kernel_for<1>(d.mode);
     const cudaError_t attr_err = allow_shared_memory(kernel, (tile.ctas - 1) * 3 + d.mode);
     if (attr_err != cudaSuccess) return (int)attr_err;

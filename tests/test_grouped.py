@@ -151,7 +151,7 @@ def test_groups(sizes, K, N, t):
 
 
 @gpu
-@pytest.mark.parametrize("tile", ["1x64", "1x128", "1x192", "1x256", "2x128", "2x256"])
+@pytest.mark.parametrize("tile", ["1x16", "1x48", "1x128", "2x32", "2x96", "2x128", "2x256"])
 @pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh", "relu"])
 def test_every_tile(tile, kind, monkeypatch):
     monkeypatch.setenv("ONNXB_GROUPED_TILE", tile)
@@ -166,7 +166,7 @@ def test_odd_widths(K, N, t):
 
 
 @gpu
-@pytest.mark.parametrize("tile", ["1x128", "2x256"])
+@pytest.mark.parametrize("tile", ["1x128", "2x128", "2x256"])
 def test_rows_of_no_group_are_left(tile, monkeypatch):
     monkeypatch.setenv("ONNXB_GROUPED_TILE", tile)
     c = Case([33, 0, 90], 96, 200, torch.float16, before=9, behind=50)
@@ -190,7 +190,7 @@ def test_rows_of_no_group_are_left(tile, monkeypatch):
 
 
 @gpu
-@pytest.mark.parametrize("tile", ["1x64", "1x256", "2x256"])
+@pytest.mark.parametrize("tile", ["1x16", "1x128", "2x128", "2x256"])
 def test_what_is_not_finite_stays_in_its_group(tile, monkeypatch):
     """A group's rows, results and gradients are its own, wherever another's rows lie in the same tile or stage."""
     monkeypatch.setenv("ONNXB_GROUPED_TILE", tile)
@@ -270,7 +270,7 @@ def test_no_rows():
 @gpu
 @pytest.mark.parametrize("offsets,ends", [([-5, 10, 300, 20], [0, 10, 100, 100]), ([20, 50, 30, 90], [20, 50, 50, 90]),
                                           ([90, 10, 5, 0], [90, 90, 90, 90]), ([0, 2 ** 31 - 1, -2 ** 31, 7], [0, 100, 100, 100])])
-@pytest.mark.parametrize("tile", ["1x128", "2x256"])
+@pytest.mark.parametrize("tile", ["1x128", "2x128", "2x256"])
 def test_offsets_that_do_not_rise(offsets, ends, tile, monkeypatch):
     """What is outside of 0 and the rows counts as the nearest end, one below the one before it as that: no row beyond the tensors is touched."""
     monkeypatch.setenv("ONNXB_GROUPED_TILE", tile)
