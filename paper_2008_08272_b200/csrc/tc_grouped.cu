@@ -257,52 +257,57 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             const bool is_a = lane < na, active = lane < na + nb;
             const int piece = is_a ? lane : lane - na;
             const uint32_t dst_off = is_a ? (uint32_t)(piece * a_box_bytes) : p.b_at + (uint32_t)(piece * b_box_bytes);
-            // the map, and where the copy begins along the tile (channels, columns or rows); along the reduction: `term`
+            // The map, and where the copy begins: weights (term, channel, group), or for dX (column, channel, group); rows (term, row, 0), or as
+            // terms themselves (channel or column, row, 0).  From stage to stage one of the first two moves on.
             const CUtensorMap *map;
-            int along;
+            int c0, c1, c2 = 0;
+            const bool second = at.x ? kGrad && is_a : true;
             if (at.x) {
                 map = !is_a ? (small ? &maps.R_small[0] : &maps.R[0]) : kGated ? &maps.W[piece & 1] : &maps.W[0];
-                along = !is_a ? at.row0 + rank * half_rows + piece * p.b_box : (at.tn * kCtas + rank) * kBM + (kGrad ? piece * kBox : 0);
+                const int along = !is_a ? at.row0 + rank * half_rows + piece * p.b_box : (at.tn * kCtas + rank) * kBM + (kGrad ? piece * kBox : 0);
+                c0 = second ? along : 0;
+                c1 = second ? 0 : along;
+                c2 = is_a ? at.g : 0;
             } else {
                 map = is_a ? &maps.D[p.w_first + at.z] : &maps.X;
-                along = is_a ? (at.tm * kCtas + rank) * kBM + piece * kBox : at.tn * p.BN + rank * bnh + piece * kBox;
+                c0 = is_a ? (at.tm * kCtas + rank) * kBM + piece * kBox : at.tn * p.BN + rank * bnh + piece * kBox;
+                c1 = at.row0;
             }
+            const int d0 = second ? 0 : kTerms, d1 = second ? kTerms : 0;
             const bool tail = has_tail(at);
-            int term = at.x ? 0 : at.row0;
-            for (int kb = 0; kb < at.kb; ++kb) {
+            uint8_t *dst = stages + dst_off;
+            auto load = [&](uint32_t cluster_bar, uint64_t *own) {
+                if (active) {
+                    if (kCtas == 2) tma_load_3d_pair(dst + (size_t)stage * p.stage_bytes, map, cluster_bar + (uint32_t)stage * 8u, c0, c1, c2);
+                    else tma_load_3d(dst + (size_t)stage * p.stage_bytes, map, own + stage, c0, c1, c2);
+                }
+                c0 += d0;
+                c1 += d1;
+                if (++stage == p.num_stages) { stage = 0; phase ^= 1; }
+            };
+            // (dX's second term: the same stages again of the other tensors)
+            const int parts = kGrad && at.x ? p.terms : 1, kb_each = kGrad && at.x ? p.num_kb : tail ? at.kb - 1 : at.kb;
+            for (int part = 0; part < parts; ++part) {
+                if (kGrad && part > 0) {
+                    map += 1;
+                    c0 -= kb_each * d0;
+                    c1 -= kb_each * d1;
+                }
+                for (int kb = 0; kb < kb_each; ++kb) {
+                    mbar_wait(&empty[stage], phase ^ 1, p.err, 1);
+                    if (lane == 0 && rank == 0) mbar_arrive_expect_tx(&full[stage], bytes * kCtas);
+                    __syncwarp();
+                    load(full_issuer, full);
+                }
+            }
+            if (tail) {
                 mbar_wait(&empty[stage], phase ^ 1, p.err, 1);
-                const bool to_clear = tail && kb == at.kb - 1;
                 if (lane == 0) {
-                    if (to_clear) {
-                        mbar_arrive_expect_tx(&tail_full[stage], bytes);
-                        if (rank == 0) mbar_arrive(&full[stage]);
-                    } else if (rank == 0) {
-                        mbar_arrive_expect_tx(&full[stage], bytes * kCtas);
-                    }
+                    mbar_arrive_expect_tx(&tail_full[stage], bytes);
+                    if (rank == 0) mbar_arrive(&full[stage]);
                 }
                 __syncwarp();
-                if (kGrad && at.x && kb == p.num_kb) {         // dX's second term
-                    map += 1;
-                    term = 0;
-                }
-                if (active) {
-                    uint8_t *dst = stages + (size_t)stage * p.stage_bytes + dst_off;
-                    const uint32_t bar = kCtas == 2 ? (to_clear ? tail_own : full_issuer) + (uint32_t)stage * 8u : 0u;
-                    uint64_t *own = to_clear ? &tail_full[stage] : &full[stage];
-                    if (at.x && is_a) {
-                        // weights: (term, channel, group), or for dX (column, channel, group)
-                        const int c0 = kGrad ? along : term, c1 = kGrad ? term : along;
-                        if (kCtas == 2) tma_load_3d_pair(dst, map, bar, c0, c1, at.g);
-                        else tma_load_3d(dst, map, own, c0, c1, at.g);
-                    } else {
-                        // rows: (term, row); as terms themselves: (channel or column, row)
-                        const int c0 = at.x ? term : along, c1 = at.x ? along : term;
-                        if (kCtas == 2) tma_load_2d_pair(dst, map, bar, c0, c1);
-                        else tma_load_2d(dst, map, own, c0, c1);
-                    }
-                }
-                term += kTerms;
-                if (++stage == p.num_stages) { stage = 0; phase ^= 1; }
+                load(tail_own, tail_full);
             }
         }
     } else if (warp == 1) {
@@ -323,37 +328,45 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 const uint64_t b_tmpl = b_mn ? mn_tmpl : k_tmpl;
                 const uint32_t b_hi = (uint32_t)(b_tmpl >> 32), b_lo = (uint32_t)b_tmpl | b_base, b16 = b_mn ? kMn16 : kK16;
                 const uint32_t idesc = b_mn ? p.idesc_w : p.idesc_x | ((uint32_t)((at.rows + 15) / 16 * 2) << 17);
-                // instructions of the last stage
-                const int last = b_mn ? (at.rows - (at.kb - 1) * kTerms + 15) / 16 : 4;
+                // instructions of the last stage, where they are not four; stages before it
+                const int last = b_mn ? (at.rows - (at.kb - 1) * kTerms + 15) / 16 : 4, whole = last == 4 && !tail ? at.kb : at.kb - 1;
                 if (kCtas == 2) mbar_wait_cluster(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 else mbar_wait(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 tc_fence_after_sync();
                 const uint32_t d_tmem = tmem_base + (uint32_t)acc * kMaxBN;
                 uint32_t accumulate = 0;
-                for (int kb = 0; kb < at.kb; ++kb) {
+                auto multiply = [&](uint32_t k) {
+                    const uint32_t al = a_lo + (uint32_t)stage * stage16 + k * kA16, bl = b_lo + (uint32_t)stage * stage16 + k * b16;
+#pragma unroll
+                    for (uint32_t w = 0; w < (kGated ? 2u : 1u); ++w) {
+                        if (kCtas == 2) mma_f16_lohi_pair(d_tmem + w * kGatedAt, al + w * (kABytes >> 4), a_hi, bl, b_hi, idesc, accumulate);
+                        else mma_f16_lohi(d_tmem + w * kGatedAt, al + w * (kABytes >> 4), a_hi, bl, b_hi, idesc, accumulate);
+                    }
+                    accumulate = 1;
+                };
+                auto done = [&]() {
+                    if (kCtas == 2) mma_commit_pair(&empty[stage]);
+                    else mma_commit(&empty[stage]);
+                    if (++stage == p.num_stages) { stage = 0; phase ^= 1; }
+                };
+                for (int kb = 0; kb < whole; ++kb) {
                     mbar_wait(&full[stage], phase, p.err, 3);
-                    if (tail && kb == at.kb - 1) {
+                    tc_fence_after_sync();
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) multiply(k);
+                    done();
+                }
+                if (kGrad && whole < at.kb) {
+                    mbar_wait(&full[stage], phase, p.err, 3);
+                    if (tail) {
                         if (kCtas == 2) mbar_wait_cluster(&cleared[stage], (clear_phase >> stage) & 1u, p.err, 5);
                         else mbar_wait(&cleared[stage], (clear_phase >> stage) & 1u, p.err, 5);
                         clear_phase ^= 1u << stage;
                     }
                     tc_fence_after_sync();
-                    const uint32_t al = a_lo + (uint32_t)stage * stage16, bl = b_lo + (uint32_t)stage * stage16;
-                    const int instructions = kb == at.kb - 1 ? last : 4;
-#pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) {
-                        if (kGrad && (int)k >= instructions) break;
-#pragma unroll
-                        for (uint32_t w = 0; w < (kGated ? 2u : 1u); ++w) {
-                            const uint32_t a = al + w * (kABytes >> 4) + k * kA16, d = d_tmem + w * kGatedAt;
-                            if (kCtas == 2) mma_f16_lohi_pair(d, a, a_hi, bl + k * b16, b_hi, idesc, accumulate);
-                            else mma_f16_lohi(d, a, a_hi, bl + k * b16, b_hi, idesc, accumulate);
-                        }
-                        accumulate = 1;
-                    }
-                    if (kCtas == 2) mma_commit_pair(&empty[stage]);
-                    else mma_commit(&empty[stage]);
-                    if (++stage == p.num_stages) { stage = 0; phase ^= 1; }
+#pragma unroll 1
+                    for (uint32_t k = 0; k < (uint32_t)last; ++k) multiply(k);
+                    done();
                 }
                 if (kCtas == 2) mma_commit_pair(&tmem_full[acc]);
                 else mma_commit(&tmem_full[acc]);
@@ -610,12 +623,13 @@ Tile pick_tile(const GroupedProblem &d) {
     return Tile{ctas, std::min(d.mode == kGroupedGated ? 128 : 128 * ctas, (d.rows + 15) / 16 * 16)};
 }
 
-// Rows that begin at multiples of 16 bytes, as (terms, rows) in boxes of 64 by `box`
+// Rows that begin at multiples of 16 bytes, as (terms, rows, 1) in boxes of 64 by `box`; groups' weights as (terms, channels, groups).  (Of three dimensions
+// both, so that a stage's copies are one instruction.)
 bool rows_map(CUtensorMap *m, const DenseOperand &o, long long rows, long long cols, int box) {
     const uint64_t pitch = (uint64_t)(rows > 1 ? o.ld * 2 : (o.ld * 2 + 15) / 16 * 16);
-    const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows};
-    const uint32_t boxes[2] = {kTerms, (uint32_t)box};
-    return tc_host::make_tmap_of(2, m, o.p, 2, dims, &pitch, boxes, tc_host::kTmapSwizzle128);
+    const uint64_t dims[3] = {(uint64_t)cols, (uint64_t)rows, 1}, pitches[2] = {pitch, pitch};
+    const uint32_t boxes[3] = {kTerms, (uint32_t)box, 1};
+    return tc_host::make_tmap_of(2, m, o.p, 3, dims, pitches, boxes, tc_host::kTmapSwizzle128);
 }
 bool weights_map(CUtensorMap *m, const GroupedWeights &w, long long groups, long long channels, long long width, int box) {
     const uint64_t pitch = (uint64_t)(channels > 1 ? w.ld * 2 : (width * 2 + 15) / 16 * 16);
