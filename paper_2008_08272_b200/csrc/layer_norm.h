@@ -25,7 +25,7 @@ struct LayerNormGradProblem {
     void *d_scale, *d_bias;      // each may be NULL
     void *partial;               // layer_norm_grad_workspace bytes
 };
-size_t layer_norm_grad_workspace(int type, int M, int K, bool weights);
+size_t layer_norm_grad_workspace(int M, int K, bool weights);
 int launch_layer_norm_grad(const LayerNormGradProblem &p, cudaStream_t stream);
 
 }  // namespace onnxb

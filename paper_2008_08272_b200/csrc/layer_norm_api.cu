@@ -45,7 +45,7 @@ extern "C" onnxb_status onnx_layer_normalization_run(const onnxb_matrix *X, cons
 
 extern "C" size_t onnx_layer_normalization_backward_workspace_bytes(const onnxb_matrix *X, const onnxb_matrix *dScale, const onnxb_matrix *dBias) {
     if (!X || X->rows < 1 || X->cols < 1 || X->rows > kMostSize || X->cols > kMostSize) return 0;
-    return layer_norm_grad_workspace(X->type, (int)X->rows, (int)X->cols, dScale || dBias);
+    return layer_norm_grad_workspace((int)X->rows, (int)X->cols, dScale || dBias);
 }
 
 extern "C" onnxb_status onnx_layer_normalization_backward_run(const onnxb_matrix *dY, const onnxb_matrix *X, const onnxb_matrix *scale,
