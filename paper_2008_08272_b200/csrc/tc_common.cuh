@@ -154,6 +154,31 @@ __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 
+// ---------------------------------------------------------------- blocks taken over
+// Asks for a block (cluster) of the grid that has not been launched yet, to be computed by this one in its place: 16 bytes of an answer, counted on an
+// mbarrier.  One request at a time, and none behind one that was answered in the negative.
+__device__ __forceinline__ void ask_for_block(void *answer, uint64_t *bar) {
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(answer)), "r"(smem_u32(bar))
+                 : "memory");
+}
+// The x coordinate of the block (of the cluster's first) that the answer grants; -1: there is none any more
+__device__ __forceinline__ int granted_block(const void *answer) {
+    int x;
+    asm volatile(
+        "{\n"
+        ".reg .pred P;\n"
+        ".reg .b128 a;\n"
+        "ld.shared.b128 a, [%1];\n"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 P, a;\n"
+        "mov.s32 %0, -1;\n"
+        "@P clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, a;\n"
+        "}\n"
+        : "=r"(x)
+        : "r"(smem_u32(answer))
+        : "memory");
+    return x;
+}
+
 // ---------------------------------------------------------------- TMA
 __device__ __forceinline__ void prefetch_tmap(const CUtensorMap *m) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");

@@ -8,7 +8,9 @@
 //   warp 10   clears what a stage holds of the next group's rows (below).
 // What is its own:
 //   - Where the groups lie only the device knows: every CTA reads the offsets, makes them rise, and counts the groups' tiles, in shared memory; a tile's
-//     number is looked up there.  The grid is what the host knows to be enough, at most one CTA an SM, and the call waits for nothing.
+//     number is looked up there.  The grid has a CTA (pair) for every tile that the host cannot rule out, and the call waits for nothing.
+//   - Tiles take different times (groups' rows differ), so none is anybody's beforehand: a CTA that has begun to load one asks for another CTA of the grid
+//     that has not been launched, computes its tile in its place, and tells its warps (of a pair, both CTAs') by a ring of tile numbers.
 //   - Products of rows (the forward ones and dX) have the weights as the instruction's 128 or 256 rows and the group's rows as its columns, of which there
 //     may be any multiple of 16 up to 256: a group's last tile then costs what it has, where 256 rows a tile would be half empty in groups of some
 //     hundred.  A group's tiles are made as alike as multiples of 16 allow.  The accumulator is the result's transpose: a lane has a channel of 32 rows, and
@@ -53,8 +55,9 @@ constexpr int kStagingBytes = kEpiWarps * kBlockBytes;         // (of gradients 
 constexpr int kABytes = kBM * kRowBytes;           // of one of the weights, or of a CTA's rows, in a stage
 constexpr int kGatedAt = 128;                      // where the second product's columns are in an accumulator
 constexpr int kBarrierBytes = 1024;
+constexpr int kSlots = 4;                          // tiles that the warps are told of ahead
 constexpr int kSmemLimit = 232448;
-static_assert((4 * kMaxStages + 5) * 8 <= kBarrierBytes, "barriers");
+static_assert((4 * kMaxStages + 5 + 2 * kSlots + 1) * 8 + 16 + 16 * kSlots <= kBarrierBytes, "barriers");
 
 struct Params {
     int rows, groups;
@@ -166,14 +169,16 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
     uint64_t *bars = reinterpret_cast<uint64_t *>(staging + (kGrad ? kStagingBytes : 0));
     uint64_t *full = bars, *empty = bars + kMaxStages, *tail_full = bars + 2 * kMaxStages, *cleared = bars + 3 * kMaxStages;
     uint64_t *tmem_full = bars + 4 * kMaxStages, *tmem_empty = tmem_full + 2;
-    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(tmem_empty + 2);
+    uint64_t *slot_full = tmem_empty + 2, *slot_empty = slot_full + kSlots, *answer_here = slot_empty + kSlots;
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(answer_here + 1);
+    uint4 *slots = reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(bars) + kBarrierBytes) - kSlots, *answer = slots - 1;
     Groups groups;
     groups.first = reinterpret_cast<int *>(reinterpret_cast<uint8_t *>(bars) + kBarrierBytes);
     groups.tiles = groups.first + p.groups + 1;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = kCtas == 2 ? (int)cluster_ctarank() : 0;
-    const int unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
+    const int unit = blockIdx.x / kCtas;
     TileAt at;
 
     if (threadIdx.x == 0) {
@@ -187,6 +192,12 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             mbar_init(&tmem_full[a], 1);
             mbar_init(&tmem_empty[a], kEpiWarps * kCtas);
         }
+        for (int i = 0; i < kSlots; ++i) {
+            mbar_init(&slot_full[i], 1);
+            // (the even CTA's, which counts all that are told: epilogue, clearing warp, MMA issuer, the other CTA's producer)
+            mbar_init(&slot_empty[i], (kEpiWarps + (kGrad ? 1 : 0)) * kCtas + kCtas);
+        }
+        mbar_init(answer_here, 1);
         mbar_fence_init();
         prefetch_tmap(kGrad && !p.with_x ? &maps.X : &maps.W[0]);
         if (kGated) prefetch_tmap(&maps.W[1]);
@@ -238,6 +249,24 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
     // Whether a tile's last stage ends inside the next group's rows, where it is not by 16 rows that it does
     auto has_tail = [&](const TileAt &t) { return kGrad && !t.x && (t.rows & 15) != 0; };
 
+    // The tile after this one, as the even CTA's producer says it; -1: none.  (By a warp's lanes, or the one that issues MMAs.  Nobody has more tiles than
+    // there are: that ends the loops where a wait has run out, too.)
+    const uint32_t told_back = kCtas == 2 ? map_to_cta(smem_u32(&slot_empty[0]), 0) : 0u;
+    int slot = 0, left = (int)gridDim.x;
+    uint32_t slot_phase = 0;
+    auto next_tile = [&](bool by_warp) {
+        if (kCtas == 2) mbar_wait_cluster(&slot_full[slot], slot_phase, p.err, 8);
+        else mbar_wait(&slot_full[slot], slot_phase, p.err, 8);
+        const int t = *reinterpret_cast<volatile int *>(&slots[slot]);
+        if (by_warp) __syncwarp();
+        if (!by_warp || lane == 0) {
+            if (kCtas == 2) mbar_arrive_remote(told_back + (uint32_t)slot * 8u);
+            else mbar_arrive(&slot_empty[slot]);
+        }
+        if (++slot == kSlots) { slot = 0; slot_phase ^= 1; }
+        return --left > 0 ? t : -1;
+    };
+
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer: every lane with a copy of its own per stage
         int stage = 0;
@@ -245,7 +274,27 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
         const uint32_t full_issuer = kCtas == 2 ? map_to_cta(smem_u32(&full[0]), 0) : 0u;
         const uint32_t tail_own = kCtas == 2 ? map_to_cta(smem_u32(&tail_full[0]), (uint32_t)rank) : 0u;
         const int bnh = p.BN / kCtas;
-        for (int n = unit; tile_at<kMode>(p, groups, n, at); n += units) {
+        uint32_t answer_phase = 0;
+        auto ask = [&]() {
+            if (lane == 0) {
+                fence_proxy_async_smem();              // (the last answer has been read)
+                mbar_arrive_expect_tx(answer_here, 16);
+                ask_for_block(answer, answer_here);
+            }
+            __syncwarp();
+        };
+        auto granted = [&]() {
+            mbar_wait(answer_here, answer_phase, p.err, 9);
+            answer_phase ^= 1;
+            const int block = granted_block(answer);
+            __syncwarp();
+            return block < 0 || --left <= 0 ? -1 : block / kCtas;
+        };
+        int t = unit;
+        while (t >= 0) {
+            const bool some = tile_at<kMode>(p, groups, t, at);
+            if (!some) break;
+            if (rank == 0) ask();
             // Tiles of rows: the weights in one copy (each of the gated block's two), for dX in two of 64 columns; then this CTA's rows, in one copy or
             // where they are few in one or two small ones.  Gradients of weights: copies of 64 channels and 64 columns by 64 rows.
             const int half_rows = ((at.rows + 15) / 16 * 16) / kCtas;
@@ -309,6 +358,35 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 __syncwarp();
                 load(tail_own, tail_full);
             }
+            // The next tile
+            if (rank == 0) {
+                t = granted();
+                TileAt after;
+                const int told = t >= 0 && tile_at<kMode>(p, groups, t, after) ? t : -1;
+                if (kCtas == 2) mbar_wait_cluster(&slot_empty[slot], slot_phase ^ 1, p.err, 10);
+                else mbar_wait(&slot_empty[slot], slot_phase ^ 1, p.err, 10);
+                if (lane == 0) {
+                    if (kCtas == 2) {
+                        mbar_arrive_expect_tx(&slot_full[slot], 16);
+                        for (uint32_t r = 0; r < 2; ++r)
+                            st_async_v4(map_to_cta(smem_u32(&slots[slot]), r), (uint32_t)told, 0u, 0u, 0u, map_to_cta(smem_u32(&slot_full[slot]), r));
+                    } else {
+                        *reinterpret_cast<volatile int *>(&slots[slot]) = told;
+                        mbar_arrive(&slot_full[slot]);
+                    }
+                }
+                __syncwarp();
+                if (++slot == kSlots) { slot = 0; slot_phase ^= 1; }
+            } else {
+                if (lane == 0) mbar_arrive_expect_tx(&slot_full[slot], 16);
+                __syncwarp();
+                t = next_tile(true);
+            }
+        }
+        // CTAs behind the last tile, for groups' tiles that might have been: taken over rather than launched
+        while (rank == 0 && t >= 0) {
+            ask();
+            t = granted();
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer (of a pair: the even CTA)
@@ -322,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), a_lo = (uint32_t)a_tmpl | ((smem_u32(stages) >> 4) & 0x3FFFu);
             const uint32_t b_base = ((smem_u32(stages) + p.b_at) >> 4) & 0x3FFFu, stage16 = p.stage_bytes >> 4;
             constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kA16 = kGrad ? kMn16 : kK16;
-            for (int n = unit; tile_at<kMode>(p, groups, n, at); n += units) {
+            for (int t = unit; t >= 0 && tile_at<kMode>(p, groups, t, at); t = next_tile(false)) {
                 if (at.kb == 0) continue;              // a group without rows
                 const bool b_mn = kGrad && !at.x, tail = has_tail(at);
                 const uint64_t b_tmpl = b_mn ? mn_tmpl : k_tmpl;
@@ -381,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             uint32_t clear_phase = 0;
             const uint32_t cleared_issuer = kCtas == 2 ? map_to_cta(smem_u32(&cleared[0]), 0) : 0u;
             const int boxes = kBM / kBox + p.BN / kCtas / kBox;
-            for (int n = unit; tile_at<kMode>(p, groups, n, at); n += units) {
+            for (int t = unit; t >= 0 && tile_at<kMode>(p, groups, t, at); t = next_tile(true)) {
                 if (at.kb == 0) continue;
                 stage += at.kb - 1;
                 stage %= p.num_stages;
@@ -412,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
         int acc = 0;
         uint32_t acc_phase = 0;
         const uint32_t peer_tmem_empty = kCtas == 2 ? map_to_cta(smem_u32(&tmem_empty[0]), 0) : 0u;
-        for (int n = unit; tile_at<kMode>(p, groups, n, at); n += units) {
+        for (int t = unit; t >= 0 && tile_at<kMode>(p, groups, t, at); t = next_tile(true)) {
             const bool some = at.kb > 0;
             if (some) {
                 mbar_wait(&tmem_full[acc], acc_phase, p.err, 4);
@@ -586,32 +664,6 @@ struct Tile {
 bool tile_allowed(int mode, Tile t) {
     return (t.ctas == 1 || t.ctas == 2) && t.rows >= 16 && t.rows % 16 == 0 && t.rows <= (mode == kGroupedGated ? 128 : 128 * t.ctas);
 }
-// CTA pairs that run at once, asked of the device's occupancy once
-int max_pairs() {
-    static std::atomic<int> cached{-1};
-    int n = cached.load(std::memory_order_acquire);
-    if (n >= 0) return n;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * 148);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmemLimit;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    n = 0;
-    const Kernel kernel = kernel_for<2>(kGroupedPlain);
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
-        cudaGetLastError();
-        n = tc_host::num_sms() / 2;
-    }
-    cached.store(n, std::memory_order_release);
-    return n;
-}
 Tile pick_tile(const GroupedProblem &d) {
     // "<CTAs>x<rows>" in ONNXB_GROUPED_TILE pins the shape for A/B measurements and tests
     if (const char *e = getenv("ONNXB_GROUPED_TILE")) {
@@ -666,7 +718,7 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     const long long w_total = (long long)d.groups * p.w_count * p.w_tiles_m * p.w_tiles_n;
     // tiles of rows: at most one more for each group than whole ones
     const long long row_tiles = grad && !p.with_x ? 0 : d.rows / tile.rows + std::min(d.groups, d.rows), most = row_tiles * p.tiles_n + w_total;
-    if (most > 0x7fffffffLL / 2 || (long long)p.band * std::max(p.tiles_n, p.w_tiles_n) > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
+    if (most > 0x7fffffffLL / 4 || (long long)p.band * std::max(p.tiles_n, p.w_tiles_n) > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
     p.w_total = (int)w_total;
     p.b_at = (uint32_t)(gated ? 2 * kABytes : kABytes);
     // (B: the rows of a CTA's part of a tile, or of the gradients of weights its columns)
@@ -706,7 +758,7 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     const Kernel kernel = tile.ctas == 2 ? kernel_for<2>(d.mode) : kernel_for<1>(d.mode);
     const cudaError_t attr_err = allow_shared_memory(kernel, (tile.ctas - 1) * 3 + d.mode);
     if (attr_err != cudaSuccess) return (int)attr_err;
-    const int units = tile.ctas == 2 ? max_pairs() : num_sms(), grid = (int)std::min<long long>(most, units) * tile.ctas;
+    const int grid = (int)most * tile.ctas;
     const cudaError_t e = tile.ctas == 2 ? launch_pdl_cluster(kernel, 2u, dim3(grid), dim3(kThreads), smem, stream, maps, p)
                                          : launch_pdl(kernel, dim3(grid), dim3(kThreads), smem, stream, maps, p);
     count_launch();
