@@ -14,8 +14,10 @@
 //   - Products of rows (the forward ones and dX) have the weights as the instruction's 128 or 256 rows and the group's rows as its columns, of which there
 //     may be any multiple of 16 up to 256: a group's last tile then costs what it has, where 256 rows a tile would be half empty in groups of some
 //     hundred.  A group's tiles are made as alike as multiples of 16 allow.  The accumulator is the result's transpose: a lane has a channel of 32 rows, and
-//     trades every other one with its neighbour, so that both store two channels of 16 rows, 64 bytes of each row a warp.  The gated block has two such
-//     products of the same rows, of up to 128, side by side in the accumulator.
+//     trades every other one with its neighbour, so that both store two channels of 16 rows, 64 bytes of each row a warp.
+//   - The gated block is one such product: of a CTA's 128 rows of weights 64 are Wg's and 64 Wu's of the same channels, so that a channel's gate and other
+//     factor are lanes of two warps, each of which gives the other half of its rows and computes the other half's results.  (Two products side by side in the
+//     accumulator instead, of up to 128 rows each, read 40 KB for what takes 32 so: 16384 x 2048 x 1408 of 64 groups 223 us, L2 at its limit.)
 //   - A copy of a group's last rows may bring the next group's too: they are columns of the accumulator that nobody stores.  Weights are three-dimensional
 //     tensors to TMA, so that what lies behind a group's last channel is zeros.
 //   - The gradients of the weights sum over a group's rows, which end inside a stage.  There, rows of the next group would be terms of the sum, and if
@@ -28,6 +30,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdlib>
+#include <type_traits>
 
 #include "dense_math.cuh"
 #include "grouped.h"
@@ -51,9 +54,8 @@ constexpr int kMaxStages = 24;
 constexpr int kThreads = 352;
 constexpr int kEpiWarps = 8;
 constexpr int kBlockBytes = 32 * kRowBytes;        // what an epilogue warp lays out: 32 rows of 128 bytes
-constexpr int kStagingBytes = kEpiWarps * kBlockBytes;         // (of gradients of weights alone)
-constexpr int kABytes = kBM * kRowBytes;           // of one of the weights, or of a CTA's rows, in a stage
-constexpr int kGatedAt = 128;                      // where the second product's columns are in an accumulator
+constexpr int kStagingBytes = kEpiWarps * kBlockBytes;         // (not of plain forward products)
+constexpr int kABytes = kBM * kRowBytes;           // of A in a stage; B is behind it
 constexpr int kBarrierBytes = 1024;
 constexpr int kSlots = 4;                          // tiles that the warps are told of ahead
 constexpr int kSmemLimit = 232448;
@@ -63,8 +65,8 @@ struct Params {
     int rows, groups;
     const int *offsets;
     int channels, width;
-    int most_rows;                 // of a tile of rows: columns of an accumulator (of the gated block: of one of its two)
-    int tiles_n, band;             // of the results' columns, 128 or 256 of them a tile
+    int most_rows;                 // of a tile of rows: columns of an accumulator
+    int tiles_n, band;             // of the results' columns, 128 or 256 of them a tile (half as many of the gated block's)
     int num_kb;                    // stages of the reduction; of one term of dX's
     int b_box;                     // rows of a small copy of rows
     int terms, with_x;             // kGroupedGrad: terms; dX is wanted
@@ -73,7 +75,7 @@ struct Params {
     int w_first, w_count;          // the first that is wanted; how many are
     int num_stages;
     uint32_t idesc_x, idesc_w;     // (of tiles of rows without their columns)
-    uint32_t stage_bytes, b_at;    // where B begins in a stage
+    uint32_t stage_bytes;
     int bf16, activation, outs;    // outs: results of a tile (the gated block: H alone, or H, G and U)
     void *Y[3];
     long long y_ld[3];
@@ -85,7 +87,7 @@ struct Params {
 };
 
 struct Maps {
-    CUtensorMap W[2];              // weights, boxes of 128 channels (for dX of 64)
+    CUtensorMap W[2];              // weights, boxes of 128 channels (of 64 where a stage has two)
     CUtensorMap R[2], R_small[2];  // rows (X, or dY or dG and dU), boxes of 128 and of b_box rows
     CUtensorMap D[2], X;           // rows as terms of the weights' gradients, boxes of 64
 };
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t *stages = smem;
     uint8_t *staging = smem + (size_t)p.num_stages * p.stage_bytes;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + (kGrad ? kStagingBytes : 0));
+    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + (kMode != kGroupedPlain ? kStagingBytes : 0));
     uint64_t *full = bars, *empty = bars + kMaxStages, *tail_full = bars + 2 * kMaxStages, *cleared = bars + 3 * kMaxStages;
     uint64_t *tmem_full = bars + 4 * kMaxStages, *tmem_empty = tmem_full + 2;
     uint64_t *slot_full = tmem_empty + 2, *slot_empty = slot_full + kSlots, *answer_here = slot_empty + kSlots;
@@ -295,17 +297,17 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             const bool some = tile_at<kMode>(p, groups, t, at);
             if (!some) break;
             if (rank == 0) ask();
-            // Tiles of rows: the weights in one copy (each of the gated block's two), for dX in two of 64 columns; then this CTA's rows, in one copy or
+            // Tiles of rows: the weights in one copy, or in two of 64 (the gated block's channels of each, dX's columns); then this CTA's rows, in one copy or
             // where they are few in one or two small ones.  Gradients of weights: copies of 64 channels and 64 columns by 64 rows.
             const int half_rows = ((at.rows + 15) / 16 * 16) / kCtas;
             const bool small = at.x && half_rows <= 2 * p.b_box;
             const int na = kMode == kGroupedPlain ? 1 : 2;
             const int nb = !at.x ? bnh / kBox : small ? (half_rows + p.b_box - 1) / p.b_box : 1;
-            const int a_box_bytes = kGrad ? kBoxBytes : kABytes, b_box_bytes = !at.x ? kBoxBytes : (small ? p.b_box : kBM) * kRowBytes;
+            const int a_box_bytes = kMode != kGroupedPlain ? kBoxBytes : kABytes, b_box_bytes = !at.x ? kBoxBytes : (small ? p.b_box : kBM) * kRowBytes;
             const uint32_t bytes = (uint32_t)(na * a_box_bytes + nb * b_box_bytes);
             const bool is_a = lane < na, active = lane < na + nb;
             const int piece = is_a ? lane : lane - na;
-            const uint32_t dst_off = is_a ? (uint32_t)(piece * a_box_bytes) : p.b_at + (uint32_t)(piece * b_box_bytes);
+            const uint32_t dst_off = is_a ? (uint32_t)(piece * a_box_bytes) : kABytes + (uint32_t)(piece * b_box_bytes);
             // The map, and where the copy begins: weights (term, channel, group), or for dX (column, channel, group); rows (term, row, 0), or as
             // terms themselves (channel or column, row, 0).  From stage to stage one of the first two moves on.
             const CUtensorMap *map;
@@ -313,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             const bool second = at.x ? kGrad && is_a : true;
             if (at.x) {
                 map = !is_a ? (small ? &maps.R_small[0] : &maps.R[0]) : kGated ? &maps.W[piece & 1] : &maps.W[0];
-                const int along = !is_a ? at.row0 + rank * half_rows + piece * p.b_box : (at.tn * kCtas + rank) * kBM + (kGrad ? piece * kBox : 0);
+                const int along = !is_a ? at.row0 + rank * half_rows + piece * p.b_box : (at.tn * kCtas + rank) * (kGated ? kBox : kBM) + (kGrad ? piece * kBox : 0);
                 c0 = second ? along : 0;
                 c1 = second ? 0 : along;
                 c2 = is_a ? at.g : 0;
@@ -398,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             const uint64_t k_tmpl = make_smem_desc(0, 16, 1024, kSwizzle128B), mn_tmpl = make_smem_desc(0, kBoxBytes, 1024, kSwizzle128B);
             const uint64_t a_tmpl = kGrad ? mn_tmpl : k_tmpl;
             const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), a_lo = (uint32_t)a_tmpl | ((smem_u32(stages) >> 4) & 0x3FFFu);
-            const uint32_t b_base = ((smem_u32(stages) + p.b_at) >> 4) & 0x3FFFu, stage16 = p.stage_bytes >> 4;
+            const uint32_t b_base = ((smem_u32(stages) + kABytes) >> 4) & 0x3FFFu, stage16 = p.stage_bytes >> 4;
             constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kA16 = kGrad ? kMn16 : kK16;
             for (int t = unit; t >= 0 && tile_at<kMode>(p, groups, t, at); t = next_tile(false)) {
                 if (at.kb == 0) continue;              // a group without rows
@@ -415,11 +417,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 uint32_t accumulate = 0;
                 auto multiply = [&](uint32_t k) {
                     const uint32_t al = a_lo + (uint32_t)stage * stage16 + k * kA16, bl = b_lo + (uint32_t)stage * stage16 + k * b16;
-#pragma unroll
-                    for (uint32_t w = 0; w < (kGated ? 2u : 1u); ++w) {
-                        if (kCtas == 2) mma_f16_lohi_pair(d_tmem + w * kGatedAt, al + w * (kABytes >> 4), a_hi, bl, b_hi, idesc, accumulate);
-                        else mma_f16_lohi(d_tmem + w * kGatedAt, al + w * (kABytes >> 4), a_hi, bl, b_hi, idesc, accumulate);
-                    }
+                    if (kCtas == 2) mma_f16_lohi_pair(d_tmem, al, a_hi, bl, b_hi, idesc, accumulate);
+                    else mma_f16_lohi(d_tmem, al, a_hi, bl, b_hi, idesc, accumulate);
                     accumulate = 1;
                 };
                 auto done = [&]() {
@@ -470,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                     const int from = at.rows - (at.kb - 1) * kTerms, pieces = ((from + 15) / 16 * 16 - from) * 8;
                     uint8_t *first = stages + (size_t)stage * p.stage_bytes + from * kRowBytes;
                     for (int b = 0; b < boxes; ++b) {
-                        uint8_t *box = first + (b < kBM / kBox ? b * kBoxBytes : (int)p.b_at + (b - kBM / kBox) * kBoxBytes);
+                        uint8_t *box = first + b * kBoxBytes;
                         for (int i = lane; i < pieces; i += 32) *reinterpret_cast<uint4 *>(box + i * 16) = make_uint4(0, 0, 0, 0);
                     }
                     fence_proxy_async_smem();
@@ -506,53 +505,77 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                     for (int i = 0; i < 16; ++i) h[i] = pack<__half2>(lo[i], hi[i]);
                 }
             };
-            if (!kGrad || at.x) {
-                // Lanes are channels (columns of the result), columns rows.  The two warps of a quarter share blocks of 32 rows of all results in turns.
-                const int all = kGrad ? p.width : p.channels, channel0 = (at.tn * kCtas + rank) * kBM + q * 32, mine = channel0 + (lane & ~1);
-                const int blocks = channel0 < all ? (at.rows + 31) / 32 : 0, odd = lane & 1;
+            // Stores rows `first` to first + kRows - 1 of the tile (those that there are) of a result, 32 channels a warp from channel0 on; `value`: a lane's channel's.
+            // Of rows 2 i and 2 i + 1 an even lane keeps the first and an odd one the second, each of its own channel and its neighbour's.
+            auto store = [&](int which, int first, int channel0, int all, auto rows_of_value, auto value) {
+                constexpr int kPairs = decltype(rows_of_value)::value / 2;
+                const int odd = lane & 1, mine = channel0 + (lane & ~1), rows = at.rows - first - odd;
+                uint32_t h[kPairs];
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) {
+                    const float a = value(2 * i), b = value(2 * i + 1), other = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
+                    const float lo = odd ? other : a, hi = odd ? b : other;
+                    h[i] = p.bf16 ? pack<__nv_bfloat162>(lo, hi) : pack<__half2>(lo, hi);
+                }
+                const long long ld = p.y_ld[which];
+                uint16_t *out = static_cast<uint16_t *>(p.Y[which]) + (at.row0 + first + odd) * ld + mine;
+                if (p.y_pairs[which] && mine + 2 <= all) {
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i)
+                        if (2 * i < rows) *reinterpret_cast<uint32_t *>(out + 2 * i * ld) = h[i];
+                } else if (mine < all) {
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i)
+                        if (2 * i < rows) {
+                            out[2 * i * ld] = (uint16_t)h[i];
+                            if (mine + 1 < all) out[2 * i * ld + 1] = (uint16_t)(h[i] >> 16);
+                        }
+                }
+            };
+            if (kGated) {
+                // Lanes are channels, 64 of the gate and the same 64 of the other factor, columns rows.  The two warps that have the same 32 channels' go through
+                // the blocks of 32 rows together; of every quarter two share them in turns.
+                const int channel0 = (at.tn * kCtas + rank) * kBox + (q & 1) * 32, blocks = channel0 < p.channels ? (at.rows + 31) / 32 : 0;
+                const bool up = q >= 2;
+                const std::integral_constant<int, 32> kAll;
+                const std::integral_constant<int, 16> kHalf;
+                float *given = reinterpret_cast<float *>(buf) + lane;
+                const float *got = reinterpret_cast<const float *>(staging + ((warp - 2) ^ 2) * kBlockBytes) + lane;
 #pragma unroll 1
-                for (int item = half; item < blocks * p.outs; item += 2) {
-                    const int which = item < blocks ? 0 : item < 2 * blocks ? 1 : 2, first = (item - which * blocks) * 32;
+                for (int b = half, turn = 0; b < blocks; b += 2, turn ^= 512) {
                     uint32_t v[32];
-                    tmem_ld_32x32(tbase + (uint32_t)(which == 2 ? kGatedAt + first : first), v);
-                    if (kGated && which == 0) {
-                        uint32_t w[32];
-                        tmem_ld_32x32(tbase + (uint32_t)(kGatedAt + first), w);
-                        tmem_ld_wait();
-#define ONNXB_GATE(kind) _Pragma("unroll") for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(activate(kind, __uint_as_float(v[j])) * __uint_as_float(w[j]))
-                        if (p.activation == ONNXB_SILU) { ONNXB_GATE(ONNXB_SILU); }
-                        else if (p.activation == ONNXB_GELU) { ONNXB_GATE(ONNXB_GELU); }
-                        else if (p.activation == ONNXB_GELU_TANH) { ONNXB_GATE(ONNXB_GELU_TANH); }
-                        else { ONNXB_GATE(ONNXB_RELU); }
-#undef ONNXB_GATE
-                    } else {
-                        tmem_ld_wait();
-                    }
-                    // of rows 2 i and 2 i + 1 an even lane keeps the first and an odd one the second, each of its own channel and its neighbour's
-                    float lo[16], hi[16];
+                    tmem_ld_32x32(tbase + (uint32_t)(b * 32), v);
+                    tmem_ld_wait();
+                    // of the other warp's results' rows, what it needs (in turns: it may still read what was given last)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) given[turn + i * 32] = __uint_as_float(up ? v[i] : v[16 + i]);
+                    if (p.outs == 3) store(up ? 2 : 1, b * 32, channel0, p.channels, kAll, [&](int i) { return __uint_as_float(v[i]); });
+                    asm volatile("bar.sync %0, 64;" ::"r"(1 + half * 2 + (q & 1)) : "memory");
+                    float g[16], u[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? v[2 * i] : v[2 * i + 1], 1);
-                        lo[i] = __uint_as_float(odd ? other : v[2 * i]);
-                        hi[i] = __uint_as_float(odd ? v[2 * i + 1] : other);
+                        const float own = __uint_as_float(up ? v[16 + i] : v[i]), other = got[turn + i * 32];
+                        g[i] = up ? other : own;
+                        u[i] = up ? own : other;
                     }
-                    uint32_t h[16];
-                    words_of(lo, hi, h);
-                    const int rows = at.rows - first - odd;                // (of those from this lane's first on)
-                    const long long ld = p.y_ld[which];
-                    uint16_t *out = static_cast<uint16_t *>(p.Y[which]) + (at.row0 + first + odd) * ld + mine;
-                    if (p.y_pairs[which] && mine + 2 <= all) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (2 * i < rows) *reinterpret_cast<uint32_t *>(out + 2 * i * ld) = h[i];
-                    } else if (mine < all) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (2 * i < rows) {
-                                out[2 * i * ld] = (uint16_t)h[i];
-                                if (mine + 1 < all) out[2 * i * ld + 1] = (uint16_t)(h[i] >> 16);
-                            }
-                    }
+#define ONNXB_GATE(kind) _Pragma("unroll") for (int i = 0; i < 16; ++i) g[i] = activate(kind, g[i]) * u[i]
+                    if (p.activation == ONNXB_SILU) { ONNXB_GATE(ONNXB_SILU); }
+                    else if (p.activation == ONNXB_GELU) { ONNXB_GATE(ONNXB_GELU); }
+                    else if (p.activation == ONNXB_GELU_TANH) { ONNXB_GATE(ONNXB_GELU_TANH); }
+                    else { ONNXB_GATE(ONNXB_RELU); }
+#undef ONNXB_GATE
+                    store(0, b * 32 + (up ? 16 : 0), channel0, p.channels, kHalf, [&](int i) { return g[i]; });
+                }
+            } else if (!kGrad || at.x) {
+                // Lanes are channels (columns of the result), columns rows.  The two warps of a quarter share blocks of 32 rows in turns.
+                const int all = kGrad ? p.width : p.channels, channel0 = (at.tn * kCtas + rank) * kBM + q * 32, blocks = channel0 < all ? (at.rows + 31) / 32 : 0;
+                const std::integral_constant<int, 32> kAll;
+#pragma unroll 1
+                for (int b = half; b < blocks; b += 2) {
+                    uint32_t v[32];
+                    tmem_ld_32x32(tbase + (uint32_t)(b * 32), v);
+                    tmem_ld_wait();
+                    store(0, b * 32, channel0, all, kAll, [&](int i) { return __uint_as_float(v[i]); });
                 }
             } else {
                 // Lanes are channels (rows of the gradient), columns its columns.  The two warps of a quarter share its blocks of 64 columns in turns.
@@ -661,18 +684,18 @@ long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 struct Tile {
     int ctas, rows;
 };
-bool tile_allowed(int mode, Tile t) {
-    return (t.ctas == 1 || t.ctas == 2) && t.rows >= 16 && t.rows % 16 == 0 && t.rows <= (mode == kGroupedGated ? 128 : 128 * t.ctas);
+bool tile_allowed(Tile t) {
+    return (t.ctas == 1 || t.ctas == 2) && t.rows >= 16 && t.rows % 16 == 0 && t.rows <= 128 * t.ctas;
 }
 Tile pick_tile(const GroupedProblem &d) {
     // "<CTAs>x<rows>" in ONNXB_GROUPED_TILE pins the shape for A/B measurements and tests
     if (const char *e = getenv("ONNXB_GROUPED_TILE")) {
         const Tile t{e[0] - '0', e[0] && e[1] == 'x' ? atoi(e + 2) : 0};
-        if (tile_allowed(d.mode, t)) return t;
+        if (tile_allowed(t)) return t;
     }
     const long long per_group = d.rows / std::min(d.rows, d.groups);
     const int ctas = per_group > 64 ? 2 : 1;
-    return Tile{ctas, std::min(d.mode == kGroupedGated ? 128 : 128 * ctas, (d.rows + 15) / 16 * 16)};
+    return Tile{ctas, std::min(128 * ctas, (d.rows + 15) / 16 * 16)};
 }
 
 // Rows that begin at multiples of 16 bytes, as (terms, rows, 1) in boxes of 64 by `box`; groups' weights as (terms, channels, groups).  (Of three dimensions
@@ -702,7 +725,7 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     p.rows = d.rows; p.groups = d.groups; p.offsets = d.offsets;
     p.channels = d.channels; p.width = d.width;
     p.most_rows = tile.rows;
-    const int columns = kBM * tile.ctas;                   // of a tile of rows
+    const int columns = (gated ? kBox : kBM) * tile.ctas;  // of a tile of rows
     p.tiles_n = (int)ceil_div(grad ? d.width : d.channels, columns);
     p.band = 8;
     p.num_kb = (int)ceil_div(grad ? d.channels : d.width, kTerms);
@@ -720,11 +743,10 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     const long long row_tiles = grad && !p.with_x ? 0 : d.rows / tile.rows + std::min(d.groups, d.rows), most = row_tiles * p.tiles_n + w_total;
     if (most > 0x7fffffffLL / 4 || (long long)p.band * std::max(p.tiles_n, p.w_tiles_n) > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
     p.w_total = (int)w_total;
-    p.b_at = (uint32_t)(gated ? 2 * kABytes : kABytes);
     // (B: the rows of a CTA's part of a tile, or of the gradients of weights its columns)
     const int b_rows = grad ? kBM : std::max(tile.rows / tile.ctas > 2 * p.b_box ? kBM : 0, 2 * p.b_box);
-    p.stage_bytes = p.b_at + (uint32_t)(b_rows * kRowBytes);
-    const int table = ((2 * d.groups + 2) * 4 + 15) / 16 * 16, staging = grad ? kStagingBytes : 0;
+    p.stage_bytes = (uint32_t)(kABytes + b_rows * kRowBytes);
+    const int table = ((2 * d.groups + 2) * 4 + 15) / 16 * 16, staging = d.mode != kGroupedPlain ? kStagingBytes : 0;
     p.num_stages = std::min(kMaxStages, (kSmemLimit - 1024 - kBarrierBytes - staging - table) / (int)p.stage_bytes);
     const int bf16 = d.type == ONNXB_BFLOAT16;
     p.idesc_x = make_idesc_f16(kBM * tile.ctas, 0, bf16, grad, 0);
@@ -746,7 +768,7 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     if (!grad || p.with_x) {
         for (int i = 0; i < terms; ++i)
             fine = fine && rows_map(&maps.R[i], d.A[i], d.rows, along, kBM) && rows_map(&maps.R_small[i], d.A[i], d.rows, along, p.b_box);
-        for (int i = 0; i < (gated ? 2 : terms); ++i) fine = fine && weights_map(&maps.W[i], d.W[i], d.groups, d.channels, d.width, grad ? kBox : kBM);
+        for (int i = 0; i < (gated ? 2 : terms); ++i) fine = fine && weights_map(&maps.W[i], d.W[i], d.groups, d.channels, d.width, d.mode != kGroupedPlain ? kBox : kBM);
     }
     if (p.w_count) {
         for (int i = 0; i < terms; ++i) fine = fine && rows_map(&maps.D[i], d.A[i], d.rows, d.channels, kBox);
