@@ -33,6 +33,9 @@ struct GroupedProblem {
     GroupedWeights D[2];                     // (written)
 };
 
+// The forward products of a few rows (grouped_few.cu).  Operands' rows and groups may begin anywhere.
+bool grouped_few_fits(int rows);
+int launch_grouped_few(const GroupedProblem &p, cudaStream_t stream);
 // On the tensor cores (tc_grouped.cu).  Operands' rows and groups begin at multiples of 16 bytes.
 int launch_tc_grouped(const GroupedProblem &p, cudaStream_t stream);
 

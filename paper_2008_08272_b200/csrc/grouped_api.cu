@@ -74,9 +74,13 @@ onnxb_status check_space(const void *workspace, size_t bytes, size_t need) { ret
 
 }  // namespace
 
-extern "C" size_t onnx_grouped_gemm_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *W) { return views::copy_bytes(X) + copy_bytes(W); }
+// (few rows are taken from wherever they and the weights begin)
+static bool few(const onnxb_matrix *X) { return X && X->rows >= 1 && X->rows <= kMostSize && grouped_few_fits((int)X->rows); }
+extern "C" size_t onnx_grouped_gemm_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *W) {
+    return few(X) ? 0 : views::copy_bytes(X) + copy_bytes(W);
+}
 extern "C" size_t onnx_grouped_gated_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu) {
-    return views::copy_bytes(X) + copy_bytes(Wg) + copy_bytes(Wu);
+    return few(X) ? 0 : views::copy_bytes(X) + copy_bytes(Wg) + copy_bytes(Wu);
 }
 
 // Both forward products: Wu NULL for the plain one
@@ -111,6 +115,12 @@ static onnxb_status forward(const onnxb_matrix *X, const onnxb_matrices *Wg, con
     d.activation = activation;
     const onnxb_matrix *outs[3] = {H, G, U};
     for (int i = 0; i < 3 && outs[i]; ++i) { d.Y[i] = outs[i]->data; d.y_ld[i] = operand(outs[i]).ld; }
+    if (few(X)) {
+        d.A[0] = operand(X);
+        d.W[0] = weights(Wg);
+        if (gated) d.W[1] = weights(Wu);
+        return status_of(launch_grouped_few(d, stream));
+    }
     Placement placed(workspace);
     d.A[0] = placed(X);
     d.W[0] = place(placed, Wg);

@@ -2,7 +2,8 @@
 // onnx_grouped_gated_run, and the products of their gradients.
 //
 // The pipeline is that of tc_dense.cu: a persistent CTA (or a pair of two on one tile) per SM,
-//   warp 0    TMA producer, a ring of stages of 64 terms of the reduction;
+//   warp 0    TMA producer, a ring of stages of one or two K blocks (64 terms of the reduction each): a stage costs its two single threads 240 cycles, and
+//             170 more for each block;
 //   warp 1    one thread issues tcgen05.mma kind::f16 into one of two TMEM accumulators;
 //   warps 2-9 epilogue: tcgen05.ld, the mathematics, stores;
 //   warp 10   clears what a stage holds of the next group's rows (below).
@@ -55,7 +56,7 @@ constexpr int kThreads = 352;
 constexpr int kEpiWarps = 8;
 constexpr int kBlockBytes = 32 * kRowBytes;        // what an epilogue warp lays out: 32 rows of 128 bytes
 constexpr int kStagingBytes = kEpiWarps * kBlockBytes;         // (not of plain forward products)
-constexpr int kABytes = kBM * kRowBytes;           // of A in a stage; B is behind it
+constexpr int kABytes = kBM * kRowBytes;           // of a block of A
 constexpr int kBarrierBytes = 1024;
 constexpr int kSlots = 4;                          // tiles that the warps are told of ahead
 constexpr int kSmemLimit = 232448;
@@ -75,7 +76,9 @@ struct Params {
     int w_first, w_count;          // the first that is wanted; how many are
     int num_stages;
     uint32_t idesc_x, idesc_w;     // (of tiles of rows without their columns)
-    uint32_t stage_bytes;
+    int ks;                        // K blocks of a stage
+    uint32_t stage_bytes, b_at;    // where B begins in a stage
+    int b_block;                   // bytes from a block's rows to the next's
     int bf16, activation, outs;    // outs: results of a tile (the gated block: H alone, or H, G and U)
     void *Y[3];
     long long y_ld[3];
@@ -144,7 +147,7 @@ __device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t,
     place(p.band, p.w_tiles_m, p.w_tiles_n, r - at.z * per, at);
     at.row0 = s.first[at.g];
     at.rows = s.first[at.g + 1] - at.row0;
-    at.kb = (at.rows + kTerms - 1) / kTerms;
+    at.kb = (at.rows + kTerms * p.ks - 1) / (kTerms * p.ks);
     return true;
 }
 
@@ -298,42 +301,50 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             if (!some) break;
             if (rank == 0) ask();
             // Tiles of rows: the weights in one copy, or in two of 64 (the gated block's channels of each, dX's columns); then this CTA's rows, in one copy or
-            // where they are few in one or two small ones.  Gradients of weights: copies of 64 channels and 64 columns by 64 rows.
+            // where they are few in one or two small ones.  Gradients of weights: copies of 64 channels and 64 columns by a stage's terms.  Where a stage has two
+            // blocks a copy brings both, but for those whose rows would not follow one another then: the gated block's weights, and small ones.
             const int half_rows = ((at.rows + 15) / 16 * 16) / kCtas;
             const bool small = at.x && half_rows <= 2 * p.b_box;
-            const int na = kMode == kGroupedPlain ? 1 : 2;
-            const int nb = !at.x ? bnh / kBox : small ? (half_rows + p.b_box - 1) / p.b_box : 1;
+            const int a_boxes = kMode == kGroupedPlain ? 1 : 2, b_boxes = !at.x ? bnh / kBox : small ? (half_rows + p.b_box - 1) / p.b_box : 1;
+            const int na = kGated ? a_boxes * p.ks : a_boxes, nb = small ? b_boxes * p.ks : b_boxes;
             const int a_box_bytes = kMode != kGroupedPlain ? kBoxBytes : kABytes, b_box_bytes = !at.x ? kBoxBytes : (small ? p.b_box : kBM) * kRowBytes;
-            const uint32_t bytes = (uint32_t)(na * a_box_bytes + nb * b_box_bytes);
+            const uint32_t bytes = (uint32_t)(p.ks * (a_boxes * a_box_bytes + b_boxes * b_box_bytes));
             const bool is_a = lane < na, active = lane < na + nb;
-            const int piece = is_a ? lane : lane - na;
-            const uint32_t dst_off = is_a ? (uint32_t)(piece * a_box_bytes) : kABytes + (uint32_t)(piece * b_box_bytes);
-            // The map, and where the copy begins: weights (term, channel, group), or for dX (column, channel, group); rows (term, row, 0), or as
-            // terms themselves (channel or column, row, 0).  From stage to stage one of the first two moves on.
+            const int piece = is_a ? lane : lane - na, boxes = is_a ? a_boxes : b_boxes, box = piece % boxes, block = piece / boxes;
+            const uint32_t dst_off = !is_a ? p.b_at + (uint32_t)(small ? block * p.b_block + box * b_box_bytes : box * b_box_bytes * p.ks)
+                                     : kGated ? (uint32_t)(block * kABytes + box * kBoxBytes) : (uint32_t)(box * a_box_bytes * p.ks);
+            // The map, and where the copy begins: along a K-major reduction by the term, or by the block (the third) in stages of two; weights (term, channel,
+            // block, group), for dX (column, channel, 0, group); rows (term, row, block, 0), or as terms themselves (channel or column, row, 0, 0).
+            // From stage to stage one of the first three moves on.
             const CUtensorMap *map;
-            int c0, c1, c2 = 0;
-            const bool second = at.x ? kGrad && is_a : true;
+            int c0 = 0, c1, c2 = 0, c3 = 0;
+            const bool second = at.x ? kGrad && is_a : true, by_block = !second && p.ks > 1;
             if (at.x) {
-                map = !is_a ? (small ? &maps.R_small[0] : &maps.R[0]) : kGated ? &maps.W[piece & 1] : &maps.W[0];
-                const int along = !is_a ? at.row0 + rank * half_rows + piece * p.b_box : (at.tn * kCtas + rank) * (kGated ? kBox : kBM) + (kGrad ? piece * kBox : 0);
-                c0 = second ? along : 0;
-                c1 = second ? 0 : along;
-                c2 = is_a ? at.g : 0;
+                map = !is_a ? (small ? &maps.R_small[0] : &maps.R[0]) : &maps.W[kGated ? box : 0];
+                c1 = !is_a ? at.row0 + rank * half_rows + box * p.b_box : (at.tn * kCtas + rank) * (kGated ? kBox : kBM);
+                if (second) {
+                    c0 = c1 + box * kBox;
+                    c1 = 0;
+                } else {
+                    c2 = block;
+                }
+                c3 = is_a ? at.g : 0;
             } else {
                 map = is_a ? &maps.D[p.w_first + at.z] : &maps.X;
-                c0 = is_a ? (at.tm * kCtas + rank) * kBM + piece * kBox : at.tn * p.BN + rank * bnh + piece * kBox;
+                c0 = is_a ? (at.tm * kCtas + rank) * kBM + box * kBox : at.tn * p.BN + rank * bnh + box * kBox;
                 c1 = at.row0;
             }
-            const int d0 = second ? 0 : kTerms, d1 = second ? kTerms : 0;
+            const int d0 = second || by_block ? 0 : kTerms, d1 = second ? kTerms * p.ks : 0, d2 = by_block ? p.ks : 0;
             const bool tail = has_tail(at);
             uint8_t *dst = stages + dst_off;
             auto load = [&](uint32_t cluster_bar, uint64_t *own) {
                 if (active) {
-                    if (kCtas == 2) tma_load_3d_pair(dst + (size_t)stage * p.stage_bytes, map, cluster_bar + (uint32_t)stage * 8u, c0, c1, c2);
-                    else tma_load_3d(dst + (size_t)stage * p.stage_bytes, map, own + stage, c0, c1, c2);
+                    if (kCtas == 2) tma_load_4d_pair(dst + (size_t)stage * p.stage_bytes, map, cluster_bar + (uint32_t)stage * 8u, c0, c1, c2, c3);
+                    else tma_load_4d(dst + (size_t)stage * p.stage_bytes, map, own + stage, c0, c1, c2, c3);
                 }
                 c0 += d0;
                 c1 += d1;
+                c2 += d2;
                 if (++stage == p.num_stages) { stage = 0; phase ^= 1; }
             };
             // (dX's second term: the same stages again of the other tensors)
@@ -343,6 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                     map += 1;
                     c0 -= kb_each * d0;
                     c1 -= kb_each * d1;
+                    c2 -= kb_each * d2;
                 }
                 for (int kb = 0; kb < kb_each; ++kb) {
                     mbar_wait(&empty[stage], phase ^ 1, p.err, 1);
@@ -395,28 +407,28 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
         if ((kCtas == 1 || rank == 0) && elect_one()) {
             int stage = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0, clear_phase = 0;        // (the last: a bit for each stage)
-            // K-major: 8-row groups 1024 bytes apart, an instruction 32 bytes further along the swizzled rows.  MN-major: blocks of 64 rows or
-            // columns a box apart, groups of 8 terms 1024 bytes apart, an instruction two of those further.
-            const uint64_t k_tmpl = make_smem_desc(0, 16, 1024, kSwizzle128B), mn_tmpl = make_smem_desc(0, kBoxBytes, 1024, kSwizzle128B);
+            // K-major: 8-row groups 1024 bytes apart, an instruction 32 bytes further along the swizzled rows, a block as far on as its rows take.  MN-major: blocks of
+            // 64 rows or columns a stage's terms of 128 bytes apart, groups of 8 terms 1024 bytes apart, an instruction two of those further.
+            const uint64_t k_tmpl = make_smem_desc(0, 16, 1024, kSwizzle128B), mn_tmpl = make_smem_desc(0, (uint32_t)(kBoxBytes * p.ks), 1024, kSwizzle128B);
             const uint64_t a_tmpl = kGrad ? mn_tmpl : k_tmpl;
             const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), a_lo = (uint32_t)a_tmpl | ((smem_u32(stages) >> 4) & 0x3FFFu);
-            const uint32_t b_base = ((smem_u32(stages) + kABytes) >> 4) & 0x3FFFu, stage16 = p.stage_bytes >> 4;
-            constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kA16 = kGrad ? kMn16 : kK16;
+            const uint32_t b_base = ((smem_u32(stages) + p.b_at) >> 4) & 0x3FFFu, stage16 = p.stage_bytes >> 4;
+            constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kA16 = kGrad ? kMn16 : kK16, kABlock16 = (kGrad ? kBoxBytes : kABytes) >> 4;
             for (int t = unit; t >= 0 && tile_at<kMode>(p, groups, t, at); t = next_tile(false)) {
                 if (at.kb == 0) continue;              // a group without rows
                 const bool b_mn = kGrad && !at.x, tail = has_tail(at);
                 const uint64_t b_tmpl = b_mn ? mn_tmpl : k_tmpl;
-                const uint32_t b_hi = (uint32_t)(b_tmpl >> 32), b_lo = (uint32_t)b_tmpl | b_base, b16 = b_mn ? kMn16 : kK16;
+                const uint32_t b_hi = (uint32_t)(b_tmpl >> 32), b_lo = (uint32_t)b_tmpl | b_base, b16 = b_mn ? kMn16 : kK16, b_block16 = (uint32_t)(b_mn ? kBoxBytes : p.b_block) >> 4;
                 const uint32_t idesc = b_mn ? p.idesc_w : p.idesc_x | ((uint32_t)((at.rows + 15) / 16 * 2) << 17);
-                // instructions of the last stage, where they are not four; stages before it
-                const int last = b_mn ? (at.rows - (at.kb - 1) * kTerms + 15) / 16 : 4, whole = last == 4 && !tail ? at.kb : at.kb - 1;
+                // instructions of the last stage, where they are not four a block; stages before it
+                const int most = 4 * p.ks, last = b_mn ? (at.rows - (at.kb - 1) * kTerms * p.ks + 15) / 16 : most, whole = last == most && !tail ? at.kb : at.kb - 1;
                 if (kCtas == 2) mbar_wait_cluster(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 else mbar_wait(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 tc_fence_after_sync();
                 const uint32_t d_tmem = tmem_base + (uint32_t)acc * kMaxBN;
                 uint32_t accumulate = 0;
-                auto multiply = [&](uint32_t k) {
-                    const uint32_t al = a_lo + (uint32_t)stage * stage16 + k * kA16, bl = b_lo + (uint32_t)stage * stage16 + k * b16;
+                auto multiply = [&](uint32_t s, uint32_t k) {
+                    const uint32_t al = a_lo + (uint32_t)stage * stage16 + s * kABlock16 + k * kA16, bl = b_lo + (uint32_t)stage * stage16 + s * b_block16 + k * b16;
                     if (kCtas == 2) mma_f16_lohi_pair(d_tmem, al, a_hi, bl, b_hi, idesc, accumulate);
                     else mma_f16_lohi(d_tmem, al, a_hi, bl, b_hi, idesc, accumulate);
                     accumulate = 1;
@@ -429,8 +441,9 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 for (int kb = 0; kb < whole; ++kb) {
                     mbar_wait(&full[stage], phase, p.err, 3);
                     tc_fence_after_sync();
+                    for (uint32_t s = 0; s < (uint32_t)p.ks; ++s)
 #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) multiply(k);
+                        for (uint32_t k = 0; k < 4; ++k) multiply(s, k);
                     done();
                 }
                 if (kGrad && whole < at.kb) {
@@ -442,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                     }
                     tc_fence_after_sync();
 #pragma unroll 1
-                    for (uint32_t k = 0; k < (uint32_t)last; ++k) multiply(k);
+                    for (uint32_t k = 0; k < (uint32_t)last; ++k) multiply(k / 4, k % 4);
                     done();
                 }
                 if (kCtas == 2) mma_commit_pair(&tmem_full[acc]);
@@ -466,10 +479,10 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                     mbar_wait(&tail_full[stage], (clear_phase >> stage) & 1u, p.err, 6);
                     clear_phase ^= 1u << stage;
                     // a box has a row of the group's, 64 columns of it, in 128 bytes (the swizzle moves pieces within them)
-                    const int from = at.rows - (at.kb - 1) * kTerms, pieces = ((from + 15) / 16 * 16 - from) * 8;
+                    const int from = at.rows - (at.kb - 1) * kTerms * p.ks, pieces = ((from + 15) / 16 * 16 - from) * 8;
                     uint8_t *first = stages + (size_t)stage * p.stage_bytes + from * kRowBytes;
                     for (int b = 0; b < boxes; ++b) {
-                        uint8_t *box = first + b * kBoxBytes;
+                        uint8_t *box = first + b * kBoxBytes * p.ks;
                         for (int i = lane; i < pieces; i += 32) *reinterpret_cast<uint4 *>(box + i * 16) = make_uint4(0, 0, 0, 0);
                     }
                     fence_proxy_async_smem();
@@ -687,31 +700,50 @@ struct Tile {
 bool tile_allowed(Tile t) {
     return (t.ctas == 1 || t.ctas == 2) && t.rows >= 16 && t.rows % 16 == 0 && t.rows <= 128 * t.ctas;
 }
+// K blocks of a stage.  Two where the reduction along K-major rows (`along`) is whole blocks and the ring still has four stages: tiles of up to 128 rows
+// (gated block of 2 rows 64 -> 60 us; tiles of 256 by 128 rows, 16384 x 2816 x 4096, 370 -> 331, but with three stages tiles of 256 by 256 265 -> 287).
+// Of gradients of weights, whose stages hold as many rows, where groups have some.  ONNXB_GROUPED_KS = 1 or 2 pins it, where the ring has three stages at least.
+int blocks_per_stage(const GroupedProblem &d, int along, int blocks_in_ring) {
+    if (along % kTerms) return 1;
+    if (const char *e = getenv("ONNXB_GROUPED_KS")) return blocks_in_ring >= 6 && e[0] == '2' ? 2 : 1;
+    return blocks_in_ring >= 8 && (d.mode != kGroupedGrad || d.rows / std::min(d.rows, d.groups) >= 256) ? 2 : 1;
+}
 Tile pick_tile(const GroupedProblem &d) {
     // "<CTAs>x<rows>" in ONNXB_GROUPED_TILE pins the shape for A/B measurements and tests
     if (const char *e = getenv("ONNXB_GROUPED_TILE")) {
         const Tile t{e[0] - '0', e[0] && e[1] == 'x' ? atoi(e + 2) : 0};
         if (tile_allowed(t)) return t;
     }
-    const long long per_group = d.rows / std::min(d.rows, d.groups);
-    const int ctas = per_group > 64 ? 2 : 1;
-    return Tile{ctas, std::min(128 * ctas, (d.rows + 15) / 16 * 16)};
+    const int all = (d.rows + 15) / 16 * 16;
+    // The gradients: pairs, and as many rows as they take (32 groups of 4 to 128 rows, 2048 x 1408: a tenth to a fifth faster than one CTA, and no slower with
+    // more rows than groups have).
+    if (d.mode == kGroupedGrad) return Tile{2, std::min(256, all)};
+    // Twice the rows that groups have on average, since some have more (32 groups of 32 rows, 2048 x 1408: gated block in tiles of 32, 64 and 128 rows 66, 60 and 63 us), and
+    // pairs from 33 rows on (64 rows: 68 us in tiles of one CTA, 66 of two); but no fewer tiles than half of the SMs have work with (2048 rows of 8 groups, 7168 x 512:
+    // tiles of 256, 128 and 64 rows 37, 29 and 28 us).
+    const int groups = std::min(d.rows, d.groups), per_group = (d.rows + groups - 1) / groups, ctas = per_group > 32 ? 2 : 1;
+    int rows = 32;
+    while (rows < 128 * ctas && rows < 2 * per_group) rows *= 2;
+    const long long across = ceil_div(d.channels, (d.mode == kGroupedGated ? kBox : kBM) * ctas);
+    while (rows > 64 && groups * ceil_div(per_group, rows) * across * ctas < 74) rows /= 2;
+    return Tile{ctas, std::min(rows, all)};
 }
 
-// Rows that begin at multiples of 16 bytes, as (terms, rows, 1) in boxes of 64 by `box`; groups' weights as (terms, channels, groups).  (Of three dimensions
-// both, so that a stage's copies are one instruction.)
-bool rows_map(CUtensorMap *m, const DenseOperand &o, long long rows, long long cols, int box) {
+// Rows that begin at multiples of 16 bytes, as (terms, rows, 1, 1) in boxes of 64 by `box`; groups' weights as (terms, channels, 1, groups).  Where `blocks` is not 0
+// (terms of a block, rows, blocks, 1) and (terms of a block, channels, blocks, groups), `blocks` of them a copy: of reductions that are whole blocks.
+bool rows_map(CUtensorMap *m, const DenseOperand &o, long long rows, long long cols, int box, int blocks = 0) {
     const uint64_t pitch = (uint64_t)(rows > 1 ? o.ld * 2 : (o.ld * 2 + 15) / 16 * 16);
-    const uint64_t dims[3] = {(uint64_t)cols, (uint64_t)rows, 1}, pitches[2] = {pitch, pitch};
-    const uint32_t boxes[3] = {kTerms, (uint32_t)box, 1};
-    return tc_host::make_tmap_of(2, m, o.p, 3, dims, pitches, boxes, tc_host::kTmapSwizzle128);
+    const uint64_t dims[4] = {(uint64_t)(blocks ? kTerms : cols), (uint64_t)rows, (uint64_t)(blocks ? cols / kTerms : 1), 1};
+    const uint64_t pitches[3] = {pitch, blocks ? (uint64_t)kRowBytes : pitch, pitch};
+    const uint32_t boxes[4] = {kTerms, (uint32_t)box, (uint32_t)(blocks ? blocks : 1), 1};
+    return tc_host::make_tmap_of(2, m, o.p, 4, dims, pitches, boxes, tc_host::kTmapSwizzle128);
 }
-bool weights_map(CUtensorMap *m, const GroupedWeights &w, long long groups, long long channels, long long width, int box) {
+bool weights_map(CUtensorMap *m, const GroupedWeights &w, long long groups, long long channels, long long width, int box, int blocks = 0) {
     const uint64_t pitch = (uint64_t)(channels > 1 ? w.ld * 2 : (width * 2 + 15) / 16 * 16);
-    const uint64_t dims[3] = {(uint64_t)width, (uint64_t)channels, (uint64_t)groups};
-    const uint64_t pitches[2] = {pitch, groups > 1 ? (uint64_t)w.stride * 2 : pitch};
-    const uint32_t boxes[3] = {kTerms, (uint32_t)box, 1};
-    return tc_host::make_tmap_of(2, m, w.p, 3, dims, pitches, boxes, tc_host::kTmapSwizzle128);
+    const uint64_t dims[4] = {(uint64_t)(blocks ? kTerms : width), (uint64_t)channels, (uint64_t)(blocks ? width / kTerms : 1), (uint64_t)groups};
+    const uint64_t pitches[3] = {pitch, blocks ? (uint64_t)kRowBytes : pitch, groups > 1 ? (uint64_t)w.stride * 2 : pitch};
+    const uint32_t boxes[4] = {kTerms, (uint32_t)box, (uint32_t)(blocks ? blocks : 1), 1};
+    return tc_host::make_tmap_of(2, m, w.p, 4, dims, pitches, boxes, tc_host::kTmapSwizzle128);
 }
 bool by_16(const void *p, long long ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; }
 
@@ -728,7 +760,6 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     const int columns = (gated ? kBox : kBM) * tile.ctas;  // of a tile of rows
     p.tiles_n = (int)ceil_div(grad ? d.width : d.channels, columns);
     p.band = 8;
-    p.num_kb = (int)ceil_div(grad ? d.channels : d.width, kTerms);
     // small copies of rows: no more than all the rows that there are
     p.b_box = d.rows <= 16 ? 16 : 32;
     p.terms = d.terms;
@@ -745,9 +776,14 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     p.w_total = (int)w_total;
     // (B: the rows of a CTA's part of a tile, or of the gradients of weights its columns)
     const int b_rows = grad ? kBM : std::max(tile.rows / tile.ctas > 2 * p.b_box ? kBM : 0, 2 * p.b_box);
-    p.stage_bytes = (uint32_t)(kABytes + b_rows * kRowBytes);
     const int table = ((2 * d.groups + 2) * 4 + 15) / 16 * 16, staging = d.mode != kGroupedPlain ? kStagingBytes : 0;
-    p.num_stages = std::min(kMaxStages, (kSmemLimit - 1024 - kBarrierBytes - staging - table) / (int)p.stage_bytes);
+    const int ring = kSmemLimit - 1024 - kBarrierBytes - staging - table, block_bytes = kABytes + b_rows * kRowBytes;
+    p.ks = blocks_per_stage(d, grad ? d.channels : d.width, ring / block_bytes);
+    p.b_block = b_rows * kRowBytes;
+    p.b_at = (uint32_t)(p.ks * kABytes);
+    p.stage_bytes = (uint32_t)(p.ks * block_bytes);
+    p.num_stages = std::min(kMaxStages, ring / (int)p.stage_bytes);
+    p.num_kb = (int)ceil_div(grad ? d.channels : d.width, kTerms * p.ks);
     const int bf16 = d.type == ONNXB_BFLOAT16;
     p.idesc_x = make_idesc_f16(kBM * tile.ctas, 0, bf16, grad, 0);
     p.idesc_w = make_idesc_f16(kBM * tile.ctas, p.BN, bf16, 1, 1);
@@ -766,13 +802,16 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     bool fine = true;
     const int terms = grad ? d.terms : 1, along = grad ? d.channels : d.width;
     if (!grad || p.with_x) {
+        const int blocks = p.ks > 1 ? p.ks : 0, single = p.ks > 1 ? 1 : 0;
         for (int i = 0; i < terms; ++i)
-            fine = fine && rows_map(&maps.R[i], d.A[i], d.rows, along, kBM) && rows_map(&maps.R_small[i], d.A[i], d.rows, along, p.b_box);
-        for (int i = 0; i < (gated ? 2 : terms); ++i) fine = fine && weights_map(&maps.W[i], d.W[i], d.groups, d.channels, d.width, d.mode != kGroupedPlain ? kBox : kBM);
+            fine = fine && rows_map(&maps.R[i], d.A[i], d.rows, along, kBM, blocks) && rows_map(&maps.R_small[i], d.A[i], d.rows, along, p.b_box, single);
+        for (int i = 0; i < (gated ? 2 : terms); ++i)
+            fine = fine && (grad ? weights_map(&maps.W[i], d.W[i], d.groups, d.channels, d.width, kBox * p.ks)
+                                 : weights_map(&maps.W[i], d.W[i], d.groups, d.channels, d.width, gated ? kBox : kBM, gated ? single : blocks));
     }
     if (p.w_count) {
-        for (int i = 0; i < terms; ++i) fine = fine && rows_map(&maps.D[i], d.A[i], d.rows, d.channels, kBox);
-        fine = fine && rows_map(&maps.X, d.X, d.rows, d.width, kBox);
+        for (int i = 0; i < terms; ++i) fine = fine && rows_map(&maps.D[i], d.A[i], d.rows, d.channels, kBox * p.ks);
+        fine = fine && rows_map(&maps.X, d.X, d.rows, d.width, kBox * p.ks);
     }
     if (!fine) return (int)cudaErrorInvalidValue;
 

@@ -139,6 +139,12 @@ def check_all(c, kind="silu"):
     check_gated_backward(c, *binding.onnx_grouped_gated_backward(c.dY, c.X, c.W, c.Wu, c.G, c.U, c.offsets, activation=kind), kind)
 
 
+@pytest.fixture(params=["0", "64"], ids=["tensor-cores", "few"])
+def few(request, monkeypatch):
+    """Up to 64 rows by either kernel."""
+    monkeypatch.setenv("ONNXB_GROUPED_FEW", request.param)
+
+
 SHAPES = [([1], 8, 8), ([3], 64, 64), ([2, 0, 1], 72, 40), ([0, 5, 0, 0, 17, 16, 15, 1, 0], 128, 200), ([64, 65, 63, 1, 128], 192, 136),
           ([100, 0, 300, 129, 256], 256, 384), ([1000, 24], 320, 520), ([40] * 33, 64, 128), ([0] * 40 + [70, 2] + [0] * 30, 136, 264)]
 
@@ -146,7 +152,7 @@ SHAPES = [([1], 8, 8), ([3], 64, 64), ([2, 0, 1], 72, 40), ([0, 5, 0, 0, 17, 16,
 @gpu
 @pytest.mark.parametrize("sizes,K,N", SHAPES, ids=lambda v: str(v) if not isinstance(v, list) else f"{len(v)}groups")
 @pytest.mark.parametrize("t", list(TYPES))
-def test_groups(sizes, K, N, t):
+def test_groups(sizes, K, N, t, few):
     check_all(Case(sizes, K, N, TYPES[t], seed=K + N))
 
 
@@ -159,9 +165,20 @@ def test_every_tile(tile, kind, monkeypatch):
 
 
 @gpu
+@pytest.mark.parametrize("tile", ["1x16", "1x48", "1x128", "2x32", "2x96", "2x128", "2x256"])
+@pytest.mark.parametrize("blocks", ["1", "2"])
+def test_blocks_of_a_stage(tile, blocks, monkeypatch):
+    """Reductions of whole blocks of 64, of an odd and an even number, in stages of one and of two; groups that end in either of a stage's blocks."""
+    monkeypatch.setenv("ONNXB_GROUPED_TILE", tile)
+    monkeypatch.setenv("ONNXB_GROUPED_KS", blocks)
+    check_all(Case([130, 0, 1, 77, 300, 16, 64, 192], 320, 448, torch.bfloat16, seed=3, before=5, behind=70))
+    check_all(Case([257, 63], 128, 64, torch.float16, seed=5))
+
+
+@gpu
 @pytest.mark.parametrize("K,N", [(1, 1), (7, 9), (65, 33), (100, 101), (777, 130), (130, 777)])
 @pytest.mark.parametrize("t", list(TYPES))
-def test_odd_widths(K, N, t):
+def test_odd_widths(K, N, t, few):
     check_all(Case([20, 0, 33, 1], K, N, TYPES[t], seed=K, behind=3))
 
 
@@ -213,7 +230,15 @@ def test_what_is_not_finite_stays_in_its_group(tile, monkeypatch):
 
 
 @gpu
-def test_views():
+@pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh", "relu"])
+def test_few_rows(kind):
+    """Rows of no group before and behind, groups of more rows than are taken at once, and more groups than a block has threads."""
+    for sizes, before, behind in (([1], 0, 0), ([0, 3, 0, 1], 2, 2), ([8], 0, 0), ([0] * 700 + [2] + [0] * 300 + [5], 1, 0)):
+        check_all(Case(sizes, 104, 70, torch.float16, seed=len(sizes), before=before, behind=behind), kind)
+
+
+@gpu
+def test_views(few):
     """Halves of one tensor, all groups' first rows first, and rows and groups that begin anywhere."""
     c = Case([50, 3, 0, 140], 72, 88, torch.bfloat16, seed=4)
     E, N, K = c.W.shape
@@ -265,6 +290,20 @@ def test_no_rows():
     binding.onnx_grouped_gemm(c.X, c.W, c.offsets, Y=Y)
     dX, dWg, dWu = binding.onnx_grouped_gated_backward(c.dY, c.X, c.W, c.Wu, c.G, c.U, c.offsets)
     assert (Y == 7.0).all() and not dWg.any() and not dWu.any()
+
+
+@gpu
+@pytest.mark.parametrize("offsets,ends", [([-5, 10, 300, 20], [0, 10, 60, 60]), ([20, 50, 30, 55], [20, 50, 50, 55]), ([59, 10, 5, 0], [59, 59, 59, 59]),
+                                          ([0, 2 ** 31 - 1, -2 ** 31, 7], [0, 60, 60, 60])])
+def test_few_rows_whose_offsets_do_not_rise(offsets, ends, few):
+    c = Case([10, 20, 30], 64, 72, torch.bfloat16)
+    c.ends, c.sizes = ends, [b - a for a, b in zip(ends, ends[1:])]
+    c.offsets = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    Y = torch.full((c.R, c.N), 7.0, dtype=c.t, device="cuda")
+    binding.onnx_grouped_gemm(c.X, c.W, c.offsets, Y=Y)
+    assert (Y[:ends[0]] == 7.0).all() and (Y[ends[-1]:] == 7.0).all()
+    if ends[0] < ends[-1]:
+        check_gemm(c, Y)
 
 
 @gpu
