@@ -451,3 +451,54 @@ def test_gradients_against_differences():
                 sides.append(loss(*a))
             # G, U, dG, dU and the result are rounded to 16 bits on the way
             assert abs((sides[0] - sides[1]) / (2 * h) - float(grad.view(-1)[i])) < 20 * half_step(c.t) * (1 + float(grad.abs().max()))
+
+
+@gpu
+def test_more_than_2_31_elements():
+    """Rows behind the 2^31-th element of X, and of dX; a group's weights behind that of W."""
+    R, K, N = (1 << 20) + 40, 2056, 8
+    g = torch.Generator(device="cuda").manual_seed(3)
+    X = torch.zeros(R, K, dtype=torch.float16, device="cuda")
+    x, dy = torch.randn(60, K, generator=g, device="cuda").half(), torch.randn(60, N, generator=g, device="cuda").half()
+    X[-60:] = x
+    dY = torch.zeros(R, N, dtype=torch.float16, device="cuda")
+    dY[-60:] = dy
+    W = (torch.randn(2, N, K, generator=g, device="cuda") / math.sqrt(K)).half()
+    offsets = torch.tensor([0, R - 60, R], dtype=torch.int32, device="cuda")
+    c = Case([60], K, N, torch.float16)
+    c.X, c.dY, c.W = x, dy, W[1:]
+    check_gemm(c, binding.onnx_grouped_gemm(X, W, offsets)[-60:])
+    dX, dW = binding.onnx_grouped_gemm_backward(dY, X, W, offsets)
+    check_gemm_backward(c, dX[-60:], dW[1:])
+    assert not dX[:-60].any() and not dW[0].any()
+    del X, dX
+    W = torch.zeros(900, 2400, 1000, dtype=torch.float16, device="cuda")
+    c = Case([0] * 899 + [33], 1000, 2400, torch.float16)
+    W[899] = c.W[899]
+    c.W, c.Wu = W, W
+    check_gemm(c, binding.onnx_grouped_gemm(c.X, W, c.offsets))
+    dX, _ = binding.onnx_grouped_gemm_backward(c.dY, c.X, W, c.offsets, wanted=(True, False))
+    check_gemm_backward(c, dX, None)
+
+
+@gpu
+def test_two_streams_at_once():
+    """Calls that overlap in time leave one another's results alone."""
+    cases = [Case([300, 0, 50, 700], 512, 384, torch.bfloat16, seed=1), Case([3, 2, 0, 1], 1024, 512, torch.bfloat16, seed=2)]
+
+    def run(c):
+        H, G, Up = binding.onnx_grouped_gated(c.X, c.W, c.Wu, c.offsets, save=True)
+        return [H, G, Up, binding.onnx_grouped_gemm(c.X, c.W, c.offsets), *binding.onnx_grouped_gated_backward(c.dY, c.X, c.W, c.Wu, c.G, c.U, c.offsets)]
+
+    want = [run(c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [None, None]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = run(cases[i])
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    assert binding.last_device_status() == 0

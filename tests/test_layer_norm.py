@@ -271,3 +271,58 @@ def test_no_cpu_path():
         binding.onnx_layer_normalization(torch.zeros(2, 4), torch.ones(4))
     with pytest.raises(TypeError):
         binding.onnx_layer_normalization_backward(torch.zeros(2, 4), torch.zeros(2, 4), torch.ones(4), torch.zeros(2), torch.ones(2))
+
+
+@gpu
+def test_checked_path_gives_the_same(monkeypatch):
+    X, scale, B, dY = inputs(70, 1000, torch.bfloat16, torch.float32)
+
+    def calls():
+        Y, m, r = binding.onnx_layer_normalization(X, scale, B, save=True)
+        return [Y, m, r, binding.onnx_layer_normalization(X, scale), *binding.onnx_layer_normalization_backward(dY, X, scale, m, r)]
+
+    native = calls()
+    monkeypatch.setattr(binding, "_fast_mod", binding._Declined())
+    for a, b in zip(native, calls()):
+        assert a.dtype == b.dtype and torch.equal(a, b)
+
+
+@gpu
+def test_more_than_2_31_elements():
+    """Rows behind the 2^31-th element, in a tensor whose other rows are zeros."""
+    M, K = (1 << 20) + 3, 2056
+    X = torch.zeros(M, K, dtype=torch.float16, device="cuda")
+    dY = torch.zeros_like(X)
+    x, scale, B, dy = inputs(5, K, torch.float16, torch.float32)
+    X[-5:], dY[-5:] = x, dy
+    Y, m, r = binding.onnx_layer_normalization(X, scale, B, save=True)
+    check_forward(x, scale, B, 1e-5, (Y[-5:], m[-5:], r[-5:]))
+    assert torch.equal(Y[:-5], B.to(torch.float16).expand(M - 5, K))
+    del Y
+    dX, dS, dB = binding.onnx_layer_normalization_backward(dY, X, scale, m, r)
+    # (rows of zeros add nothing to the sums)
+    check_backward(dy, x, scale, m[-5:], r[-5:], (dX[-5:], dS, dB))
+    assert not dX[:-5].any()
+
+
+@gpu
+def test_two_streams_at_once():
+    """Calls that overlap in time leave one another's results alone."""
+    cases = [inputs(3000, 1024, torch.bfloat16, torch.float32, seed=1), inputs(500, 12288, torch.bfloat16, torch.float32, seed=2)]
+
+    def run(case):
+        X, scale, B, dY = case
+        Y, m, r = binding.onnx_layer_normalization(X, scale, B, save=True)
+        return [Y, *binding.onnx_layer_normalization_backward(dY, X, scale, m, r)]
+
+    want = [run(c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [None, None]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = run(cases[i])
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
