@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(1024) layer_norm_long_kernel(const Forward p) 
 // A team: the threads that have a row's columns (or of a cluster's a block's part of them), 8 or 16 each; a block has one, or eight of a warp each.  Rows that
 // a team takes at once; blocks an SM.  (512 threads an SM of 128 registers, or 1024 of 64: 16384 x 4096 of bf16 76 and 88 us.)
 constexpr int kMostStages = 16;
-__host__ __device__ constexpr int rows_of(int threads, int element, bool whole) { return element == 4 || !whole ? 1 : 2; }
+__host__ __device__ constexpr int rows_of(int threads, int element, bool whole) { return element == 4 ? 1 : 2; }
 __host__ __device__ constexpr int per_sm(int threads) { return 512 / block_of(threads); }
 
 // Sums of N values (a power of 2) each over a warp: a lane has one of them in the end, that of index lane / (32 / N).  (Of values that it does not keep a lane
@@ -620,33 +620,40 @@ __global__ void __launch_bounds__(256) layer_norm_columns_kernel(const LongBackw
     p.partial[(2ll * blockIdx.y + group) * p.pitch + column] = sum;
 }
 
-// What the blocks left, added up: 64 columns a block, four a thread, 32 groups of threads with a share of the blocks each.  dScale's columns
-// first, then dB's.
+// What the blocks left, added up: 32 columns a block, four a thread, 64 groups of threads with a share of the blocks each, which is little enough to be on its
+// way at once.  dScale's columns first, then dB's.
 template <typename W>
 __global__ void __launch_bounds__(512) layer_norm_sums_kernel(int K, int blocks, const float *partial, long long pitch, W *d_scale, W *d_bias) {
-    __shared__ float4 sums[32][16];
-    const int lane = threadIdx.x % 16, group = threadIdx.x / 16, which = blockIdx.y;
-    const long long c = ((long long)blockIdx.x * 16 + lane) * 4;
+    __shared__ float4 sums[16][8];
+    const int lane = threadIdx.x % 8, group = threadIdx.x / 8, which = blockIdx.y;
+    const long long c = ((long long)blockIdx.x * 8 + lane) * 4;
     tc::pdl_launch_dependents();
     tc::pdl_wait();
     W *out = which ? d_bias : d_scale;
     if (!out) return;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c < pitch) {
-#pragma unroll 4
-        for (int b = group; b < blocks; b += 32) {
+#pragma unroll 5
+        for (int b = group; b < blocks; b += 64) {
             const float4 v = *reinterpret_cast<const float4 *>(partial + (2ll * b + which) * pitch + c);
             sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
         }
     }
-    sums[group][lane] = sum;
+#pragma unroll
+    for (int o = 8; o < 32; o *= 2) {
+        sum.x += __shfl_xor_sync(0xffffffffu, sum.x, o);
+        sum.y += __shfl_xor_sync(0xffffffffu, sum.y, o);
+        sum.z += __shfl_xor_sync(0xffffffffu, sum.z, o);
+        sum.w += __shfl_xor_sync(0xffffffffu, sum.w, o);
+    }
+    if (threadIdx.x % 32 < 8) sums[threadIdx.x / 32][lane] = sum;
     __syncthreads();
-    if (threadIdx.x >= 64) return;
-    const long long at = (long long)blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x >= 32) return;
+    const long long at = (long long)blockIdx.x * 32 + threadIdx.x;
     if (at >= K) return;
     float total = 0.f;
 #pragma unroll
-    for (int g = 0; g < 32; ++g) total += reinterpret_cast<const float *>(&sums[g][threadIdx.x / 4])[threadIdx.x % 4];
+    for (int w = 0; w < 16; ++w) total += reinterpret_cast<const float *>(&sums[w][threadIdx.x / 4])[threadIdx.x % 4];
     out[at] = from_float<W>(total);
 }
 
@@ -659,7 +666,7 @@ struct RowShape {
 };
 constexpr int kShapes = 8;
 constexpr RowShape kWholeRows[kShapes] = {{32, 1, 4}, {32, 2, 2}, {32, 4, 1}, {64, 4, 2}, {128, 4, 2}, {256, 4, 2}, {512, 4, 2}, {512, 8, 1}};
-constexpr RowShape kSingleRows[kShapes] = {{32, 4, 2}, {32, 8, 1}, {32, 16, 1}, {128, 8, 1}, {128, 16, 1}, {512, 8, 1}, {512, 16, 1}, {0, 0, 0}};
+constexpr RowShape kSingleRows[kShapes] = {{32, 4, 2}, {32, 8, 1}, {32, 16, 1}, {128, 8, 2}, {256, 8, 2}, {512, 8, 2}, {512, 16, 1}, {0, 0, 0}};
 // of few rows
 constexpr RowShape kWholeFew[kShapes] = {{32, 1, 1}, {256, 2, 1}, {512, 4, 1}, {512, 8, 1}, {0, 0, 0}};
 constexpr RowShape kSingleFew[kShapes] = {{32, 4, 1}, {256, 4, 1}, {512, 16, 1}, {0, 0, 0}};
@@ -775,7 +782,7 @@ int launch(const LayerNormGradProblem &q, int &blocks, cudaStream_t stream) {
 template <typename W>
 int launch_sums(int K, int blocks, const float *partial, void *d_scale, void *d_bias, cudaStream_t stream) {
     const long long pitch = grad_pitch(K);
-    return (int)tc_host::launch_pdl(layer_norm_sums_kernel<W>, dim3((unsigned)((pitch + 63) / 64), 2), dim3(512), 0, stream, K, blocks, partial, pitch,
+    return (int)tc_host::launch_pdl(layer_norm_sums_kernel<W>, dim3((unsigned)((pitch + 31) / 32), 2), dim3(512), 0, stream, K, blocks, partial, pitch,
                                     static_cast<W *>(d_scale), static_cast<W *>(d_bias));
 }
 
