@@ -14,7 +14,7 @@ using namespace dense;
 
 // Rows that TMA cannot address (they do not begin at multiples of 16 bytes) laid out so that it can, zeros up to the next one: 16 bytes a lane
 // and step, a warp per row, several where rows are few and long, or one for several rows of less than 32 steps.  All tensors of a call in
-// one launch.
+// one launch.  Groups without rows (offsets that do not rise) are left out: nobody reads their weights.
 __global__ void __launch_bounds__(256) repack_rows_kernel(const RepackProblem p) {
     tc::pdl_launch_dependents();
     tc::pdl_wait();
@@ -22,6 +22,7 @@ __global__ void __launch_bounds__(256) repack_rows_kernel(const RepackProblem p)
     const int per_row = job.dst_pitch >= 512 ? 32 : job.dst_pitch >= 256 ? 16 : 8, rows = 256 / per_row, lane = threadIdx.x % per_row;
     for (int row = blockIdx.x * rows + threadIdx.x / per_row; row < job.rows; row += gridDim.x * rows) {
         const int group = job.group_rows ? row / job.group_rows : 0;
+        if (job.offsets && job.offsets[group + 1] <= job.offsets[group]) continue;
         const uint8_t *src = job.src + group * job.group_pitch + (row - group * job.group_rows) * job.src_pitch;
         uint8_t *dst = job.dst + row * job.dst_pitch;
         for (long long at = (long long)(blockIdx.z * per_row + lane) * 16; at < job.dst_pitch; at += (long long)gridDim.z * per_row * 16)

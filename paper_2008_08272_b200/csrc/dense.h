@@ -88,6 +88,7 @@ struct RepackJob {
     long long dst_pitch;
     int group_rows;          // src's rows lie in groups of so many, group_pitch apart (0: in one)
     long long group_pitch;
+    const int *offsets;      // or NULL: groups whose next offset is not above their own are left out
 };
 struct RepackProblem {
     RepackJob job[3];

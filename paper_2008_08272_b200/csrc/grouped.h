@@ -34,7 +34,8 @@ struct GroupedProblem {
 };
 
 // The forward products of a few rows (grouped_few.cu).  Operands' rows and groups may begin anywhere.
-bool grouped_few_fits(int rows);
+// (in_place: the weights begin where the tensor cores' kernel can read them)
+bool grouped_few_fits(int rows, int groups, bool in_place);
 int launch_grouped_few(const GroupedProblem &p, cudaStream_t stream);
 // On the tensor cores (tc_grouped.cu).  Operands' rows and groups begin at multiples of 16 bytes.
 int launch_tc_grouped(const GroupedProblem &p, cudaStream_t stream);

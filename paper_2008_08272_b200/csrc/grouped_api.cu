@@ -43,12 +43,12 @@ size_t copy_bytes(const onnxb_matrices *m) {
     return (size_t)(copy_pitch(m) * m->rows * m->count);
 }
 // Groups' weights as the kernels read them: where they lie, or copied to the workspace with the other operands
-GroupedWeights place(Placement &placed, const onnxb_matrices *m) {
+GroupedWeights place(Placement &placed, const onnxb_matrices *m, const int32_t *offsets) {
     const size_t bytes = copy_bytes(m);
     const GroupedWeights w = weights(m);
     if (bytes == 0) return w;
     placed.repack.job[placed.repack.count++] = RepackJob{static_cast<const uint8_t *>(m->data), w.ld * 2, m->cols * 2, (int)(m->count * m->rows), 2,
-                                                         reinterpret_cast<uint8_t *>(placed.workspace), copy_pitch(m), (int)m->rows, w.stride * 2};
+                                                         reinterpret_cast<uint8_t *>(placed.workspace), copy_pitch(m), (int)m->rows, w.stride * 2, offsets};
     const GroupedWeights copy{placed.workspace, copy_pitch(m) / 2, copy_pitch(m) / 2 * m->rows};
     placed.workspace += bytes;
     return copy;
@@ -75,12 +75,15 @@ onnxb_status check_space(const void *workspace, size_t bytes, size_t need) { ret
 }  // namespace
 
 // (few rows are taken from wherever they and the weights begin)
-static bool few(const onnxb_matrix *X) { return X && X->rows >= 1 && X->rows <= kMostSize && grouped_few_fits((int)X->rows); }
+static bool few(const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu) {
+    if (!X || !Wg || X->rows < 1 || X->rows > kMostSize || Wg->count < 1 || Wg->count > kMostGroups) return false;
+    return grouped_few_fits((int)X->rows, (int)Wg->count, in_place(Wg) && (!Wu || in_place(Wu)));
+}
 extern "C" size_t onnx_grouped_gemm_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *W) {
-    return few(X) ? 0 : views::copy_bytes(X) + copy_bytes(W);
+    return few(X, W, nullptr) ? 0 : views::copy_bytes(X) + copy_bytes(W);
 }
 extern "C" size_t onnx_grouped_gated_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu) {
-    return few(X) ? 0 : views::copy_bytes(X) + copy_bytes(Wg) + copy_bytes(Wu);
+    return few(X, Wg, Wu) ? 0 : views::copy_bytes(X) + copy_bytes(Wg) + copy_bytes(Wu);
 }
 
 // Both forward products: Wu NULL for the plain one
@@ -115,7 +118,7 @@ static onnxb_status forward(const onnxb_matrix *X, const onnxb_matrices *Wg, con
     d.activation = activation;
     const onnxb_matrix *outs[3] = {H, G, U};
     for (int i = 0; i < 3 && outs[i]; ++i) { d.Y[i] = outs[i]->data; d.y_ld[i] = operand(outs[i]).ld; }
-    if (few(X)) {
+    if (few(X, Wg, Wu)) {
         d.A[0] = operand(X);
         d.W[0] = weights(Wg);
         if (gated) d.W[1] = weights(Wu);
@@ -123,8 +126,8 @@ static onnxb_status forward(const onnxb_matrix *X, const onnxb_matrices *Wg, con
     }
     Placement placed(workspace);
     d.A[0] = placed(X);
-    d.W[0] = place(placed, Wg);
-    if (gated) d.W[1] = place(placed, Wu);
+    d.W[0] = place(placed, Wg, offsets);
+    if (gated) d.W[1] = place(placed, Wu, offsets);
     const int err = placed.run(stream);
     return status_of(err ? err : launch_tc_grouped(d, stream));
 }
@@ -231,7 +234,7 @@ static onnxb_status backward(const onnxb_matrix *dY, const onnxb_matrix *X, cons
     if (!gated) d.A[0] = placed(dY);
     if (of_weights) d.X = placed(X);
     for (int i = 0; i < terms; ++i) {
-        if (dX) d.W[i] = place(placed, W[i]);
+        if (dX) d.W[i] = place(placed, W[i], offsets);
         if (D[i]) d.D[i] = weights(D[i]);
     }
     if (dX) { d.Y[0] = dX->data; d.y_ld[0] = operand(dX).ld; }

@@ -62,7 +62,7 @@ struct Placement {
         if (bytes == 0) return operand(m);
         const int element = type_bytes(m->type);
         repack.job[repack.count++] = RepackJob{static_cast<const uint8_t *>(m->data), operand(m).ld * element, m->cols * element, (int)m->rows, element,
-                                               reinterpret_cast<uint8_t *>(workspace), copy_pitch(m), 0, 0};
+                                               reinterpret_cast<uint8_t *>(workspace), copy_pitch(m), 0, 0, nullptr};
         const DenseOperand o{workspace, copy_pitch(m) / element};
         workspace += bytes;
         return o;

@@ -49,7 +49,7 @@ def lib():
 
 
 def test_grouped_gemm(lib):
-    good = dict(X=mat(30, 41), W=mats(4, 50, 41), Y=mat(30, 50))
+    good = dict(X=mat(90, 41), W=mats(4, 50, 41), Y=mat(90, 50))
 
     def call(a, offsets=OFFSETS, ws=None, size=0):
         return lib.onnx_grouped_gemm_run(a["X"], a["W"], offsets, a["Y"], ws, size, None)
@@ -60,7 +60,7 @@ def test_grouped_gemm(lib):
             assert got == status or (status == UNSUPPORTED and got == SHAPE), (name, bad, got)
         assert call({**good, name: None}) == NULL
     need = lib.onnx_grouped_gemm_workspace_bytes(good["X"], good["W"])
-    assert need == 128 * (30 + 4 * 50) and call(good) == WORKSPACE and call(good, ws=WS, size=need - 1) == WORKSPACE
+    assert need == 128 * (90 + 4 * 50) and call(good) == WORKSPACE and call(good, ws=WS, size=need - 1) == WORKSPACE
     assert call(good, None, WS, need) == NULL and call(good, ctypes.c_void_p(6), WS, need) == UNSUPPORTED
     assert call(good, ws=ctypes.c_void_p(8), size=need) == UNSUPPORTED
     for name in ("X", "W", "Y"):
@@ -68,20 +68,20 @@ def test_grouped_gemm(lib):
         if name != "Y":
             assert call({**good, "Y": change(good["Y"], data=good[name].data)}, ws=WS, size=need) == UNSUPPORTED
     assert call({**good, "Y": change(good["Y"], data=1 << 40)}, ws=WS, size=need) == UNSUPPORTED
-    for other in (dict(X=mat(30, 40)), dict(Y=mat(30, 51)), dict(Y=mat(29, 50)), dict(W=mats(4, 50, 40))):
+    for other in (dict(X=mat(90, 40)), dict(Y=mat(90, 51)), dict(Y=mat(89, 50)), dict(W=mats(4, 50, 40))):
         assert call({**good, **other}) == SHAPE
     for name, m in good.items():
         assert call({**good, name: change(m, type=BF16)}) == ATTR
     # groups that lie between one another's rows are fine, groups that overlap are not
     between = mats(4, 50, 40, ld=4 * 40, stride=40)
-    assert lib.onnx_grouped_gemm_workspace_bytes(mat(30, 40), between) == 0
-    assert call(dict(X=mat(30, 40), W=change(between, ld=159), Y=mat(30, 50))) == SHAPE
-    assert call(dict(X=mat(30, 40), W=change(between, stride=39), Y=mat(30, 50))) == SHAPE
-    assert lib.onnx_grouped_gemm_workspace_bytes(mat(30, 40), change(between, stride=41, ld=164)) == 128 * 200
+    assert lib.onnx_grouped_gemm_workspace_bytes(mat(90, 40), between) == 0
+    assert call(dict(X=mat(90, 40), W=change(between, ld=159), Y=mat(90, 50))) == SHAPE
+    assert call(dict(X=mat(90, 40), W=change(between, stride=39), Y=mat(90, 50))) == SHAPE
+    assert lib.onnx_grouped_gemm_workspace_bytes(mat(90, 40), change(between, stride=41, ld=164)) == 128 * 200
 
 
 def test_grouped_gated(lib):
-    good = dict(X=mat(30, 41), Wg=mats(4, 50, 41), Wu=mats(4, 50, 41), H=mat(30, 50), G=mat(30, 50), U=mat(30, 50))
+    good = dict(X=mat(90, 41), Wg=mats(4, 50, 41), Wu=mats(4, 50, 41), H=mat(90, 50), G=mat(90, 50), U=mat(90, 50))
 
     def call(a, act=0, offsets=OFFSETS, ws=None, size=0):
         ref = lambda m: None if m is None else ctypes.byref(m)
@@ -95,7 +95,7 @@ def test_grouped_gated(lib):
     assert call(good) == WORKSPACE and call({**good, "G": None, "U": None}) == WORKSPACE
     assert call(good, act=4) == ATTR and call(good, act=-1) == ATTR
     need = lib.onnx_grouped_gated_workspace_bytes(good["X"], good["Wg"], good["Wu"])
-    assert need == 128 * (30 + 2 * 4 * 50)
+    assert need == 128 * (90 + 2 * 4 * 50)
     for a, b in (("H", "G"), ("H", "U"), ("G", "U"), ("H", "X"), ("G", "Wg"), ("U", "Wu")):
         assert call({**good, a: change(good[a], data=good[b].data)}, ws=WS, size=need) == UNSUPPORTED
     assert call({**good, "Wu": mats(3, 50, 41)}) == SHAPE and call({**good, "Wu": mats(4, 49, 41)}) == SHAPE
@@ -103,7 +103,7 @@ def test_grouped_gated(lib):
 
 def test_grouped_backward(lib):
     ref = lambda m: None if m is None else ctypes.byref(m)
-    good = dict(dY=mat(30, 50), X=mat(30, 41), W=mats(4, 50, 41), dX=mat(30, 41), dW=mats(4, 50, 41))
+    good = dict(dY=mat(90, 50), X=mat(90, 41), W=mats(4, 50, 41), dX=mat(90, 41), dW=mats(4, 50, 41))
 
     def call(a, offsets=OFFSETS, ws=None, size=0):
         return lib.onnx_grouped_gemm_backward_run(ref(a["dY"]), ref(a["X"]), ref(a["W"]), offsets, ref(a["dX"]), ref(a["dW"]), ws, size, None)
@@ -116,11 +116,11 @@ def test_grouped_backward(lib):
         assert call({**good, name: None}) == NULL
     assert call({**good, "dX": None, "dW": None}) == NULL and call(good) == WORKSPACE
     need = lib.onnx_grouped_gemm_backward_workspace_bytes(*[ctypes.byref(good[n]) for n in ("dY", "X", "W", "dX", "dW")])
-    assert need == 128 * (30 + 30 + 200)
+    assert need == 128 * (90 + 90 + 200)
     for a, b in (("dX", "dY"), ("dX", "X"), ("dW", "W"), ("dX", "dW"), ("dW", "X")):
         assert call({**good, a: change(good[a], data=good[b].data)}, ws=WS, size=need) == UNSUPPORTED
 
-    full = dict(dH=mat(30, 50), X=mat(30, 41), Wg=mats(4, 50, 41), Wu=mats(4, 50, 41), G=mat(30, 50), U=mat(30, 50), dX=mat(30, 41), dWg=mats(4, 50, 41),
+    full = dict(dH=mat(90, 50), X=mat(90, 41), Wg=mats(4, 50, 41), Wu=mats(4, 50, 41), G=mat(90, 50), U=mat(90, 50), dX=mat(90, 41), dWg=mats(4, 50, 41),
                 dWu=mats(4, 50, 41))
 
     def gated(a, act=0, offsets=OFFSETS, ws=None, size=0):
