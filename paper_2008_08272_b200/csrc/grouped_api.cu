@@ -11,6 +11,8 @@ using namespace onnxb::views;
 namespace {
 
 constexpr int64_t kMostStride = 1ll << 36, kMostRows = 2147483647ll;
+// Terms of a reduction on the tensor cores, whose waits are bounded: a tile of so many takes a second at most
+constexpr int64_t kMostTerms = 1ll << 27;
 
 // What holds for groups' weights by themselves: sizes, no rows that overlap, in whichever order they lie
 onnxb_status check_groups(const onnxb_matrices *m) {
@@ -106,6 +108,7 @@ static onnxb_status forward(const onnxb_matrix *X, const onnxb_matrices *Wg, con
     }
     CHECK(check_offsets(offsets));
     if (R == 0) return ONNXB_OK;
+    if (!few(X, Wg, Wu) && K > kMostTerms) return ONNXB_ERR_UNSUPPORTED;
     const size_t need = onnx_grouped_gated_workspace_bytes(X, Wg, Wu);
     CHECK(check_space(workspace, workspace_bytes, need));
     const void *all[7] = {data_of(H), data_of(G), data_of(U), data_of(X), data_of(Wg), data_of(Wu), offsets};
@@ -207,6 +210,7 @@ static onnxb_status backward(const onnxb_matrix *dY, const onnxb_matrix *X, cons
             }
         return ONNXB_OK;
     }
+    if ((of_weights && R > kMostTerms) || (dX && N > kMostTerms)) return ONNXB_ERR_UNSUPPORTED;
     CHECK(check_space(workspace, workspace_bytes, need));
     CHECK(check_places(all, 3, 10, workspace, need));
     GroupedProblem d{};

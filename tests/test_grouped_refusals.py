@@ -138,6 +138,23 @@ def test_grouped_backward(lib):
     assert gated({**full, "dWg": change(full["dWg"], data=full["dWu"].data)}, ws=WS, size=1 << 30) == UNSUPPORTED
 
 
+def test_sums_of_too_many_terms(lib):
+    """(Without the limit each of these would ask for a workspace.)"""
+    ref = ctypes.byref
+    long, most = (1 << 27) + 1, 1 << 27
+    for K, status in ((long, UNSUPPORTED), (most, WORKSPACE)):
+        X = mat(90, K, ld=K + 3)
+        assert lib.onnx_grouped_gemm_run(X, mats(2, 8, K), OFFSETS, mat(90, 8), None, 0, None) == status
+        assert lib.onnx_grouped_gated_run(X, mats(2, 8, K), mats(2, 8, K), OFFSETS, 0, mat(90, 8), None, None, None, 0, None) == status
+    for R, N, wanted, status in ((long, 9, (0, 1), UNSUPPORTED), (most, 9, (0, 1), WORKSPACE), (long, 9, (1, 0), WORKSPACE), (90, long, (1, 0), UNSUPPORTED),
+                                 (90, most, (1, 0), WORKSPACE), (90, long, (0, 1), WORKSPACE)):
+        dY, X, W = mat(R, N, ld=N + 4 - N % 2), mat(R, 9), mats(2, N, 9)
+        dX, dW = mat(R, 9) if wanted[0] else None, mats(2, N, 9) if wanted[1] else None
+        assert lib.onnx_grouped_gemm_backward_run(ref(dY), ref(X), ref(W), OFFSETS, dX and ref(dX), dW and ref(dW), None, 0, None) == status
+        assert lib.onnx_grouped_gated_backward_run(ref(dY), ref(X), ref(W), ref(W), ref(dY), ref(dY), OFFSETS, 0, dX and ref(dX), dW and ref(dW), None, None, 0,
+                                                   None) == status
+
+
 def test_layer_normalization(lib):
     ref = lambda m: None if m is None else ctypes.byref(m)
     X, s, b, Y = mat(4, 40, BF16), mat(1, 40, BF16), mat(1, 40, BF16), mat(4, 40, BF16)
