@@ -487,7 +487,7 @@ onnxb_status onnx_layer_normalization_backward_run(const onnxb_matrix *dY, const
  * free (all groups' first rows may come first), but none of their rows overlap (ERR_SHAPE).  At most 1024 groups, count * rows at most 2^31-1,
  * and `stride` at most 2^36; sums of at most 2^27 terms (K, of dX N, of the weights' gradients R), but of forward products of up to 16 rows (ERR_UNSUPPORTED).
  * All else is as said above at onnxb_matrix, alignment among it: what TMA cannot address, rows or groups that do not begin at multiples of 16 bytes, is laid
- * out in the workspace first, weights as a whole.
+ * out in the workspace first, weights as a whole.  Long sums of few results are in parts there, by the sizes alone.
  */
 typedef struct {
     void *data;              /* device (inputs are only read) */

@@ -31,12 +31,15 @@ struct GroupedProblem {
     void *Y[3];
     long long y_ld[3];
     GroupedWeights D[2];                     // (written)
+    void *planes;                            // tc_grouped_workspace bytes, at a multiple of 16
 };
 
 // The forward products of a few rows (grouped_few.cu).  Operands' rows and groups may begin anywhere.
 // (in_place: the weights begin where the tensor cores' kernel can read them)
 bool grouped_few_fits(int rows, int groups, bool in_place);
 int launch_grouped_few(const GroupedProblem &p, cudaStream_t stream);
+// Scratch that launch_tc_grouped needs, by `mode`, `rows`, `groups`, `channels`, `width` and `terms` alone, for so many weights' gradients (of gradients)
+size_t tc_grouped_workspace(const GroupedProblem &p, int weights);
 // On the tensor cores (tc_grouped.cu).  Operands' rows and groups begin at multiples of 16 bytes.
 int launch_tc_grouped(const GroupedProblem &p, cudaStream_t stream);
 

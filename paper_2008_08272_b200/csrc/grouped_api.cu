@@ -81,8 +81,19 @@ static bool few(const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_mat
     if (!X || !Wg || X->rows < 1 || X->rows > kMostSize || Wg->count < 1 || Wg->count > kMostGroups) return false;
     return grouped_few_fits((int)X->rows, (int)Wg->count, in_place(Wg) && (!Wu || in_place(Wu)));
 }
+static bool sizes_are_some(const onnxb_matrix *m) { return m && m->rows >= 1 && m->cols >= 1 && m->rows <= kMostSize && m->cols <= kMostSize; }
+// The reductions' parts (from the sizes alone)
+static GroupedProblem sizes_of(int mode, const onnxb_matrix *rows, int64_t channels, int64_t width, int64_t groups, int terms) {
+    GroupedProblem d{};
+    d.mode = mode;
+    d.rows = (int)rows->rows; d.groups = (int)groups; d.channels = (int)channels; d.width = (int)width;
+    d.terms = terms;
+    return d;
+}
+static bool groups_are_some(const onnxb_matrices *m) { return m && m->count >= 1 && m->count <= kMostGroups && m->rows >= 1 && m->rows <= kMostSize && m->cols >= 1 && m->cols <= kMostSize; }
 extern "C" size_t onnx_grouped_gemm_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *W) {
-    return few(X, W, nullptr) ? 0 : views::copy_bytes(X) + copy_bytes(W);
+    if (!sizes_are_some(X) || !groups_are_some(W) || few(X, W, nullptr)) return 0;
+    return views::copy_bytes(X) + copy_bytes(W) + tc_grouped_workspace(sizes_of(kGroupedPlain, X, W->rows, W->cols, W->count, 1), 0);
 }
 extern "C" size_t onnx_grouped_gated_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu) {
     return few(X, Wg, Wu) ? 0 : views::copy_bytes(X) + copy_bytes(Wg) + copy_bytes(Wu);
@@ -109,7 +120,7 @@ static onnxb_status forward(const onnxb_matrix *X, const onnxb_matrices *Wg, con
     CHECK(check_offsets(offsets));
     if (R == 0) return ONNXB_OK;
     if (!few(X, Wg, Wu) && K > kMostTerms) return ONNXB_ERR_UNSUPPORTED;
-    const size_t need = onnx_grouped_gated_workspace_bytes(X, Wg, Wu);
+    const size_t need = gated ? onnx_grouped_gated_workspace_bytes(X, Wg, Wu) : onnx_grouped_gemm_workspace_bytes(X, Wg);
     CHECK(check_space(workspace, workspace_bytes, need));
     const void *all[7] = {data_of(H), data_of(G), data_of(U), data_of(X), data_of(Wg), data_of(Wu), offsets};
     CHECK(check_places(all, 3, 7, workspace, need));
@@ -131,6 +142,7 @@ static onnxb_status forward(const onnxb_matrix *X, const onnxb_matrices *Wg, con
     d.A[0] = placed(X);
     d.W[0] = place(placed, Wg, offsets);
     if (gated) d.W[1] = place(placed, Wu, offsets);
+    d.planes = placed.workspace;
     const int err = placed.run(stream);
     return status_of(err ? err : launch_tc_grouped(d, stream));
 }
@@ -148,16 +160,23 @@ extern "C" onnxb_status onnx_grouped_gated_run(const onnxb_matrix *X, const onnx
 // dG and dU: rows at multiples of 16 bytes
 static int64_t slope_pitch(int64_t channels) { return (channels + 7) / 8 * 8; }
 static size_t slope_bytes(int64_t rows, int64_t channels) { return (size_t)(rows * slope_pitch(channels) * 2); }
-static bool sizes_are_some(const onnxb_matrix *m) { return m && m->rows >= 1 && m->cols >= 1 && m->rows <= kMostSize && m->cols <= kMostSize; }
+// What the gradients' products need: the width and the groups, from the first result or weights that have them
+static size_t planes_bytes(const onnxb_matrix *dY, const onnxb_matrices *const *W, const onnxb_matrix *dX, const onnxb_matrices *const *D, int terms) {
+    const onnxb_matrices *one = dX ? W[0] : D[0] ? D[0] : D[1];
+    if (!sizes_are_some(dY) || !groups_are_some(one)) return 0;
+    return tc_grouped_workspace(sizes_of(kGroupedGrad, dY, dY->cols, one->cols, one->count, terms), (D[0] != nullptr) + (D[1] != nullptr));
+}
 
 extern "C" size_t onnx_grouped_gemm_backward_workspace_bytes(const onnxb_matrix *dY, const onnxb_matrix *X, const onnxb_matrices *W, const onnxb_matrix *dX,
                                                              const onnxb_matrices *dW) {
-    return views::copy_bytes(dY) + (dW ? views::copy_bytes(X) : 0) + (dX ? copy_bytes(W) : 0);
+    const onnxb_matrices *w[2] = {W, nullptr}, *d[2] = {dW, nullptr};
+    return views::copy_bytes(dY) + (dW ? views::copy_bytes(X) : 0) + (dX ? copy_bytes(W) : 0) + planes_bytes(dY, w, dX, d, 1);
 }
 extern "C" size_t onnx_grouped_gated_backward_workspace_bytes(const onnxb_matrix *dH, const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu,
                                                               const onnxb_matrix *dX, const onnxb_matrices *dWg, const onnxb_matrices *dWu) {
     if (!sizes_are_some(dH)) return 0;
-    return 2 * slope_bytes(dH->rows, dH->cols) + (dWg || dWu ? views::copy_bytes(X) : 0) + (dX ? copy_bytes(Wg) + copy_bytes(Wu) : 0);
+    const onnxb_matrices *w[2] = {Wg, Wu}, *d[2] = {dWg, dWu};
+    return 2 * slope_bytes(dH->rows, dH->cols) + (dWg || dWu ? views::copy_bytes(X) : 0) + (dX ? copy_bytes(Wg) + copy_bytes(Wu) : 0) + planes_bytes(dH, w, dX, d, 2);
 }
 
 // Both forms' gradients: of the plain product G and U are NULL, and W[1] and D[1].  `gated` says which.
@@ -242,6 +261,7 @@ static onnxb_status backward(const onnxb_matrix *dY, const onnxb_matrix *X, cons
         if (D[i]) d.D[i] = weights(D[i]);
     }
     if (dX) { d.Y[0] = dX->data; d.y_ld[0] = operand(dX).ld; }
+    d.planes = placed.workspace;
     if (err == 0) err = placed.run(stream);
     return status_of(err ? err : launch_tc_grouped(d, stream));
 }

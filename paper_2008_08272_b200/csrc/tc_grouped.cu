@@ -25,12 +25,16 @@
 //     they are not finite zeros on the other side would not help: warp 10 clears them on both sides, up to the next multiple of 16 rows, and the
 //     stage's instructions end there.  Such a stage's copies complete on a barrier of this CTA's own, since of a pair each CTA clears what it holds.
 //   - Groups without rows: their weights' gradients are zeros, stored without a product.
+//   - Where a forward product or the weights' gradients have few tiles and a long reduction, tiles have parts of it, whose sums go to planes of fp32 that a second kernel adds
+//     up (73 rows of 17 groups, 6912 -> 64: 20.2 -> 11.8 us; gradients of 10272 rows of one group, 3712 x 72, 53.9 -> 36.7).  Not dX, whose reduction is the
+//     shorter one where it has few tiles: a microsecond at most.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
 #include <atomic>
 #include <cstdlib>
+#include <cstring>
 #include <type_traits>
 
 #include "dense_math.cuh"
@@ -74,6 +78,9 @@ struct Params {
     int BN;                        // columns of a tile of the weights' gradients
     int w_tiles_m, w_tiles_n, w_total;     // row and column tiles of one weights' gradient; tiles of all of them
     int w_first, w_count;          // the first that is wanted; how many are
+    int parts;                     // of the reductions (of the weights' gradients, or of the forward product), where they are several,
+    float *planes;                 // each with a plane of fp32 of its own
+    long long pitch;               // floats of their rows
     int num_stages;
     uint32_t idesc_x, idesc_w;     // (of tiles of rows without their columns)
     int ks;                        // K blocks of a stage
@@ -107,7 +114,8 @@ __device__ __forceinline__ int rows_per_tile(int rows, int most) {
 struct TileAt {
     int g, tm, tn, z;          // z: which of the weights' gradients
     int row0, rows;            // the tile's rows (gradients of weights: the group's)
-    int kb;                    // stages
+    int part, kb0, kb;         // of the reduction; its first stage, and how many
+    bool ends;                 // with the reduction's last
     bool x;                    // of rows: the forward products and dX
 };
 // Of `tiles_m` by `tiles_n` tiles the r-th, in bands of `band` row tiles, a band's columns one after the other: the tiles in flight share operands in L2
@@ -116,12 +124,31 @@ __device__ __forceinline__ void place(int band, int tiles_m, int tiles_n, int r,
     at.tn = rr / rows;
     at.tm = b * band + rr - at.tn * rows;
 }
-template <int kMode>
+template <int kMode, bool kParts>
 __device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t, TileAt &at) {
     constexpr bool kGrad = kMode == kGroupedGrad;
-    const int of_rows = !kGrad || p.with_x ? s.tiles[p.groups] * p.tiles_n : 0;
+    const int parts = kParts ? p.parts : 1, of_rows = !kGrad || p.with_x ? s.tiles[p.groups] * p.tiles_n * (kGrad ? 1 : parts) : 0;
     at.x = t < of_rows;
     at.z = 0;
+    t = at.x ? t : t - of_rows;
+    at.part = 0;
+    if (kParts && at.x != kGrad) {
+        // a tile's parts one after the other
+        const int q = t / parts;
+        at.part = t - q * parts;
+        t = q;
+    }
+    auto share = [&](int stages) {
+        const int each = (stages + parts - 1) / parts;
+        at.kb0 = min(at.part * each, stages);
+        at.kb = min(each, stages - at.kb0);
+        at.ends = at.kb > 0 && at.kb0 + at.kb == stages;       // (parts behind the last stage have none)
+    };
+    auto whole = [&](int stages) {
+        at.kb0 = 0;
+        at.kb = stages;
+        at.ends = true;
+    };
     if (at.x) {
         const int q = t / p.tiles_n;
         int lo = 0, hi = p.groups;             // tiles[lo] <= q < tiles[hi]
@@ -135,10 +162,10 @@ __device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t,
         const int all = s.first[lo + 1] - s.first[lo], per = rows_per_tile(all, p.most_rows);
         at.row0 = s.first[lo] + at.tm * per;
         at.rows = min(per, all - at.tm * per);
-        at.kb = kGrad ? p.terms * p.num_kb : p.num_kb;
+        if (kParts && !kGrad) share(p.num_kb);
+        else whole(kGrad ? p.terms * p.num_kb : p.num_kb);
         return true;
     }
-    t -= of_rows;
     if (!kGrad || t >= p.w_total) return false;
     const int per = p.w_tiles_m * p.w_tiles_n;
     at.g = t / (per * p.w_count);
@@ -147,7 +174,9 @@ __device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t,
     place(p.band, p.w_tiles_m, p.w_tiles_n, r - at.z * per, at);
     at.row0 = s.first[at.g];
     at.rows = s.first[at.g + 1] - at.row0;
-    at.kb = (at.rows + kTerms * p.ks - 1) / (kTerms * p.ks);
+    const int stages = (at.rows + kTerms * p.ks - 1) / (kTerms * p.ks);
+    if (kParts) share(stages);
+    else whole(stages);
     return true;
 }
 
@@ -164,7 +193,7 @@ __device__ __forceinline__ uint32_t pack<__nv_bfloat162>(float a, float b) {
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-template <int kCtas, int kMode>
+template <int kCtas, int kMode, bool kParts>
 __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_constant__ Maps maps, const Params p) {
     constexpr bool kGrad = kMode == kGroupedGrad, kGated = kMode == kGroupedGated;
     extern __shared__ uint8_t smem_raw[];
@@ -252,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
     if (kCtas == 2) cluster_sync_all();     // the peer's barriers exist before anything arrives on them
 
     // Whether a tile's last stage ends inside the next group's rows, where it is not by 16 rows that it does
-    auto has_tail = [&](const TileAt &t) { return kGrad && !t.x && (t.rows & 15) != 0; };
+    auto has_tail = [&](const TileAt &t) { return kGrad && !t.x && t.ends && (t.rows & 15) != 0; };
 
     // The tile after this one, as the even CTA's producer says it; -1: none.  (By a warp's lanes, or the one that issues MMAs.  Nobody has more tiles than
     // there are: that ends the loops where a wait has run out, too.)
@@ -297,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
         };
         int t = unit;
         while (t >= 0) {
-            const bool some = tile_at<kMode>(p, groups, t, at);
+            const bool some = tile_at<kMode, kParts>(p, groups, t, at);
             if (!some) break;
             if (rank == 0) ask();
             // Tiles of rows: the weights in one copy, or in two of 64 (the gated block's channels of each, dX's columns); then this CTA's rows, in one copy or
@@ -347,21 +376,27 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 c2 += d2;
                 if (++stage == p.num_stages) { stage = 0; phase ^= 1; }
             };
-            // (dX's second term: the same stages again of the other tensors)
-            const int parts = kGrad && at.x ? p.terms : 1, kb_each = kGrad && at.x ? p.num_kb : tail ? at.kb - 1 : at.kb;
-            for (int part = 0; part < parts; ++part) {
-                if (kGrad && part > 0) {
-                    map += 1;
-                    c0 -= kb_each * d0;
-                    c1 -= kb_each * d1;
-                    c2 -= kb_each * d2;
-                }
-                for (int kb = 0; kb < kb_each; ++kb) {
+            auto load_whole = [&](int stages_of_it) {
+                for (int kb = 0; kb < stages_of_it; ++kb) {
                     mbar_wait(&empty[stage], phase ^ 1, p.err, 1);
                     if (lane == 0 && rank == 0) mbar_arrive_expect_tx(&full[stage], bytes * kCtas);
                     __syncwarp();
                     load(full_issuer, full);
                 }
+            };
+            auto move = [&](int by) {
+                c0 += by * d0;
+                c1 += by * d1;
+                c2 += by * d2;
+            };
+            if (kParts) move(at.kb0);
+            // (dX's second term: the same stages again of the other tensors)
+            const int whole = at.kb - (tail ? 1 : 0), of_term = kGrad && at.x ? p.num_kb : whole;
+            load_whole(of_term);
+            if (kGrad && of_term < whole) {
+                map += 1;
+                move(-of_term);
+                load_whole(of_term);
             }
             if (tail) {
                 mbar_wait(&empty[stage], phase ^ 1, p.err, 1);
@@ -376,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             if (rank == 0) {
                 t = granted();
                 TileAt after;
-                const int told = t >= 0 && tile_at<kMode>(p, groups, t, after) ? t : -1;
+                const int told = t >= 0 && tile_at<kMode, kParts>(p, groups, t, after) ? t : -1;
                 if (kCtas == 2) mbar_wait_cluster(&slot_empty[slot], slot_phase ^ 1, p.err, 10);
                 else mbar_wait(&slot_empty[slot], slot_phase ^ 1, p.err, 10);
                 if (lane == 0) {
@@ -414,14 +449,14 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), a_lo = (uint32_t)a_tmpl | ((smem_u32(stages) >> 4) & 0x3FFFu);
             const uint32_t b_base = ((smem_u32(stages) + p.b_at) >> 4) & 0x3FFFu, stage16 = p.stage_bytes >> 4;
             constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kA16 = kGrad ? kMn16 : kK16, kABlock16 = (kGrad ? kBoxBytes : kABytes) >> 4;
-            for (int t = unit; t >= 0 && tile_at<kMode>(p, groups, t, at); t = next_tile(false)) {
+            for (int t = unit; t >= 0 && tile_at<kMode, kParts>(p, groups, t, at); t = next_tile(false)) {
                 if (at.kb == 0) continue;              // a group without rows
                 const bool b_mn = kGrad && !at.x, tail = has_tail(at);
                 const uint64_t b_tmpl = b_mn ? mn_tmpl : k_tmpl;
                 const uint32_t b_hi = (uint32_t)(b_tmpl >> 32), b_lo = (uint32_t)b_tmpl | b_base, b16 = b_mn ? kMn16 : kK16, b_block16 = (uint32_t)(b_mn ? kBoxBytes : p.b_block) >> 4;
                 const uint32_t idesc = b_mn ? p.idesc_w : p.idesc_x | ((uint32_t)((at.rows + 15) / 16 * 2) << 17);
                 // instructions of the last stage, where they are not four a block; stages before it
-                const int most = 4 * p.ks, last = b_mn ? (at.rows - (at.kb - 1) * kTerms * p.ks + 15) / 16 : most, whole = last == most && !tail ? at.kb : at.kb - 1;
+                const int most = 4 * p.ks, last = b_mn && (!kParts || at.ends) ? (at.rows - (at.kb0 + at.kb - 1) * kTerms * p.ks + 15) / 16 : most, whole = last == most && !tail ? at.kb : at.kb - 1;
                 if (kCtas == 2) mbar_wait_cluster(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 else mbar_wait(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 tc_fence_after_sync();
@@ -471,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             uint32_t clear_phase = 0;
             const uint32_t cleared_issuer = kCtas == 2 ? map_to_cta(smem_u32(&cleared[0]), 0) : 0u;
             const int boxes = kBM / kBox + p.BN / kCtas / kBox;
-            for (int t = unit; t >= 0 && tile_at<kMode>(p, groups, t, at); t = next_tile(true)) {
+            for (int t = unit; t >= 0 && tile_at<kMode, kParts>(p, groups, t, at); t = next_tile(true)) {
                 if (at.kb == 0) continue;
                 stage += at.kb - 1;
                 stage %= p.num_stages;
@@ -479,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                     mbar_wait(&tail_full[stage], (clear_phase >> stage) & 1u, p.err, 6);
                     clear_phase ^= 1u << stage;
                     // a box has a row of the group's, 64 columns of it, in 128 bytes (the swizzle moves pieces within them)
-                    const int from = at.rows - (at.kb - 1) * kTerms * p.ks, pieces = ((from + 15) / 16 * 16 - from) * 8;
+                    const int from = at.rows - (at.kb0 + at.kb - 1) * kTerms * p.ks, pieces = ((from + 15) / 16 * 16 - from) * 8;
                     uint8_t *first = stages + (size_t)stage * p.stage_bytes + from * kRowBytes;
                     for (int b = 0; b < boxes; ++b) {
                         uint8_t *box = first + b * kBoxBytes * p.ks;
@@ -502,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
         int acc = 0;
         uint32_t acc_phase = 0;
         const uint32_t peer_tmem_empty = kCtas == 2 ? map_to_cta(smem_u32(&tmem_empty[0]), 0) : 0u;
-        for (int t = unit; t >= 0 && tile_at<kMode>(p, groups, t, at); t = next_tile(true)) {
+        for (int t = unit; t >= 0 && tile_at<kMode, kParts>(p, groups, t, at); t = next_tile(true)) {
             const bool some = at.kb > 0;
             if (some) {
                 mbar_wait(&tmem_full[acc], acc_phase, p.err, 4);
@@ -590,8 +625,23 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
 #pragma unroll 1
                 for (int b = half; b < blocks; b += 2) {
                     uint32_t v[32];
-                    tmem_ld_32x32(tbase + (uint32_t)(b * 32), v);
-                    tmem_ld_wait();
+                    if (!kParts || kGrad || some) {
+                        tmem_ld_32x32(tbase + (uint32_t)(b * 32), v);
+                        tmem_ld_wait();
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = 0u;
+                    }
+                    if (kParts && !kGrad) {
+                        // a part of the reduction: as it is, 128 bytes of a row a warp
+                        const int rows = at.rows - b * 32;
+                        float *out = p.planes + ((long long)at.part * p.rows + at.row0 + b * 32) * p.pitch + channel0 + lane;
+                        if (channel0 + lane < all)
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j < rows) out[j * p.pitch] = __uint_as_float(v[j]);
+                        continue;
+                    }
                     store(0, b * 32, channel0, all, kAll, [&](int i) { return __uint_as_float(v[i]); });
                 }
             } else {
@@ -610,6 +660,22 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
 #pragma unroll
                             for (int j = 0; j < 32; ++j) v[j] = 0u;
                         }
+                        if (kParts) {
+                            // a part of the reduction: 32 columns of 32 rows laid out, and stored as they are, four rows at a time
+                            if (b * 64 + c >= p.width - n0) break;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                *reinterpret_cast<uint4 *>(buf + lane * kRowBytes + ((i ^ (lane & 7)) << 4)) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                            __syncwarp();
+                            const int piece = lane & 7, col = n0 + b * 64 + c + piece * 4;
+                            float *out = p.planes + (((long long)at.part * p.w_count + at.z) * p.groups + at.g) * p.channels * p.pitch + row0 * p.pitch + col;
+                            if (col < p.width)
+#pragma unroll 4
+                                for (int r = lane >> 3; r < rows; r += 4)
+                                    *reinterpret_cast<uint4 *>(out + r * p.pitch) = *reinterpret_cast<const uint4 *>(buf + r * kRowBytes + ((piece ^ (r & 7)) << 4));
+                            __syncwarp();
+                            continue;
+                        }
                         float lo[16], hi[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
@@ -623,6 +689,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                             *reinterpret_cast<uint4 *>(buf + lane * kRowBytes + (((c / 8 + i) ^ (lane & 7)) << 4)) =
                                 make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
                     }
+                    if (kParts) continue;
                     __syncwarp();
                     // Stored by rows, four at a time in pieces of 16 bytes, or one in pairs of elements
                     const int w = p.w_first + at.z, left = min(64, p.width - n0 - b * 64);
@@ -678,15 +745,70 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
     }
 }
 
+// The parts' planes added up, in their order, and rounded: four columns a thread, 8 rows by 128 columns a block
+struct SumProblem {
+    const float *planes;
+    long long pitch, of_result, plane;       // floats of a row, of one result's planes, of all results'
+    int parts, rows, cols;
+    uint16_t *out[2];
+    long long ld[2], stride[2];
+    int group_rows;                          // rows of a group's result
+    const int *offsets;                      // of results by row (else NULL), of which those alone are written that are a group's
+    int groups, bf16;
+};
+__global__ void __launch_bounds__(256) grouped_sum_kernel(const __grid_constant__ SumProblem p) {
+    const int which = blockIdx.z, j = (blockIdx.x * 32 + threadIdx.x % 32) * 4;
+    pdl_launch_dependents();
+    pdl_wait();
+    // (the offsets are on their way while the planes are read, of rows of no group too)
+    int first = 0, last = p.rows;
+    if (p.offsets) {
+        first = max(p.offsets[0], 0);
+        last = 0;
+        for (int i = threadIdx.x % 32; i <= p.groups; i += 32) last = max(last, p.offsets[i]);
+    }
+    bool known = !p.offsets;
+    for (long long i = blockIdx.y * 8 + threadIdx.x / 32; i < p.rows; i += gridDim.y * 8) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float *from = p.planes + which * p.of_result + i * p.pitch + j;
+        if (j < p.cols)
+            for (int s = 0; s < p.parts; s += 4, from += 4 * p.plane) {
+                float4 w[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) w[u] = s + u < p.parts ? *reinterpret_cast<const float4 *>(from + u * p.plane) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v = make_float4(v.x + w[u].x, v.y + w[u].y, v.z + w[u].z, v.w + w[u].w);
+            }
+        if (!known) {
+            last = min(__reduce_max_sync(0xffffffffu, last), p.rows);
+            known = true;
+        }
+        if (i < first || i >= last || j >= p.cols) continue;
+        const uint32_t lo = p.bf16 ? pack<__nv_bfloat162>(v.x, v.y) : pack<__half2>(v.x, v.y), hi = p.bf16 ? pack<__nv_bfloat162>(v.z, v.w) : pack<__half2>(v.z, v.w);
+        const int g = p.offsets ? 0 : (int)i / p.group_rows;
+        uint16_t *to = p.out[which] + g * p.stride[which] + (i - (long long)g * p.group_rows) * p.ld[which] + j;
+        if (j + 4 <= p.cols && reinterpret_cast<uintptr_t>(to) % 8 == 0) *reinterpret_cast<uint2 *>(to) = make_uint2(lo, hi);
+        else {
+            const uint16_t e[4] = {(uint16_t)lo, (uint16_t)(lo >> 16), (uint16_t)hi, (uint16_t)(hi >> 16)};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (j + k < p.cols) to[k] = e[k];
+        }
+    }
+}
+
 typedef void (*Kernel)(const Maps, const Params);
+// (of reductions in parts kernels of their own: one for both took 99 us instead of 91 for the gradients of a gated block of 512 rows, 16 groups, 1024 -> 2816)
 template <int kCtas>
-Kernel kernel_for(int mode) {
-    return mode == kGroupedPlain ? tc_grouped_kernel<kCtas, kGroupedPlain> : mode == kGroupedGated ? tc_grouped_kernel<kCtas, kGroupedGated> : tc_grouped_kernel<kCtas, kGroupedGrad>;
+Kernel kernel_for(int mode, bool parts) {
+    if (parts) return mode == kGroupedPlain ? tc_grouped_kernel<kCtas, kGroupedPlain, true> : tc_grouped_kernel<kCtas, kGroupedGrad, true>;
+    return mode == kGroupedPlain ? tc_grouped_kernel<kCtas, kGroupedPlain, false> : mode == kGroupedGated ? tc_grouped_kernel<kCtas, kGroupedGated, false>
+                                                                                : tc_grouped_kernel<kCtas, kGroupedGrad, false>;
 }
 
 // The kernel's shared memory allowed for, once a device
 cudaError_t allow_shared_memory(Kernel kernel, int index) {
-    static std::atomic<uint64_t> done[6];
+    static std::atomic<uint64_t> done[12];
     int dev = 0;
     const cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
@@ -714,27 +836,93 @@ int blocks_per_stage(const GroupedProblem &d, int along, int blocks_in_ring) {
     if (const char *e = getenv("ONNXB_GROUPED_KS")) return blocks_in_ring >= 6 && e[0] == '2' ? 2 : 1;
     return blocks_in_ring >= 8 && (d.mode != kGroupedGrad || d.rows / std::min(d.rows, d.groups) >= 256) ? 2 : 1;
 }
-Tile pick_tile(const GroupedProblem &d) {
-    // "<CTAs>x<rows>" in ONNXB_GROUPED_TILE pins the shape for A/B measurements and tests
-    if (const char *e = getenv("ONNXB_GROUPED_TILE")) {
-        const Tile t{e[0] - '0', e[0] && e[1] == 'x' ? atoi(e + 2) : 0};
-        if (tile_allowed(t)) return t;
-    }
-    const int all = (d.rows + 15) / 16 * 16;
-    // The gradients: pairs, and as many rows as they take (32 groups of 4 to 128 rows, 2048 x 1408: a tenth to a fifth faster than one CTA, and no slower with
-    // more rows than groups have).
-    if (d.mode == kGroupedGrad) return Tile{2, std::min(256, all)};
-    // Twice the rows that groups have on average, since some have more (32 groups of 32 rows, 2048 x 1408: gated block in tiles of 32, 64 and 128 rows 66, 60 and 63 us), and
-    // pairs from 33 rows on (64 rows: 68 us in tiles of one CTA, 66 of two); but no fewer tiles than half of the SMs have work with (2048 rows of 8 groups, 7168 x 512:
-    // tiles of 256, 128 and 64 rows 37, 29 and 28 us).
-    const int groups = std::min(d.rows, d.groups), per_group = (d.rows + groups - 1) / groups, ctas = per_group > 32 ? 2 : 1;
-    int rows = 32;
-    while (rows < 128 * ctas && rows < 2 * per_group) rows *= 2;
-    const long long across = ceil_div(d.channels, (d.mode == kGroupedGated ? kBox : kBM) * ctas);
-    while (rows > 64 && groups * ceil_div(per_group, rows) * across * ctas < 74) rows /= 2;
-    return Tile{ctas, std::min(rows, all)};
+long long plane_pitch(int cols) { return (cols + 3ll) / 4 * 4; }
+// Tiles, and parts of the reductions (of the weights' gradients, or of the forward product): by the sizes alone, since the workspace depends on the parts, and whichever
+// gradients are wanted, so that each is the same bit by bit with others and without.
+struct Plan {
+    Tile tile;
+    int parts;
+};
+// SM cycles a B200's 148 SMs take for a forward product, roughly: waves of tiles whose stages cost what the single threads take (measured: 300 to 350 cycles a block in
+// stages of two, 400 to 440 of one), or what L2 or DRAM bring.  Groups have rows that differ: a tile more each than whole ones.  Parts cost a launch, and planes of fp32.
+double forward_cost(const GroupedProblem &d, Tile t, int parts) {
+    const int groups = std::min(d.rows, d.groups), per = (d.rows + groups - 1) / groups, b = t.rows / t.ctas, ks = d.width % kTerms == 0 && b <= 64 ? 2 : 1;
+    const double across = (double)ceil_div(d.channels, (d.mode == kGroupedGated ? kBox : kBM) * t.ctas), kb = (double)ceil_div(d.width, kTerms);
+    const double tiles = (double)groups * (groups > 1 ? per / t.rows + 1 : ceil_div(per, t.rows)) * across, waves = tiles * parts * t.ctas / 148;
+    const double each = ceil(kb / parts) * (ks == 2 ? 270 + 1.2 * b : 380 + 0.5 * b) + 1500 + (d.mode == kGroupedGated ? 24 : 12) * t.rows;
+    const double l2 = tiles * t.ctas * kb * (kABytes + b * kRowBytes) / 8900, dram = 2.0 * groups * d.channels * d.width * (d.mode == kGroupedGated ? 2 : 1) / 3400;
+    const double cost = std::max({(waves > 4 ? waves + 0.5 : ceil(waves)) * each, l2, dram});
+    return cost + 11000 + (parts > 1 ? 4000 + (8.0 * parts + 2) * d.rows * (double)d.channels / 4500 : 0);
 }
-
+// The same of gradients: the tiles of rows first, then the weights', each taken by the pair that is free first
+double backward_cost(const GroupedProblem &d, Tile t, int parts) {
+    const int groups = std::min(d.rows, d.groups), per = (d.rows + groups - 1) / groups, units = 148 / t.ctas;
+    const double across = (double)ceil_div(d.width, kBM * t.ctas), of_rows = groups * (groups > 1 ? per / t.rows + 1 : ceil_div(per, t.rows)) * across;
+    const double of_weights = d.groups * d.terms * ceil_div(d.channels, kBM * t.ctas) * across * parts;
+    const double x = d.terms * ceil_div(d.channels, kTerms) * 450 + 4500, w = ceil((double)ceil_div(per, kTerms) / parts) * 550 + 4500;
+    // pairs that end their last tile of rows early, and late; until a time they have so many of the weights'
+    const double waves = floor(of_rows / units), late = of_rows - waves * units, begins = waves * x, begins_late = begins + (late > 0 ? x : 0);
+    auto has = [&](double until) { return late * floor(std::max(0.0, until - begins_late) / w) + (units - late) * floor(std::max(0.0, until - begins) / w); };
+    double end = begins_late;
+    for (double k = 1; has(end) < of_weights; ++k) {
+        end = std::max(begins_late, begins + k * w);
+        if (has(end) < of_weights) end = begins_late + k * w;
+    }
+    return end + 11000 + (parts > 1 ? 4000 + (8.0 * parts + 2) * d.groups * d.terms * (double)d.channels * d.width / 3000 : 0);
+}
+// Forward products.  Twice the rows that groups have on average, since some have more (32 groups of 32 rows, 2048 x 1408: gated block in tiles of 32, 64 and 128 rows 66, 60 and
+// 63 us), and pairs from 33 rows on (64 rows: 68 us in tiles of one CTA, 66 of two).  Where that would be fewer tiles than SMs, what costs least (512 rows of 4 groups, 8192 ->
+// 1024: 27.1 us in 40 tiles of 64 rows, 35.0 in 16 of 256, 20.9 with four parts of each; 13926 rows of one, 64 -> 72: in tiles of 256 rows 9.7, of 128 6.6).
+Plan forward_plan(const GroupedProblem &d, bool any_tile, Plan plan, bool any_parts) {
+    const int groups = std::min(d.rows, d.groups), per_group = (d.rows + groups - 1) / groups, all = (d.rows + 15) / 16 * 16, kb = (int)ceil_div(d.width, kTerms);
+    if (any_tile) {
+        plan.tile = Tile{per_group > 32 ? 2 : 1, 32};
+        while (plan.tile.rows < 128 * plan.tile.ctas && plan.tile.rows < 2 * per_group) plan.tile.rows *= 2;
+        plan.tile.rows = std::min(plan.tile.rows, all);
+    }
+    const bool gated = d.mode == kGroupedGated;
+    if (groups * ceil_div(per_group, plan.tile.rows) * ceil_div(d.channels, (gated ? kBox : kBM) * plan.tile.ctas) * plan.tile.ctas >= 148) return plan;
+    const Plan first = plan;
+    double best = 0.93 * forward_cost(d, first.tile, first.parts);
+    for (int ctas = 1; ctas <= 2; ++ctas)
+        for (int rows = 32; rows <= 128 * ctas; rows *= 2)
+            for (int parts = 1; parts <= (gated ? 1 : 16); parts *= 2) {
+                if (parts > 1 && kb < 8 * parts) continue;
+                const Plan other{any_tile ? Tile{ctas, std::min(rows, all)} : first.tile, any_parts ? parts : first.parts};
+                const double cost = forward_cost(d, other.tile, other.parts);
+                if (cost < best) {
+                    best = cost;
+                    plan = other;
+                }
+            }
+    return plan;
+}
+// Gradients: pairs, and as many rows as they take (32 groups of 4 to 128 rows, 2048 x 1408: a tenth to a fifth faster than one CTA, and no slower with more rows than groups
+// have).  Parts of the weights' gradients where there are few tiles and much to add up (4096 rows of one group, 512 x 512: 25.3 us in one, 19.1, 15.7 and 16.8 in 2, 4 and 8;
+// but 4096 of 4, 128 x 2048, 19.9, 22.8 and 25.9 in 1, 2 and 4).
+Plan backward_plan(const GroupedProblem &d, bool any_tile, Plan plan, bool any_parts) {
+    const int groups = std::min(d.rows, d.groups), per_group = (d.rows + groups - 1) / groups;
+    if (any_tile) plan.tile = Tile{2, std::min(256, (d.rows + 15) / 16 * 16)};
+    const long long across = ceil_div(d.width, kBM * plan.tile.ctas);
+    const double tiles = (double)across * (groups * ceil_div(per_group, plan.tile.rows) + groups * d.terms * ceil_div(d.channels, kBM * plan.tile.ctas));
+    if (!any_parts || tiles * plan.tile.ctas > 4 * 148) return plan;
+    double best = backward_cost(d, plan.tile, 1);
+    for (int parts = 2; parts <= 16 && per_group >= 4 * parts * kTerms; parts *= 2) {
+        const double cost = backward_cost(d, plan.tile, parts);
+        if (cost < 0.93 * best) {
+            best = cost;
+            plan.parts = parts;
+        }
+    }
+    return plan;
+}
+Plan pick_plan(const GroupedProblem &d) {
+    // "<CTAs>x<rows>" in ONNXB_GROUPED_TILE, and ONNXB_GROUPED_PARTS, pin them for A/B measurements and tests
+    const char *shape = getenv("ONNXB_GROUPED_TILE"), *parts = getenv("ONNXB_GROUPED_PARTS");
+    const Tile tile{shape && shape[0] ? shape[0] - '0' : 0, shape && shape[0] && shape[1] == 'x' ? atoi(shape + 2) : 0};
+    const Plan plan{tile, parts && d.mode != kGroupedGated ? std::max(1, std::min(16, atoi(parts))) : 1};
+    return d.mode == kGroupedGrad ? backward_plan(d, !tile_allowed(tile), plan, !parts) : forward_plan(d, !tile_allowed(tile), plan, !parts);
+}
 // Rows that begin at multiples of 16 bytes, as (terms, rows, 1, 1) in boxes of 64 by `box`; groups' weights as (terms, channels, 1, groups).  Where `blocks` is not 0
 // (terms of a block, rows, blocks, 1) and (terms of a block, channels, blocks, groups), `blocks` of them a copy: of reductions that are whole blocks.
 bool rows_map(CUtensorMap *m, const DenseOperand &o, long long rows, long long cols, int box, int blocks = 0) {
@@ -755,10 +943,18 @@ bool by_16(const void *p, long long ld) { return reinterpret_cast<uintptr_t>(p) 
 
 }  // namespace
 
+size_t tc_grouped_workspace(const GroupedProblem &d, int weights) {
+    const bool grad = d.mode == kGroupedGrad;
+    const int parts = pick_plan(d).parts;
+    const long long rows = grad ? (long long)weights * d.groups * d.channels : d.rows;
+    return parts > 1 ? (size_t)(parts * rows * plane_pitch(grad ? d.width : d.channels)) * 4 : 0;
+}
+
 int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     using namespace tc_host;
     const bool gated = d.mode == kGroupedGated, grad = d.mode == kGroupedGrad;
-    const Tile tile = pick_tile(d);
+    const Plan plan = pick_plan(d);
+    const Tile tile = plan.tile;
     Params p{};
     p.rows = d.rows; p.groups = d.groups; p.offsets = d.offsets;
     p.channels = d.channels; p.width = d.width;
@@ -775,9 +971,10 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     p.BN = kBM * tile.ctas;
     p.w_tiles_m = (int)ceil_div(d.channels, kBM * tile.ctas);
     p.w_tiles_n = (int)ceil_div(d.width, p.BN);
+    p.parts = grad && !p.w_count ? 1 : plan.parts;
     const long long w_total = (long long)d.groups * p.w_count * p.w_tiles_m * p.w_tiles_n;
     // tiles of rows: at most one more for each group than whole ones
-    const long long row_tiles = grad && !p.with_x ? 0 : d.rows / tile.rows + std::min(d.groups, d.rows), most = row_tiles * p.tiles_n + w_total;
+    const long long row_tiles = grad && !p.with_x ? 0 : d.rows / tile.rows + std::min(d.groups, d.rows), most = row_tiles * p.tiles_n * (grad ? 1 : p.parts) + w_total * p.parts;
     if (most > 0x7fffffffLL / 4 || (long long)p.band * std::max(p.tiles_n, p.w_tiles_n) > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
     p.w_total = (int)w_total;
     // (B: the rows of a CTA's part of a tile, or of the gradients of weights its columns)
@@ -803,6 +1000,8 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     }
     p.err = device_status_ptr();
     if (!p.err) return (int)cudaErrorUnknown;
+    p.planes = static_cast<float *>(d.planes);
+    p.pitch = plane_pitch(grad ? d.width : d.channels);
 
     Maps maps{};
     bool fine = true;
@@ -822,14 +1021,34 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     if (!fine) return (int)cudaErrorInvalidValue;
 
     const size_t smem = smem_with_tmem(1024 + (size_t)p.num_stages * p.stage_bytes + staging + kBarrierBytes + table, 512);
-    const Kernel kernel = tile.ctas == 2 ? kernel_for<2>(d.mode) : kernel_for<1>(d.mode);
-    const cudaError_t attr_err = allow_shared_memory(kernel, (tile.ctas - 1) * 3 + d.mode);
+    const bool in_parts = p.parts > 1;
+    const Kernel kernel = tile.ctas == 2 ? kernel_for<2>(d.mode, in_parts) : kernel_for<1>(d.mode, in_parts);
+    const cudaError_t attr_err = allow_shared_memory(kernel, ((tile.ctas - 1) * 2 + in_parts) * 3 + d.mode);
     if (attr_err != cudaSuccess) return (int)attr_err;
     const int grid = (int)most * tile.ctas;
     const cudaError_t e = tile.ctas == 2 ? launch_pdl_cluster(kernel, 2u, dim3(grid), dim3(kThreads), smem, stream, maps, p)
                                          : launch_pdl(kernel, dim3(grid), dim3(kThreads), smem, stream, maps, p);
     count_launch();
-    return (int)e;
+    if (e != cudaSuccess || !in_parts) return (int)e;
+    SumProblem sum{};
+    sum.planes = p.planes; sum.pitch = p.pitch; sum.parts = p.parts;
+    sum.offsets = grad ? nullptr : d.offsets; sum.groups = d.groups; sum.bf16 = bf16;
+    sum.rows = grad ? d.groups * d.channels : d.rows;
+    sum.group_rows = d.channels;
+    sum.cols = grad ? d.width : d.channels;
+    const int results = grad ? p.w_count : 1;
+    sum.of_result = sum.rows * p.pitch;
+    sum.plane = results * sum.of_result;
+    for (int i = 0; i < results; ++i) {
+        const int w = p.w_first + i;
+        sum.out[i] = static_cast<uint16_t *>(grad ? p.D[w] : p.Y[0]);
+        sum.ld[i] = grad ? p.d_ld[w] : p.y_ld[0];
+        sum.stride[i] = grad ? p.d_stride[w] : 0;
+    }
+    const dim3 sum_grid((unsigned)ceil_div(sum.cols, 128), (unsigned)std::min(65535ll, ceil_div(sum.rows, 8)), (unsigned)results);
+    const cudaError_t sum_err = launch_pdl(grouped_sum_kernel, sum_grid, dim3(256), 0, stream, sum);
+    count_launch();
+    return (int)sum_err;
 }
 
 }  // namespace onnxb

@@ -176,6 +176,50 @@ def test_blocks_of_a_stage(tile, blocks, monkeypatch):
 
 
 @gpu
+@pytest.mark.parametrize("parts", ["2", "3", "16"])
+@pytest.mark.parametrize("tile", ["1x48", "2x32", "2x256"])
+@pytest.mark.parametrize("t", list(TYPES))
+def test_parts_of_the_sums(parts, tile, t, monkeypatch):
+    """Reductions in parts, some of which have no stages: of groups with few rows or none, and with the last stage in either; rows of no group stay as they were."""
+    monkeypatch.setenv("ONNXB_GROUPED_TILE", tile)
+    monkeypatch.setenv("ONNXB_GROUPED_PARTS", parts)
+    for case in (Case([130, 0, 1, 77, 300, 16, 64, 192], 320, 448, TYPES[t], seed=3, before=5, behind=70), Case([257, 63, 129], 129, 65, TYPES[t], seed=5, behind=1),
+                 Case([5], 1000, 8, TYPES[t], seed=6), Case([1500, 700], 40, 136, TYPES[t], seed=7)):
+        check_all(case)
+        outside = torch.ones(case.R, dtype=torch.bool, device="cuda")
+        outside[case.rows()] = False
+        Y, dX = (torch.full((case.R, n), 7.0, dtype=case.t, device="cuda") for n in (case.N, case.K))
+        binding.onnx_grouped_gemm(case.X, case.W, case.offsets, Y=Y)
+        binding.onnx_grouped_gemm_backward(case.dY, case.X, case.W, case.offsets, dX=dX)
+        assert (Y[outside] == 7.0).all() and (dX[outside] == 7.0).all()
+        every = binding.onnx_grouped_gated_backward(case.dY, case.X, case.W, case.Wu, case.G, case.U, case.offsets)
+        for i in range(1, 7):
+            wanted = [bool(i & b) for b in (1, 2, 4)]
+            some = binding.onnx_grouped_gated_backward(case.dY, case.X, case.W, case.Wu, case.G, case.U, case.offsets, wanted=wanted)
+            for w, a, b in zip(wanted, some, every):
+                assert not w or torch.equal(a[outside.logical_not()] if a.dim() == 2 else a, b[outside.logical_not()] if b.dim() == 2 else b)
+
+
+@gpu
+def test_long_sums_of_few_tiles():
+    """Sizes whose sums are in parts by themselves, also of views, of offsets that do not rise and of a group that has all rows."""
+    for c in (Case([2000, 1500], 4224, 64, torch.bfloat16, seed=1), Case([4000], 64, 200, torch.float16, seed=2, before=3, behind=9),
+              Case([0, 900, 3], 72, 4104, torch.bfloat16, seed=3), Case([3, 0, 0, 3000], 96, 96, torch.bfloat16, seed=4)):
+        check_all(c)
+        wide = torch.full((c.R, c.N + 3), 7.0, dtype=c.t, device="cuda")
+        binding.onnx_grouped_gemm(c.X, c.W, c.offsets, Y=wide[:, 1:1 + c.N])
+        check_gemm(c, wide[:, 1:1 + c.N])
+        assert (wide[:, 0] == 7.0).all() and (wide[:, 1 + c.N:] == 7.0).all()
+        store = torch.full((len(c.sizes), c.N + 1, c.K + 5), 7.0, dtype=c.t, device="cuda")
+        dX, dW = binding.onnx_grouped_gemm_backward(c.dY, c.X, c.W, c.offsets, dW=store[:, :c.N, :c.K])
+        check_gemm_backward(c, dX, dW)
+        assert (store[:, c.N:] == 7.0).all() and (store[:, :, c.K:] == 7.0).all()
+    c.ends, c.sizes = [0, 50, 50, 3003, 3003], [50, 0, 2953, 0]
+    c.offsets = torch.tensor([-7, 50, 20, 2 ** 31 - 1, 5], dtype=torch.int32, device="cuda")
+    check_all(c)
+
+
+@gpu
 @pytest.mark.parametrize("K,N", [(1, 1), (7, 9), (65, 33), (100, 101), (777, 130), (130, 777)])
 @pytest.mark.parametrize("t", list(TYPES))
 def test_odd_widths(K, N, t, few):
