@@ -38,8 +38,9 @@ struct GroupedProblem {
 // (in_place: the weights begin where the tensor cores' kernel can read them)
 bool grouped_few_fits(int rows, int groups, bool in_place);
 int launch_grouped_few(const GroupedProblem &p, cudaStream_t stream);
-// Scratch that launch_tc_grouped needs, by `mode`, `rows`, `groups`, `channels`, `width` and `terms` alone, for so many weights' gradients (of gradients)
-size_t tc_grouped_workspace(const GroupedProblem &p, int weights);
+// Scratch that launch_tc_grouped needs, by `mode`, `rows`, `groups`, `channels`, `width` and `terms` alone, for results by row (dX, or a forward product) and so many
+// weights' gradients
+size_t tc_grouped_workspace(const GroupedProblem &p, bool rows, int weights);
 // On the tensor cores (tc_grouped.cu).  Operands' rows and groups begin at multiples of 16 bytes.
 int launch_tc_grouped(const GroupedProblem &p, cudaStream_t stream);
 

@@ -93,7 +93,7 @@ static GroupedProblem sizes_of(int mode, const onnxb_matrix *rows, int64_t chann
 static bool groups_are_some(const onnxb_matrices *m) { return m && m->count >= 1 && m->count <= kMostGroups && m->rows >= 1 && m->rows <= kMostSize && m->cols >= 1 && m->cols <= kMostSize; }
 extern "C" size_t onnx_grouped_gemm_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *W) {
     if (!sizes_are_some(X) || !groups_are_some(W) || few(X, W, nullptr)) return 0;
-    return views::copy_bytes(X) + copy_bytes(W) + tc_grouped_workspace(sizes_of(kGroupedPlain, X, W->rows, W->cols, W->count, 1), 0);
+    return views::copy_bytes(X) + copy_bytes(W) + tc_grouped_workspace(sizes_of(kGroupedPlain, X, W->rows, W->cols, W->count, 1), true, 0);
 }
 extern "C" size_t onnx_grouped_gated_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu) {
     return few(X, Wg, Wu) ? 0 : views::copy_bytes(X) + copy_bytes(Wg) + copy_bytes(Wu);
@@ -164,7 +164,7 @@ static size_t slope_bytes(int64_t rows, int64_t channels) { return (size_t)(rows
 static size_t planes_bytes(const onnxb_matrix *dY, const onnxb_matrices *const *W, const onnxb_matrix *dX, const onnxb_matrices *const *D, int terms) {
     const onnxb_matrices *one = dX ? W[0] : D[0] ? D[0] : D[1];
     if (!sizes_are_some(dY) || !groups_are_some(one)) return 0;
-    return tc_grouped_workspace(sizes_of(kGroupedGrad, dY, dY->cols, one->cols, one->count, terms), (D[0] != nullptr) + (D[1] != nullptr));
+    return tc_grouped_workspace(sizes_of(kGroupedGrad, dY, dY->cols, one->cols, one->count, terms), dX != nullptr, (D[0] != nullptr) + (D[1] != nullptr));
 }
 
 extern "C" size_t onnx_grouped_gemm_backward_workspace_bytes(const onnxb_matrix *dY, const onnxb_matrix *X, const onnxb_matrices *W, const onnxb_matrix *dX,

@@ -25,13 +25,13 @@
 //     they are not finite zeros on the other side would not help: warp 10 clears them on both sides, up to the next multiple of 16 rows, and the
 //     stage's instructions end there.  Such a stage's copies complete on a barrier of this CTA's own, since of a pair each CTA clears what it holds.
 //   - Groups without rows: their weights' gradients are zeros, stored without a product.
-//   - Where a forward product or the weights' gradients have few tiles and a long reduction, tiles have parts of it, whose sums go to planes of fp32 that a second kernel adds
-//     up (73 rows of 17 groups, 6912 -> 64: 20.2 -> 11.8 us; gradients of 10272 rows of one group, 3712 x 72, 53.9 -> 36.7).  Not dX, whose reduction is the
-//     shorter one where it has few tiles: a microsecond at most.
+//   - Where a forward product, dX or the weights' gradients have few tiles and a long reduction, tiles have parts of it, whose sums go to planes of fp32 that a second kernel adds
+//     up (73 rows of 17 groups, 6912 -> 64: 20.2 -> 11.8 us; gradients of 10272 rows of one group, 3712 x 72, 53.9 -> 36.7).
 #include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <array>
 #include <atomic>
 #include <cstdlib>
 #include <cstring>
@@ -78,9 +78,9 @@ struct Params {
     int BN;                        // columns of a tile of the weights' gradients
     int w_tiles_m, w_tiles_n, w_total;     // row and column tiles of one weights' gradient; tiles of all of them
     int w_first, w_count;          // the first that is wanted; how many are
-    int parts;                     // of the reductions (of the weights' gradients, or of the forward product), where they are several,
-    float *planes;                 // each with a plane of fp32 of its own
-    long long pitch;               // floats of their rows
+    int x_parts, w_parts;          // of the reductions of tiles of rows, and of the weights' gradients; where they are several,
+    float *x_planes, *w_planes;    // each with a plane of fp32 of its own
+    long long x_pitch, w_pitch;    // floats of their rows
     int num_stages;
     uint32_t idesc_x, idesc_w;     // (of tiles of rows without their columns)
     int ks;                        // K blocks of a stage
@@ -127,27 +127,23 @@ __device__ __forceinline__ void place(int band, int tiles_m, int tiles_n, int r,
 template <int kMode, bool kParts>
 __device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t, TileAt &at) {
     constexpr bool kGrad = kMode == kGroupedGrad;
-    const int parts = kParts ? p.parts : 1, of_rows = !kGrad || p.with_x ? s.tiles[p.groups] * p.tiles_n * (kGrad ? 1 : parts) : 0;
+    const int of_rows = !kGrad || p.with_x ? s.tiles[p.groups] * p.tiles_n * (kParts ? p.x_parts : 1) : 0;
     at.x = t < of_rows;
     at.z = 0;
     t = at.x ? t : t - of_rows;
     at.part = 0;
-    if (kParts && at.x != kGrad) {
+    const int parts = !kParts ? 1 : at.x ? p.x_parts : p.w_parts;
+    if (kParts) {
         // a tile's parts one after the other
         const int q = t / parts;
         at.part = t - q * parts;
         t = q;
     }
     auto share = [&](int stages) {
-        const int each = (stages + parts - 1) / parts;
-        at.kb0 = min(at.part * each, stages);
-        at.kb = min(each, stages - at.kb0);
-        at.ends = at.kb > 0 && at.kb0 + at.kb == stages;       // (parts behind the last stage have none)
-    };
-    auto whole = [&](int stages) {
-        at.kb0 = 0;
-        at.kb = stages;
-        at.ends = true;
+        const int each = kParts ? (stages + parts - 1) / parts : stages;
+        at.kb0 = kParts ? min(at.part * each, stages) : 0;
+        at.kb = kParts ? min(each, stages - at.kb0) : stages;
+        at.ends = !kParts || (at.kb > 0 && at.kb0 + at.kb == stages);      // (parts behind the last stage have none)
     };
     if (at.x) {
         const int q = t / p.tiles_n;
@@ -162,8 +158,7 @@ __device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t,
         const int all = s.first[lo + 1] - s.first[lo], per = rows_per_tile(all, p.most_rows);
         at.row0 = s.first[lo] + at.tm * per;
         at.rows = min(per, all - at.tm * per);
-        if (kParts && !kGrad) share(p.num_kb);
-        else whole(kGrad ? p.terms * p.num_kb : p.num_kb);
+        share(kGrad ? p.terms * p.num_kb : p.num_kb);
         return true;
     }
     if (!kGrad || t >= p.w_total) return false;
@@ -174,9 +169,7 @@ __device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t,
     place(p.band, p.w_tiles_m, p.w_tiles_n, r - at.z * per, at);
     at.row0 = s.first[at.g];
     at.rows = s.first[at.g + 1] - at.row0;
-    const int stages = (at.rows + kTerms * p.ks - 1) / (kTerms * p.ks);
-    if (kParts) share(stages);
-    else whole(stages);
+    share((at.rows + kTerms * p.ks - 1) / (kTerms * p.ks));
     return true;
 }
 
@@ -389,14 +382,17 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 c1 += by * d1;
                 c2 += by * d2;
             };
-            if (kParts) move(at.kb0);
             // (dX's second term: the same stages again of the other tensors)
             const int whole = at.kb - (tail ? 1 : 0), of_term = kGrad && at.x ? p.num_kb : whole;
-            load_whole(of_term);
-            if (kGrad && of_term < whole) {
+            const bool second_term = kParts && kGrad && at.x && at.kb0 >= of_term;
+            if (second_term) map += 1;
+            if (kParts) move(second_term ? at.kb0 - of_term : at.kb0);
+            const int now = kParts && kGrad && at.x && !second_term ? min(whole, of_term - at.kb0) : kParts ? whole : of_term;
+            load_whole(now);
+            if (kGrad && now < whole) {
                 map += 1;
                 move(-of_term);
-                load_whole(of_term);
+                load_whole(whole - now);
             }
             if (tail) {
                 mbar_wait(&empty[stage], phase ^ 1, p.err, 1);
@@ -625,21 +621,21 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
 #pragma unroll 1
                 for (int b = half; b < blocks; b += 2) {
                     uint32_t v[32];
-                    if (!kParts || kGrad || some) {
+                    if (!kParts || some) {
                         tmem_ld_32x32(tbase + (uint32_t)(b * 32), v);
                         tmem_ld_wait();
                     } else {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = 0u;
                     }
-                    if (kParts && !kGrad) {
+                    if (kParts && p.x_parts > 1) {
                         // a part of the reduction: as it is, 128 bytes of a row a warp
                         const int rows = at.rows - b * 32;
-                        float *out = p.planes + ((long long)at.part * p.rows + at.row0 + b * 32) * p.pitch + channel0 + lane;
+                        float *out = p.x_planes + ((long long)at.part * p.rows + at.row0 + b * 32) * p.x_pitch + channel0 + lane;
                         if (channel0 + lane < all)
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
-                                if (j < rows) out[j * p.pitch] = __uint_as_float(v[j]);
+                                if (j < rows) out[j * p.x_pitch] = __uint_as_float(v[j]);
                         continue;
                     }
                     store(0, b * 32, channel0, all, kAll, [&](int i) { return __uint_as_float(v[i]); });
@@ -660,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
 #pragma unroll
                             for (int j = 0; j < 32; ++j) v[j] = 0u;
                         }
-                        if (kParts) {
+                        if (kParts && p.w_parts > 1) {
                             // a part of the reduction: 32 columns of 32 rows laid out, and stored as they are, four rows at a time
                             if (b * 64 + c >= p.width - n0) break;
 #pragma unroll
@@ -668,11 +664,11 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                                 *reinterpret_cast<uint4 *>(buf + lane * kRowBytes + ((i ^ (lane & 7)) << 4)) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                             __syncwarp();
                             const int piece = lane & 7, col = n0 + b * 64 + c + piece * 4;
-                            float *out = p.planes + (((long long)at.part * p.w_count + at.z) * p.groups + at.g) * p.channels * p.pitch + row0 * p.pitch + col;
+                            float *out = p.w_planes + (((long long)at.part * p.w_count + at.z) * p.groups + at.g) * p.channels * p.w_pitch + row0 * p.w_pitch + col;
                             if (col < p.width)
 #pragma unroll 4
                                 for (int r = lane >> 3; r < rows; r += 4)
-                                    *reinterpret_cast<uint4 *>(out + r * p.pitch) = *reinterpret_cast<const uint4 *>(buf + r * kRowBytes + ((piece ^ (r & 7)) << 4));
+                                    *reinterpret_cast<uint4 *>(out + r * p.w_pitch) = *reinterpret_cast<const uint4 *>(buf + r * kRowBytes + ((piece ^ (r & 7)) << 4));
                             __syncwarp();
                             continue;
                         }
@@ -689,7 +685,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                             *reinterpret_cast<uint4 *>(buf + lane * kRowBytes + (((c / 8 + i) ^ (lane & 7)) << 4)) =
                                 make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
                     }
-                    if (kParts) continue;
+                    if (kParts && p.w_parts > 1) continue;
                     __syncwarp();
                     // Stored by rows, four at a time in pieces of 16 bytes, or one in pairs of elements
                     const int w = p.w_first + at.z, left = min(64, p.width - n0 - b * 64);
@@ -746,18 +742,22 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
 }
 
 // The parts' planes added up, in their order, and rounded: four columns a thread, 8 rows by 128 columns a block
-struct SumProblem {
+struct SumJob {
     const float *planes;
-    long long pitch, of_result, plane;       // floats of a row, of one result's planes, of all results'
+    long long pitch, plane;          // floats of a row, of a plane
     int parts, rows, cols;
-    uint16_t *out[2];
-    long long ld[2], stride[2];
-    int group_rows;                          // rows of a group's result
-    const int *offsets;                      // of results by row (else NULL), of which those alone are written that are a group's
+    uint16_t *out;
+    long long ld, stride;
+    int group_rows;                  // rows of a group's result
+    const int *offsets;              // of results by row (else NULL), of which those alone are written that are a group's
+};
+struct SumProblem {
+    SumJob job[3];
     int groups, bf16;
 };
-__global__ void __launch_bounds__(256) grouped_sum_kernel(const __grid_constant__ SumProblem p) {
-    const int which = blockIdx.z, j = (blockIdx.x * 32 + threadIdx.x % 32) * 4;
+__global__ void __launch_bounds__(256) grouped_sum_kernel(const __grid_constant__ SumProblem problem) {
+    const SumJob &p = problem.job[blockIdx.z];
+    const int j = (blockIdx.x * 32 + threadIdx.x % 32) * 4;
     pdl_launch_dependents();
     pdl_wait();
     // (the offsets are on their way while the planes are read, of rows of no group too)
@@ -765,12 +765,12 @@ __global__ void __launch_bounds__(256) grouped_sum_kernel(const __grid_constant_
     if (p.offsets) {
         first = max(p.offsets[0], 0);
         last = 0;
-        for (int i = threadIdx.x % 32; i <= p.groups; i += 32) last = max(last, p.offsets[i]);
+        for (int i = threadIdx.x % 32; i <= problem.groups; i += 32) last = max(last, p.offsets[i]);
     }
     bool known = !p.offsets;
     for (long long i = blockIdx.y * 8 + threadIdx.x / 32; i < p.rows; i += gridDim.y * 8) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        const float *from = p.planes + which * p.of_result + i * p.pitch + j;
+        const float *from = p.planes + i * p.pitch + j;
         if (j < p.cols)
             for (int s = 0; s < p.parts; s += 4, from += 4 * p.plane) {
                 float4 w[4];
@@ -784,9 +784,9 @@ __global__ void __launch_bounds__(256) grouped_sum_kernel(const __grid_constant_
             known = true;
         }
         if (i < first || i >= last || j >= p.cols) continue;
-        const uint32_t lo = p.bf16 ? pack<__nv_bfloat162>(v.x, v.y) : pack<__half2>(v.x, v.y), hi = p.bf16 ? pack<__nv_bfloat162>(v.z, v.w) : pack<__half2>(v.z, v.w);
+        const uint32_t lo = problem.bf16 ? pack<__nv_bfloat162>(v.x, v.y) : pack<__half2>(v.x, v.y), hi = problem.bf16 ? pack<__nv_bfloat162>(v.z, v.w) : pack<__half2>(v.z, v.w);
         const int g = p.offsets ? 0 : (int)i / p.group_rows;
-        uint16_t *to = p.out[which] + g * p.stride[which] + (i - (long long)g * p.group_rows) * p.ld[which] + j;
+        uint16_t *to = p.out + g * p.stride + (i - (long long)g * p.group_rows) * p.ld + j;
         if (j + 4 <= p.cols && reinterpret_cast<uintptr_t>(to) % 8 == 0) *reinterpret_cast<uint2 *>(to) = make_uint2(lo, hi);
         else {
             const uint16_t e[4] = {(uint16_t)lo, (uint16_t)(lo >> 16), (uint16_t)hi, (uint16_t)(hi >> 16)};
@@ -837,11 +837,11 @@ int blocks_per_stage(const GroupedProblem &d, int along, int blocks_in_ring) {
     return blocks_in_ring >= 8 && (d.mode != kGroupedGrad || d.rows / std::min(d.rows, d.groups) >= 256) ? 2 : 1;
 }
 long long plane_pitch(int cols) { return (cols + 3ll) / 4 * 4; }
-// Tiles, and parts of the reductions (of the weights' gradients, or of the forward product): by the sizes alone, since the workspace depends on the parts, and whichever
+// Tiles, and parts of the reductions (of tiles of rows, of the weights' gradients): by the sizes alone, since the workspace depends on the parts, and whichever
 // gradients are wanted, so that each is the same bit by bit with others and without.
 struct Plan {
     Tile tile;
-    int parts;
+    int x, w;
 };
 // SM cycles a B200's 148 SMs take for a forward product, roughly: waves of tiles whose stages cost what the single threads take (measured: 300 to 350 cycles a block in
 // stages of two, 400 to 440 of one), or what L2 or DRAM bring.  Groups have rows that differ: a tile more each than whole ones.  Parts cost a launch, and planes of fp32.
@@ -855,20 +855,22 @@ double forward_cost(const GroupedProblem &d, Tile t, int parts) {
     return cost + 11000 + (parts > 1 ? 4000 + (8.0 * parts + 2) * d.rows * (double)d.channels / 4500 : 0);
 }
 // The same of gradients: the tiles of rows first, then the weights', each taken by the pair that is free first
-double backward_cost(const GroupedProblem &d, Tile t, int parts) {
+double backward_cost(const GroupedProblem &d, Tile t, int x_parts, int w_parts) {
     const int groups = std::min(d.rows, d.groups), per = (d.rows + groups - 1) / groups, units = 148 / t.ctas;
-    const double across = (double)ceil_div(d.width, kBM * t.ctas), of_rows = groups * (groups > 1 ? per / t.rows + 1 : ceil_div(per, t.rows)) * across;
-    const double of_weights = d.groups * d.terms * ceil_div(d.channels, kBM * t.ctas) * across * parts;
-    const double x = d.terms * ceil_div(d.channels, kTerms) * 450 + 4500, w = ceil((double)ceil_div(per, kTerms) / parts) * 550 + 4500;
+    const double across = (double)ceil_div(d.width, kBM * t.ctas), of_rows = groups * (groups > 1 ? per / t.rows + 1 : ceil_div(per, t.rows)) * across * x_parts;
+    const double of_weights = d.groups * d.terms * ceil_div(d.channels, kBM * t.ctas) * across * w_parts;
+    const double x = ceil((double)d.terms * ceil_div(d.channels, kTerms) / x_parts) * 450 + 4500, w = ceil((double)ceil_div(per, kTerms) / w_parts) * 550 + 4500;
     // pairs that end their last tile of rows early, and late; until a time they have so many of the weights'
     const double waves = floor(of_rows / units), late = of_rows - waves * units, begins = waves * x, begins_late = begins + (late > 0 ? x : 0);
     auto has = [&](double until) { return late * floor(std::max(0.0, until - begins_late) / w) + (units - late) * floor(std::max(0.0, until - begins) / w); };
+    // (not before all pairs would be done if they were done together)
     double end = begins_late;
-    for (double k = 1; has(end) < of_weights; ++k) {
+    for (double k = std::max(0.0, floor((late * begins_late + (units - late) * begins + of_weights * w) / units / w - begins_late / w)); has(end) < of_weights; ++k) {
         end = std::max(begins_late, begins + k * w);
         if (has(end) < of_weights) end = begins_late + k * w;
     }
-    return end + 11000 + (parts > 1 ? 4000 + (8.0 * parts + 2) * d.groups * d.terms * (double)d.channels * d.width / 3000 : 0);
+    return end + 11000 + (x_parts > 1 || w_parts > 1 ? 4000 : 0) + (x_parts > 1 ? (8.0 * x_parts + 2) * d.rows * (double)d.width / 3000 : 0) +
+           (w_parts > 1 ? (8.0 * w_parts + 2) * d.groups * d.terms * (double)d.channels * d.width / 3000 : 0);
 }
 // Forward products.  Twice the rows that groups have on average, since some have more (32 groups of 32 rows, 2048 x 1408: gated block in tiles of 32, 64 and 128 rows 66, 60 and
 // 63 us), and pairs from 33 rows on (64 rows: 68 us in tiles of one CTA, 66 of two).  Where that would be fewer tiles than SMs, what costs least (512 rows of 4 groups, 8192 ->
@@ -883,13 +885,13 @@ Plan forward_plan(const GroupedProblem &d, bool any_tile, Plan plan, bool any_pa
     const bool gated = d.mode == kGroupedGated;
     if (groups * ceil_div(per_group, plan.tile.rows) * ceil_div(d.channels, (gated ? kBox : kBM) * plan.tile.ctas) * plan.tile.ctas >= 148) return plan;
     const Plan first = plan;
-    double best = 0.93 * forward_cost(d, first.tile, first.parts);
+    double best = 0.93 * forward_cost(d, first.tile, first.x);
     for (int ctas = 1; ctas <= 2; ++ctas)
         for (int rows = 32; rows <= 128 * ctas; rows *= 2)
             for (int parts = 1; parts <= (gated ? 1 : 16); parts *= 2) {
                 if (parts > 1 && kb < 8 * parts) continue;
-                const Plan other{any_tile ? Tile{ctas, std::min(rows, all)} : first.tile, any_parts ? parts : first.parts};
-                const double cost = forward_cost(d, other.tile, other.parts);
+                const Plan other{any_tile ? Tile{ctas, std::min(rows, all)} : first.tile, any_parts ? parts : first.x, 1};
+                const double cost = forward_cost(d, other.tile, other.x);
                 if (cost < best) {
                     best = cost;
                     plan = other;
@@ -898,30 +900,54 @@ Plan forward_plan(const GroupedProblem &d, bool any_tile, Plan plan, bool any_pa
     return plan;
 }
 // Gradients: pairs, and as many rows as they take (32 groups of 4 to 128 rows, 2048 x 1408: a tenth to a fifth faster than one CTA, and no slower with more rows than groups
-// have).  Parts of the weights' gradients where there are few tiles and much to add up (4096 rows of one group, 512 x 512: 25.3 us in one, 19.1, 15.7 and 16.8 in 2, 4 and 8;
-// but 4096 of 4, 128 x 2048, 19.9, 22.8 and 25.9 in 1, 2 and 4).
+// have).  Parts where there are few tiles and much to add up: of the weights' gradients (4096 rows of one group, 512 x 512: 25.3 us in one, 19.1, 15.7 and 16.8 in 2, 4 and 8;
+// but 4096 of 4, 128 x 2048, 19.9, 22.8 and 25.9 in 1, 2 and 4), and of dX (gated block of 64 rows of one, 8192 x 512: 67.3 us in one, 30.3, 24.9 and 23.8 in 4, 8 and 16; but 300 of 4,
+// plain, 4096 x 1024, 26.9, 26.9 and 28.0 in 1, 2 and 4).
 Plan backward_plan(const GroupedProblem &d, bool any_tile, Plan plan, bool any_parts) {
     const int groups = std::min(d.rows, d.groups), per_group = (d.rows + groups - 1) / groups;
     if (any_tile) plan.tile = Tile{2, std::min(256, (d.rows + 15) / 16 * 16)};
     const long long across = ceil_div(d.width, kBM * plan.tile.ctas);
     const double tiles = (double)across * (groups * ceil_div(per_group, plan.tile.rows) + groups * d.terms * ceil_div(d.channels, kBM * plan.tile.ctas));
-    if (!any_parts || tiles * plan.tile.ctas > 4 * 148) return plan;
-    double best = backward_cost(d, plan.tile, 1);
-    for (int parts = 2; parts <= 16 && per_group >= 4 * parts * kTerms; parts *= 2) {
-        const double cost = backward_cost(d, plan.tile, parts);
-        if (cost < 0.93 * best) {
-            best = cost;
-            plan.parts = parts;
-        }
+    if (!any_parts || tiles * plan.tile.ctas > 16 * 148) return plan;
+    // Twice or four times the parts of either, as long as twice gains 7 %
+    const int of_rows = d.terms * (int)ceil_div(d.channels, kTerms), of_weights = (int)ceil_div(per_group, kTerms);
+    double best = backward_cost(d, plan.tile, 1, 1);
+    for (bool gains = true; gains;) {
+        const Plan from = plan;
+        gains = false;
+        for (int more = 2; more <= 4; more *= 2)
+            for (int which = 0; which < 2; ++which) {
+                const int x = which ? from.x : from.x * more, w = which ? from.w * more : from.w;
+                if (x > 16 || w > 16 || (which ? of_weights < 4 * w : of_rows < 4 * x)) continue;
+                const double cost = backward_cost(d, plan.tile, x, w), margin = more == 2 ? 1.07 : 1.145;
+                if (cost * margin >= best) continue;
+                best = cost * margin;
+                plan.x = x;
+                plan.w = w;
+                gains = true;
+            }
+        if (gains) best = backward_cost(d, plan.tile, plan.x, plan.w);
     }
     return plan;
 }
 Plan pick_plan(const GroupedProblem &d) {
-    // "<CTAs>x<rows>" in ONNXB_GROUPED_TILE, and ONNXB_GROUPED_PARTS, pin them for A/B measurements and tests
-    const char *shape = getenv("ONNXB_GROUPED_TILE"), *parts = getenv("ONNXB_GROUPED_PARTS");
+    // "<CTAs>x<rows>" in ONNXB_GROUPED_TILE, and "<parts>" or "<of rows>,<of weights>" in ONNXB_GROUPED_PARTS, pin them for A/B measurements and tests
+    const char *shape = getenv("ONNXB_GROUPED_TILE"), *parts = getenv("ONNXB_GROUPED_PARTS"), *comma = parts ? strchr(parts, ',') : nullptr;
     const Tile tile{shape && shape[0] ? shape[0] - '0' : 0, shape && shape[0] && shape[1] == 'x' ? atoi(shape + 2) : 0};
-    const Plan plan{tile, parts && d.mode != kGroupedGated ? std::max(1, std::min(16, atoi(parts))) : 1};
-    return d.mode == kGroupedGrad ? backward_plan(d, !tile_allowed(tile), plan, !parts) : forward_plan(d, !tile_allowed(tile), plan, !parts);
+    auto count = [](const char *e) { return std::max(1, std::min(16, atoi(e))); };
+    const Plan plan{tile, parts && d.mode != kGroupedGated ? count(parts) : 1, parts && d.mode == kGroupedGrad ? count(comma ? comma + 1 : parts) : 1};
+    // (the last sizes' plan is kept: a call asks twice, and it takes a microsecond)
+    const std::array<int, 6> sizes{d.mode, d.rows, d.groups, d.channels, d.width, d.terms};
+    static thread_local std::array<int, 6> last_sizes{-1};
+    static thread_local Plan last;
+    const bool pinned = shape || parts;
+    if (!pinned && sizes == last_sizes) return last;
+    const Plan found = d.mode == kGroupedGrad ? backward_plan(d, !tile_allowed(tile), plan, !parts) : forward_plan(d, !tile_allowed(tile), plan, !parts);
+    if (!pinned) {
+        last_sizes = sizes;
+        last = found;
+    }
+    return found;
 }
 // Rows that begin at multiples of 16 bytes, as (terms, rows, 1, 1) in boxes of 64 by `box`; groups' weights as (terms, channels, 1, groups).  Where `blocks` is not 0
 // (terms of a block, rows, blocks, 1) and (terms of a block, channels, blocks, groups), `blocks` of them a copy: of reductions that are whole blocks.
@@ -943,11 +969,11 @@ bool by_16(const void *p, long long ld) { return reinterpret_cast<uintptr_t>(p) 
 
 }  // namespace
 
-size_t tc_grouped_workspace(const GroupedProblem &d, int weights) {
-    const bool grad = d.mode == kGroupedGrad;
-    const int parts = pick_plan(d).parts;
-    const long long rows = grad ? (long long)weights * d.groups * d.channels : d.rows;
-    return parts > 1 ? (size_t)(parts * rows * plane_pitch(grad ? d.width : d.channels)) * 4 : 0;
+size_t tc_grouped_workspace(const GroupedProblem &d, bool rows, int weights) {
+    const Plan plan = pick_plan(d);
+    const long long of_rows = rows && plan.x > 1 ? plan.x * (long long)d.rows * plane_pitch(d.mode == kGroupedGrad ? d.width : d.channels) : 0;
+    const long long of_weights = plan.w > 1 ? (long long)plan.w * weights * d.groups * d.channels * plane_pitch(d.width) : 0;
+    return (size_t)(of_rows + of_weights) * 4;
 }
 
 int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
@@ -971,10 +997,11 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     p.BN = kBM * tile.ctas;
     p.w_tiles_m = (int)ceil_div(d.channels, kBM * tile.ctas);
     p.w_tiles_n = (int)ceil_div(d.width, p.BN);
-    p.parts = grad && !p.w_count ? 1 : plan.parts;
+    p.x_parts = grad && !p.with_x ? 1 : plan.x;
+    p.w_parts = p.w_count ? plan.w : 1;
     const long long w_total = (long long)d.groups * p.w_count * p.w_tiles_m * p.w_tiles_n;
     // tiles of rows: at most one more for each group than whole ones
-    const long long row_tiles = grad && !p.with_x ? 0 : d.rows / tile.rows + std::min(d.groups, d.rows), most = row_tiles * p.tiles_n * (grad ? 1 : p.parts) + w_total * p.parts;
+    const long long row_tiles = grad && !p.with_x ? 0 : d.rows / tile.rows + std::min(d.groups, d.rows), most = row_tiles * p.tiles_n * p.x_parts + w_total * p.w_parts;
     if (most > 0x7fffffffLL / 4 || (long long)p.band * std::max(p.tiles_n, p.w_tiles_n) > 0x7fffffffLL) return (int)cudaErrorInvalidValue;
     p.w_total = (int)w_total;
     // (B: the rows of a CTA's part of a tile, or of the gradients of weights its columns)
@@ -1000,8 +1027,11 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     }
     p.err = device_status_ptr();
     if (!p.err) return (int)cudaErrorUnknown;
-    p.planes = static_cast<float *>(d.planes);
-    p.pitch = plane_pitch(grad ? d.width : d.channels);
+    const int cols = grad ? d.width : d.channels;
+    p.x_pitch = plane_pitch(cols);
+    p.w_pitch = plane_pitch(d.width);
+    p.x_planes = static_cast<float *>(d.planes);
+    p.w_planes = p.x_planes + (p.x_parts > 1 ? p.x_parts * (long long)d.rows * p.x_pitch : 0);
 
     Maps maps{};
     bool fine = true;
@@ -1021,7 +1051,7 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     if (!fine) return (int)cudaErrorInvalidValue;
 
     const size_t smem = smem_with_tmem(1024 + (size_t)p.num_stages * p.stage_bytes + staging + kBarrierBytes + table, 512);
-    const bool in_parts = p.parts > 1;
+    const bool in_parts = p.x_parts > 1 || p.w_parts > 1;
     const Kernel kernel = tile.ctas == 2 ? kernel_for<2>(d.mode, in_parts) : kernel_for<1>(d.mode, in_parts);
     const cudaError_t attr_err = allow_shared_memory(kernel, ((tile.ctas - 1) * 2 + in_parts) * 3 + d.mode);
     if (attr_err != cudaSuccess) return (int)attr_err;
@@ -1031,21 +1061,20 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     count_launch();
     if (e != cudaSuccess || !in_parts) return (int)e;
     SumProblem sum{};
-    sum.planes = p.planes; sum.pitch = p.pitch; sum.parts = p.parts;
-    sum.offsets = grad ? nullptr : d.offsets; sum.groups = d.groups; sum.bf16 = bf16;
-    sum.rows = grad ? d.groups * d.channels : d.rows;
-    sum.group_rows = d.channels;
-    sum.cols = grad ? d.width : d.channels;
-    const int results = grad ? p.w_count : 1;
-    sum.of_result = sum.rows * p.pitch;
-    sum.plane = results * sum.of_result;
-    for (int i = 0; i < results; ++i) {
-        const int w = p.w_first + i;
-        sum.out[i] = static_cast<uint16_t *>(grad ? p.D[w] : p.Y[0]);
-        sum.ld[i] = grad ? p.d_ld[w] : p.y_ld[0];
-        sum.stride[i] = grad ? p.d_stride[w] : 0;
+    sum.groups = d.groups; sum.bf16 = bf16;
+    int jobs = 0, most_rows = 1;
+    if (p.x_parts > 1) {
+        sum.job[jobs++] = SumJob{p.x_planes, p.x_pitch, d.rows * p.x_pitch, p.x_parts, d.rows, cols, static_cast<uint16_t *>(p.Y[0]), p.y_ld[0], 0, 1, d.offsets};
+        most_rows = d.rows;
     }
-    const dim3 sum_grid((unsigned)ceil_div(sum.cols, 128), (unsigned)std::min(65535ll, ceil_div(sum.rows, 8)), (unsigned)results);
+    for (int i = 0; p.w_parts > 1 && i < p.w_count; ++i) {
+        const int w = p.w_first + i, rows = d.groups * d.channels;
+        const long long result = rows * p.w_pitch;
+        sum.job[jobs++] = SumJob{p.w_planes + i * result, p.w_pitch, p.w_count * result, p.w_parts, rows, d.width, static_cast<uint16_t *>(p.D[w]), p.d_ld[w],
+                                 p.d_stride[w], d.channels, nullptr};
+        most_rows = std::max(most_rows, rows);
+    }
+    const dim3 sum_grid((unsigned)ceil_div(cols, 128), (unsigned)std::min(65535ll, ceil_div(most_rows, 8)), (unsigned)jobs);
     const cudaError_t sum_err = launch_pdl(grouped_sum_kernel, sum_grid, dim3(256), 0, stream, sum);
     count_launch();
     return (int)sum_err;

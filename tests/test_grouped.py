@@ -176,7 +176,7 @@ def test_blocks_of_a_stage(tile, blocks, monkeypatch):
 
 
 @gpu
-@pytest.mark.parametrize("parts", ["2", "3", "16"])
+@pytest.mark.parametrize("parts", ["2", "3", "16", "3,1", "1,3"])
 @pytest.mark.parametrize("tile", ["1x48", "2x32", "2x256"])
 @pytest.mark.parametrize("t", list(TYPES))
 def test_parts_of_the_sums(parts, tile, t, monkeypatch):
@@ -204,7 +204,7 @@ def test_parts_of_the_sums(parts, tile, t, monkeypatch):
 def test_long_sums_of_few_tiles():
     """Sizes whose sums are in parts by themselves, also of views, of offsets that do not rise and of a group that has all rows."""
     for c in (Case([2000, 1500], 4224, 64, torch.bfloat16, seed=1), Case([4000], 64, 200, torch.float16, seed=2, before=3, behind=9),
-              Case([0, 900, 3], 72, 4104, torch.bfloat16, seed=3), Case([3, 0, 0, 3000], 96, 96, torch.bfloat16, seed=4)):
+              Case([0, 900, 3], 72, 4104, torch.bfloat16, seed=3), Case([120, 0, 130, 7], 64, 5184, torch.bfloat16, seed=8), Case([3, 0, 0, 3000], 96, 96, torch.bfloat16, seed=4)):
         check_all(c)
         wide = torch.full((c.R, c.N + 3), 7.0, dtype=c.t, device="cuda")
         binding.onnx_grouped_gemm(c.X, c.W, c.offsets, Y=wide[:, 1:1 + c.N])
