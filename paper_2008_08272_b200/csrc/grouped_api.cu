@@ -93,10 +93,11 @@ static GroupedProblem sizes_of(int mode, const onnxb_matrix *rows, int64_t chann
 static bool groups_are_some(const onnxb_matrices *m) { return m && m->count >= 1 && m->count <= kMostGroups && m->rows >= 1 && m->rows <= kMostSize && m->cols >= 1 && m->cols <= kMostSize; }
 extern "C" size_t onnx_grouped_gemm_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *W) {
     if (!sizes_are_some(X) || !groups_are_some(W) || few(X, W, nullptr)) return 0;
-    return views::copy_bytes(X) + copy_bytes(W) + tc_grouped_workspace(sizes_of(kGroupedPlain, X, W->rows, W->cols, W->count, 1), true, 0);
+    return views::copy_bytes(X) + copy_bytes(W) + tc_grouped_workspace(sizes_of(kGroupedPlain, X, W->rows, W->cols, W->count, 0), true, 0);
 }
 extern "C" size_t onnx_grouped_gated_workspace_bytes(const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu) {
-    return few(X, Wg, Wu) ? 0 : views::copy_bytes(X) + copy_bytes(Wg) + copy_bytes(Wu);
+    if (!sizes_are_some(X) || !groups_are_some(Wg) || few(X, Wg, Wu)) return 0;
+    return views::copy_bytes(X) + copy_bytes(Wg) + copy_bytes(Wu) + tc_grouped_workspace(sizes_of(kGroupedGated, X, Wg->rows, Wg->cols, Wg->count, 0), true, 0);
 }
 
 // Both forward products: Wu NULL for the plain one

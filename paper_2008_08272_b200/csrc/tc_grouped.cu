@@ -25,7 +25,7 @@
 //     they are not finite zeros on the other side would not help: warp 10 clears them on both sides, up to the next multiple of 16 rows, and the
 //     stage's instructions end there.  Such a stage's copies complete on a barrier of this CTA's own, since of a pair each CTA clears what it holds.
 //   - Groups without rows: their weights' gradients are zeros, stored without a product.
-//   - Where a forward product, dX or the weights' gradients have few tiles and a long reduction, tiles have parts of it, whose sums go to planes of fp32 that a second kernel adds
+//   - Where a product of rows or the weights' gradients have few tiles and a long reduction, tiles have parts of it, whose sums go to planes of fp32 that a second kernel adds
 //     up (73 rows of 17 groups, 6912 -> 64: 20.2 -> 11.8 us; gradients of 10272 rows of one group, 3712 x 72, 53.9 -> 36.7).
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -580,7 +580,29 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                         }
                 }
             };
-            if (kGated) {
+            // A part of the reduction: the tile's rows from `first` on as they are, 128 bytes of a row a warp
+            auto store_part = [&](int plane, int first, int channel0, int all) {
+                uint32_t v[32];
+                if (some) {
+                    tmem_ld_32x32(tbase + (uint32_t)first, v);
+                    tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = 0u;
+                }
+                const int rows = at.rows - first;
+                float *out = p.x_planes + ((long long)plane * p.rows + at.row0 + first) * p.x_pitch + channel0 + lane;
+                if (channel0 + lane < all)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j < rows) out[j * p.x_pitch] = __uint_as_float(v[j]);
+            };
+            if (kGated && kParts) {
+                // (as below; the gate's planes and the other factor's in turns)
+                const int channel0 = (at.tn * kCtas + rank) * kBox + (q & 1) * 32, blocks = channel0 < p.channels ? (at.rows + 31) / 32 : 0;
+#pragma unroll 1
+                for (int b = half; b < blocks; b += 2) store_part(at.part * 2 + (q >> 1), b * 32, channel0, p.channels);
+            } else if (kGated) {
                 // Lanes are channels, 64 of the gate and the same 64 of the other factor, columns rows.  The two warps that have the same 32 channels' go through
                 // the blocks of 32 rows together; of every quarter two share them in turns.
                 const int channel0 = (at.tn * kCtas + rank) * kBox + (q & 1) * 32, blocks = channel0 < p.channels ? (at.rows + 31) / 32 : 0;
@@ -620,24 +642,13 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 const std::integral_constant<int, 32> kAll;
 #pragma unroll 1
                 for (int b = half; b < blocks; b += 2) {
-                    uint32_t v[32];
-                    if (!kParts || some) {
-                        tmem_ld_32x32(tbase + (uint32_t)(b * 32), v);
-                        tmem_ld_wait();
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = 0u;
-                    }
                     if (kParts && p.x_parts > 1) {
-                        // a part of the reduction: as it is, 128 bytes of a row a warp
-                        const int rows = at.rows - b * 32;
-                        float *out = p.x_planes + ((long long)at.part * p.rows + at.row0 + b * 32) * p.x_pitch + channel0 + lane;
-                        if (channel0 + lane < all)
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j < rows) out[j * p.x_pitch] = __uint_as_float(v[j]);
+                        store_part(at.part, b * 32, channel0, all);
                         continue;
                     }
+                    uint32_t v[32];
+                    tmem_ld_32x32(tbase + (uint32_t)(b * 32), v);
+                    tmem_ld_wait();
                     store(0, b * 32, channel0, all, kAll, [&](int i) { return __uint_as_float(v[i]); });
                 }
             } else {
@@ -741,20 +752,22 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
     }
 }
 
-// The parts' planes added up, in their order, and rounded: four columns a thread, 8 rows by 128 columns a block
+// The parts' planes added up, in their order, and rounded: four columns a thread, 8 rows by 128 columns a block.  Of the gated block (kGated) those of both factors, and the
+// activation.
 struct SumJob {
     const float *planes;
-    long long pitch, plane;          // floats of a row, of a plane
+    long long pitch, plane, factor;  // floats of a row, of a plane (of both factors), of one factor's
     int parts, rows, cols;
-    uint16_t *out;
-    long long ld, stride;
+    uint16_t *out[3];                // (the gated block: H, and G and U or NULL)
+    long long ld[3], stride;
     int group_rows;                  // rows of a group's result
     const int *offsets;              // of results by row (else NULL), of which those alone are written that are a group's
 };
 struct SumProblem {
     SumJob job[3];
-    int groups, bf16;
+    int groups, bf16, activation;
 };
+template <bool kGated>
 __global__ void __launch_bounds__(256) grouped_sum_kernel(const __grid_constant__ SumProblem problem) {
     const SumJob &p = problem.job[blockIdx.z];
     const int j = (blockIdx.x * 32 + threadIdx.x % 32) * 4;
@@ -767,32 +780,50 @@ __global__ void __launch_bounds__(256) grouped_sum_kernel(const __grid_constant_
         last = 0;
         for (int i = threadIdx.x % 32; i <= problem.groups; i += 32) last = max(last, p.offsets[i]);
     }
-    bool known = !p.offsets;
-    for (long long i = blockIdx.y * 8 + threadIdx.x / 32; i < p.rows; i += gridDim.y * 8) {
+    auto sum = [&](const float *from) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        const float *from = p.planes + i * p.pitch + j;
-        if (j < p.cols)
-            for (int s = 0; s < p.parts; s += 4, from += 4 * p.plane) {
-                float4 w[4];
+        for (int s = 0; s < p.parts; s += 4, from += 4 * p.plane) {
+            float4 w[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) w[u] = s + u < p.parts ? *reinterpret_cast<const float4 *>(from + u * p.plane) : make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int u = 0; u < 4; ++u) w[u] = s + u < p.parts ? *reinterpret_cast<const float4 *>(from + u * p.plane) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) v = make_float4(v.x + w[u].x, v.y + w[u].y, v.z + w[u].z, v.w + w[u].w);
-            }
-        if (!known) {
-            last = min(__reduce_max_sync(0xffffffffu, last), p.rows);
-            known = true;
+            for (int u = 0; u < 4; ++u) v = make_float4(v.x + w[u].x, v.y + w[u].y, v.z + w[u].z, v.w + w[u].w);
         }
-        if (i < first || i >= last || j >= p.cols) continue;
+        return v;
+    };
+    auto put = [&](uint16_t *to, const float4 &v) {
         const uint32_t lo = problem.bf16 ? pack<__nv_bfloat162>(v.x, v.y) : pack<__half2>(v.x, v.y), hi = problem.bf16 ? pack<__nv_bfloat162>(v.z, v.w) : pack<__half2>(v.z, v.w);
-        const int g = p.offsets ? 0 : (int)i / p.group_rows;
-        uint16_t *to = p.out + g * p.stride + (i - (long long)g * p.group_rows) * p.ld + j;
         if (j + 4 <= p.cols && reinterpret_cast<uintptr_t>(to) % 8 == 0) *reinterpret_cast<uint2 *>(to) = make_uint2(lo, hi);
         else {
             const uint16_t e[4] = {(uint16_t)lo, (uint16_t)(lo >> 16), (uint16_t)hi, (uint16_t)(hi >> 16)};
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (j + k < p.cols) to[k] = e[k];
+        }
+    };
+    bool known = !p.offsets;
+    for (long long i = blockIdx.y * 8 + threadIdx.x / 32; i < p.rows; i += gridDim.y * 8) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f), u = v;
+        const float *from = p.planes + i * p.pitch + j;
+        if (j < p.cols) {
+            v = sum(from);
+            if (kGated) u = sum(from + p.factor);
+        }
+        if (!known) {
+            last = min(__reduce_max_sync(0xffffffffu, last), p.rows);
+            known = true;
+        }
+        if (i < first || i >= last || j >= p.cols) continue;
+        if (kGated) {
+            if (p.out[1]) {
+                put(p.out[1] + i * p.ld[1] + j, v);
+                put(p.out[2] + i * p.ld[2] + j, u);
+            }
+            const int kind = problem.activation;
+            put(p.out[0] + i * p.ld[0] + j, make_float4(activate(kind, v.x) * u.x, activate(kind, v.y) * u.y, activate(kind, v.z) * u.z, activate(kind, v.w) * u.w));
+        } else {
+            const int g = p.offsets ? 0 : (int)i / p.group_rows;
+            put(p.out[0] + g * p.stride + (i - (long long)g * p.group_rows) * p.ld[0] + j, v);
         }
     }
 }
@@ -801,7 +832,9 @@ typedef void (*Kernel)(const Maps, const Params);
 // (of reductions in parts kernels of their own: one for both took 99 us instead of 91 for the gradients of a gated block of 512 rows, 16 groups, 1024 -> 2816)
 template <int kCtas>
 Kernel kernel_for(int mode, bool parts) {
-    if (parts) return mode == kGroupedPlain ? tc_grouped_kernel<kCtas, kGroupedPlain, true> : tc_grouped_kernel<kCtas, kGroupedGrad, true>;
+    if (parts)
+        return mode == kGroupedPlain ? tc_grouped_kernel<kCtas, kGroupedPlain, true> : mode == kGroupedGated ? tc_grouped_kernel<kCtas, kGroupedGated, true>
+                                                                                   : tc_grouped_kernel<kCtas, kGroupedGrad, true>;
     return mode == kGroupedPlain ? tc_grouped_kernel<kCtas, kGroupedPlain, false> : mode == kGroupedGated ? tc_grouped_kernel<kCtas, kGroupedGated, false>
                                                                                 : tc_grouped_kernel<kCtas, kGroupedGrad, false>;
 }
@@ -847,12 +880,13 @@ struct Plan {
 // stages of two, 400 to 440 of one), or what L2 or DRAM bring.  Groups have rows that differ: a tile more each than whole ones.  Parts cost a launch, and planes of fp32.
 double forward_cost(const GroupedProblem &d, Tile t, int parts) {
     const int groups = std::min(d.rows, d.groups), per = (d.rows + groups - 1) / groups, b = t.rows / t.ctas, ks = d.width % kTerms == 0 && b <= 64 ? 2 : 1;
-    const double across = (double)ceil_div(d.channels, (d.mode == kGroupedGated ? kBox : kBM) * t.ctas), kb = (double)ceil_div(d.width, kTerms);
+    const int factors = d.mode == kGroupedGated ? 2 : 1;
+    const double across = (double)ceil_div(d.channels, kBM / factors * t.ctas), kb = (double)ceil_div(d.width, kTerms);
     const double tiles = (double)groups * (groups > 1 ? per / t.rows + 1 : ceil_div(per, t.rows)) * across, waves = tiles * parts * t.ctas / 148;
-    const double each = ceil(kb / parts) * (ks == 2 ? 270 + 1.2 * b : 380 + 0.5 * b) + 1500 + (d.mode == kGroupedGated ? 24 : 12) * t.rows;
-    const double l2 = tiles * t.ctas * kb * (kABytes + b * kRowBytes) / 8900, dram = 2.0 * groups * d.channels * d.width * (d.mode == kGroupedGated ? 2 : 1) / 3400;
+    const double each = ceil(kb / parts) * (ks == 2 ? 270 + 1.2 * b : 380 + 0.5 * b) + 1500 + 12 * factors * t.rows + (t.ctas - 1) * 1000;
+    const double l2 = tiles * t.ctas * kb * (kABytes + b * kRowBytes) / 8900, dram = 2.0 * groups * d.channels * d.width * factors / 3400;
     const double cost = std::max({(waves > 4 ? waves + 0.5 : ceil(waves)) * each, l2, dram});
-    return cost + 11000 + (parts > 1 ? 4000 + (8.0 * parts + 2) * d.rows * (double)d.channels / 4500 : 0);
+    return cost + 11000 + (parts > 1 ? 3000 + 2000 * factors + (8.0 * parts + 2) * d.rows * (double)d.channels * factors / 4500 : 0);
 }
 // The same of gradients: the tiles of rows first, then the weights', each taken by the pair that is free first
 double backward_cost(const GroupedProblem &d, Tile t, int x_parts, int w_parts) {
@@ -874,7 +908,7 @@ double backward_cost(const GroupedProblem &d, Tile t, int x_parts, int w_parts) 
 }
 // Forward products.  Twice the rows that groups have on average, since some have more (32 groups of 32 rows, 2048 x 1408: gated block in tiles of 32, 64 and 128 rows 66, 60 and
 // 63 us), and pairs from 33 rows on (64 rows: 68 us in tiles of one CTA, 66 of two).  Where that would be fewer tiles than SMs, what costs least (512 rows of 4 groups, 8192 ->
-// 1024: 27.1 us in 40 tiles of 64 rows, 35.0 in 16 of 256, 20.9 with four parts of each; 13926 rows of one, 64 -> 72: in tiles of 256 rows 9.7, of 128 6.6).
+// 1024: 27.1 us in 40 tiles of 64 rows, 35.0 in 16 of 256, 20.9 with four parts of each; gated block, 512 of 8, 7168 -> 256, 24.6 and 17.9; 13926 rows of one, 64 -> 72: in tiles of 256 rows 9.7, of 128 6.6).
 Plan forward_plan(const GroupedProblem &d, bool any_tile, Plan plan, bool any_parts) {
     const int groups = std::min(d.rows, d.groups), per_group = (d.rows + groups - 1) / groups, all = (d.rows + 15) / 16 * 16, kb = (int)ceil_div(d.width, kTerms);
     if (any_tile) {
@@ -888,7 +922,7 @@ Plan forward_plan(const GroupedProblem &d, bool any_tile, Plan plan, bool any_pa
     double best = 0.93 * forward_cost(d, first.tile, first.x);
     for (int ctas = 1; ctas <= 2; ++ctas)
         for (int rows = 32; rows <= 128 * ctas; rows *= 2)
-            for (int parts = 1; parts <= (gated ? 1 : 16); parts *= 2) {
+            for (int parts = 1; parts <= 16; parts *= 2) {
                 if (parts > 1 && kb < 8 * parts) continue;
                 const Plan other{any_tile ? Tile{ctas, std::min(rows, all)} : first.tile, any_parts ? parts : first.x, 1};
                 const double cost = forward_cost(d, other.tile, other.x);
@@ -935,7 +969,7 @@ Plan pick_plan(const GroupedProblem &d) {
     const char *shape = getenv("ONNXB_GROUPED_TILE"), *parts = getenv("ONNXB_GROUPED_PARTS"), *comma = parts ? strchr(parts, ',') : nullptr;
     const Tile tile{shape && shape[0] ? shape[0] - '0' : 0, shape && shape[0] && shape[1] == 'x' ? atoi(shape + 2) : 0};
     auto count = [](const char *e) { return std::max(1, std::min(16, atoi(e))); };
-    const Plan plan{tile, parts && d.mode != kGroupedGated ? count(parts) : 1, parts && d.mode == kGroupedGrad ? count(comma ? comma + 1 : parts) : 1};
+    const Plan plan{tile, parts ? count(parts) : 1, parts && d.mode == kGroupedGrad ? count(comma ? comma + 1 : parts) : 1};
     // (the last sizes' plan is kept: a call asks twice, and it takes a microsecond)
     const std::array<int, 6> sizes{d.mode, d.rows, d.groups, d.channels, d.width, d.terms};
     static thread_local std::array<int, 6> last_sizes{-1};
@@ -971,7 +1005,7 @@ bool by_16(const void *p, long long ld) { return reinterpret_cast<uintptr_t>(p) 
 
 size_t tc_grouped_workspace(const GroupedProblem &d, bool rows, int weights) {
     const Plan plan = pick_plan(d);
-    const long long of_rows = rows && plan.x > 1 ? plan.x * (long long)d.rows * plane_pitch(d.mode == kGroupedGrad ? d.width : d.channels) : 0;
+    const long long of_rows = rows && plan.x > 1 ? plan.x * (d.mode == kGroupedGated ? 2ll : 1ll) * d.rows * plane_pitch(d.mode == kGroupedGrad ? d.width : d.channels) : 0;
     const long long of_weights = plan.w > 1 ? (long long)plan.w * weights * d.groups * d.channels * plane_pitch(d.width) : 0;
     return (size_t)(of_rows + of_weights) * 4;
 }
@@ -1061,21 +1095,24 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     count_launch();
     if (e != cudaSuccess || !in_parts) return (int)e;
     SumProblem sum{};
-    sum.groups = d.groups; sum.bf16 = bf16;
+    sum.groups = d.groups; sum.bf16 = bf16; sum.activation = d.activation;
     int jobs = 0, most_rows = 1;
     if (p.x_parts > 1) {
-        sum.job[jobs++] = SumJob{p.x_planes, p.x_pitch, d.rows * p.x_pitch, p.x_parts, d.rows, cols, static_cast<uint16_t *>(p.Y[0]), p.y_ld[0], 0, 1, d.offsets};
+        const long long factor = d.rows * p.x_pitch;
+        SumJob &job = sum.job[jobs++];
+        job = SumJob{p.x_planes, p.x_pitch, gated ? 2 * factor : factor, factor, p.x_parts, d.rows, cols, {}, {}, 0, 1, d.offsets};
+        for (int i = 0; i < p.outs; ++i) { job.out[i] = static_cast<uint16_t *>(p.Y[i]); job.ld[i] = p.y_ld[i]; }
         most_rows = d.rows;
     }
     for (int i = 0; p.w_parts > 1 && i < p.w_count; ++i) {
         const int w = p.w_first + i, rows = d.groups * d.channels;
         const long long result = rows * p.w_pitch;
-        sum.job[jobs++] = SumJob{p.w_planes + i * result, p.w_pitch, p.w_count * result, p.w_parts, rows, d.width, static_cast<uint16_t *>(p.D[w]), p.d_ld[w],
+        sum.job[jobs++] = SumJob{p.w_planes + i * result, p.w_pitch, p.w_count * result, 0, p.w_parts, rows, d.width, {static_cast<uint16_t *>(p.D[w])}, {p.d_ld[w]},
                                  p.d_stride[w], d.channels, nullptr};
         most_rows = std::max(most_rows, rows);
     }
     const dim3 sum_grid((unsigned)ceil_div(cols, 128), (unsigned)std::min(65535ll, ceil_div(most_rows, 8)), (unsigned)jobs);
-    const cudaError_t sum_err = launch_pdl(grouped_sum_kernel, sum_grid, dim3(256), 0, stream, sum);
+    const cudaError_t sum_err = launch_pdl(gated ? grouped_sum_kernel<true> : grouped_sum_kernel<false>, sum_grid, dim3(256), 0, stream, sum);
     count_launch();
     return (int)sum_err;
 }

@@ -183,15 +183,18 @@ def test_parts_of_the_sums(parts, tile, t, monkeypatch):
     """Reductions in parts, some of which have no stages: of groups with few rows or none, and with the last stage in either; rows of no group stay as they were."""
     monkeypatch.setenv("ONNXB_GROUPED_TILE", tile)
     monkeypatch.setenv("ONNXB_GROUPED_PARTS", parts)
-    for case in (Case([130, 0, 1, 77, 300, 16, 64, 192], 320, 448, TYPES[t], seed=3, before=5, behind=70), Case([257, 63, 129], 129, 65, TYPES[t], seed=5, behind=1),
-                 Case([5], 1000, 8, TYPES[t], seed=6), Case([1500, 700], 40, 136, TYPES[t], seed=7)):
-        check_all(case)
+    cases = (Case([130, 0, 1, 77, 300, 16, 64, 192], 320, 448, TYPES[t], seed=3, before=5, behind=70), Case([257, 63, 129], 129, 65, TYPES[t], seed=5, behind=1),
+             Case([5], 1000, 8, TYPES[t], seed=6), Case([1500, 700], 40, 136, TYPES[t], seed=7))
+    for case, kind in zip(cases, ("silu", "gelu", "gelu_tanh", "relu")):
+        check_all(case, kind)
         outside = torch.ones(case.R, dtype=torch.bool, device="cuda")
         outside[case.rows()] = False
-        Y, dX = (torch.full((case.R, n), 7.0, dtype=case.t, device="cuda") for n in (case.N, case.K))
+        Y, H, G, Up, dX = (torch.full((case.R, n), 7.0, dtype=case.t, device="cuda") for n in (case.N, case.N, case.N, case.N, case.K))
         binding.onnx_grouped_gemm(case.X, case.W, case.offsets, Y=Y)
+        binding.onnx_grouped_gated(case.X, case.W, case.Wu, case.offsets, H=H, G=G, U=Up)
         binding.onnx_grouped_gemm_backward(case.dY, case.X, case.W, case.offsets, dX=dX)
-        assert (Y[outside] == 7.0).all() and (dX[outside] == 7.0).all()
+        for y in (Y, H, G, Up, dX):
+            assert (y[outside] == 7.0).all()
         every = binding.onnx_grouped_gated_backward(case.dY, case.X, case.W, case.Wu, case.G, case.U, case.offsets)
         for i in range(1, 7):
             wanted = [bool(i & b) for b in (1, 2, 4)]
@@ -210,6 +213,11 @@ def test_long_sums_of_few_tiles():
         binding.onnx_grouped_gemm(c.X, c.W, c.offsets, Y=wide[:, 1:1 + c.N])
         check_gemm(c, wide[:, 1:1 + c.N])
         assert (wide[:, 0] == 7.0).all() and (wide[:, 1 + c.N:] == 7.0).all()
+        both = torch.full((c.R, 3 * c.N + 1), 7.0, dtype=c.t, device="cuda")
+        H, G, Up = (both[:, 1 + i * c.N:1 + (i + 1) * c.N] for i in range(3))
+        binding.onnx_grouped_gated(c.X, c.W, c.Wu, c.offsets, activation="gelu", H=H, G=G, U=Up)
+        check_gated(c, H, G, Up, "gelu")
+        assert (both[:, 0] == 7.0).all()
         store = torch.full((len(c.sizes), c.N + 1, c.K + 5), 7.0, dtype=c.t, device="cuda")
         dX, dW = binding.onnx_grouped_gemm_backward(c.dY, c.X, c.W, c.offsets, dW=store[:, :c.N, :c.K])
         check_gemm_backward(c, dX, dW)
