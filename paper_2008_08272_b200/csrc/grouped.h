@@ -36,7 +36,7 @@ struct GroupedProblem {
 
 // The forward products of a few rows (grouped_few.cu).  Operands' rows and groups may begin anywhere.
 // (in_place: the weights begin where the tensor cores' kernel can read them)
-bool grouped_few_fits(int rows, int groups, bool in_place);
+bool grouped_few_fits(int rows, int groups, int width, bool in_place);
 int launch_grouped_few(const GroupedProblem &p, cudaStream_t stream);
 // Scratch that launch_tc_grouped needs, by `mode`, `rows`, `groups`, `channels`, `width` and `terms` alone, for results by row (dX, or a forward product) and so many
 // weights' gradients

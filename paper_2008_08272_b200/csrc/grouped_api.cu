@@ -76,12 +76,12 @@ onnxb_status check_space(const void *workspace, size_t bytes, size_t need) { ret
 
 }  // namespace
 
+static bool sizes_are_some(const onnxb_matrix *m) { return m && m->rows >= 1 && m->cols >= 1 && m->rows <= kMostSize && m->cols <= kMostSize; }
 // (few rows are taken from wherever they and the weights begin)
 static bool few(const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu) {
-    if (!X || !Wg || X->rows < 1 || X->rows > kMostSize || Wg->count < 1 || Wg->count > kMostGroups) return false;
-    return grouped_few_fits((int)X->rows, (int)Wg->count, in_place(Wg) && (!Wu || in_place(Wu)));
+    if (!sizes_are_some(X) || !Wg || Wg->count < 1 || Wg->count > kMostGroups) return false;
+    return grouped_few_fits((int)X->rows, (int)Wg->count, (int)X->cols, in_place(Wg) && (!Wu || in_place(Wu)));
 }
-static bool sizes_are_some(const onnxb_matrix *m) { return m && m->rows >= 1 && m->cols >= 1 && m->rows <= kMostSize && m->cols <= kMostSize; }
 // The reductions' parts (from the sizes alone)
 static GroupedProblem sizes_of(int mode, const onnxb_matrix *rows, int64_t channels, int64_t width, int64_t groups, int terms) {
     GroupedProblem d{};
