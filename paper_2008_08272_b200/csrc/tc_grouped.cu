@@ -530,7 +530,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
         // ------------------------------------------------------------ epilogue
         const int q = warp & 3, half = (warp - 2) >> 2;
         uint8_t *buf = staging + (warp - 2) * kBlockBytes;
-        int acc = 0;
+        int acc = 0, turn = 0;                         // turn: the half of a buffer that the gated block's next exchange takes, from tile to tile
         uint32_t acc_phase = 0;
         const uint32_t peer_tmem_empty = kCtas == 2 ? map_to_cta(smem_u32(&tmem_empty[0]), 0) : 0u;
         for (int t = unit; t >= 0 && tile_at<kMode, kParts>(p, groups, t, at); t = next_tile(true)) {
@@ -612,11 +612,12 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 float *given = reinterpret_cast<float *>(buf) + lane;
                 const float *got = reinterpret_cast<const float *>(staging + ((warp - 2) ^ 2) * kBlockBytes) + lane;
 #pragma unroll 1
-                for (int b = half, turn = 0; b < blocks; b += 2, turn ^= 512) {
+                for (int b = half; b < blocks; b += 2, turn ^= 512) {
                     uint32_t v[32];
                     tmem_ld_32x32(tbase + (uint32_t)(b * 32), v);
                     tmem_ld_wait();
-                    // of the other warp's results' rows, what it needs (in turns: it may still read what was given last)
+                    // of the other warp's results' rows, what it needs (in turns, the tile before among them: it may still read what was given last, and has read
+                    // what was given before that once it is at the barrier of the last)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) given[turn + i * 32] = __uint_as_float(up ? v[i] : v[16 + i]);
                     if (p.outs == 3) store(up ? 2 : 1, b * 32, channel0, p.channels, kAll, [&](int i) { return __uint_as_float(v[i]); });

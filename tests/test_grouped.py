@@ -560,3 +560,17 @@ def test_two_streams_at_once():
     for a, b in zip(want, got):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
     assert binding.last_device_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("tile", ["1x32", "1x64", "1x96", "2x160", "2x192"])
+@pytest.mark.parametrize("kind", ["silu", "relu"])
+def test_gated_exchange_from_tile_to_tile(tile, kind, monkeypatch):
+    """Several short tiles a CTA, one after the other, whose warps exchange an odd number of blocks in each: what one gives in a tile is not what the other still
+    reads of the tile before."""
+    monkeypatch.setenv("ONNXB_GROUPED_TILE", tile)
+    c = Case([1500, 33, 1, 0, 900, 161], 64, 1000, torch.bfloat16, seed=12)
+    H, G, Up = binding.onnx_grouped_gated(c.X, c.W, c.Wu, c.offsets, activation=kind, save=True)
+    check_gated(c, H, G, Up, kind)
+    for _ in range(50):
+        assert torch.equal(H, binding.onnx_grouped_gated(c.X, c.W, c.Wu, c.offsets, activation=kind))
