@@ -124,10 +124,19 @@ __device__ __forceinline__ void place(int band, int tiles_m, int tiles_n, int r,
     at.tn = rr / rows;
     at.tm = b * band + rr - at.tn * rows;
 }
+// Tiles of rows; all of a call, of the weights' gradients too
 template <int kMode, bool kParts>
-__device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t, TileAt &at) {
+__device__ __forceinline__ int row_tiles(const Params &p, const Groups &s) {
+    return kMode != kGroupedGrad || p.with_x ? s.tiles[p.groups] * p.tiles_n * (kParts ? p.x_parts : 1) : 0;
+}
+template <int kMode, bool kParts>
+__device__ __forceinline__ int all_tiles(const Params &p, const Groups &s) {
+    return row_tiles<kMode, kParts>(p, s) + (kMode == kGroupedGrad ? p.w_total * (kParts ? p.w_parts : 1) : 0);
+}
+template <int kMode, bool kParts>
+__device__ __forceinline__ void tile_at(const Params &p, const Groups &s, int t, TileAt &at) {
     constexpr bool kGrad = kMode == kGroupedGrad;
-    const int of_rows = !kGrad || p.with_x ? s.tiles[p.groups] * p.tiles_n * (kParts ? p.x_parts : 1) : 0;
+    const int of_rows = row_tiles<kMode, kParts>(p, s);
     at.x = t < of_rows;
     at.z = 0;
     t = at.x ? t : t - of_rows;
@@ -159,9 +168,9 @@ __device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t,
         at.row0 = s.first[lo] + at.tm * per;
         at.rows = min(per, all - at.tm * per);
         share(kGrad ? p.terms * p.num_kb : p.num_kb);
-        return true;
+        return;
     }
-    if (!kGrad || t >= p.w_total) return false;
+    if (!kGrad) return;
     const int per = p.w_tiles_m * p.w_tiles_n;
     at.g = t / (per * p.w_count);
     const int r = t - at.g * per * p.w_count;
@@ -170,7 +179,6 @@ __device__ __forceinline__ bool tile_at(const Params &p, const Groups &s, int t,
     at.row0 = s.first[at.g];
     at.rows = s.first[at.g + 1] - at.row0;
     share((at.rows + kTerms * p.ks - 1) / (kTerms * p.ks));
-    return true;
 }
 
 template <typename T2>
@@ -205,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = kCtas == 2 ? (int)cluster_ctarank() : 0;
-    const int unit = blockIdx.x / kCtas;
+    int unit = blockIdx.x / kCtas;
     TileAt at;
 
     if (threadIdx.x == 0) {
@@ -273,13 +281,50 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
     const uint32_t tmem_base = *tmem_holder;
     if (kCtas == 2) cluster_sync_all();     // the peer's barriers exist before anything arrives on them
 
+    // Another CTA of the grid taken over, and its number or -1 (by the even CTA's warp 0)
+    int left = (int)gridDim.x;
+    uint32_t answer_phase = 0;
+    auto ask = [&]() {
+        if (lane == 0) {
+            fence_proxy_async_smem();              // (the last answer has been read)
+            mbar_arrive_expect_tx(answer_here, 16);
+            ask_for_block(answer, answer_here);
+        }
+        __syncwarp();
+    };
+    auto granted = [&]() {
+        mbar_wait(answer_here, answer_phase, p.err, 9);
+        answer_phase ^= 1;
+        const int block = granted_block(answer);
+        __syncwarp();
+        return block < 0 || --left <= 0 ? -1 : block / kCtas;
+    };
+    // There may be CTAs behind the last tile, for groups' tiles that might have been.  Which CTAs are granted goes by no order: such are passed over until there
+    // are none to ask for.  One that is such itself does as much at once, and has the tile that it finds for its own (of a pair both have).
+    const int tiles = all_tiles<kMode, kParts>(p, groups);
+    if (unit >= tiles) {
+        int *found = reinterpret_cast<int *>(tmem_holder + 1);
+        if (warp == 0 && rank == 0) {
+            do {
+                ask();
+                unit = granted();
+            } while (unit >= tiles);
+            if (lane == 0) *found = unit;
+            if (kCtas == 2 && lane == 0)
+                asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(map_to_cta(smem_u32(found), 1)), "r"(unit) : "memory");
+        }
+        __syncthreads();
+        if (kCtas == 2) cluster_sync_all();
+        unit = *reinterpret_cast<volatile int *>(found);
+    }
+
     // Whether a tile's last stage ends inside the next group's rows, where it is not by 16 rows that it does
     auto has_tail = [&](const TileAt &t) { return kGrad && !t.x && t.ends && (t.rows & 15) != 0; };
 
     // The tile after this one, as the even CTA's producer says it; -1: none.  (By a warp's lanes, or the one that issues MMAs.  Nobody has more tiles than
     // there are: that ends the loops where a wait has run out, too.)
     const uint32_t told_back = kCtas == 2 ? map_to_cta(smem_u32(&slot_empty[0]), 0) : 0u;
-    int slot = 0, left = (int)gridDim.x;
+    int slot = 0;
     uint32_t slot_phase = 0;
     auto next_tile = [&](bool by_warp) {
         if (kCtas == 2) mbar_wait_cluster(&slot_full[slot], slot_phase, p.err, 8);
@@ -301,26 +346,9 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
         const uint32_t full_issuer = kCtas == 2 ? map_to_cta(smem_u32(&full[0]), 0) : 0u;
         const uint32_t tail_own = kCtas == 2 ? map_to_cta(smem_u32(&tail_full[0]), (uint32_t)rank) : 0u;
         const int bnh = p.BN / kCtas;
-        uint32_t answer_phase = 0;
-        auto ask = [&]() {
-            if (lane == 0) {
-                fence_proxy_async_smem();              // (the last answer has been read)
-                mbar_arrive_expect_tx(answer_here, 16);
-                ask_for_block(answer, answer_here);
-            }
-            __syncwarp();
-        };
-        auto granted = [&]() {
-            mbar_wait(answer_here, answer_phase, p.err, 9);
-            answer_phase ^= 1;
-            const int block = granted_block(answer);
-            __syncwarp();
-            return block < 0 || --left <= 0 ? -1 : block / kCtas;
-        };
         int t = unit;
         while (t >= 0) {
-            const bool some = tile_at<kMode, kParts>(p, groups, t, at);
-            if (!some) break;
+            tile_at<kMode, kParts>(p, groups, t, at);
             if (rank == 0) ask();
             // Tiles of rows: the weights in one copy, or in two of 64 (the gated block's channels of each, dX's columns); then this CTA's rows, in one copy or
             // where they are few in one or two small ones.  Gradients of weights: copies of 64 channels and 64 columns by a stage's terms.  Where a stage has two
@@ -405,18 +433,20 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             }
             // The next tile
             if (rank == 0) {
-                t = granted();
-                TileAt after;
-                const int told = t >= 0 && tile_at<kMode, kParts>(p, groups, t, after) ? t : -1;
                 if (kCtas == 2) mbar_wait_cluster(&slot_empty[slot], slot_phase ^ 1, p.err, 10);
                 else mbar_wait(&slot_empty[slot], slot_phase ^ 1, p.err, 10);
+                t = granted();
+                while (t >= tiles) {
+                    ask();
+                    t = granted();
+                }
                 if (lane == 0) {
                     if (kCtas == 2) {
                         mbar_arrive_expect_tx(&slot_full[slot], 16);
                         for (uint32_t r = 0; r < 2; ++r)
-                            st_async_v4(map_to_cta(smem_u32(&slots[slot]), r), (uint32_t)told, 0u, 0u, 0u, map_to_cta(smem_u32(&slot_full[slot]), r));
+                            st_async_v4(map_to_cta(smem_u32(&slots[slot]), r), (uint32_t)t, 0u, 0u, 0u, map_to_cta(smem_u32(&slot_full[slot]), r));
                     } else {
-                        *reinterpret_cast<volatile int *>(&slots[slot]) = told;
+                        *reinterpret_cast<volatile int *>(&slots[slot]) = t;
                         mbar_arrive(&slot_full[slot]);
                     }
                 }
@@ -427,11 +457,6 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 __syncwarp();
                 t = next_tile(true);
             }
-        }
-        // CTAs behind the last tile, for groups' tiles that might have been: taken over rather than launched
-        while (rank == 0 && t >= 0) {
-            ask();
-            t = granted();
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer (of a pair: the even CTA)
@@ -445,7 +470,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), a_lo = (uint32_t)a_tmpl | ((smem_u32(stages) >> 4) & 0x3FFFu);
             const uint32_t b_base = ((smem_u32(stages) + p.b_at) >> 4) & 0x3FFFu, stage16 = p.stage_bytes >> 4;
             constexpr uint32_t kK16 = 32u >> 4, kMn16 = 2048u >> 4, kA16 = kGrad ? kMn16 : kK16, kABlock16 = (kGrad ? kBoxBytes : kABytes) >> 4;
-            for (int t = unit; t >= 0 && tile_at<kMode, kParts>(p, groups, t, at); t = next_tile(false)) {
+            for (int t = unit; t >= 0; t = next_tile(false)) {
+                tile_at<kMode, kParts>(p, groups, t, at);
                 if (at.kb == 0) continue;              // a group without rows
                 const bool b_mn = kGrad && !at.x, tail = has_tail(at);
                 const uint64_t b_tmpl = b_mn ? mn_tmpl : k_tmpl;
@@ -502,7 +528,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             uint32_t clear_phase = 0;
             const uint32_t cleared_issuer = kCtas == 2 ? map_to_cta(smem_u32(&cleared[0]), 0) : 0u;
             const int boxes = kBM / kBox + p.BN / kCtas / kBox;
-            for (int t = unit; t >= 0 && tile_at<kMode, kParts>(p, groups, t, at); t = next_tile(true)) {
+            for (int t = unit; t >= 0; t = next_tile(true)) {
+                tile_at<kMode, kParts>(p, groups, t, at);
                 if (at.kb == 0) continue;
                 stage += at.kb - 1;
                 stage %= p.num_stages;
@@ -533,7 +560,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
         int acc = 0, turn = 0;                         // turn: the half of a buffer that the gated block's next exchange takes, from tile to tile
         uint32_t acc_phase = 0;
         const uint32_t peer_tmem_empty = kCtas == 2 ? map_to_cta(smem_u32(&tmem_empty[0]), 0) : 0u;
-        for (int t = unit; t >= 0 && tile_at<kMode, kParts>(p, groups, t, at); t = next_tile(true)) {
+        for (int t = unit; t >= 0; t = next_tile(true)) {
+            tile_at<kMode, kParts>(p, groups, t, at);
             const bool some = at.kb > 0;
             if (some) {
                 mbar_wait(&tmem_full[acc], acc_phase, p.err, 4);

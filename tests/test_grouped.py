@@ -574,3 +574,17 @@ def test_gated_exchange_from_tile_to_tile(tile, kind, monkeypatch):
     check_gated(c, H, G, Up, kind)
     for _ in range(50):
         assert torch.equal(H, binding.onnx_grouped_gated(c.X, c.W, c.Wu, c.offsets, activation=kind))
+
+
+@gpu
+@pytest.mark.parametrize("tile", ["1x16", "1x128", "2x32", "2x256"])
+@pytest.mark.parametrize("sizes", [[0] * 899 + [950], [700] + [0] * 600, [0] * 300 + [40] * 10 + [0] * 300], ids=["last", "first", "middle"])
+def test_most_of_the_grid_has_no_tile(tile, sizes, monkeypatch):
+    """Few groups have rows: the grid has thousands of blocks behind the last tile, which are passed over, and no tile with them; also in parts of the sums."""
+    monkeypatch.setenv("ONNXB_GROUPED_TILE", tile)
+    c = Case(sizes, 136, 1032, torch.bfloat16, seed=13)
+    check_all(c)
+    dX, _ = binding.onnx_grouped_gemm_backward(c.dY, None, c.W, c.offsets, wanted=(True, False))
+    check_gemm_backward(c, dX, None)
+    monkeypatch.setenv("ONNXB_GROUPED_PARTS", "2")
+    check_all(c)
