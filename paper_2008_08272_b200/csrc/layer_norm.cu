@@ -1,7 +1,8 @@
 // onnx_layer_normalization_run and its gradients.
 //
 // Bound by the bytes of X and Y (of dY, X and dX): every element is read once, and what counts is that enough of them are on their way while others are
-// computed with.  The mean is taken away before the squares are added up, in 32 bits: a row far from zero loses nothing.
+// computed with.  The mean is taken away before the squares are added up, in 32 bits; what that mean, a sum of 32 bits, is off by is the mean of what is left, added
+// up beside the squares and taken away, too: a row far from zero loses nothing but what its mean's rounding takes of the mean that is kept.
 //
 // Forward: a row is held in registers, by one warp up to 4096 elements of 16 bits, which then waits for nobody: its 20 or so neighbours on the SM hide
 // what it waits for.  Longer rows have some warps, and few rows as many threads as leave each two pieces.
@@ -159,6 +160,12 @@ __device__ __forceinline__ void sum_over_row(float (&v)[kSums], float (*shared)[
 __host__ __device__ constexpr int block_of(int threads) { return threads == 32 ? 256 : threads; }
 __host__ __device__ constexpr int teams_of(int threads) { return threads == 32 ? 8 : 1; }
 
+// Of a row's squares and deviations, added up, the variance and what the mean was off by.  (Squares that are infinite stay so, and their row becomes the bias.)
+__device__ __forceinline__ float2 variance_and_drift(float squares, float deviations, float per_row) {
+    const float drift = deviations * per_row, variance = squares * per_row;
+    return make_float2(variance < INFINITY ? fmaxf(fmaf(-drift, drift, variance), 0.f) : variance, drift);
+}
+
 struct Forward {
     int M, K, parts;             // of a row: 16 bytes each, or single elements
     const void *X, *scale, *bias;
@@ -173,7 +180,7 @@ template <typename T, typename W, bool kWhole, int kThreads, int kParts, int kRo
 __global__ void __launch_bounds__(block_of(kThreads), 1024 / block_of(kThreads)) layer_norm_kernel(const Forward p) {
     typedef Part<T, kWhole, kThreads> P;
     constexpr int kPairs = P::kPairs;
-    __shared__ float shared[2][kRows][32];
+    __shared__ float shared[3 * kRows][32];
     const int at = threadIdx.x % kThreads;
     const long long i0 = ((long long)blockIdx.x * teams_of(kThreads) + threadIdx.x / kThreads) * kRows;
     tc::pdl_launch_dependents();
@@ -185,7 +192,7 @@ __global__ void __launch_bounds__(block_of(kThreads), 1024 / block_of(kThreads))
 #pragma unroll
         for (int k = 0; k < kParts; ++k)
             if (i0 + r < p.M && P::any(at, k, p.parts)) v[r][k].load(static_cast<const T *>(p.X) + (i0 + r) * p.x_ld, at, k, p.parts);
-    float mean[kRows], inv_std[kRows];
+    float mean[kRows], inv_std[kRows], shift[kRows], left[2 * kRows];
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
         float2 sum = both(0.f);
@@ -198,10 +205,10 @@ __global__ void __launch_bounds__(block_of(kThreads), 1024 / block_of(kThreads))
         }
         mean[r] = sum.x + sum.y;
     }
-    sum_over_row<kThreads, kRows>(mean, shared[0]);
+    sum_over_row<kThreads, kRows>(mean, shared);
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
-        float2 squares = both(0.f);
+        float2 squares = both(0.f), deviations = both(0.f);
         mean[r] *= p.per_row;
 #pragma unroll
         for (int k = 0; k < kParts; ++k) {
@@ -210,17 +217,21 @@ __global__ void __launch_bounds__(block_of(kThreads), 1024 / block_of(kThreads))
                 for (int e = 0; e < kPairs; ++e) {
                     const float2 d = P::own(add(v[r][k].pair(e), both(-mean[r])), at, k, p.parts);
                     squares = fma(d, d, squares);
+                    deviations = add(deviations, d);
                 }
             v[r][k].again();
         }
-        inv_std[r] = squares.x + squares.y;
+        left[2 * r] = squares.x + squares.y;
+        left[2 * r + 1] = deviations.x + deviations.y;
     }
-    sum_over_row<kThreads, kRows>(inv_std, shared[1]);
+    sum_over_row<kThreads, 2 * kRows>(left, shared + kRows);
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
-        inv_std[r] = __frsqrt_rn(fmaf(inv_std[r], p.per_row, p.epsilon));
+        const float2 of_row = variance_and_drift(left[2 * r], left[2 * r + 1], p.per_row);
+        inv_std[r] = __frsqrt_rn(of_row.x + p.epsilon);
+        shift[r] = -of_row.y * inv_std[r];
         if (at == 0 && p.mean && i0 + r < p.M) {
-            p.mean[i0 + r] = mean[r];
+            p.mean[i0 + r] = mean[r] + of_row.y;
             p.inv_std[i0 + r] = inv_std[r];
         }
     }
@@ -235,7 +246,7 @@ __global__ void __launch_bounds__(block_of(kThreads), 1024 / block_of(kThreads))
             if (i0 + r >= p.M) continue;
             P out;
 #pragma unroll
-            for (int e = 0; e < kPairs; ++e) out.set(e, fma(mul(add(v[r][k].pair(e), both(-mean[r])), both(inv_std[r])), scale[e], bias[e]));
+            for (int e = 0; e < kPairs; ++e) out.set(e, fma(fma(add(v[r][k].pair(e), both(-mean[r])), both(inv_std[r]), both(shift[r])), scale[e], bias[e]));
             out.store(static_cast<T *>(p.Y) + (i0 + r) * p.y_ld, at, k, p.parts);
         }
     }
@@ -246,14 +257,14 @@ template <typename T, typename W, bool kWhole>
 __global__ void __launch_bounds__(1024) layer_norm_long_kernel(const Forward p) {
     typedef Part<T, kWhole, 1024> P;
     constexpr int kPairs = P::kPairs;
-    __shared__ float shared[2][1][32];
+    __shared__ float shared[3][32];
     const long long i = blockIdx.x;
     const int at = threadIdx.x;
     tc::pdl_launch_dependents();
     tc::pdl_wait();
     const T *x = static_cast<const T *>(p.X) + i * p.x_ld;
     P v;
-    float2 sum = both(0.f), squares = both(0.f);
+    float2 sum = both(0.f), squares = both(0.f), deviations = both(0.f);
 #pragma unroll 4
     for (int k = 0; P::any(at, k, p.parts); ++k) {
         v.load(x, at, k, p.parts);
@@ -261,7 +272,7 @@ __global__ void __launch_bounds__(1024) layer_norm_long_kernel(const Forward p) 
         for (int e = 0; e < kPairs; ++e) sum = add(sum, v.pair(e));
     }
     float all[1] = {sum.x + sum.y};
-    sum_over_row<1024, 1>(all, shared[0]);
+    sum_over_row<1024, 1>(all, shared);
     const float mean = all[0] * p.per_row;
 #pragma unroll 4
     for (int k = 0; P::any(at, k, p.parts); ++k) {
@@ -270,13 +281,15 @@ __global__ void __launch_bounds__(1024) layer_norm_long_kernel(const Forward p) 
         for (int e = 0; e < kPairs; ++e) {
             const float2 d = P::own(add(v.pair(e), both(-mean)), at, k, p.parts);
             squares = fma(d, d, squares);
+            deviations = add(deviations, d);
         }
     }
-    all[0] = squares.x + squares.y;
-    sum_over_row<1024, 1>(all, shared[1]);
-    const float inv_std = __frsqrt_rn(fmaf(all[0], p.per_row, p.epsilon));
+    float left[2] = {squares.x + squares.y, deviations.x + deviations.y};
+    sum_over_row<1024, 2>(left, shared + 1);
+    const float2 of_row = variance_and_drift(left[0], left[1], p.per_row);
+    const float inv_std = __frsqrt_rn(of_row.x + p.epsilon), shift = -of_row.y * inv_std;
     if (at == 0 && p.mean) {
-        p.mean[i] = mean;
+        p.mean[i] = mean + of_row.y;
         p.inv_std[i] = inv_std;
     }
 #pragma unroll 2
@@ -286,7 +299,7 @@ __global__ void __launch_bounds__(1024) layer_norm_long_kernel(const Forward p) 
         if (p.bias) P::weights(static_cast<const W *>(p.bias), at, k, p.parts, bias);
         v.load(x, at, k, p.parts);
 #pragma unroll
-        for (int e = 0; e < kPairs; ++e) v.set(e, fma(mul(add(v.pair(e), both(-mean)), both(inv_std)), scale[e], bias[e]));
+        for (int e = 0; e < kPairs; ++e) v.set(e, fma(fma(add(v.pair(e), both(-mean)), both(inv_std), both(shift)), scale[e], bias[e]));
         v.store(static_cast<T *>(p.Y) + i * p.y_ld, at, k, p.parts);
     }
 }

@@ -326,3 +326,38 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for a, b in zip(want, got):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@gpu
+@pytest.mark.parametrize("M,K", [(3, 20), (2, 777), (5, 4096), (700, 1000), (640, 4096), (700, 1003), (3, 16384), (2, 25600), (2, 70001)])
+@pytest.mark.parametrize("t,far", [("float32", 1e4), ("float32", -3e5), ("float16", 500.0), ("bfloat16", -60.0)])
+def test_mean_far_from_zero(M, K, t, far):
+    """The mean that is kept is off by its own rounding, and what is left of its error by roundings of the deviations alone, not of the mean."""
+    X, scale, B, _ = inputs(M, K, TYPES[t], torch.float32, seed=M + K, far=far)
+    Y, m, r = binding.onnx_layer_normalization(X, scale, B, save=True)
+    y, mean, inv_std, n = definition(X, scale, B, 1e-5)
+    D = additions(K)
+    # the first mean is off by at most D roundings of the magnitudes' mean; deviations from it are rounded once and added up in D steps, and the mean of those is
+    # rounded twice more
+    first = U * D * X.double().abs().mean(1, keepdim=True)
+    away = (X.double() - mean).abs()
+    drift = U * (D + 3) * (away.mean(1, keepdim=True) + first)
+    assert ((m.double() - mean[:, 0]).abs() <= 1.01 * (U * mean.abs() + drift)[:, 0]).all()
+    # the variance: D roundings of the squares' sum, two of each square, and of what the first mean was off by, which is taken away again, as many; the deviations' sums
+    # enter by their square; inv_std by half of it and its own
+    rel = U * (D + 8) * (1 + (first * inv_std) ** 2) + (drift * inv_std) ** 2
+    assert ((r.double() / inv_std[:, 0] - 1).abs() <= 1.01 * rel[:, 0]).all()
+    s = scale.double().abs()
+    tol = ((U * (away + first) + drift) * inv_std + n.abs() * rel) * s + 3 * U * ((n * scale.double()).abs() + y.abs()) + half_step(Y.dtype) * y.abs() + smallest(Y.dtype)
+    assert ((Y.double() - y).abs() <= 1.01 * tol).all(), float(((Y.double() - y).abs() / tol).max())
+
+
+@gpu
+def test_squares_that_are_not_finite():
+    """A row whose deviations have no square in 32 bits becomes the bias, however far from zero it is."""
+    for K in (64, 1000, 4096, 70000):
+        X = torch.full((2, K), 1e30, device="cuda")
+        X[:, ::3] = -0.7e30
+        scale, B = torch.ones(K, device="cuda"), torch.randn(K, device="cuda")
+        Y, m, r = binding.onnx_layer_normalization(X, scale, B, save=True)
+        assert torch.equal(Y, B.expand(2, K)) and not r.any() and m.isfinite().all()
