@@ -208,13 +208,15 @@ void (*kernel_for(bool gated))(const Params) {
 
 // Up to 16 rows: 2 rows of 8 groups, gated block 4096 -> 10240, 54.7 us here and 60.6 on the tensor cores, 16 of 64 groups 4096 -> 1408 54.5 and 61.7, one row
 // 8192 -> 1024 10.7 and 22.5, whose few tiles read one SM's share of the bandwidth each; but 32 of 64 groups 1408 -> 2048 34 and 26.4.  And where the tensor
-// cores would have the weights copied first (they begin at other than multiples of 16 bytes), up to 4 rows a group on average: 72 rows of 86 groups 633 -> 8166
-// 220 us and 390, but 1745 of 128 groups 241 -> 227 43 and 20), if rows are long enough for loads of 16 bytes a lane (30 groups, 2176 channels: gated block of 49 rows of 197 45 and
-// 53 us, of 133 51 and 41, of 69 39 and 36; plain, 100 rows, 34 and 38 of 261, 34 and 31 of 197, 34 and 26 of 133).
+// cores would have the weights copied first (they begin at other than multiples of 16 bytes), up to 128 rows, of 4 a group on average, that are long enough.  How the rows lie the
+// host does not know: weights are read once for every eight rows of a group, so that rows all of one group cost what even ones gain.  Here and on the tensor cores, rows lying
+// evenly and all in one group: 72 rows of 86 groups, 633 -> 8166, 305 and 544 us, 86 and 62; 128 of 128, 1409 -> 2048, 227 and 471, 80 and 33; 64 of 16, 4097 -> 4096, 139 and 326,
+// 108 and 33; 128 of 1024, 513 -> 264, 31 and 63, 109 and 45.  More rows, 512 of 128, 1409 -> 2048: 233 and 473, 309 and 39; 4096 of 1024, 513 -> 264: 190 and 266, 3660 and 56.
+// Shorter ones, 49 of 30 groups, gated block 197 -> 2176: 46 and 59, 115 and 18.
 // ONNXB_GROUPED_FEW = the most rows pins it for A/B measurements and tests.
 bool grouped_few_fits(int rows, int groups, int width, bool in_place) {
     if (const char *e = getenv("ONNXB_GROUPED_FEW")) return rows <= atoi(e);
-    return rows <= 16 || (!in_place && rows <= 4ll * groups && width >= 160);
+    return rows <= 16 || (!in_place && rows <= std::min(128, 4 * groups) && width >= 512);
 }
 
 int launch_grouped_few(const GroupedProblem &d, cudaStream_t stream) {

@@ -189,3 +189,15 @@ def test_layer_normalization(lib):
         assert back(**kw) == UNSUPPORTED
     assert back(ws=None, size=0) == WORKSPACE and back(size=16) == WORKSPACE
     assert lib.onnx_layer_normalization_backward_workspace_bytes(X, None, None) == 0
+
+
+def test_how_many_rows_take_weights_as_they_lie(lib):
+    """Weights that begin anywhere are read as they lie (no workspace) by up to 128 rows of 4 a group on average, however many groups there are: those that one
+    group may have are few passes over its weights.  Else they are copied."""
+    for E, R, K, as_they_lie in ((1024, 16, 41, True), (1024, 128, 513, True), (32, 128, 513, True), (31, 128, 513, False), (1024, 129, 513, False), (1024, 4096, 513, False),
+                                 (1024, 128, 511, False), (1, 17, 513, False), (1, 16, 513, True)):
+        X, W = mat(R, K), mats(E, 24, K)
+        assert (lib.onnx_grouped_gemm_workspace_bytes(X, W) == 0) == as_they_lie, (E, R, K)
+        assert (lib.onnx_grouped_gated_workspace_bytes(X, W, W) == 0) == as_they_lie, (E, R, K)
+        aligned = mats(E, 24, K + 7 & ~7)
+        assert (lib.onnx_grouped_gemm_workspace_bytes(mat(R, aligned.cols), aligned) == 0)
