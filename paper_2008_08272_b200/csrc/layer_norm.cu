@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(1024) layer_norm_long_kernel(const Forward p) 
 // A team: the threads that have a row's columns (or of a cluster's a block's part of them), 8 or 16 each; a block has one, or eight of a warp each.  Rows that
 // a team takes at once; blocks an SM.  (512 threads an SM of 128 registers, or 1024 of 64: 16384 x 4096 of bf16 76 and 88 us.)
 constexpr int kMostStages = 16;
-__host__ __device__ constexpr int rows_of(int threads, int element, bool whole) { return element == 4 ? 1 : 2; }
+__host__ __device__ constexpr int rows_of(int element) { return element == 4 ? 1 : 2; }
 __host__ __device__ constexpr int per_sm(int threads) { return 512 / block_of(threads); }
 
 // Sums of N values (a power of 2) each over a warp: a lane has one of them in the end, that of index lane / (32 / N).  (Of values that it does not keep a lane
@@ -360,7 +360,7 @@ struct Backward {
 template <typename T, typename W, bool kWhole, int kThreads, int kElements>
 __global__ void __launch_bounds__(block_of(kThreads), per_sm(kThreads)) layer_norm_grad_kernel(const Backward p) {
     typedef Part<T, kWhole, kThreads> P;
-    constexpr int kPairs = P::kPairs, kParts = kElements / P::kCount, kTeams = teams_of(kThreads), kRows = rows_of(kThreads, sizeof(T), kWhole), kWarps = kThreads / 32;
+    constexpr int kPairs = P::kPairs, kParts = kElements / P::kCount, kTeams = teams_of(kThreads), kRows = rows_of(sizeof(T)), kWarps = kThreads / 32;
     extern __shared__ __align__(16) uint8_t memory[];
     __shared__ uint64_t full_of[kTeams][kMostStages];
     constexpr int kSums = 2 * kRows, kGroup = 32 / kSums;        // a row's two sums, or two rows'; lanes that have the same one
@@ -742,7 +742,7 @@ Ring ring_of(int K, int element, int threads, bool whole) {
     r.columns = columns_of(K);
     const int row = r.columns * element, budget = 200 * 1024 / (per_sm(threads) * teams_of(threads));
     r.pitch = whole ? row : (row + 15) / 16 * 16 + 16;
-    r.stage_bytes = 2 * rows_of(threads, element, whole) * r.pitch;
+    r.stage_bytes = 2 * rows_of(element) * r.pitch;
     r.stages = std::max(2, std::min(kMostStages, budget / r.stage_bytes));
     return r;
 }
@@ -778,7 +778,7 @@ int launch(const LayerNormGradProblem &q, int &blocks, cudaStream_t stream) {
                          const_cast<void *>(q.dX.p), q.dX.ld, q.mean, q.inv_std, partial, grad_pitch(q.K), (float)(1.0 / q.K), ring, device_status_ptr()};
         if (!p.err) return (int)cudaErrorUnknown;
         constexpr int kTeams = teams_of(threads);
-        const int rows = rows_of(threads, sizeof(T), kWhole) * kTeams;
+        const int rows = rows_of(sizeof(T)) * kTeams;
         blocks = (int)std::min<long long>(((long long)q.M + rows - 1) / rows, std::max(1, std::min(kMostBlocks, 148 * per_sm(threads)) / ring.blocks));
         // (where the warps' sums are added up there is room for them)
         const size_t smem = std::max<size_t>((size_t)kTeams * ring.stages * ring.stage_bytes, kTeams > 1 ? kTeams * 2 * threads * elements * 4 : 0);

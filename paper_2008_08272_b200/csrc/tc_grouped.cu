@@ -2,7 +2,7 @@
 // onnx_grouped_gated_run, and the products of their gradients.
 //
 // The pipeline is that of tc_dense.cu: a persistent CTA (or a pair of two on one tile) per SM,
-//   warp 0    TMA producer, a ring of stages of one or two K blocks (64 terms of the reduction each): a stage costs its two single threads 240 cycles, and
+//   warp 0    TMA producer, a ring of stages of one K block or, of forward products, two (64 terms of the reduction each): a stage costs its two single threads 240 cycles, and
 //             170 more for each block;
 //   warp 1    one thread issues tcgen05.mma kind::f16 into one of two TMEM accumulators;
 //   warps 2-9 epilogue: tcgen05.ld, the mathematics, stores;
@@ -83,7 +83,7 @@ struct Params {
     long long x_pitch, w_pitch;    // floats of their rows
     int num_stages;
     uint32_t idesc_x, idesc_w;     // (of tiles of rows without their columns)
-    int ks;                        // K blocks of a stage
+    int ks;                        // K blocks of a stage (of gradients one)
     uint32_t stage_bytes, b_at;    // where B begins in a stage
     int b_block;                   // bytes from a block's rows to the next's
     int bf16, activation, outs;    // outs: results of a tile (the gated block: H alone, or H, G and U)
@@ -178,7 +178,7 @@ __device__ __forceinline__ void tile_at(const Params &p, const Groups &s, int t,
     place(p.band, p.w_tiles_m, p.w_tiles_n, r - at.z * per, at);
     at.row0 = s.first[at.g];
     at.rows = s.first[at.g + 1] - at.row0;
-    share((at.rows + kTerms * p.ks - 1) / (kTerms * p.ks));
+    share((at.rows + kTerms - 1) / kTerms);
 }
 
 template <typename T2>
@@ -213,6 +213,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = kCtas == 2 ? (int)cluster_ctarank() : 0;
+    const int ks = kGrad ? 1 : p.ks;
     int unit = blockIdx.x / kCtas;
     TileAt at;
 
@@ -356,19 +357,19 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             const int half_rows = ((at.rows + 15) / 16 * 16) / kCtas;
             const bool small = at.x && half_rows <= 2 * p.b_box;
             const int a_boxes = kMode == kGroupedPlain ? 1 : 2, b_boxes = !at.x ? bnh / kBox : small ? (half_rows + p.b_box - 1) / p.b_box : 1;
-            const int na = kGated ? a_boxes * p.ks : a_boxes, nb = small ? b_boxes * p.ks : b_boxes;
+            const int na = kGated ? a_boxes * ks : a_boxes, nb = small ? b_boxes * ks : b_boxes;
             const int a_box_bytes = kMode != kGroupedPlain ? kBoxBytes : kABytes, b_box_bytes = !at.x ? kBoxBytes : (small ? p.b_box : kBM) * kRowBytes;
-            const uint32_t bytes = (uint32_t)(p.ks * (a_boxes * a_box_bytes + b_boxes * b_box_bytes));
+            const uint32_t bytes = (uint32_t)(ks * (a_boxes * a_box_bytes + b_boxes * b_box_bytes));
             const bool is_a = lane < na, active = lane < na + nb;
             const int piece = is_a ? lane : lane - na, boxes = is_a ? a_boxes : b_boxes, box = piece % boxes, block = piece / boxes;
-            const uint32_t dst_off = !is_a ? p.b_at + (uint32_t)(small ? block * p.b_block + box * b_box_bytes : box * b_box_bytes * p.ks)
-                                     : kGated ? (uint32_t)(block * kABytes + box * kBoxBytes) : (uint32_t)(box * a_box_bytes * p.ks);
+            const uint32_t dst_off = !is_a ? p.b_at + (uint32_t)(small ? block * p.b_block + box * b_box_bytes : box * b_box_bytes * ks)
+                                     : kGated ? (uint32_t)(block * kABytes + box * kBoxBytes) : (uint32_t)(box * a_box_bytes * ks);
             // The map, and where the copy begins: along a K-major reduction by the term, or by the block (the third) in stages of two; weights (term, channel,
             // block, group), for dX (column, channel, 0, group); rows (term, row, block, 0), or as terms themselves (channel or column, row, 0, 0).
             // From stage to stage one of the first three moves on.
             const CUtensorMap *map;
             int c0 = 0, c1, c2 = 0, c3 = 0;
-            const bool second = at.x ? kGrad && is_a : true, by_block = !second && p.ks > 1;
+            const bool second = at.x ? kGrad && is_a : true, by_block = !second && ks > 1;
             if (at.x) {
                 map = !is_a ? (small ? &maps.R_small[0] : &maps.R[0]) : &maps.W[kGated ? box : 0];
                 c1 = !is_a ? at.row0 + rank * half_rows + box * p.b_box : (at.tn * kCtas + rank) * (kGated ? kBox : kBM);
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 c0 = is_a ? (at.tm * kCtas + rank) * kBM + box * kBox : at.tn * p.BN + rank * bnh + box * kBox;
                 c1 = at.row0;
             }
-            const int d0 = second || by_block ? 0 : kTerms, d1 = second ? kTerms * p.ks : 0, d2 = by_block ? p.ks : 0;
+            const int d0 = second || by_block ? 0 : kTerms, d1 = second ? kTerms : 0, d2 = by_block ? ks : 0;
             const bool tail = has_tail(at);
             uint8_t *dst = stages + dst_off;
             auto load = [&](uint32_t cluster_bar, uint64_t *own) {
@@ -464,8 +465,8 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
             int stage = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0, clear_phase = 0;        // (the last: a bit for each stage)
             // K-major: 8-row groups 1024 bytes apart, an instruction 32 bytes further along the swizzled rows, a block as far on as its rows take.  MN-major: blocks of
-            // 64 rows or columns a stage's terms of 128 bytes apart, groups of 8 terms 1024 bytes apart, an instruction two of those further.
-            const uint64_t k_tmpl = make_smem_desc(0, 16, 1024, kSwizzle128B), mn_tmpl = make_smem_desc(0, (uint32_t)(kBoxBytes * p.ks), 1024, kSwizzle128B);
+            // 64 rows or columns 64 terms of 128 bytes apart, groups of 8 terms 1024 bytes apart, an instruction two of those further.
+            const uint64_t k_tmpl = make_smem_desc(0, 16, 1024, kSwizzle128B), mn_tmpl = make_smem_desc(0, (uint32_t)kBoxBytes, 1024, kSwizzle128B);
             const uint64_t a_tmpl = kGrad ? mn_tmpl : k_tmpl;
             const uint32_t a_hi = (uint32_t)(a_tmpl >> 32), a_lo = (uint32_t)a_tmpl | ((smem_u32(stages) >> 4) & 0x3FFFu);
             const uint32_t b_base = ((smem_u32(stages) + p.b_at) >> 4) & 0x3FFFu, stage16 = p.stage_bytes >> 4;
@@ -478,7 +479,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 const uint32_t b_hi = (uint32_t)(b_tmpl >> 32), b_lo = (uint32_t)b_tmpl | b_base, b16 = b_mn ? kMn16 : kK16, b_block16 = (uint32_t)(b_mn ? kBoxBytes : p.b_block) >> 4;
                 const uint32_t idesc = b_mn ? p.idesc_w : p.idesc_x | ((uint32_t)((at.rows + 15) / 16 * 2) << 17);
                 // instructions of the last stage, where they are not four a block; stages before it
-                const int most = 4 * p.ks, last = b_mn && (!kParts || at.ends) ? (at.rows - (at.kb0 + at.kb - 1) * kTerms * p.ks + 15) / 16 : most, whole = last == most && !tail ? at.kb : at.kb - 1;
+                const int most = 4 * ks, last = b_mn && (!kParts || at.ends) ? (at.rows - (at.kb0 + at.kb - 1) * kTerms + 15) / 16 : most, whole = last == most && !tail ? at.kb : at.kb - 1;
                 if (kCtas == 2) mbar_wait_cluster(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 else mbar_wait(&tmem_empty[acc], acc_phase ^ 1, p.err, 2);
                 tc_fence_after_sync();
@@ -498,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                 for (int kb = 0; kb < whole; ++kb) {
                     mbar_wait(&full[stage], phase, p.err, 3);
                     tc_fence_after_sync();
-                    for (uint32_t s = 0; s < (uint32_t)p.ks; ++s)
+                    for (uint32_t s = 0; s < (uint32_t)ks; ++s)
 #pragma unroll
                         for (uint32_t k = 0; k < 4; ++k) multiply(s, k);
                     done();
@@ -512,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                     }
                     tc_fence_after_sync();
 #pragma unroll 1
-                    for (uint32_t k = 0; k < (uint32_t)last; ++k) multiply(k / 4, k % 4);
+                    for (uint32_t k = 0; k < (uint32_t)last; ++k) multiply(0, k);
                     done();
                 }
                 if (kCtas == 2) mma_commit_pair(&tmem_full[acc]);
@@ -537,10 +538,10 @@ __global__ void __launch_bounds__(kThreads, 1) tc_grouped_kernel(const __grid_co
                     mbar_wait(&tail_full[stage], (clear_phase >> stage) & 1u, p.err, 6);
                     clear_phase ^= 1u << stage;
                     // a box has a row of the group's, 64 columns of it, in 128 bytes (the swizzle moves pieces within them)
-                    const int from = at.rows - (at.kb0 + at.kb - 1) * kTerms * p.ks, pieces = ((from + 15) / 16 * 16 - from) * 8;
+                    const int from = at.rows - (at.kb0 + at.kb - 1) * kTerms, pieces = ((from + 15) / 16 * 16 - from) * 8;
                     uint8_t *first = stages + (size_t)stage * p.stage_bytes + from * kRowBytes;
                     for (int b = 0; b < boxes; ++b) {
-                        uint8_t *box = first + b * kBoxBytes * p.ks;
+                        uint8_t *box = first + b * kBoxBytes;
                         for (int i = lane; i < pieces; i += 32) *reinterpret_cast<uint4 *>(box + i * 16) = make_uint4(0, 0, 0, 0);
                     }
                     fence_proxy_async_smem();
@@ -890,13 +891,13 @@ struct Tile {
 bool tile_allowed(Tile t) {
     return (t.ctas == 1 || t.ctas == 2) && t.rows >= 16 && t.rows % 16 == 0 && t.rows <= 128 * t.ctas;
 }
-// K blocks of a stage.  Two where the reduction along K-major rows (`along`) is whole blocks and the ring still has four stages: tiles of up to 128 rows
+// K blocks of a stage.  Two where a forward product's reduction is whole blocks and the ring still has four stages: tiles of up to 128 rows
 // (gated block of 2 rows 64 -> 60 us; tiles of 256 by 128 rows, 16384 x 2816 x 4096, 370 -> 331, but with three stages tiles of 256 by 256 265 -> 287).
-// Of gradients of weights, whose stages hold as many rows, where groups have some.  ONNXB_GROUPED_KS = 1 or 2 pins it, where the ring has three stages at least.
-int blocks_per_stage(const GroupedProblem &d, int along, int blocks_in_ring) {
-    if (along % kTerms) return 1;
+// Of gradients, whose ring has five or six blocks, one.  ONNXB_GROUPED_KS = 1 or 2 pins it for forward products, where the ring has three stages at least.
+int blocks_per_stage(const GroupedProblem &d, int blocks_in_ring) {
+    if (d.mode == kGroupedGrad || d.width % kTerms) return 1;
     if (const char *e = getenv("ONNXB_GROUPED_KS")) return blocks_in_ring >= 6 && e[0] == '2' ? 2 : 1;
-    return blocks_in_ring >= 8 && (d.mode != kGroupedGrad || d.rows / std::min(d.rows, d.groups) >= 256) ? 2 : 1;
+    return blocks_in_ring >= 8 ? 2 : 1;
 }
 long long plane_pitch(int cols) { return (cols + 3ll) / 4 * 4; }
 // Tiles, and parts of the reductions (of tiles of rows, of the weights' gradients): by the sizes alone, since the workspace depends on the parts, and whichever
@@ -1071,7 +1072,7 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
     const int b_rows = grad ? kBM : std::max(tile.rows / tile.ctas > 2 * p.b_box ? kBM : 0, 2 * p.b_box);
     const int table = ((2 * d.groups + 2) * 4 + 15) / 16 * 16, staging = d.mode != kGroupedPlain ? kStagingBytes : 0;
     const int ring = kSmemLimit - 1024 - kBarrierBytes - staging - table, block_bytes = kABytes + b_rows * kRowBytes;
-    p.ks = blocks_per_stage(d, grad ? d.channels : d.width, ring / block_bytes);
+    p.ks = blocks_per_stage(d, ring / block_bytes);
     p.b_block = b_rows * kRowBytes;
     p.b_at = (uint32_t)(p.ks * kABytes);
     p.stage_bytes = (uint32_t)(p.ks * block_bytes);
@@ -1104,12 +1105,12 @@ int launch_tc_grouped(const GroupedProblem &d, cudaStream_t stream) {
         for (int i = 0; i < terms; ++i)
             fine = fine && rows_map(&maps.R[i], d.A[i], d.rows, along, kBM, blocks) && rows_map(&maps.R_small[i], d.A[i], d.rows, along, p.b_box, single);
         for (int i = 0; i < (gated ? 2 : terms); ++i)
-            fine = fine && (grad ? weights_map(&maps.W[i], d.W[i], d.groups, d.channels, d.width, kBox * p.ks)
+            fine = fine && (grad ? weights_map(&maps.W[i], d.W[i], d.groups, d.channels, d.width, kBox)
                                  : weights_map(&maps.W[i], d.W[i], d.groups, d.channels, d.width, gated ? kBox : kBM, gated ? single : blocks));
     }
     if (p.w_count) {
-        for (int i = 0; i < terms; ++i) fine = fine && rows_map(&maps.D[i], d.A[i], d.rows, d.channels, kBox * p.ks);
-        fine = fine && rows_map(&maps.X, d.X, d.rows, d.width, kBox * p.ks);
+        for (int i = 0; i < terms; ++i) fine = fine && rows_map(&maps.D[i], d.A[i], d.rows, d.channels, kBox);
+        fine = fine && rows_map(&maps.X, d.X, d.rows, d.width, kBox);
     }
     if (!fine) return (int)cudaErrorInvalidValue;
 
