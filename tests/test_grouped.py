@@ -588,3 +588,86 @@ def test_most_of_the_grid_has_no_tile(tile, sizes, monkeypatch):
     check_gemm_backward(c, dX, None)
     monkeypatch.setenv("ONNXB_GROUPED_PARTS", "2")
     check_all(c)
+
+
+@gpu
+@pytest.mark.parametrize("tile", ["1x16", "1x64", "1x128", "2x128", "2x256"])
+@pytest.mark.parametrize("parts", [None, "2"])
+@pytest.mark.parametrize("kind", ["silu", "relu"])
+def test_gated_block_of_what_is_not_finite(tile, parts, kind, monkeypatch):
+    """A group's rows and weights that are not finite: the other groups' H, G and U are the same bit by bit, whichever values the warps exchange."""
+    monkeypatch.setenv("ONNXB_GROUPED_TILE", tile)
+    if parts:
+        monkeypatch.setenv("ONNXB_GROUPED_PARTS", parts)
+    c = Case([21, 30, 5, 64, 9, 100], 136, 200, torch.bfloat16, seed=9, before=3, behind=4)
+    clean = binding.onnx_grouped_gated(c.X, c.W, c.Wu, c.offsets, activation=kind, save=True)
+    for g, bad in ((1, float("nan")), (3, float("inf"))):
+        c.X[c.ends[g]:c.ends[g + 1]] = bad
+        c.W[g], c.Wu[g] = bad, -bad
+    dirty = binding.onnx_grouped_gated(c.X, c.W, c.Wu, c.offsets, activation=kind, save=True)
+    for a, b in zip(clean, dirty):
+        for g in (0, 2, 4, 5):
+            assert torch.equal(a[c.ends[g]:c.ends[g + 1]], b[c.ends[g]:c.ends[g + 1]])
+        for g in (1, 3):
+            assert not b[c.ends[g]:c.ends[g + 1]].isfinite().any()
+
+
+@gpu
+def test_more_than_2_31_elements_of_gradients():
+    """Weights' gradients behind the 2^31-th element of dW, by group and by row."""
+    for sizes, N, K in (([70, 0, 33, 201], 24000, 24008), ([130], 46400, 46408)):
+        E, R, t = len(sizes), sum(sizes), torch.bfloat16
+        g = torch.Generator(device="cuda").manual_seed(5)
+        X, dY = torch.randn(R, K, generator=g, device="cuda").to(t), torch.randn(R, N, generator=g, device="cuda").to(t)
+        ends = [0] + torch.tensor(sizes).cumsum(0).tolist()
+        dW = torch.full((E, N, K), 7.0, dtype=t, device="cuda")
+        binding.onnx_grouped_gemm_backward(dY, X, None, torch.tensor(ends, dtype=torch.int32, device="cuda"), wanted=(False, True), dW=dW)
+        for e in range(E):
+            x, d = X[ends[e]:ends[e + 1]].double(), dY[ends[e]:ends[e + 1]].double()
+            for n in (slice(0, 300), slice(N // 2, N // 2 + 300), slice(N - 300, N)):
+                close(dW[e, n], d[:, n].T @ x, d[:, n].abs().T @ x.abs(), max(sizes), t)
+        del dW
+
+
+@gpu
+def test_planes_of_more_than_2_31_elements(monkeypatch):
+    """Parts of the sums behind the 2^31-th element of their planes: of the weights' gradients, and of results by row."""
+    t = torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(6)
+    monkeypatch.setenv("ONNXB_GROUPED_PARTS", "1,4")
+    N, K, sizes = 16000, 17000, [300, 210]
+    X, dY = torch.randn(510, K, generator=g, device="cuda").to(t), torch.randn(510, N, generator=g, device="cuda").to(t)
+    dW = torch.full((2, N, K), 7.0, dtype=t, device="cuda")
+    binding.onnx_grouped_gemm_backward(dY, X, None, torch.tensor([0, 300, 510], dtype=torch.int32, device="cuda"), wanted=(False, True), dW=dW)
+    for e, rows in enumerate((slice(0, 300), slice(300, 510))):
+        x, d = X[rows].double(), dY[rows].double()
+        for n in (slice(0, 300), slice(N // 2, N // 2 + 300), slice(N - 300, N)):
+            close(dW[e, n], d[:, n].T @ x, d[:, n].abs().T @ x.abs(), 300, t)
+    del dW
+    monkeypatch.setenv("ONNXB_GROUPED_PARTS", "4")
+    R, K, N = 40000, 320, 13600
+    X, W = torch.randn(R, K, generator=g, device="cuda").to(t), (torch.randn(2, N, K, generator=g, device="cuda") / math.sqrt(K)).to(t)
+    offsets = torch.tensor([0, 20000, R], dtype=torch.int32, device="cuda")
+    Y = binding.onnx_grouped_gemm(X, W, offsets)
+    H, G, Up = binding.onnx_grouped_gated(X, W, W, offsets, save=True)
+    for first, e in ((0, 0), (20000, 1), (R - 100, 1)):
+        c = Case([100], K, N, t)
+        c.X, c.W, c.Wu = X[first:first + 100], W[e:e + 1], W[e:e + 1]
+        check_gemm(c, Y[first:first + 100])
+        check_gated(c, *(v[first:first + 100] for v in (H, G, Up)), "silu")
+
+
+@gpu
+def test_the_same_bit_by_bit_from_call_to_call():
+    """Which CTA has which tile goes by no order; the results do not depend on it."""
+    for sizes, K, N, t in (([700, 0, 33, 1, 300, 512], 520, 1000, torch.bfloat16), ([3000], 192, 2000, torch.float16), ([2, 0, 5], 1032, 600, torch.bfloat16)):
+        c = Case(sizes, K, N, t, seed=3)
+
+        def calls():
+            return [binding.onnx_grouped_gemm(c.X, c.W, c.offsets), *binding.onnx_grouped_gated(c.X, c.W, c.Wu, c.offsets, save=True),
+                    *binding.onnx_grouped_gemm_backward(c.dY, c.X, c.W, c.offsets),
+                    *binding.onnx_grouped_gated_backward(c.dY, c.X, c.W, c.Wu, c.G, c.U, c.offsets)]
+
+        first = calls()
+        for _ in range(20):
+            assert all(torch.equal(a, b) for a, b in zip(first, calls()))
