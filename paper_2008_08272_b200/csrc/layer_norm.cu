@@ -1,8 +1,8 @@
 // onnx_layer_normalization_run and its gradients.
 //
 // Bound by the bytes of X and Y (of dY, X and dX): every element is read once, and what counts is that enough of them are on their way while others are
-// computed with.  The mean is taken away before the squares are added up, in 32 bits; what that mean, a sum of 32 bits, is off by is the mean of what is left, added
-// up beside the squares and taken away, too: a row far from zero loses nothing but what its mean's rounding takes of the mean that is kept.
+// computed with.  The mean is taken away before the squares are added up, in 32 bits; what the mean of a row far from zero, a sum of 32 bits, is off by is the mean of
+// what is left, added up beside the squares and taken away, too: such a row loses nothing but what rounding takes of the mean that is kept.
 //
 // Forward: a row is held in registers, by one warp up to 4096 elements of 16 bits, which then waits for nobody: its 20 or so neighbours on the SM hide
 // what it waits for.  Longer rows have some warps, and few rows as many threads as leave each two pieces.
@@ -160,10 +160,11 @@ __device__ __forceinline__ void sum_over_row(float (&v)[kSums], float (*shared)[
 __host__ __device__ constexpr int block_of(int threads) { return threads == 32 ? 256 : threads; }
 __host__ __device__ constexpr int teams_of(int threads) { return threads == 32 ? 8 : 1; }
 
-// Of a row's squares and deviations, added up, the variance and what the mean was off by.  (Squares that are infinite stay so, and their row becomes the bias.)
-__device__ __forceinline__ float2 variance_and_drift(float squares, float deviations, float per_row) {
-    const float drift = deviations * per_row, variance = squares * per_row;
-    return make_float2(variance < INFINITY ? fmaxf(fmaf(-drift, drift, variance), 0.f) : variance, drift);
+// Of a row's squares and deviations, added up, the variance and what the mean was off by.  That is taken from rows four standard deviations from zero on: the
+// deviations' sum has roundings of its own, which nearer to zero are no less than the mean's.  (Squares that are infinite stay so, and their row becomes the bias.)
+__device__ __forceinline__ float2 variance_and_drift(float mean, float squares, float deviations, float per_row) {
+    const float variance = squares * per_row, drift = mean * mean > 16.f * variance ? deviations * per_row : 0.f;
+    return make_float2(drift != 0.f ? fmaxf(fmaf(-drift, drift, variance), 0.f) : variance, drift);
 }
 
 struct Forward {
@@ -227,7 +228,7 @@ __global__ void __launch_bounds__(block_of(kThreads), 1024 / block_of(kThreads))
     sum_over_row<kThreads, 2 * kRows>(left, shared + kRows);
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
-        const float2 of_row = variance_and_drift(left[2 * r], left[2 * r + 1], p.per_row);
+        const float2 of_row = variance_and_drift(mean[r], left[2 * r], left[2 * r + 1], p.per_row);
         inv_std[r] = __frsqrt_rn(of_row.x + p.epsilon);
         shift[r] = -of_row.y * inv_std[r];
         if (at == 0 && p.mean && i0 + r < p.M) {
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(1024) layer_norm_long_kernel(const Forward p) 
     }
     float left[2] = {squares.x + squares.y, deviations.x + deviations.y};
     sum_over_row<1024, 2>(left, shared + 1);
-    const float2 of_row = variance_and_drift(left[0], left[1], p.per_row);
+    const float2 of_row = variance_and_drift(mean, left[0], left[1], p.per_row);
     const float inv_std = __frsqrt_rn(of_row.x + p.epsilon), shift = -of_row.y * inv_std;
     if (at == 0 && p.mean) {
         p.mean[i] = mean + of_row.y;

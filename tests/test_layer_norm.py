@@ -361,3 +361,16 @@ def test_squares_that_are_not_finite():
         scale, B = torch.ones(K, device="cuda"), torch.randn(K, device="cuda")
         Y, m, r = binding.onnx_layer_normalization(X, scale, B, save=True)
         assert torch.equal(Y, B.expand(2, K)) and not r.any() and m.isfinite().all()
+
+
+@gpu
+@pytest.mark.parametrize("M,K", [(3, 20), (2, 777), (5, 4096), (700, 1000), (640, 4096), (700, 1003), (3, 16384), (2, 25600), (2, 70001)])
+@pytest.mark.parametrize("t", list(TYPES))
+def test_mean_near_zero(M, K, t):
+    """Rows of whole numbers, whose sums are exact in 32 bits: the mean is off by the rounding of 1 / K and its own alone."""
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    X = torch.randint(-100, 101, (M, K), generator=gen, device="cuda").to(TYPES[t])
+    scale = torch.ones(K, dtype=TYPES[t], device="cuda")
+    _, m, _ = binding.onnx_layer_normalization(X, scale, save=True)
+    mean = X.double().mean(1)
+    assert ((m.double() - mean).abs() <= 2.01 * U * mean.abs()).all()
