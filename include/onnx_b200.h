@@ -450,8 +450,8 @@ onnxb_status onnx_gated_backward_run(const onnxb_matrix *dH, const onnxb_matrix 
  *
  * X and Y [M,K] of one type, 32- or 16-bit floats; scale and bias views of one row of K, of X's type or of 32-bit floats (both of one type);
  * bias may be NULL.  mean and inv_std: 32-bit floats [M], ONNX's Mean and InvStdDev, which the gradients want; both NULL where they are
- * not kept.  epsilon: finite, not negative.  Computed in 32 bits, the mean taken away before the squares are added up; each result is rounded once.  (Sums and squares
- * of deviations have to be finite in 32 bits: values up to about 1e18 in magnitude.)
+ * not kept.  epsilon: finite, not negative.  Computed in 32 bits, the mean taken away before the squares are added up, and of rows far from zero what that mean was
+ * off by, too; each result is rounded once.  (Sums and squares of deviations have to be finite in 32 bits: values up to about 1e18 in magnitude.)
  * What the tensors may be is said above at onnxb_matrix; errors are those of that list (ERR_ATTR also: epsilon).
  */
 onnxb_status onnx_layer_normalization_run(const onnxb_matrix *X, const onnxb_matrix *scale, const onnxb_matrix *bias, float epsilon,
@@ -466,8 +466,8 @@ onnxb_status onnx_layer_normalization_run(const onnxb_matrix *X, const onnxb_mat
  *
  * dY, X and dX [M,K] of one type; scale, dScale and dBias one row of K each, of that type or of 32-bit floats (all of one type).  dX, dScale and dBias:
  * each may be NULL where it is not wanted (not all of them); scale may be NULL without dX.  Sums are in 32 bits, in an order that the
- * sizes and types fix, and whether all rows (of dY, X and dX) begin at multiples of 16 bytes: results are the same bit by bit from call to call, and, of tensors that
- * do alike in that, whichever others are wanted.  No rows: dScale and dBias are zeros.
+ * sizes and types fix, and whether scale and all rows (of dY, X and dX) begin at multiples of 16 bytes: results are the same bit by bit from call to call, and, of
+ * tensors that do alike in that, whichever others are wanted.  No rows: dScale and dBias are zeros.
  */
 size_t onnx_layer_normalization_backward_workspace_bytes(const onnxb_matrix *X, const onnxb_matrix *dScale, const onnxb_matrix *dBias);   /* host only */
 onnxb_status onnx_layer_normalization_backward_run(const onnxb_matrix *dY, const onnxb_matrix *X, const onnxb_matrix *scale, const float *mean,
@@ -485,9 +485,12 @@ onnxb_status onnx_layer_normalization_backward_run(const onnxb_matrix *dY, const
  *
  * onnxb_matrices: `count` views of [rows, cols] each, the weights of one group after the other, `stride` elements apart.  Their order in memory is
  * free (all groups' first rows may come first), but none of their rows overlap (ERR_SHAPE).  At most 1024 groups, count * rows at most 2^31-1,
- * and `stride` at most 2^36; sums of at most 2^27 terms (K, of dX N, of the weights' gradients R), but of forward products of up to 16 rows (ERR_UNSUPPORTED).
- * All else is as said above at onnxb_matrix, alignment among it: what TMA cannot address, rows or groups that do not begin at multiples of 16 bytes, is laid
- * out in the workspace first, weights as a whole.  Long sums of few results are in parts there, by the sizes alone.
+ * and `stride` at most 2^36; sums of at most 2^27 terms (K, of dX N, of the weights' gradients R), but of forward products that read their operands as they lie
+ * (ERR_UNSUPPORTED).  All else is as said above at onnxb_matrix, alignment among it: what TMA cannot address, rows or groups that do not begin at multiples of 16
+ * bytes, is laid out in the workspace first, of weights the groups that have rows (room is asked for all).  Forward products read everything as it lies, and need
+ * no workspace, of up to 16 rows, and where the weights would be laid out otherwise of up to 128 rows, no more than 4 a group on average, of 512 columns or
+ * more.  Long sums of few results are in parts in the workspace, by the sizes alone.  Results are the same bit by bit from call to call; the order of a forward
+ * product's sum goes by the sizes, and in the cases that read operands as they lie by how these begin.
  */
 typedef struct {
     void *data;              /* device (inputs are only read) */

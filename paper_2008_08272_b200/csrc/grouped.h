@@ -34,7 +34,7 @@ struct GroupedProblem {
     void *planes;                            // tc_grouped_workspace bytes, at a multiple of 16
 };
 
-// The forward products of a few rows (grouped_few.cu).  Operands' rows and groups may begin anywhere.
+// The forward products of a few rows (grouped_few.cu): of up to 16, or 128 where the weights would have to be copied.  Operands' rows and groups may begin anywhere.
 // (in_place: the weights begin where the tensor cores' kernel can read them)
 bool grouped_few_fits(int rows, int groups, int width, bool in_place);
 int launch_grouped_few(const GroupedProblem &p, cudaStream_t stream);

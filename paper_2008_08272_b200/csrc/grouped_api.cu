@@ -77,7 +77,7 @@ onnxb_status check_space(const void *workspace, size_t bytes, size_t need) { ret
 }  // namespace
 
 static bool sizes_are_some(const onnxb_matrix *m) { return m && m->rows >= 1 && m->cols >= 1 && m->rows <= kMostSize && m->cols <= kMostSize; }
-// (few rows are taken from wherever they and the weights begin)
+// (few rows are taken from wherever they and the weights begin: grouped_few_fits says how many)
 static bool few(const onnxb_matrix *X, const onnxb_matrices *Wg, const onnxb_matrices *Wu) {
     if (!sizes_are_some(X) || !Wg || Wg->count < 1 || Wg->count > kMostGroups) return false;
     return grouped_few_fits((int)X->rows, (int)Wg->count, (int)X->cols, in_place(Wg) && (!Wu || in_place(Wu)));
@@ -242,6 +242,8 @@ static onnxb_status backward(const onnxb_matrix *dY, const onnxb_matrix *X, cons
     char *ws = static_cast<char *>(workspace);
     int err = 0;
     if (gated) {
+        // dG and dU are rounded to 16 bits, as the tensor cores take them: the results' error is 1.4 times that of rounding the results alone (bf16 2.3e-3 instead of
+        // 1.7e-3 in the norm).  What rounding leaves of them as rows of their own (as the dense block has of up to 32 tokens) would be twice the products.
         GatedSlopeProblem s{};
         s.type = dY->type; s.activation = activation;
         s.M = (int)R; s.F = (int)N;

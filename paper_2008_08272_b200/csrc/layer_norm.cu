@@ -4,8 +4,8 @@
 // computed with.  The mean is taken away before the squares are added up, in 32 bits; what the mean of a row far from zero, a sum of 32 bits, is off by is the mean of
 // what is left, added up beside the squares and taken away, too: such a row loses nothing but what rounding takes of the mean that is kept.
 //
-// Forward: a row is held in registers, by one warp up to 4096 elements of 16 bits, which then waits for nobody: its 20 or so neighbours on the SM hide
-// what it waits for.  Longer rows have some warps, and few rows as many threads as leave each two pieces.
+// Forward: a row is held in registers, by one warp up to 1024 elements of 16 bits, which then waits for nobody, and by 2 to 16 warps up to 32768 (4096: 4 warps,
+// two rows at once); of few rows by as many threads as leave each two pieces or four.  The SM's other rows hide what one waits for.
 //
 // Gradients: a thread adds up its 8 or 16 columns over its block's rows, so all columns of a row have to be a block's (of long rows a cluster's).  The block
 // brings its next rows by asynchronous bulk copies into a ring in shared memory, takes one or two of them into registers, agrees on their sums,
@@ -736,7 +736,7 @@ int columns_of(int K) {
     const int blocks = cluster_of(K);
     return blocks == 1 ? K : ((K + blocks - 1) / blocks + 7) / 8 * 8;
 }
-// The ring, as deep as an SM's shared memory allows (three stages at least)
+// The ring, as deep as an SM's shared memory allows (three stages at least: 200 KB for stages of 64 KB and a little, those of 8192 columns)
 Ring ring_of(int K, int element, int threads, bool whole) {
     Ring r{};
     r.blocks = cluster_of(K);
@@ -744,7 +744,7 @@ Ring ring_of(int K, int element, int threads, bool whole) {
     const int row = r.columns * element, budget = 200 * 1024 / (per_sm(threads) * teams_of(threads));
     r.pitch = whole ? row : (row + 15) / 16 * 16 + 16;
     r.stage_bytes = 2 * rows_of(element) * r.pitch;
-    r.stages = std::max(2, std::min(kMostStages, budget / r.stage_bytes));
+    r.stages = std::min(kMostStages, budget / r.stage_bytes);
     return r;
 }
 Source source_of(const DenseOperand &o, int M, int K, int element, bool one_block) {
